@@ -20,8 +20,8 @@
  * Around them: kap_decode_schedule writes, once per view, the split map that
  * kap_selected_decode_scheduled then reads instead of computing it in every
  * proposal step (the view is fixed across the k steps of a cycle);
- * kap_selected_decode_masked takes token-granular views; kap_append_kv and
- * kap_compact_view maintain the pool; kap_fallback_update switches sequences
+ * kap_selected_decode_masked takes token-granular views; kap_append_kv,
+ * kap_rope_append_kv and kap_compact_view maintain the pool; kap_fallback_update switches sequences
  * to full-context access (Sec. 3.2, "Runtime stability and fallback");
  * kap_accept_top3 scores draft windows.
  *
@@ -392,6 +392,46 @@ size_t kap_verify_workspace_bytes(const kap_kv_cache *kv, int32_t batch, int32_t
 kap_status kap_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const void *k_new,
                          const void *v_new, const int64_t *slot_mapping, int32_t *bad_slots,
                          void *stream);
+
+/*
+ * kap_rope_append_kv -- kap_append_kv for keys and queries as the projection
+ * leaves them: they are turned by the tokens' positions on the way, so that
+ * one launch takes a step's q, k and v to the rotated q and the written pages.
+ *
+ * Token t's frequency j < rot_dim / 2 has the angle
+ *   a = positions[axis][t] * inv_freq[j],  axis = freq_axis[j] (NULL: 0)
+ * and turns one pair (x, y) of each head's first rot_dim dims into
+ *   (x cos a - y sin a, y cos a + x sin a):
+ * dims (j, j + rot_dim / 2) with KAP_ROPE_HALVES, (2 j, 2 j + 1) with
+ * KAP_ROPE_PAIRS. Several axes (time, height, width) are several rows of
+ * positions, and freq_axis shares the frequencies out among them; an axis
+ * outside [0, num_axes) turns nothing. The angle is taken in 64 bits, the
+ * rotation in 32; each output is rounded once.
+ *   q_new, k_new, v_new: rows of Hq * D, Hkv * D, Hkv * D values (q_dtype of
+ *   kv), *_stride elements apart (slices of one fused projection, say);
+ *   q_new NULL: no queries. q_out [num_tokens][Hq][D] (q_dtype, 16-byte
+ *   aligned); it may be q_new itself where q_stride = Hq * D (or num_tokens =
+ *   1), else it overlaps no input. positions [num_axes][num_tokens] int32,
+ *   inv_freq [rot_dim / 2] float32, freq_axis [rot_dim / 2] int32.
+ * K and V go to slot_mapping's slots of the pool as with kap_append_kv (a
+ * negative slot: padding; a slot past the pool: skipped and counted into
+ * *bad_slots; the same slot twice: either token's values), float32 and bf16 as
+ * they are, fp8 as the nearest code of x / scale with the page's K or V scale
+ * (+-448 beyond the range; NaN stays NaN; kv_scales are read, not changed).
+ * The queries of padding tokens are turned like any other.
+ * 1 <= num_axes <= 4; rot_dim a multiple of 16, 16 <= rot_dim <= head_dim.
+ * num_tokens = 0 is a no-op.
+ */
+typedef int32_t kap_rope_style;
+enum { KAP_ROPE_HALVES = 0, KAP_ROPE_PAIRS = 1 };
+
+kap_status kap_rope_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const void *q_new,
+                              int64_t q_stride, void *q_out, const void *k_new,
+                              int64_t k_stride, const void *v_new, int64_t v_stride,
+                              const int64_t *slot_mapping, const int32_t *positions,
+                              int32_t num_axes, const float *inv_freq,
+                              const int32_t *freq_axis, int32_t rot_dim, kap_rope_style style,
+                              int32_t *bad_slots, void *stream);
 
 /*
  * kap_compact_view -- materialise the selected-KV view as a compact physical

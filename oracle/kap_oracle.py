@@ -20,6 +20,9 @@ Systems" (arXiv 2607.24260). What is computed, and where it is defined:
   workspace (Alg. 1, AssignCompactSlots / BuildBlockTable): placing new
   tokens into their KV slots, and copying a view's pages into a compact
   workspace of fixed capacity.
+* ``rotate`` / ``rope_append_kv`` -- rotary positions along one or several
+  axes (the standard definition, not stated in the paper), and the append of
+  keys that are turned by them on the way.
 * ``accept_top_k`` -- Sec. 3.2 target-guided tolerant verification (the
   Top-3 rule): accepted prefix length and the verifier's carry token.
 * ``access_modes`` / ``active_view`` -- Sec. 3.2, "Runtime stability and
@@ -528,6 +531,64 @@ def append_kv(pool: KVPool, k_new: np.ndarray, v_new: np.ndarray, slot_mapping):
         k[page, :, :, off, :] = np.asarray(k_new[t]).reshape(Hkv, C, E)
         v[page, :, :, off] = np.asarray(v_new[t])
     return KVPool(k, v, pool.dtype, pool.scales), bad
+
+
+def rotate(x: np.ndarray, positions, inv_freq, freq_axis=None, pairs: bool = False) -> np.ndarray:
+    """Rotary positions: x [T][H][D] with the first 2 * len(inv_freq) dims of
+    every head turned, in fp64.
+
+    Frequency j of token t turns a pair of dims, read as the complex number
+    x + i y, by the angle positions[axis][t] * inv_freq[j], axis =
+    freq_axis[j] (0 where there is none; an axis that does not exist turns
+    nothing): dims (j, j + n) of n frequencies, or (2 j, 2 j + 1) if ``pairs``.
+    positions: [T] or [axes][T].
+    """
+    out = np.array(x, dtype=np.float64, copy=True)
+    pos = np.atleast_2d(np.asarray(positions, dtype=np.int64))
+    f = np.asarray(inv_freq, dtype=np.float64)
+    n = len(f)
+    for j in range(n):
+        axis = 0 if freq_axis is None else int(freq_axis[j])
+        a = pos[axis].astype(np.float64) * f[j] if 0 <= axis < len(pos) else np.zeros(pos.shape[1])
+        c, s = np.cos(a)[:, None], np.sin(a)[:, None]
+        d0, d1 = (2 * j, 2 * j + 1) if pairs else (j, j + n)
+        u, v = np.asarray(x[:, :, d0], np.float64), np.asarray(x[:, :, d1], np.float64)
+        out[:, :, d0] = u * c - v * s
+        out[:, :, d1] = v * c + u * s
+    return out
+
+
+def rope_append_kv(pool: KVPool, q, k_new, v_new, slot_mapping, positions, inv_freq,
+                   freq_axis=None, pairs: bool = False):
+    """The append of keys turned by their positions, before any rounding.
+
+    q [T][Hq][D], k_new, v_new [T][Hkv][D] as numbers. Returns (turned q, K
+    values, V values, number of out-of-range slots): K [P][Hkv][D/8][16][8] and
+    V [P][Hkv][D][16] fp64 hold what each written slot is to store -- for fp8
+    pools the value over the page's scale, limited to +-448 -- and NaN in every
+    slot that is not written.
+    """
+    P, Hkv, C, _, E = pool.k_pages.shape
+    k = np.full(pool.k_pages.shape, np.nan)
+    v = np.full(pool.v_pages.shape, np.nan)
+    turned = rotate(k_new, positions, inv_freq, freq_axis, pairs)
+    bad = 0
+    for t, s in enumerate(np.asarray(slot_mapping, dtype=np.int64)):
+        s = int(s)
+        if s < 0:
+            continue
+        if s >= P * PAGE:
+            bad += 1
+            continue
+        page, off = divmod(s, PAGE)
+        kt, vt = turned[t], np.asarray(v_new[t], np.float64)
+        if pool.scales is not None:
+            kt = np.clip(kt / float(pool.scales[page, 0]), -448.0, 448.0)
+            vt = np.clip(vt / float(pool.scales[page, 1]), -448.0, 448.0)
+        k[page, :, :, off, :] = kt.reshape(Hkv, C, E)
+        v[page, :, :, off] = vt
+    q = None if q is None else rotate(q, positions, inv_freq, freq_axis, pairs)
+    return q, k, v, bad
 
 
 def compact_view(pool: KVPool, view_block_table, view_num_blocks, capacity: int):

@@ -880,6 +880,91 @@ kap_status kap_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const void 
   return ok();
 }
 
+// Whether [p, p + n) and [q, q + m) share a byte.
+static bool overlap(const void *p, size_t n, const void *q, size_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b + m && b < a + n;
+}
+
+kap_status kap_rope_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const void *q_new,
+                              int64_t q_stride, void *q_out, const void *k_new,
+                              int64_t k_stride, const void *v_new, int64_t v_stride,
+                              const int64_t *slot_mapping, const int32_t *positions,
+                              int32_t num_axes, const float *inv_freq,
+                              const int32_t *freq_axis, int32_t rot_dim, kap_rope_style style,
+                              int32_t *bad_slots, void *stream) {
+  kap_status st = check_kv(kv);
+  if (st != KAP_OK) return st;
+  if (num_tokens < 0) return fail(KAP_ERR_INVALID_ARGUMENT, "num_tokens < 0");
+  if (num_axes < 1 || num_axes > 4)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "num_axes %d outside [1, 4]", num_axes);
+  if (rot_dim < 16 || rot_dim % 16 || rot_dim > kv->head_dim)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "rot_dim %d is no multiple of 16 in [16, head_dim = %d]",
+                rot_dim, kv->head_dim);
+  if (style != KAP_ROPE_HALVES && style != KAP_ROPE_PAIRS)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "unknown style %d", style);
+  if (num_tokens == 0) return ok();
+  if (num_tokens > 0x7fffffff / 2) return fail(KAP_ERR_UNSUPPORTED, "too many tokens");
+  if (!k_new || !v_new || !slot_mapping || !positions || !inv_freq)
+    return fail(KAP_ERR_INVALID_ARGUMENT,
+                "k_new, v_new, slot_mapping, positions and inv_freq are required");
+  if (!q_new != !q_out) return fail(KAP_ERR_INVALID_ARGUMENT, "q_new and q_out go together");
+  if (kv->num_pages < 1) return fail(KAP_ERR_INVALID_ARGUMENT, "KV pool has no pages");
+  const int es = kv->q_dtype == KAP_DT_F32 ? 4 : 2;
+  const int64_t q_row = (int64_t)kv->num_q_heads * kv->head_dim;
+  const int64_t k_row = (int64_t)kv->num_kv_heads * kv->head_dim;
+  if (q_row > 0x7fffffff / 64) return fail(KAP_ERR_UNSUPPORTED, "too many heads");
+  if ((q_new && q_stride < q_row) || k_stride < k_row || v_stride < k_row)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "a stride is less than its row");
+  const int64_t far = INT64_MAX / 16 / num_tokens;
+  if ((q_new && q_stride > far) || k_stride > far || v_stride > far)
+    return fail(KAP_ERR_UNSUPPORTED, "a stride is too large");
+  if (!aligned(q_new, es) || !aligned(k_new, es) || !aligned(v_new, es) ||
+      !aligned(slot_mapping, 8) || !aligned(positions, 4) || !aligned(inv_freq, 4) ||
+      !aligned(freq_axis, 4) || !aligned(q_out, 16))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "an array is misaligned (q_out: 16 bytes)");
+  if (q_out) {
+    const size_t out = (size_t)num_tokens * q_row * es;
+    auto extent = [&](int64_t stride, int64_t row) {
+      return (size_t)((num_tokens - 1) * stride + row) * es;
+    };
+    const bool in_place = q_out == q_new && (q_stride == q_row || num_tokens == 1);
+    if ((!in_place && overlap(q_out, out, q_new, extent(q_stride, q_row))) ||
+        overlap(q_out, out, k_new, extent(k_stride, k_row)) ||
+        overlap(q_out, out, v_new, extent(v_stride, k_row)))
+      return fail(KAP_ERR_INVALID_ARGUMENT, "q_out overlaps an input");
+  }
+  kap::RopeAppendArgs a;
+  a.num_tokens = num_tokens;
+  a.Hq = kv->num_q_heads;
+  a.Hkv = kv->num_kv_heads;
+  a.D = kv->head_dim;
+  a.kv_type = kv->kv_dtype;
+  a.rot = rot_dim;
+  a.halves = style == KAP_ROPE_HALVES;
+  a.num_axes = num_axes;
+  a.q_new = q_new;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = q_out;
+  a.slots = slot_mapping;
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.freq_axis = freq_axis;
+  a.k_pages = const_cast<void *>(kv->k_pages);
+  a.v_pages = const_cast<void *>(kv->v_pages);
+  a.kv_scales = kv->kv_scales;
+  a.num_pages = kv->num_pages;
+  a.bad_slots = bad_slots;
+  (void)hipGetLastError();
+  const hipError_t e = kap::launch_rope_append(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(KAP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
 kap_status kap_compact_view(const kap_kv_cache *src, int32_t batch,
                             const int32_t *view_block_table, int32_t view_stride,
                             const int32_t *view_num_blocks, int32_t view_capacity,

@@ -127,6 +127,25 @@ struct AppendArgs {
   int32_t *bad_slots;            // may be NULL
 };
 
+// kap_rope_append_kv after host validation.
+struct RopeAppendArgs {
+  int num_tokens, Hq, Hkv, D, kv_type, rot, halves, num_axes;
+  const void *q_new, *k_new, *v_new;        // rows of Hq * D (q_new may be NULL) or Hkv * D
+  int64_t q_stride, k_stride, v_stride;     // elements between tokens
+  void *q_out;                              // [num_tokens][Hq][D]
+  const int64_t *slots;                     // [num_tokens]
+  const int32_t *positions;                 // [num_axes][num_tokens]
+  const float *inv_freq;                    // [rot / 2]
+  const int32_t *freq_axis;                 // [rot / 2], NULL: axis 0
+  void *k_pages, *v_pages;                  // the pool written into
+  const float *kv_scales;                   // fp8 only
+  int64_t num_pages;
+  int32_t *bad_slots;                       // may be NULL
+  // set at launch: tokens per workgroup that rotates, workgroups per tile of
+  // tokens for Q and K, workgroups that share a tile's V columns
+  int tile, q_slices, k_slices, v_share;
+};
+
 // kap_compact_view after host validation.
 struct CompactArgs {
   int batch, capacity, view_stride, Hkv, D, elem_bytes;
@@ -172,6 +191,7 @@ hipError_t launch_compile_plan(const PlanArgs &a, hipStream_t s);
 hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);
 hipError_t launch_fallback_update(const FallbackArgs &a, hipStream_t s);
 hipError_t launch_append_kv(const AppendArgs &a, hipStream_t s);
+hipError_t launch_rope_append(const RopeAppendArgs &a, hipStream_t s);
 hipError_t launch_compact_view(const CompactArgs &a, int grid, hipStream_t s);
 hipError_t launch_attn_wide(const AttnArgs &a, hipStream_t s);
 hipError_t launch_decode_fast(const AttnArgs &a, hipStream_t s);

@@ -34,6 +34,9 @@ KAP_DT_FP8_E4M3FN = 2
 KAP_SELECT_SKIP = 0
 KAP_SELECT_STOP = 1
 
+KAP_ROPE_HALVES = 0
+KAP_ROPE_PAIRS = 1
+
 KAP_PLAN_OK = 0
 KAP_PLAN_OVER_CAPACITY = 1
 KAP_PLAN_BAD_SCORE = 2
@@ -49,7 +52,7 @@ EXPORTS = (
     "kap_selected_decode_noalloc", "kap_decode_schedule_bytes", "kap_decode_schedule",
     "kap_selected_decode_scheduled",
     "kap_verify", "kap_verify_workspace_bytes",
-    "kap_append_kv", "kap_compact_view", "kap_fallback_update", "kap_fallback_update_masked",
+    "kap_append_kv", "kap_rope_append_kv", "kap_compact_view", "kap_fallback_update", "kap_fallback_update_masked",
     "kap_accept_top3", "kap_accept_top3_workspace_bytes",
     "kap_status_string", "kap_last_error", "kap_abi_version",
     "kap_stream_read",
@@ -137,6 +140,10 @@ def load_library(path: str = LIB_PATH):
         ctypes.POINTER(KVCacheStruct), _I32, _I32, _I32, _I32]
     lib.kap_append_kv.restype = _I32
     lib.kap_append_kv.argtypes = [ctypes.POINTER(KVCacheStruct), _I32, _P, _P, _P, _P, _P]
+    lib.kap_rope_append_kv.restype = _I32
+    lib.kap_rope_append_kv.argtypes = [
+        ctypes.POINTER(KVCacheStruct), _I32, _P, _I64, _P, _P, _I64, _P, _I64, _P, _P, _I32, _P,
+        _P, _I32, _I32, _P, _P]
     lib.kap_compact_view.restype = _I32
     lib.kap_compact_view.argtypes = [
         ctypes.POINTER(KVCacheStruct), _I32, _P, _I32, _P, _I32, ctypes.POINTER(KVCacheStruct),
@@ -192,6 +199,39 @@ def _dev(t: torch.Tensor, name: str, dtype=None, ndim=None):
     if ndim is not None and t.dim() != ndim:
         raise ValueError(f"{name} must have {ndim} dims, got {tuple(t.shape)}")
     return t
+
+
+def _rows(t: torch.Tensor, name: str, dtype, shape):
+    """A tensor of ``shape`` whose rows (all dims but the first) are contiguous,
+    any distance apart; returns that distance in elements."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (got {t.device}); libkap has no CPU path")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    width = 1
+    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n != 1 and s != width:
+            raise ValueError(f"{name}: the dims of a row must be contiguous")
+        width *= n
+    stride = t.stride(0) if t.shape[0] > 1 else width
+    if stride < width:
+        raise ValueError(f"{name}: rows must not overlap")
+    return stride
+
+
+def _here(*tensors, stream=None):
+    """Every tensor (None: not given) on the current device, and the stream too."""
+    at = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{at}")
+    if stream is not None and stream.device_index != at:
+        raise ValueError(f"the stream is on cuda:{stream.device_index}, the current device is "
+                         f"cuda:{at}")
 
 
 def _stream(stream):
@@ -287,6 +327,78 @@ def append_kv(kv: KVCache, k_new, v_new, slot_mapping, bad_slots=None, stream=No
         _dev(bad_slots, "bad_slots", torch.int32)
     _check(lib.kap_append_kv(ctypes.byref(kv.struct), T, _ptr(k_new), _ptr(v_new),
                              _ptr(slot_mapping), _ptr(bad_slots), _stream(stream)))
+
+
+def _rope_call(kv: KVCache, k_new, v_new, slot_mapping, positions, inv_freq, q_new, q_out,
+               freq_axis, style, bad_slots, stream):
+    """Validate and marshal one kap_rope_append_kv call: (args, q_out, keep)."""
+    _dev(slot_mapping, "slot_mapping", torch.int64, 1)
+    T = int(slot_mapping.shape[0])
+    _dev(positions, "positions", torch.int32)
+    if positions.dim() not in (1, 2) or positions.shape[-1] != T:
+        raise ValueError(f"positions must be [{T}] or [axes][{T}], got {tuple(positions.shape)}")
+    axes = positions.shape[0] if positions.dim() == 2 else 1
+    _dev(inv_freq, "inv_freq", torch.float32, 1)
+    if freq_axis is not None:
+        _dev(freq_axis, "freq_axis", torch.int32, 1)
+        if freq_axis.shape != inv_freq.shape:
+            raise ValueError("freq_axis must have an entry for each of inv_freq's")
+    strides = [_rows(t, name, kv.q_dtype, (T, kv.num_kv_heads, kv.head_dim))
+               for name, t in (("k_new", k_new), ("v_new", v_new))]
+    q_stride = 0
+    if q_new is not None:
+        q_shape = (T, kv.num_q_heads, kv.head_dim)
+        q_stride = _rows(q_new, "q_new", kv.q_dtype, q_shape)
+        if q_out is None:
+            with torch.cuda.stream(stream):
+                q_out = torch.empty(q_shape, dtype=kv.q_dtype, device=kv.device)
+        _dev(q_out, "q_out", kv.q_dtype)
+        if tuple(q_out.shape) != q_shape:
+            raise ValueError(f"q_out must be {q_shape}, got {tuple(q_out.shape)}")
+    elif q_out is not None:
+        raise ValueError("q_out without q_new")
+    if bad_slots is not None:
+        _dev(bad_slots, "bad_slots", torch.int32)
+        if bad_slots.numel() < 1:
+            raise ValueError("bad_slots is empty")
+    keep = (kv, q_new, q_out, k_new, v_new, slot_mapping, positions, inv_freq, freq_axis,
+            bad_slots)
+    _here(kv.k_pages, *keep[1:], stream=stream)
+    args = (ctypes.byref(kv.struct), T, _ptr(q_new), q_stride, _ptr(q_out), _ptr(k_new),
+            strides[0], _ptr(v_new), strides[1], _ptr(slot_mapping), _ptr(positions), int(axes),
+            _ptr(inv_freq), _ptr(freq_axis), 2 * inv_freq.shape[0], int(style), _ptr(bad_slots),
+            _stream(stream))
+    return args, q_out, keep
+
+
+def rope_append_kv(kv: KVCache, k_new, v_new, slot_mapping, positions, inv_freq, *, q_new=None,
+                   q_out=None, freq_axis=None, style: int = KAP_ROPE_HALVES, bad_slots=None,
+                   stream=None):
+    """Turn ``k_new`` [T][Hkv][D] (and ``q_new`` [T][Hq][D]) by the tokens'
+    ``positions`` ([T] or [axes][T] int32) at the frequencies ``inv_freq``
+    (float32, half as many as dims are turned; ``freq_axis`` names each one's
+    axis), write K and V into their slots of ``kv`` as append_kv does -- fp8
+    pools: as codes, with the scales their pages have -- and return the turned
+    queries (None without q_new). All in ``kv.q_dtype``; rows may lie apart, as
+    slices of a fused projection do. ``q_out`` may be a contiguous ``q_new``."""
+    lib = load_library()
+    args, q_out, _ = _rope_call(kv, k_new, v_new, slot_mapping, positions, inv_freq, q_new, q_out,
+                                freq_axis, style, bad_slots, stream)
+    _check(lib.kap_rope_append_kv(*args))
+    return q_out
+
+
+def bind_rope_append_kv(kv: KVCache, k_new, v_new, slot_mapping, positions, inv_freq, *,
+                        q_new=None, q_out=None, freq_axis=None, style: int = KAP_ROPE_HALVES,
+                        bad_slots=None, stream=None) -> "BoundCall":
+    """rope_append_kv marshalled once (not run here: the call writes the pool);
+    ``q_out`` is needed with q_new."""
+    lib = load_library()
+    if q_new is not None and q_out is None:
+        raise ValueError("a bound call needs q_out")
+    args, _, keep = _rope_call(kv, k_new, v_new, slot_mapping, positions, inv_freq, q_new, q_out,
+                               freq_axis, style, bad_slots, stream)
+    return BoundCall(lib.kap_rope_append_kv, args, keep)
 
 
 def compact_view(src: KVCache, view_block_table, view_num_blocks, view_capacity: int,

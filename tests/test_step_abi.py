@@ -1,0 +1,65 @@
+"""Refusals of the calls around a step -- kap_rope_append_kv, kap_verify_shared,
+kap_sample -- before anything is enqueued (no GPU: fake pointers are never
+dereferenced on those paths)."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2607_24260_amd import kap as K
+
+FAKE = 0x100000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(K.LIB_PATH):
+        pytest.fail("libkap.so is not built; run __graft_entry__.build() first")
+    return K.load_library()
+
+
+def kv_struct(kv_dtype=K.KAP_DT_BF16, q_dtype=K.KAP_DT_BF16, Hq=32, Hkv=8, D=128, page=16,
+              scales=None, num_pages=100):
+    return K.KVCacheStruct(Hq, Hkv, D, page, kv_dtype, q_dtype, FAKE, FAKE, scales, num_pages)
+
+
+def rope(lib, kv=None, **over):
+    a = dict(T=5, q=FAKE, qs=4096, qo=8 * FAKE, k=2 * FAKE, ks=1024, v=3 * FAKE, vs=1024, slots=FAKE,
+             pos=FAKE, axes=1, inv=FAKE, fa=None, rot=128, style=0, bad=None)
+    assert set(over) <= set(a)
+    a.update(over)
+    kv = kv or kv_struct()
+    return lib.kap_rope_append_kv(ctypes.byref(kv), a["T"], a["q"], a["qs"], a["qo"], a["k"],
+                                  a["ks"], a["v"], a["vs"], a["slots"], a["pos"], a["axes"],
+                                  a["inv"], a["fa"], a["rot"], a["style"], a["bad"], None)
+
+
+BAD, UNS = K.KAP_ERR_INVALID_ARGUMENT, K.KAP_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("over, status", [
+    (dict(T=-1), BAD), (dict(axes=0), BAD), (dict(axes=5), BAD), (dict(rot=0), BAD),
+    (dict(rot=24), BAD), (dict(rot=144), BAD), (dict(style=2), BAD), (dict(k=None), BAD),
+    (dict(v=None), BAD), (dict(slots=None), BAD), (dict(pos=None), BAD), (dict(inv=None), BAD),
+    (dict(q=None), BAD), (dict(qo=None), BAD), (dict(qs=4095), BAD), (dict(ks=1023), BAD),
+    (dict(vs=1), BAD), (dict(qs=2**62), UNS), (dict(vs=2**60), UNS), (dict(T=2**30), UNS),
+    (dict(k=2 * FAKE + 1), BAD), (dict(slots=FAKE + 4), BAD), (dict(pos=FAKE + 2), BAD),
+    (dict(fa=FAKE + 1), BAD), (dict(qo=8 * FAKE + 8), BAD),
+    # q_out over an input, except q itself where its rows are contiguous
+    (dict(qo=FAKE, qs=4096 + 2048), BAD), (dict(qo=FAKE + 4096), BAD),
+    (dict(qo=2 * FAKE + 16), BAD), (dict(qo=3 * FAKE - 16, T=1), BAD),
+])
+def test_rope_append_refuses(lib, over, status):
+    assert rope(lib, **over) == status
+    assert lib.kap_last_error()
+
+
+def test_rope_append_refuses_pools(lib):
+    assert rope(lib, kv_struct(page=32)) == UNS
+    assert rope(lib, kv_struct(D=96), rot=96) == UNS
+    assert rope(lib, kv_struct(kv_dtype=K.KAP_DT_F32)) == UNS
+    assert rope(lib, kv_struct(kv_dtype=K.KAP_DT_FP8_E4M3FN)) == BAD
+    assert b"kv_scales" in lib.kap_last_error()
+    assert rope(lib, kv_struct(num_pages=0)) == BAD
+    assert rope(lib, T=0, q=None, qo=None, k=None, v=None, slots=None, pos=None, inv=None) == K.KAP_OK
+    assert lib.kap_last_error() == b""
