@@ -23,7 +23,7 @@
  * kap_selected_decode_masked takes token-granular views; kap_append_kv,
  * kap_rope_append_kv and kap_compact_view maintain the pool; kap_fallback_update switches sequences
  * to full-context access (Sec. 3.2, "Runtime stability and fallback");
- * kap_accept_top3 scores draft windows.
+ * kap_sample draws tokens; kap_accept_top3 scores draft windows.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -536,6 +536,38 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
                            size_t workspace_bytes, void *stream);
 
 size_t kap_accept_top3_workspace_bytes(int32_t batch, int32_t window);
+
+/*
+ * kap_sample -- one token per row of logits, drawn with given uniform numbers
+ * after temperature, top-k, top-p and min-p: the proposal's next token, or the
+ * carry token after a window.
+ *
+ * Row r has the weights w_i = exp((x_i - max x) / temperature[r]) and its
+ * tokens in descending order of x_i, equal logits by ascending index. The
+ * filters keep leading runs of that order: the first top_k[r]; the shortest
+ * one that holds top_p[r] of the weight of the top-k run (one token at least);
+ * the tokens with w_i >= min_p[r], that is min_p times the largest probability.
+ * From the shortest of the three, of total weight W, token[r] is the first at
+ * which the running weight exceeds uniform[r] * W, and prob[r] its w_i / W.
+ *   logits [rows][vocab] (F32 or BF16), stride elements between rows; uniform
+ *   [rows] float32 in [0, 1) (limited to it; NaN: 0); temperature, top_p, min_p
+ *   [rows] float32 and top_k [rows] int32, each NULL for "none"; token [rows]
+ *   int32; prob [rows] float32 or NULL.
+ * temperature <= 0 (or NaN): the largest logit, lowest index first, with prob
+ * 1. top_k <= 0 or >= vocab, top_p >= 1 (or NaN) and min_p <= 0 (or NaN) filter
+ * nothing; min_p > 1 counts as 1. A NaN logit counts as -inf, and -inf is never
+ * drawn: a row with nothing else gets token -1, prob 0. If +inf is there, the
+ * tokens that have it share the weight.
+ * Weights are taken in 64 bits and summed as integers, so that a result depends
+ * on its row alone. 1 <= vocab < 2^30, rows <= 65535.
+ */
+kap_status kap_sample(int32_t rows, int32_t vocab, const void *logits, int64_t stride,
+                      kap_dtype logits_dtype, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const float *uniform,
+                      int32_t *token, float *prob, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+size_t kap_sample_workspace_bytes(int32_t rows, int32_t vocab);
 
 /* Static description of a status code. */
 const char *kap_status_string(kap_status status);

@@ -29,6 +29,8 @@ Systems" (arXiv 2607.24260). What is computed, and where it is defined:
   fallback": per cycle, whether a sequence's proposal steps read its plan's
   view or the full context (h from Eq. (5) against s from Eq. (4), the
   margin condition h > s of Eq. (12)), and the view rows that mode reads.
+* ``sample`` -- the draw of a token from logits filtered by temperature,
+  top-k, top-p and min-p (standard definitions, not stated in the paper).
 * ``lse_merge`` -- the exact softmax identity used to combine attention over
   disjoint key sets (a standard identity, not stated in the paper).
 * ``e4m3fn_to_f64`` / ``bf16_to_f64`` -- decoding of stored KV bits (OCP 8-bit
@@ -737,3 +739,55 @@ def accept_top_k(logits: np.ndarray, drafts: np.ndarray, top_k: int = 3):
         m[b] = i
         carry[b] = int(np.argmax(logits[b, i]))
     return m, carry
+
+
+# --------------------------------------------------------------------------
+# Drawing a token
+# --------------------------------------------------------------------------
+
+def sample(row: np.ndarray, u: float, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+           min_p: float = 0.0):
+    """One token of a logits row: (token, its probability among the kept ones,
+    distance). ``distance`` is how far, relative to the kept weight, the
+    nearest boundary between two outcomes lies: by how much the running weights
+    may be off for the same answer (inf for a greedy row).
+
+    Tokens in descending order of their logit (ties: ascending index), weights
+    w = exp((x - max) / temperature). Kept: the shortest of three leading runs --
+    the first top_k; the shortest with top_p of the top-k run's weight; those
+    with w >= min_p. Drawn: the first whose running weight exceeds u times the
+    kept weight. temperature <= 0: the first token. A NaN logit is as -inf;
+    (-1, 0, inf) if nothing is above -inf; with +inf present only such tokens weigh.
+    """
+    x = np.array(row, dtype=np.float64, copy=True)
+    x[np.isnan(x)] = -np.inf
+    order = np.argsort(-x, kind="stable")
+    x = x[order]
+    if x[0] == -np.inf:
+        return -1, 0.0, math.inf
+    if not temperature > 0:
+        return int(order[0]), 1.0, math.inf
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = np.where(x == x[0], 1.0, np.exp((x - x[0]) / float(temperature)))
+    w[x == -np.inf] = 0.0
+    n = len(w)
+    k = top_k if 0 < top_k < n else n
+    kept, near = k, []
+    if top_p < 1:
+        sums = np.cumsum(w[:k])
+        goal = top_p * sums[-1]
+        run = int(np.searchsorted(sums, goal)) + 1
+        kept = min(kept, run)
+        near.append(np.min(np.abs(sums - goal)) / sums[-1])
+    if min_p > 0:
+        least = min(min_p, 1.0)
+        kept = min(kept, int(np.sum(w >= least)))
+        differ = np.abs(w - least)
+        near.append(np.min(differ[differ > 0]) if np.any(differ > 0) else math.inf)
+    sums = np.cumsum(w[:kept])
+    u = min(max(float(u), 0.0), 1.0 - 2.0 ** -24) if u == u else 0.0
+    goal = u * sums[-1]
+    r = min(int(np.searchsorted(sums, goal, side="right")), kept - 1)
+    if u > 0:
+        near.append(np.min(np.abs(sums - goal)) / sums[-1])
+    return int(order[r]), float(w[r] / sums[-1]), float(min(near, default=math.inf))

@@ -1164,6 +1164,62 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
 }
 
 // ---------------------------------------------------------------------------
+// kap_sample
+// ---------------------------------------------------------------------------
+
+size_t kap_sample_workspace_bytes(int32_t rows, int32_t vocab) {
+  if (rows <= 0 || rows > 65535 || vocab < 1 || vocab >= (1 << 30)) return 0;
+  return 0;
+}
+
+kap_status kap_sample(int32_t rows, int32_t vocab, const void *logits, int64_t stride,
+                      kap_dtype logits_dtype, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const float *uniform,
+                      int32_t *token, float *prob, void *workspace, size_t workspace_bytes,
+                      void *stream) {
+  if (rows < 0) return fail(KAP_ERR_INVALID_ARGUMENT, "rows < 0");
+  if (vocab < 1 || vocab >= (1 << 30))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "vocab %d outside [1, 2^30)", vocab);
+  if (logits_dtype != KAP_DT_F32 && logits_dtype != KAP_DT_BF16)
+    return fail(KAP_ERR_UNSUPPORTED, "logits must be F32 or BF16");
+  if (stride < vocab) return fail(KAP_ERR_INVALID_ARGUMENT, "stride is less than vocab");
+  if (rows == 0) return ok();
+  if (rows > 65535) return fail(KAP_ERR_UNSUPPORTED, "rows %d > 65535", rows);
+  if (stride > INT64_MAX / 16 / rows) return fail(KAP_ERR_UNSUPPORTED, "stride is too large");
+  if (!logits || !uniform || !token)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "logits, uniform and token are required");
+  if (!aligned(logits, logits_dtype == KAP_DT_F32 ? 4 : 2) || !aligned(temperature, 4) ||
+      !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(uniform, 4) ||
+      !aligned(token, 4) || !aligned(prob, 4))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "an array is misaligned");
+  const size_t need = kap_sample_workspace_bytes(rows, vocab);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return fail(KAP_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
+  if (need > 0 && !aligned(workspace, 256))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
+  int log2v = 0;
+  while ((1 << log2v) < vocab) ++log2v;
+  kap::SampleArgs a;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.f32 = logits_dtype == KAP_DT_F32;
+  a.bits = 62 - log2v;
+  a.stride = stride;
+  a.logits = logits;
+  a.temperature = temperature;
+  a.top_k = top_k;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.uniform = uniform;
+  a.token = token;
+  a.prob = prob;
+  (void)hipGetLastError();
+  const hipError_t e = kap::launch_sample(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(KAP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+// ---------------------------------------------------------------------------
 // kap_stream_read (measurement helper)
 // ---------------------------------------------------------------------------
 

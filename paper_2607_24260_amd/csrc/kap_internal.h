@@ -187,8 +187,23 @@ struct AcceptArgs {
   unsigned long long *row_best;  // workspace [batch * window], zero between calls
 };
 
+// kap_sample after host validation.
+struct SampleArgs {
+  int rows, vocab, f32;
+  int bits;                      // weights are summed in units of 2^-bits
+  int64_t stride;                // elements between rows
+  const void *logits;
+  const float *temperature;      // [rows] each; NULL: 1, 0, 1, 0
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+  const float *uniform;          // [rows]
+  int32_t *token;                // [rows]
+  float *prob;                   // [rows] or NULL
+};
+
 hipError_t launch_compile_plan(const PlanArgs &a, hipStream_t s);
 hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);
+hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
 hipError_t launch_fallback_update(const FallbackArgs &a, hipStream_t s);
 hipError_t launch_append_kv(const AppendArgs &a, hipStream_t s);
 hipError_t launch_rope_append(const RopeAppendArgs &a, hipStream_t s);

@@ -53,7 +53,8 @@ EXPORTS = (
     "kap_selected_decode_scheduled",
     "kap_verify", "kap_verify_workspace_bytes",
     "kap_append_kv", "kap_rope_append_kv", "kap_compact_view", "kap_fallback_update", "kap_fallback_update_masked",
-    "kap_accept_top3", "kap_accept_top3_workspace_bytes",
+    "kap_accept_top3", "kap_accept_top3_workspace_bytes", "kap_sample",
+    "kap_sample_workspace_bytes",
     "kap_status_string", "kap_last_error", "kap_abi_version",
     "kap_stream_read",
 )
@@ -160,6 +161,10 @@ def load_library(path: str = LIB_PATH):
     lib.kap_accept_top3.argtypes = [_I32, _I32, _I32, _P, _I32, _P, _I32, _P, _P, _P, _SZ, _P]
     lib.kap_accept_top3_workspace_bytes.restype = _SZ
     lib.kap_accept_top3_workspace_bytes.argtypes = [_I32, _I32]
+    lib.kap_sample.restype = _I32
+    lib.kap_sample.argtypes = [_I32, _I32, _P, _I64, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]
+    lib.kap_sample_workspace_bytes.restype = _SZ
+    lib.kap_sample_workspace_bytes.argtypes = [_I32, _I32]
     lib.kap_stream_read.restype = _I32
     lib.kap_stream_read.argtypes = [_P, _SZ, _P, _P]
     lib.kap_status_string.restype = ctypes.c_char_p
@@ -525,6 +530,80 @@ def accept_top3(logits, draft_tokens, top_k: int = 3, accepted=None, carry=None,
                                _ptr(accepted), _ptr(carry), _ptr(workspace), have,
                                _stream(stream)))
     return accepted, carry
+
+
+# --------------------------------------------------------------------------
+# kap_sample
+# --------------------------------------------------------------------------
+
+def sample_workspace_bytes(rows: int, vocab: int) -> int:
+    return int(load_library().kap_sample_workspace_bytes(rows, vocab))
+
+
+def _sample_call(logits, uniform, temperature, top_k, top_p, min_p, token, prob, workspace,
+                 stream):
+    """Validate and marshal one kap_sample call: (args, (token, prob), keep)."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise ValueError("logits must be a tensor [rows][vocab]")
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("logits must be float32 or bfloat16")
+    R, V = logits.shape
+    stride = _rows(logits, "logits", logits.dtype, (R, V))
+    _dev(uniform, "uniform", torch.float32, 1)
+    if uniform.shape[0] != R:
+        raise ValueError(f"uniform must have {R} entries")
+    for name, t, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                        ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32),
+                        ("token", token, torch.int32), ("prob", prob, torch.float32)):
+        if t is not None:
+            _dev(t, name, dt, 1)
+            if t.shape[0] != R:
+                raise ValueError(f"{name} must have {R} entries")
+    dev = logits.device
+    need = sample_workspace_bytes(R, V)
+    if token is None or prob is None or (workspace is None and need):
+        with torch.cuda.stream(stream):
+            token = torch.empty(R, dtype=torch.int32, device=dev) if token is None else token
+            prob = torch.empty(R, dtype=torch.float32, device=dev) if prob is None else prob
+            workspace, _ = _workspace(need, dev, workspace)
+    have = 0
+    if workspace is not None:
+        _dev(workspace, "workspace")
+        have = workspace.numel() * workspace.element_size()
+    keep = (logits, uniform, temperature, top_k, top_p, min_p, token, prob, workspace)
+    _here(*keep, stream=stream)
+    dt = KAP_DT_F32 if logits.dtype == torch.float32 else KAP_DT_BF16
+    args = (R, V, _ptr(logits), stride, dt, _ptr(temperature), _ptr(top_k), _ptr(top_p),
+            _ptr(min_p), _ptr(uniform), _ptr(token), _ptr(prob), _ptr(workspace), have,
+            _stream(stream))
+    return args, (token, prob), keep
+
+
+def sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min_p=None, token=None,
+           prob=None, workspace=None, stream=None):
+    """Draw one token per row of ``logits`` [rows][vocab] (float32 / bfloat16;
+    rows may lie apart) with the uniform numbers ``uniform`` [rows], after
+    temperature, top-k, top-p and min-p (a tensor [rows] each, or None). Returns
+    (token [rows] int32, prob [rows] float32: its probability among the kept
+    tokens); see kap.h."""
+    args, res, _ = _sample_call(logits, uniform, temperature, top_k, top_p, min_p, token, prob,
+                                workspace, stream)
+    _check(load_library().kap_sample(*args))
+    return res
+
+
+def bind_sample(logits, uniform, *, token, prob, workspace=None, temperature=None, top_k=None,
+                top_p=None, min_p=None, stream=None) -> "BoundCall":
+    """sample marshalled once (and run once here) for tight loops and graph capture."""
+    need = sample_workspace_bytes(*logits.shape)
+    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if need > have:
+        raise ValueError(f"workspace of {need} bytes required")
+    args, _, keep = _sample_call(logits, uniform, temperature, top_k, top_p, min_p, token, prob,
+                                 workspace, stream)
+    fn = load_library().kap_sample
+    _check(fn(*args))                                             # validates once
+    return BoundCall(fn, args, keep)
 
 
 # --------------------------------------------------------------------------

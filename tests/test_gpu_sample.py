@@ -1,0 +1,208 @@
+"""GPU parity of kap_sample with the oracle: the same token, and its probability
+to single precision.
+
+A token may differ only where two outcomes lie closer together than the running
+weights are exact: each weight is rounded to half a unit of 2^-(62 - ceil(log2 n))
+of the largest one, n of them are added, and the kept weight is at least 1:
+2^2 n^2 2^-63 with n rounded up to a power of two, plus 2^-45 for the 64-bit
+exponentials and products (over a hundred half steps of 2^-53). Rows whose
+nearest boundary (the oracle's distance) is closer are not compared; at the sizes
+here there is hardly one.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kap_oracle as O
+from paper_2607_24260_amd import kap as K
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def exactness(n):
+    return 4.0 * n * n * 2.0 ** -63 + 2.0 ** -45
+
+
+def check(x, u, t=None, k=None, p=None, q=None, least=0.97, **kw):
+    """Compares with the oracle; x a GPU tensor [rows][vocab], the rest lists or None."""
+    dev = lambda v, dt=torch.float32: None if v is None else torch.as_tensor(
+        np.asarray(v)).to(dt).cuda()
+    args = dict(temperature=dev(t), top_k=dev(k, torch.int32), top_p=dev(p), min_p=dev(q))
+    before = x.clone()
+    token, prob = K.sample(x, dev(u), **args, **kw)
+    torch.cuda.synchronize()
+    raw = lambda y: y.contiguous().view(torch.int16 if y.dtype == torch.bfloat16 else torch.int32)
+    assert torch.equal(raw(x), raw(before))
+    token, prob, xs = token.cpu().numpy(), prob.cpu().numpy(), x.float().cpu().numpy()
+    f32 = lambda v, i, none: none if v is None else float(np.float32(v[i]))
+    compared = 0
+    for i in range(len(xs)):
+        want, wp, far = O.sample(xs[i], f32(u, i, 0), f32(t, i, 1.0), 0 if k is None else int(k[i]),
+                                 f32(p, i, 1.0), f32(q, i, 0.0))
+        if far < exactness(xs.shape[1]):
+            continue
+        compared += 1
+        assert token[i] == want, (i, token[i], want, far)
+        assert abs(prob[i] - wp) <= 2.0 ** -23 * wp + exactness(xs.shape[1]) * wp
+    assert compared >= least * len(xs)
+    return token, prob
+
+
+def logits(rows, vocab, dtype, seed, spread=2.5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((rows, vocab), generator=g, device="cuda") * spread
+    at = torch.randint(0, vocab, (rows, 8), generator=g, device="cuda")
+    x.scatter_add_(1, at, torch.rand((rows, 8), generator=g, device="cuda") * 12)
+    return x.to(DT[dtype])
+
+
+def mixed(rows, vocab, rng):
+    return dict(t=rng.choice([0.0, 0.2, 0.7, 1.0, 1.4, 30.0], rows),
+                k=rng.choice([-1, 0, 1, 2, 40, vocab - 1, vocab, vocab + 9], rows),
+                p=rng.choice([0.0, 1e-6, 0.3, 0.9, 0.99, 1.0, 1.5], rows),
+                q=rng.choice([-1.0, 0.0, 0.01, 0.1, 0.7, 1.0, 3.0], rows))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, vocab", [(5, 1), (9, 2), (33, 63), (64, 1000), (40, 4097), (24, 32000),
+                                         (7, 151937)])
+def test_mixed_parameters(dtype, rows, vocab):
+    rng = np.random.default_rng(vocab)
+    check(logits(rows, vocab, dtype, vocab + 1), rng.random(rows), **mixed(rows, vocab, rng))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("which", ["none", "t", "k", "p", "q"])
+def test_one_filter(dtype, which):
+    rng = np.random.default_rng(3)
+    rows, vocab = 48, 5003
+    par = dict(t=rng.uniform(0.3, 2, rows), k=rng.integers(1, 400, rows), p=rng.uniform(0.1, 1, rows),
+               q=rng.uniform(0, 0.3, rows))
+    check(logits(rows, vocab, dtype, 4), rng.random(rows),
+          **({} if which == "none" else {which: par[which]}))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_flat_rows(dtype):
+    # every token about as likely as every other: the boundaries are close together
+    rng = np.random.default_rng(4)
+    x = logits(32, 50021, dtype, 5, spread=0.1)
+    check(x, rng.random(32), t=[5.0] * 32, p=rng.uniform(0.2, 1, 32))
+    check(x, rng.random(32), t=[0.01] * 32)                       # and the opposite
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [7, 300, 9001, 40000])
+def test_equal_logits(dtype, vocab):
+    # a few values only, and one: ties go to the lowest index
+    rng = np.random.default_rng(6)
+    rows = 24
+    x = torch.as_tensor(rng.integers(-2, 3, (rows, vocab))).to(DT[dtype]).cuda()
+    x[:6] = 1.25
+    x[6, ::2] = -0.0
+    x[6, 1::2] = 0.0
+    # (with whole weights, boundaries are met exactly: the uniform numbers keep off them)
+    u = (rng.integers(0, 1000, rows) + 0.37) / 1000.1
+    check(x, u, k=rng.integers(0, vocab, rows), t=rng.choice([0.0, 0.5, 1.0], rows))
+    check(x, u, p=rng.uniform(0.1, 1, rows), q=rng.uniform(0, 1, rows), least=0.9)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_masked_and_not_finite(dtype):
+    inf, nan, low = math.inf, math.nan, torch.finfo(DT[dtype]).min
+    x = logits(12, 2000, dtype, 7)
+    x[0] = -inf
+    x[1] = nan
+    x[2] = -inf
+    x[2, 1234] = -5.0
+    x[3, :1990] = -inf
+    x[4, ::3] = nan
+    x[5, [3, 77, 1999]] = inf
+    x[6] = low
+    x[7, 5:] = low
+    x[8] = -inf
+    x[8, 1999] = nan
+    x[9, :] = low
+    x[9, 3] = -inf
+    x[10, 1::2] = -inf
+    rng = np.random.default_rng(8)
+    for _ in range(4):
+        token, prob = check(x, rng.random(12), **mixed(12, 2000, rng))
+        assert token[0] == token[1] == token[8] == -1 and prob[0] == prob[1] == prob[8] == 0
+        assert token[2] == 1234 and prob[2] == 1
+    token, _ = check(x, rng.random(12), t=[0.0] * 12)
+    assert token[5] == 3 and token[6] == 0
+
+
+def test_edges_of_the_parameters():
+    nan, inf = math.nan, math.inf
+    x = logits(1, 3000, "f32", 9).expand(40, -1).contiguous()
+    x[20:] = logits(1, 3000, "bf16", 10).float()
+    u = [0.0, 1.0, 2.0, -1.0, nan, inf, 1 - 2.0 ** -24, 1e-30, 0.5, 0.25] * 4
+    check(x, u)
+    check(x, u, t=[nan, inf, -1.0, 1e-30, 1e-40, 1e30, 0.0, -0.0, 1.0, -inf] * 4)
+    check(x, u, p=[nan, inf, -1.0, 1e-30, 0.0, 1.0, 2.0, 0.5, 0.999999, -inf] * 4)
+    check(x, u, q=[nan, inf, -1.0, 1e-30, 0.0, 1.0, 2.0, 0.5, 0.999999, -inf] * 4)
+    check(x, u, k=[0, -2**31, 2**31 - 1, 1, 3000, 3001, 2999, 2, 64, 65] * 4)
+
+
+def test_rows_that_lie_apart():
+    buf = logits(30, 3001, "bf16", 11)
+    rng = np.random.default_rng(12)
+    check(buf[:, 1:2500], rng.random(30), **mixed(30, 2499, rng))
+    check(logits(1, 3001, "f32", 13)[:, 3:], rng.random(1))
+    x = logits(12, 700, "f32", 14).view(4, 3, 700)[:, 1]           # one position of each window
+    check(x, rng.random(4), **mixed(4, 700, rng))
+
+
+def test_rows_do_not_depend_on_each_other():
+    rng = np.random.default_rng(15)
+    x = logits(70, 20000, "bf16", 16)
+    par = {n: torch.as_tensor(v).to(dt).cuda() for (n, v), dt in zip(
+        zip(("temperature", "top_k", "top_p", "min_p"), mixed(70, 20000, rng).values()),
+        (torch.float32, torch.int32, torch.float32, torch.float32))}
+    u = torch.rand(70, device="cuda")
+    token, prob = K.sample(x, u, **par)
+    for a, b in ((0, 1), (13, 20), (69, 70)):
+        t, p = K.sample(x[a:b], u[a:b], **{n: v[a:b] for n, v in par.items()})
+        assert torch.equal(t, token[a:b]) and torch.equal(p, prob[a:b])
+
+
+def test_replayed_graph_on_another_stream():
+    x = logits(20, 10007, "bf16", 17)
+    u = torch.rand(20, device="cuda")
+    p = torch.full((20,), 0.9, device="cuda")
+    token = torch.zeros(20, dtype=torch.int32, device="cuda")
+    prob = torch.zeros(20, device="cuda")
+    ws = torch.zeros(max(256, K.sample_workspace_bytes(20, 10007)), dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    call = K.bind_sample(x, u, token=token, prob=prob, top_p=p, workspace=ws, stream=s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        call()
+    for i in range(4):
+        u.uniform_()
+        x.copy_(logits(20, 10007, "bf16", 18 + i))
+        token.zero_(), prob.zero_()
+        g.replay()
+        want = K.sample(x, u, top_p=p)
+        torch.cuda.synchronize()
+        assert torch.equal(token, want[0]) and torch.equal(prob, want[1])
+
+
+def test_binding_refuses():
+    x, u = torch.zeros((4, 50), device="cuda"), torch.zeros(4, device="cuda")
+    good = dict(logits=x, uniform=u)
+    for over in (dict(logits=x[0]), dict(logits=x.half()), dict(logits=x.cpu()), dict(logits=x.T),
+                 dict(logits=x[:1].expand(4, 50)), dict(uniform=u[:3]), dict(uniform=u.double()),
+                 dict(temperature=u[:1]), dict(top_k=u), dict(top_p=u.cpu()), dict(min_p=x),
+                 dict(token=u), dict(prob=u[:2])):
+        with pytest.raises((ValueError, TypeError, K.KapError)):
+            K.sample(**{**good, **over})
+    token, prob = K.sample(x[:0], u[:0])
+    assert token.shape == prob.shape == (0,)

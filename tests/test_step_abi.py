@@ -63,3 +63,32 @@ def test_rope_append_refuses_pools(lib):
     assert rope(lib, kv_struct(num_pages=0)) == BAD
     assert rope(lib, T=0, q=None, qo=None, k=None, v=None, slots=None, pos=None, inv=None) == K.KAP_OK
     assert lib.kap_last_error() == b""
+
+
+def draw(lib, **over):
+    a = dict(rows=4, vocab=1000, x=FAKE, stride=1000, dt=K.KAP_DT_BF16, t=FAKE, k=FAKE, p=FAKE, q=FAKE,
+             u=FAKE, token=FAKE, prob=FAKE, ws="enough", have=None)
+    assert set(over) <= set(a)
+    a.update(over)
+    need = lib.kap_sample_workspace_bytes(max(a["rows"], 0), max(a["vocab"], 0))
+    ws = FAKE if a["ws"] == "enough" else a["ws"]
+    have = need if a["have"] is None else a["have"]
+    return lib.kap_sample(a["rows"], a["vocab"], a["x"], a["stride"], a["dt"], a["t"], a["k"], a["p"],
+                          a["q"], a["u"], a["token"], a["prob"], ws, have, None)
+
+
+@pytest.mark.parametrize("over, status", [
+    (dict(rows=-1), BAD), (dict(vocab=0), BAD), (dict(vocab=1 << 30, stride=1 << 30), BAD),
+    (dict(dt=K.KAP_DT_FP8_E4M3FN), UNS), (dict(stride=999), BAD), (dict(rows=65536), UNS),
+    (dict(stride=2**61), UNS), (dict(x=None), BAD), (dict(u=None), BAD), (dict(token=None), BAD),
+    (dict(x=FAKE + 1), BAD), (dict(x=FAKE + 2, dt=K.KAP_DT_F32), BAD), (dict(t=FAKE + 2), BAD),
+    (dict(k=FAKE + 1), BAD), (dict(prob=FAKE + 2), BAD),
+])
+def test_sample_refuses(lib, over, status):
+    assert draw(lib, **over) == status
+    assert lib.kap_last_error()
+
+
+def test_sample_of_no_rows(lib):
+    assert draw(lib, rows=0, x=None, u=None, token=None) == K.KAP_OK
+    assert lib.kap_sample_workspace_bytes(0, 1000) == lib.kap_sample_workspace_bytes(4, 0) == 0
