@@ -373,6 +373,35 @@ size_t kap_verify_workspace_bytes(const kap_kv_cache *kv, int32_t batch, int32_t
                                   int32_t max_seq_len, int32_t num_splits);
 
 /*
+ * kap_verify_shared -- kap_verify for sequences that share leading pages:
+ * requests over one document, samples of one prompt. The shared pages are read
+ * once for all sequences of a group rather than once each; with q_len = 1 it is
+ * their full-context decode step.
+ *
+ * Group i holds the sequences group_offsets[i] .. group_offsets[i + 1] - 1, and
+ * the first shared_blocks[i] pages of all of them are those that the table row
+ * of its first sequence names (the other rows are not read there). Sequences in
+ * no group share nothing. Everything else is as for kap_verify: window row r of
+ * sequence b sees positions 0 .. seq_lens[b] - q_len + r, so that a sequence
+ * that ends within the shared pages sees only its part of them, and the results
+ * are kap_verify's to rounding.
+ *   group_offsets [num_groups + 1] int32, ascending within [0, batch] (other
+ *   values: unspecified results); shared_blocks [num_groups] int32, limited to
+ *   [0, ceil(max_seq_len / 16)]; both NULL only if num_groups = 0. 0 <=
+ *   num_groups <= batch. The other arguments are kap_verify's; 1 <= q_len <= 16.
+ * The workspace holds scratch only (no counters: its contents do not matter).
+ */
+kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_len, const void *q,
+                             const int32_t *seq_lens, const int32_t *full_block_table,
+                             int32_t fbt_stride, int32_t max_seq_len, int32_t num_groups,
+                             const int32_t *group_offsets, const int32_t *shared_blocks,
+                             float sm_scale, float *out, float *lse, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+size_t kap_verify_shared_workspace_bytes(const kap_kv_cache *kv, int32_t batch, int32_t q_len,
+                                         int32_t max_seq_len, int32_t num_groups);
+
+/*
  * kap_append_kv -- place newly scheduled tokens' K/V into their physical KV
  * slots (the slot mapping of Sec. 3.1, "Selected-KV view materialization"):
  * how verification advances the full-context KV state KV^{full,+} of Sec. 3.2

@@ -842,6 +842,125 @@ kap_status kap_verify(const kap_kv_cache *kv, int32_t batch, int32_t q_len, cons
 }
 
 // ---------------------------------------------------------------------------
+// kap_verify_shared
+// ---------------------------------------------------------------------------
+
+// Sizes of a call's work map and workspace: [parts of groups][parts of
+// sequences][partial o][partial lse].
+struct SharedPlan {
+  int shared_rows, own_rows, target, least;
+  long long slots_shared, slots_own;           // bounds on the parts of either kind
+  long long part_rows;
+  size_t seq_parts, part_o, part_lse, total;
+};
+
+static SharedPlan plan_shared(const kap_kv_cache *kv, int batch, int q_len, int num_groups) {
+  SharedPlan p;
+  const long long per = (long long)q_len * (kv->num_q_heads / kv->num_kv_heads);
+  const long long rows = per * batch;
+  p.shared_rows = 32;
+  p.own_rows = (int)std::min<long long>(32, per);
+  p.target = 2 * device_cus();
+  p.least = 8;
+  const long long blocks = rows / p.shared_rows + num_groups;
+  p.slots_shared = num_groups ? p.target + blocks * kv->num_kv_heads : 0;
+  p.slots_own = p.target + (long long)batch * cdiv(per, p.own_rows) * kv->num_kv_heads;
+  p.part_rows = p.slots_shared * p.shared_rows + p.slots_own * p.own_rows;
+  const size_t part_rows = (size_t)p.part_rows;
+  p.seq_parts = round_up((size_t)num_groups * sizeof(kap::PartsOf), 256);
+  p.part_o = p.seq_parts + round_up((size_t)batch * sizeof(kap::PartsOf), 256);
+  p.part_lse = p.part_o + round_up(part_rows * kv->head_dim * sizeof(float), 256);
+  p.total = p.part_lse + round_up(part_rows * sizeof(float), 256);
+  return p;
+}
+
+size_t kap_verify_shared_workspace_bytes(const kap_kv_cache *kv, int32_t batch, int32_t q_len,
+                                         int32_t max_seq_len, int32_t num_groups) {
+  if (check_kv(kv) != KAP_OK || batch <= 0 || batch > 65535 || q_len < 1 || q_len > 16 ||
+      max_seq_len < 0 || num_groups < 0 || num_groups > batch)
+    return 0;
+  return plan_shared(kv, batch, q_len, num_groups).total;
+}
+
+kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_len, const void *q,
+                             const int32_t *seq_lens, const int32_t *full_block_table,
+                             int32_t fbt_stride, int32_t max_seq_len, int32_t num_groups,
+                             const int32_t *group_offsets, const int32_t *shared_blocks,
+                             float sm_scale, float *out, float *lse, void *workspace,
+                             size_t workspace_bytes, void *stream) {
+  kap_status st = check_kv(kv);
+  if (st != KAP_OK) return st;
+  if (batch < 0) return fail(KAP_ERR_INVALID_ARGUMENT, "batch < 0");
+  if (batch > 65535) return fail(KAP_ERR_UNSUPPORTED, "batch %d > 65535", batch);
+  if (q_len < 1 || q_len > 16) return fail(KAP_ERR_INVALID_ARGUMENT, "q_len %d outside [1, 16]", q_len);
+  if (max_seq_len < 0) return fail(KAP_ERR_INVALID_ARGUMENT, "max_seq_len < 0");
+  const int max_pages = cdiv(max_seq_len, 16);
+  if (fbt_stride < max_pages)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "fbt_stride %d < ceil(max_seq_len/16) = %d", fbt_stride, max_pages);
+  if (num_groups < 0 || num_groups > batch)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "num_groups %d outside [0, batch = %d]", num_groups, batch);
+  if (!(sm_scale == sm_scale) || sm_scale > 3.0e38f || sm_scale < -3.0e38f)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "sm_scale must be finite");
+  if ((long long)q_len * kv->num_q_heads > 65535) return fail(KAP_ERR_UNSUPPORTED, "too many rows");
+  if ((long long)batch * q_len * kv->num_q_heads > 0x3fffffff)
+    return fail(KAP_ERR_UNSUPPORTED, "batch * q_len * num_q_heads too large");
+  if (batch == 0) return ok();
+  if (kv->num_pages < 1) return fail(KAP_ERR_INVALID_ARGUMENT, "KV pool has no pages");
+  if (!q || !seq_lens || !out || !lse) return fail(KAP_ERR_INVALID_ARGUMENT, "a required pointer is NULL");
+  if (max_pages > 0 && !full_block_table)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "full_block_table is NULL");
+  if (num_groups > 0 && (!group_offsets || !shared_blocks))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "group_offsets / shared_blocks is NULL");
+  if (!aligned(q, 16) || !aligned(out, 16))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "q and out must be 16-byte aligned");
+  const SharedPlan p = plan_shared(kv, batch, q_len, num_groups);
+  if (!workspace || workspace_bytes < p.total)
+    return fail(KAP_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", p.total, workspace_bytes);
+  if (!aligned(workspace, 256))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
+  char *base = static_cast<char *>(workspace);
+  kap::SharedArgs a;
+  a.batch = batch;
+  a.Hq = kv->num_q_heads;
+  a.Hkv = kv->num_kv_heads;
+  a.G = kv->num_q_heads / kv->num_kv_heads;
+  a.D = kv->head_dim;
+  a.kv_type = kv->kv_dtype;
+  a.q_len = q_len;
+  a.k_pages = kv->k_pages;
+  a.v_pages = kv->v_pages;
+  a.kv_scales = kv->kv_scales;
+  a.num_pages = kv->num_pages;
+  a.q = q;
+  a.seq_lens = seq_lens;
+  a.table = full_block_table;
+  a.stride = fbt_stride;
+  a.max_pages = max_pages;
+  a.num_groups = num_groups;
+  a.offsets = group_offsets;
+  a.shared = shared_blocks;
+  a.scale_log2 = sm_scale * kap::kLog2e;
+  a.shared_rows = p.shared_rows;
+  a.own_rows = p.own_rows;
+  a.shared_cost = 1;
+  a.own_cost = 1;
+  a.target = p.target;
+  a.least = p.least;
+  a.grid = p.slots_shared + p.slots_own - (num_groups ? p.target : 0);
+  a.part_rows = p.part_rows;
+  a.group_parts = reinterpret_cast<kap::PartsOf *>(base);
+  a.seq_parts = reinterpret_cast<kap::PartsOf *>(base + p.seq_parts);
+  a.part_o = reinterpret_cast<float *>(base + p.part_o);
+  a.part_lse = reinterpret_cast<float *>(base + p.part_lse);
+  a.out = out;
+  a.lse = lse;
+  (void)hipGetLastError();
+  const hipError_t e = kap::launch_attn_shared(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(KAP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+// ---------------------------------------------------------------------------
 // kap_append_kv / kap_compact_view
 // ---------------------------------------------------------------------------
 

@@ -187,6 +187,34 @@ struct AcceptArgs {
   unsigned long long *row_best;  // workspace [batch * window], zero between calls
 };
 
+// kap_verify_shared after host validation. Partial rows of a unit (a group's
+// shared pages, a sequence's own): [row block][KV head][split][rows of a block],
+// from row0 on.
+struct PartsOf {
+  int64_t row0;
+  int32_t n, unused;             // splits
+};
+struct SharedArgs {
+  int batch, Hq, Hkv, G, D, kv_type, q_len;
+  const void *k_pages, *v_pages;
+  const float *kv_scales;
+  int64_t num_pages;
+  const void *q;                 // [batch][q_len][Hq][D]
+  const int32_t *seq_lens, *table;
+  int stride, max_pages;
+  int num_groups;
+  const int32_t *offsets;        // [num_groups + 1]
+  const int32_t *shared;         // [num_groups] shared pages
+  float scale_log2;              // sm_scale * log2(e)
+  int shared_rows, own_rows;     // rows of a block
+  int shared_cost, own_cost;     // of a step
+  int target, least;             // workgroups the work is spread over; least cost of one
+  int64_t grid, part_rows;       // workgroups; rows of the partials
+  PartsOf *group_parts, *seq_parts;
+  float *part_o, *part_lse;      // [rows][D], [rows]: normalised, log2 domain
+  float *out, *lse;
+};
+
 // kap_sample after host validation.
 struct SampleArgs {
   int rows, vocab, f32;
@@ -203,6 +231,7 @@ struct SampleArgs {
 
 hipError_t launch_compile_plan(const PlanArgs &a, hipStream_t s);
 hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);
+hipError_t launch_attn_shared(const SharedArgs &a, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
 hipError_t launch_fallback_update(const FallbackArgs &a, hipStream_t s);
 hipError_t launch_append_kv(const AppendArgs &a, hipStream_t s);

@@ -52,6 +52,7 @@ EXPORTS = (
     "kap_selected_decode_noalloc", "kap_decode_schedule_bytes", "kap_decode_schedule",
     "kap_selected_decode_scheduled",
     "kap_verify", "kap_verify_workspace_bytes",
+    "kap_verify_shared", "kap_verify_shared_workspace_bytes",
     "kap_append_kv", "kap_rope_append_kv", "kap_compact_view", "kap_fallback_update", "kap_fallback_update_masked",
     "kap_accept_top3", "kap_accept_top3_workspace_bytes", "kap_sample",
     "kap_sample_workspace_bytes",
@@ -138,6 +139,13 @@ def load_library(path: str = LIB_PATH):
         _P, _P, _P, _SZ, _P]
     lib.kap_verify_workspace_bytes.restype = _SZ
     lib.kap_verify_workspace_bytes.argtypes = [
+        ctypes.POINTER(KVCacheStruct), _I32, _I32, _I32, _I32]
+    lib.kap_verify_shared.restype = _I32
+    lib.kap_verify_shared.argtypes = [
+        ctypes.POINTER(KVCacheStruct), _I32, _I32, _P, _P, _P, _I32, _I32, _I32, _P, _P, _F,
+        _P, _P, _P, _SZ, _P]
+    lib.kap_verify_shared_workspace_bytes.restype = _SZ
+    lib.kap_verify_shared_workspace_bytes.argtypes = [
         ctypes.POINTER(KVCacheStruct), _I32, _I32, _I32, _I32]
     lib.kap_append_kv.restype = _I32
     lib.kap_append_kv.argtypes = [ctypes.POINTER(KVCacheStruct), _I32, _P, _P, _P, _P, _P]
@@ -898,6 +906,63 @@ def verify(kv: KVCache, q, seq_lens, full_block_table, max_seq_len: int, sm_scal
     return out, lse
 
 
+def verify_shared_workspace_bytes(kv: KVCache, batch: int, q_len: int, max_seq_len: int,
+                                  num_groups: int) -> int:
+    return int(load_library().kap_verify_shared_workspace_bytes(
+        ctypes.byref(kv.struct), batch, q_len, max_seq_len, num_groups))
+
+
+def _verify_shared_call(kv: KVCache, q, seq_lens, full_block_table, max_seq_len, group_offsets,
+                        shared_blocks, sm_scale, out, lse, workspace, stream):
+    """Validate and marshal one kap_verify_shared call: (args, (out, lse), keep)."""
+    _dev(q, "q", kv.q_dtype, 4)
+    B, q_len = q.shape[0], q.shape[1]
+    if tuple(q.shape[2:]) != (kv.num_q_heads, kv.head_dim):
+        raise ValueError("q must be [batch][q_len][num_q_heads][head_dim]")
+    _dev(seq_lens, "seq_lens", torch.int32, 1)
+    _dev(full_block_table, "full_block_table", torch.int32, 2)
+    if seq_lens.shape[0] != B or full_block_table.shape[0] != B:
+        raise ValueError("seq_lens / full_block_table must have batch rows")
+    _dev(group_offsets, "group_offsets", torch.int32, 1)
+    _dev(shared_blocks, "shared_blocks", torch.int32, 1)
+    N = int(shared_blocks.shape[0])
+    if group_offsets.shape[0] != N + 1:
+        raise ValueError("group_offsets must have an entry more than shared_blocks")
+    if N > B:
+        raise ValueError(f"{N} groups of {B} sequences")
+    need = verify_shared_workspace_bytes(kv, B, q_len, max_seq_len, N)
+    shape = (B, q_len, kv.num_q_heads, kv.head_dim)
+    with torch.cuda.stream(stream):
+        out, lse = _outputs(shape, q.device, out, lse)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    have = 0
+    if workspace is not None:
+        _dev(workspace, "workspace")
+        have = workspace.numel() * workspace.element_size()
+    keep = (kv, q, seq_lens, full_block_table, group_offsets, shared_blocks, out, lse, workspace)
+    _here(kv.k_pages, *keep[1:], stream=stream)
+    args = (ctypes.byref(kv.struct), B, q_len, _ptr(q), _ptr(seq_lens), _ptr(full_block_table),
+            full_block_table.shape[1], int(max_seq_len), N, _ptr(group_offsets),
+            _ptr(shared_blocks), float(sm_scale), _ptr(out), _ptr(lse), _ptr(workspace), have,
+            _stream(stream))
+    return args, (out, lse), keep
+
+
+def verify_shared(kv: KVCache, q, seq_lens, full_block_table, max_seq_len: int, group_offsets,
+                  shared_blocks, sm_scale: float, *, out=None, lse=None, workspace=None,
+                  stream=None):
+    """verify for sequences in groups that share leading pages (int32
+    ``group_offsets`` [groups + 1], ``shared_blocks`` [groups]): those are read
+    once per group, through its first sequence's table row. q [B][q_len][Hq][D],
+    q_len 1 for a decode step; returns (out, lse) as verify does, to rounding."""
+    args, res, _ = _verify_shared_call(kv, q, seq_lens, full_block_table, max_seq_len,
+                                       group_offsets, shared_blocks, sm_scale, out, lse,
+                                       workspace, stream)
+    _check(load_library().kap_verify_shared(*args))
+    return res
+
+
 def stream_read(buf, sink, stream=None):
     """kap_stream_read (measurement helper): read every byte of the device
     tensor ``buf`` once with a plain streaming kernel, XOR-folding its words
@@ -963,6 +1028,22 @@ def bind_verify(kv: KVCache, q, seq_lens, full_block_table, max_seq_len: int, sm
             _stream(stream))
     return BoundCall(lib.kap_verify, args,
                      (kv, q, seq_lens, full_block_table, out, lse, workspace))
+
+
+def bind_verify_shared(kv: KVCache, q, seq_lens, full_block_table, max_seq_len: int,
+                       group_offsets, shared_blocks, sm_scale: float, out, lse, workspace, *,
+                       stream=None) -> BoundCall:
+    need = verify_shared_workspace_bytes(kv, q.shape[0], q.shape[1], max_seq_len,
+                                         shared_blocks.shape[0])
+    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if need > have:
+        raise ValueError(f"workspace of {need} bytes required")
+    args, _, keep = _verify_shared_call(kv, q, seq_lens, full_block_table, max_seq_len,
+                                        group_offsets, shared_blocks, sm_scale, out, lse,
+                                        workspace, stream)
+    fn = load_library().kap_verify_shared
+    _check(fn(*args))                                             # validates once
+    return BoundCall(fn, args, keep)
 
 
 def bind_compile_plan(seq_lens, full_block_table, span_offsets, span_start, span_len,

@@ -92,3 +92,46 @@ def test_sample_refuses(lib, over, status):
 def test_sample_of_no_rows(lib):
     assert draw(lib, rows=0, x=None, u=None, token=None) == K.KAP_OK
     assert lib.kap_sample_workspace_bytes(0, 1000) == lib.kap_sample_workspace_bytes(4, 0) == 0
+
+
+def shared(lib, kv=None, **over):
+    a = dict(B=4, w=5, q=FAKE, lens=FAKE, table=FAKE, stride=64, most=1024, groups=2, off=FAKE, blocks=FAKE,
+             scale=1.0, out=FAKE, lse=FAKE, ws=FAKE, have=None)
+    assert set(over) <= set(a)
+    a.update(over)
+    kv = kv or kv_struct()
+    have = a["have"]
+    if have is None:
+        have = lib.kap_verify_shared_workspace_bytes(ctypes.byref(kv), a["B"], a["w"], a["most"],
+                                                     a["groups"])
+    return lib.kap_verify_shared(ctypes.byref(kv), a["B"], a["w"], a["q"], a["lens"], a["table"],
+                                 a["stride"], a["most"], a["groups"], a["off"], a["blocks"],
+                                 a["scale"], a["out"], a["lse"], a["ws"], have, None)
+
+
+@pytest.mark.parametrize("over, status", [
+    (dict(B=-1), BAD), (dict(B=65536), UNS), (dict(w=0), BAD), (dict(w=17), BAD), (dict(most=-1), BAD),
+    (dict(stride=63), BAD), (dict(groups=-1), BAD), (dict(groups=5), BAD), (dict(q=None), BAD),
+    (dict(lens=None), BAD), (dict(table=None), BAD), (dict(off=None), BAD), (dict(blocks=None), BAD),
+    (dict(out=None), BAD), (dict(lse=None), BAD), (dict(scale=float("nan")), BAD),
+    (dict(scale=float("inf")), BAD), (dict(q=FAKE + 8), BAD), (dict(out=FAKE + 4), BAD),
+    (dict(ws=None), K.KAP_ERR_WORKSPACE_TOO_SMALL), (dict(have=1000), K.KAP_ERR_WORKSPACE_TOO_SMALL),
+    (dict(ws=FAKE + 128), BAD),
+])
+def test_verify_shared_refuses(lib, over, status):
+    assert shared(lib, **over) == status
+    assert lib.kap_last_error()
+
+
+def test_verify_shared_pools_and_empty_batch(lib):
+    assert shared(lib, kv_struct(page=32)) == UNS
+    assert shared(lib, kv_struct(D=96)) == UNS
+    assert shared(lib, kv_struct(num_pages=0)) == BAD
+    assert shared(lib, kv_struct(Hq=4096, Hkv=1), w=16) == UNS
+    assert shared(lib, kv_struct(Hq=2048, Hkv=1), B=65535, w=16, have=0) == UNS
+    assert shared(lib, kv_struct(kv_dtype=K.KAP_DT_FP8_E4M3FN)) == BAD
+    assert shared(lib, B=0, groups=0, q=None, lens=None, table=None) == K.KAP_OK
+    size = lib.kap_verify_shared_workspace_bytes
+    kv = kv_struct()
+    assert size(ctypes.byref(kv), 0, 5, 1024, 0) == size(ctypes.byref(kv), 4, 17, 1024, 1) == 0
+    assert 0 < size(ctypes.byref(kv), 4, 5, 1024, 1) <= size(ctypes.byref(kv), 8, 5, 1024, 2)
