@@ -1288,7 +1288,7 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
 
 size_t kap_sample_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows <= 0 || rows > 65535 || vocab < 1 || vocab >= (1 << 30)) return 0;
-  return 0;
+  return kap::sample_layout(rows, vocab, device_cus()).total;
 }
 
 kap_status kap_sample(int32_t rows, int32_t vocab, const void *logits, int64_t stride,
@@ -1311,10 +1311,10 @@ kap_status kap_sample(int32_t rows, int32_t vocab, const void *logits, int64_t s
       !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(uniform, 4) ||
       !aligned(token, 4) || !aligned(prob, 4))
     return fail(KAP_ERR_INVALID_ARGUMENT, "an array is misaligned");
-  const size_t need = kap_sample_workspace_bytes(rows, vocab);
-  if (need > 0 && (!workspace || workspace_bytes < need))
-    return fail(KAP_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", need, workspace_bytes);
-  if (need > 0 && !aligned(workspace, 256))
+  const kap::SampleLayout l = kap::sample_layout(rows, vocab, device_cus());
+  if (!workspace || workspace_bytes < l.total)
+    return fail(KAP_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", l.total, workspace_bytes);
+  if (!aligned(workspace, 256))
     return fail(KAP_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
   int log2v = 0;
   while ((1 << log2v) < vocab) ++log2v;
@@ -1322,7 +1322,7 @@ kap_status kap_sample(int32_t rows, int32_t vocab, const void *logits, int64_t s
   a.rows = rows;
   a.vocab = vocab;
   a.f32 = logits_dtype == KAP_DT_F32;
-  a.bits = 62 - log2v;
+  a.bits = std::min(51, 62 - log2v);   // (51: a weight fits a double's mantissa)
   a.stride = stride;
   a.logits = logits;
   a.temperature = temperature;
@@ -1332,6 +1332,13 @@ kap_status kap_sample(int32_t rows, int32_t vocab, const void *logits, int64_t s
   a.uniform = uniform;
   a.token = token;
   a.prob = prob;
+  char *base = static_cast<char *>(workspace);
+  a.chunks = l.chunks;
+  a.tops = reinterpret_cast<unsigned long long *>(base);
+  a.weight = reinterpret_cast<unsigned long long *>(base + l.weight);
+  a.count = reinterpret_cast<int32_t *>(base + l.count);
+  a.list = reinterpret_cast<unsigned long long *>(base + l.list);
+  a.state = reinterpret_cast<int32_t *>(base + l.state);
   (void)hipGetLastError();
   const hipError_t e = kap::launch_sample(a, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(KAP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));

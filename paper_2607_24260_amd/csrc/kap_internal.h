@@ -227,7 +227,18 @@ struct SampleArgs {
   const float *uniform;          // [rows]
   int32_t *token;                // [rows]
   float *prob;                   // [rows] or NULL
+  int chunks;                    // workgroups of a row
+  unsigned long long *tops;      // workspace: [rows][chunks] largest token,
+  unsigned long long *weight;    // [rows][bins + 1] sums by bin of weight, last: the rest,
+  int32_t *count;                // the same of tokens,
+  unsigned long long *list;      // tokens collected for a row,
+  int32_t *state;                // [rows][2] how many, and workgroups done
 };
+struct SampleLayout {            // the workspace's parts, in bytes
+  int chunks;
+  size_t weight, count, list, state, total;
+};
+SampleLayout sample_layout(int rows, int vocab, int cus);
 
 hipError_t launch_compile_plan(const PlanArgs &a, hipStream_t s);
 hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);

@@ -83,6 +83,8 @@ def draw(lib, **over):
     (dict(stride=2**61), UNS), (dict(x=None), BAD), (dict(u=None), BAD), (dict(token=None), BAD),
     (dict(x=FAKE + 1), BAD), (dict(x=FAKE + 2, dt=K.KAP_DT_F32), BAD), (dict(t=FAKE + 2), BAD),
     (dict(k=FAKE + 1), BAD), (dict(prob=FAKE + 2), BAD),
+    (dict(ws=None), K.KAP_ERR_WORKSPACE_TOO_SMALL), (dict(have=99), K.KAP_ERR_WORKSPACE_TOO_SMALL),
+    (dict(ws=FAKE + 64), BAD),
 ])
 def test_sample_refuses(lib, over, status):
     assert draw(lib, **over) == status
