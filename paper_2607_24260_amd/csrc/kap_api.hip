@@ -1334,7 +1334,9 @@ kap_status kap_sample(int32_t rows, int32_t vocab, const void *logits, int64_t s
   a.prob = prob;
   char *base = static_cast<char *>(workspace);
   a.chunks = l.chunks;
+  a.draws = l.draws;
   a.tops = reinterpret_cast<unsigned long long *>(base);
+  a.lows = reinterpret_cast<float *>(base + l.lows);
   a.weight = reinterpret_cast<unsigned long long *>(base + l.weight);
   a.count = reinterpret_cast<int32_t *>(base + l.count);
   a.list = reinterpret_cast<unsigned long long *>(base + l.list);

@@ -227,16 +227,17 @@ struct SampleArgs {
   const float *uniform;          // [rows]
   int32_t *token;                // [rows]
   float *prob;                   // [rows] or NULL
-  int chunks;                    // workgroups of a row
+  int chunks, draws;             // workgroups of a row: sums, draws
   unsigned long long *tops;      // workspace: [rows][chunks] largest token,
+  float *lows;                   // and smallest logit above -inf,
   unsigned long long *weight;    // [rows][bins + 1] sums by bin of weight, last: the rest,
   int32_t *count;                // the same of tokens,
   unsigned long long *list;      // tokens collected for a row,
-  int32_t *state;                // [rows][2] how many, and workgroups done
+  int32_t *state;                // [rows] how many, and workgroups done
 };
 struct SampleLayout {            // the workspace's parts, in bytes
-  int chunks;
-  size_t weight, count, list, state, total;
+  int chunks, draws;
+  size_t lows, weight, count, list, state, total;
 };
 SampleLayout sample_layout(int rows, int vocab, int cus);
 

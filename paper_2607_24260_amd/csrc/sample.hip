@@ -12,15 +12,15 @@
 // So every step asks at which token the running weight or count crosses a
 // target. Nothing is sorted but the few tokens around the answers, in three
 // launches over (row, chunk of the vocabulary):
-//   1  the largest logit of every chunk;
-//   2  a histogram of weights and counts over bins of 2^(1/32) of weight below
-//      the largest, down to 2^-32 (one bin for all that is less);
+//   1  the largest and smallest logit of every chunk;
+//   2  a histogram of weights and counts over 2048 bins of equal ratio, from the
+//      largest weight down to the smallest, or to 2^-32 (one bin for what is less);
 //   3  from the running sums of the bins, those that an answer can lie in; their
 //      tokens are collected, and the last workgroup of the row sorts them and
 //      finds the answers among them.
-// Rows for which that is not few tokens (thousands of equal logits, a top-k or
-// draw among weights below 2^-32) are descended eight bits of the logit at a
-// time over the whole row instead, by the same last workgroup.
+// Rows for which that is not few tokens (thousands of equal logits, a draw from
+// weights below 2^-32) are descended eight bits of the logit at a time over the
+// whole row instead, by the same last workgroup.
 //
 // The weights are summed as integers, in units of 2^-s with s = 62 - ceil(log2
 // vocab): the sums do not depend on their order, and a running weight is off by
@@ -35,9 +35,13 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kSampleWaves = kThreads / 64;
-// Bins: kPerOctave per factor of two in weight, kOctaves of them.
+// Weights are split at 32 steps per factor of two; the bins are a power of two
+// times as fine, 2 at least (2048 bins then reach down to 2^-32) and kFinest at
+// most: as fine as the row's smallest logit allows. 150K logits a few factors
+// apart would else put thousands into a bin.
 constexpr int kPerOctave = 32;
-constexpr int kBins = 1024;
+constexpr int kFinest = 64;
+constexpr int kBins = 2048;
 constexpr int kMost = 2048;                    // tokens sorted for a row
 
 // Monotone map of a float to an unsigned key (-0 as +0, NaN as -inf).
@@ -79,35 +83,40 @@ struct Row {
     if constexpr (F32) return reinterpret_cast<const float *>(x)[i];
     return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(x)[i] << 16);
   }
-  // f(logit, index) for every token of a chunk, a thread's tokens in ascending order
+  // f(logits, index of the first) for the tokens of a chunk, kVec or one at a time,
+  // a thread's tokens in ascending order. Four loads are in flight.
   template <class F>
-  __device__ void each(int chunk, int chunks, F f) const {
-    if (chunk == 0 && (int)threadIdx.x < head) f(one(threadIdx.x), (int)threadIdx.x);
+  __device__ __forceinline__ void each(int chunk, int chunks, F f) const {
+    constexpr int kLoads = 4;
+    auto single = [&](int i) {
+      const float y[1] = {one(i)};
+      f(y, i);
+    };
+    if (chunk == 0 && (int)threadIdx.x < head) single(threadIdx.x);
     const kv_u32x4 *v = reinterpret_cast<const kv_u32x4 *>(x + (size_t)head * (F32 ? 4 : 2));
     const int per = (vecs + chunks - 1) / chunks;
     const int v0 = chunk * per, v1 = min(vecs, v0 + per);
-    auto use = [&](const kv_u32x4 &w, int j) {
+    for (int j = v0 + threadIdx.x; j < v1; j += kLoads * kThreads) {
+      kv_u32x4 w[kLoads];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float y = F32 ? __uint_as_float(w[e & 3])
-                            : ((e & 1) ? bf16_hi(w[(e >> 1) & 3]) : bf16_lo(w[(e >> 1) & 3]));
-        f(y, head + j * kVec + e);
+      for (int u = 0; u < kLoads; ++u) w[u] = v[min(j + u * kThreads, v1 - 1)];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        if (j + u * kThreads >= v1) break;
+        float y[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          y[e] = F32 ? __uint_as_float(w[u][e & 3])
+                     : ((e & 1) ? bf16_hi(w[u][(e >> 1) & 3]) : bf16_lo(w[u][(e >> 1) & 3]));
+        f(y, head + (j + u * kThreads) * kVec);
       }
-    };
-    int j = v0 + threadIdx.x;
-    for (; j + kThreads < v1; j += 2 * kThreads) {
-      const kv_u32x4 w0 = v[j], w1 = v[j + kThreads];
-      use(w0, j);
-      use(w1, j + kThreads);
     }
-    if (j < v1) use(v[j], j);
     if (chunk == chunks - 1) {
       const int i = head + vecs * kVec + (int)threadIdx.x;
-      if (i < n) f(one(i), i);
+      if (i < n) single(i);
     }
   }
 };
-
 // ---------------------------------------------------------------------------
 // weights
 // ---------------------------------------------------------------------------
@@ -131,16 +140,20 @@ struct Weights {
 struct FastWeights {
   double slope, offset;                        // y = x * slope + offset
   double unit;                                 // 2^bits
+  double fine;                                 // bins per step of y
   const double *table;                         // 2^(i / 32), in LDS
   __device__ static constexpr double magic() { return 6755399441055744.0; }   // 1.5 * 2^52
-  __device__ double shifted(float x) const { return fma((double)x, slope, offset) + magic(); }
-  // whether a logit has a bin (NaN and -inf have none)
-  __device__ static bool binned(double t) { return t > magic() - kBins; }
-  __device__ static int bin(double t) { return -(int)(uint32_t)__double_as_longlong(t); }
-  __device__ u64 units(float x, double t) const {
+  // y, at least -2000: a weight of 2^-62, which is no unit (NaN and -inf too)
+  __device__ double power(float x) const { return fmax(fma((double)x, slope, offset), -2000.0); }
+  // kBins and more: below the last one
+  __device__ int bin(double y) const {
+    return -(int)(uint32_t)__double_as_longlong(fma(y, fine, magic()));
+  }
+  __device__ u64 units(double y) const {
     constexpr double c = 0.69314718055994530942 / 32;
+    const double t = y + magic();              // rint(y) in the lower half
     const int n = (int)(uint32_t)__double_as_longlong(t);
-    const double f = fma((double)x, slope, offset) - (t - magic());
+    const double f = y - (t - magic());
     const double p =
         f * (c + f * (c * c / 2 + f * (c * c * c / 6 +
                                        f * (c * c * c * c / 24 + f * (c * c * c * c * c / 120)))));
@@ -148,12 +161,18 @@ struct FastWeights {
     const double w = ldexp(fma(s, p, s), n >> 5);
     return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull;
   }
+  __device__ int bin_of(float x) const { return bin(power(x)); }
+  __device__ u64 units_of(float x) const { return units(power(x)); }
 };
 
-__device__ __forceinline__ FastWeights fast_weights(float top, float t, int bits, double *table) {
-  if (threadIdx.x < 32) table[threadIdx.x] = exp2(threadIdx.x / 32.0);
-  const double slope = 32 * 1.4426950408889634074 / (double)t;
-  return FastWeights{slope, -(double)top * slope, ldexp(1.0, bits), table};
+__device__ __forceinline__ FastWeights fast_weights(float top, float low, float t, int bits,
+                                                    double *table) {
+  if (threadIdx.x < kPerOctave) table[threadIdx.x] = exp2(threadIdx.x / (double)kPerOctave);
+  const double slope = kPerOctave * 1.4426950408889634074 / (double)t;
+  const double span = ((double)top - (double)low) * slope + 1.0;
+  double fine = 2.0;
+  while (fine < kFinest && span * (2 * fine) < kBins) fine *= 2;
+  return FastWeights{slope, -(double)top * slope, ldexp(1.0, bits), fine, table};
 }
 
 // What a row asks for.
@@ -174,13 +193,24 @@ __device__ __forceinline__ Wants wants_of(const SampleArgs &a, int r) {
   return w;
 }
 
-// The largest token of a row from its chunks' (every wavefront by itself).
-__device__ __forceinline__ u64 row_top(const SampleArgs &a, int r) {
-  u64 best = 0;
-  for (int c = threadIdx.x & 63; c < a.chunks; c += 64) best = max(best, a.tops[(size_t)r * a.chunks + c]);
+// The largest token and the smallest logit of a row from its chunks' (every
+// wavefront by itself).
+struct Ends {
+  u64 best;
+  float low;
+};
+__device__ __forceinline__ Ends row_ends(const SampleArgs &a, int r) {
+  Ends e{0, INFINITY};
+  for (int c = threadIdx.x & 63; c < a.chunks; c += 64) {
+    e.best = max(e.best, a.tops[(size_t)r * a.chunks + c]);
+    e.low = fminf(e.low, a.lows[(size_t)r * a.chunks + c]);
+  }
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) best = max(best, __shfl_xor(best, o, 64));
-  return best;
+  for (int o = 32; o >= 1; o >>= 1) {
+    e.best = max(e.best, __shfl_xor(e.best, o, 64));
+    e.low = fminf(e.low, __shfl_xor(e.low, o, 64));
+  }
+  return e;
 }
 
 // Whether the histogram serves a row: a drawn one whose largest logit and
@@ -196,29 +226,44 @@ __device__ __forceinline__ bool by_bins(const Wants &w, uint32_t top, float t) {
 template <int F32>
 __global__ __launch_bounds__(kThreads) void sample_top_kernel(SampleArgs a) {
   __shared__ u64 s_best[kSampleWaves];
+  __shared__ float s_low[kSampleWaves];
   const int chunk = blockIdx.x, r = blockIdx.y;
   const Row<F32> row(a, r);
-  float best = -INFINITY;
+  float best = -INFINITY, low = INFINITY;      // low: of those above -inf
   int at = -1;
-  row.each(chunk, a.chunks, [&](float x, int i) {
-    if (x > best) {
-      best = x;
-      at = i;
+  row.each(chunk, a.chunks, [&](const auto &x, int i) {
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
+      if (x[e] > best) {
+        best = x[e];
+        at = i + e;
+      }
+      low = fminf(low, x[e] == -INFINITY ? INFINITY : x[e]);
     }
   });
   u64 token = at < 0 ? 0 : token_of(order_key(best), at);
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) token = max(token, __shfl_xor(token, o, 64));
-  if ((threadIdx.x & 63) == 0) s_best[threadIdx.x >> 6] = token;
+  for (int o = 32; o >= 1; o >>= 1) {
+    token = max(token, __shfl_xor(token, o, 64));
+    low = fminf(low, __shfl_xor(low, o, 64));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    s_best[threadIdx.x >> 6] = token;
+    s_low[threadIdx.x >> 6] = low;
+  }
   for (int i = chunk * kThreads + threadIdx.x; i <= kBins; i += a.chunks * kThreads) {
     a.weight[(size_t)r * (kBins + 1) + i] = 0;
     a.count[(size_t)r * (kBins + 1) + i] = 0;
   }
-  if (chunk == 0 && threadIdx.x < 2) a.state[2 * r + threadIdx.x] = 0;
+  if (chunk == 0 && threadIdx.x == 0) a.state[r] = 0;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kSampleWaves; ++w) token = max(token, s_best[w]);
+    for (int w = 1; w < kSampleWaves; ++w) {
+      token = max(token, s_best[w]);
+      low = fminf(low, s_low[w]);
+    }
     a.tops[(size_t)r * a.chunks + chunk] = token;
+    a.lows[(size_t)r * a.chunks + chunk] = low;
   }
 }
 
@@ -230,13 +275,14 @@ template <int F32>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   __shared__ u64 s_weight[kBins + 1];
   __shared__ int s_count[kBins + 1];
-  __shared__ double s_table[32];
+  __shared__ double s_table[kPerOctave];
   const int chunk = blockIdx.x, r = blockIdx.y;
   const Wants want = wants_of(a, r);
-  const uint32_t top = (uint32_t)(row_top(a, r) >> 32);
+  const Ends ends = row_ends(a, r);
+  const uint32_t top = (uint32_t)(ends.best >> 32);
   const float t = a.temperature ? a.temperature[r] : 1.f;
   if (top == 0 || !by_bins(want, top, t)) return;
-  const FastWeights w = fast_weights(key_value(top), t, a.bits, s_table);
+  const FastWeights w = fast_weights(key_value(top), ends.low, t, a.bits, s_table);
   for (int i = threadIdx.x; i <= kBins; i += kThreads) {
     s_weight[i] = 0;
     s_count[i] = 0;
@@ -246,18 +292,27 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   u64 rest = 0;
   int rest_n = 0;
   const Row<F32> row(a, r);
-  row.each(chunk, a.chunks, [&](float x, int) {
-    const double s = w.shifted(x);
-    const int b = FastWeights::bin(s);
-    if (FastWeights::binned(s)) {
-      atomicAdd(&s_weight[b], w.units(x, s));
-      if (counts) atomicAdd(&s_count[b], 1);
-    } else {
-      // below 2^-32: 32-bit exponentials are exact to 2^-55
-      const float y = (float)fma((double)x, w.slope, w.offset) * (1.f / kPerOctave);
-      const float e = exp2f(y);
-      rest += e > 0.f ? (u64)(e * (float)w.unit) : 0;
-      ++rest_n;
+  row.each(chunk, a.chunks, [&](const auto &x, int) {
+    constexpr int N = sizeof(x) / sizeof(float);
+    int b[N];
+    u64 v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const double y = w.power(x[e]);
+      b[e] = w.bin(y);
+      v[e] = w.units(y);
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const bool in = b[e] < kBins;            // the many below stay in registers
+      rest += in ? 0 : v[e];
+      rest_n += !in;
+      if (in) atomicAdd(&s_weight[b[e]], v[e]);
+    }
+    if (counts) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (b[e] < kBins) atomicAdd(&s_count[b[e]], 1);
     }
   });
 #pragma unroll
@@ -285,11 +340,14 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
 struct Shared {
   u64 weight[kBins + 1];                       // running, by bin
   int count[kBins + 1];
-  u64 token[kMost];                            // sorted: descending
-  u64 sum[kMost];                              // running units of the sorted tokens
+  u64 token[2][kMost];                         // collected, and sorted: descending;
+                                               // then, in the place of the former,
+                                               // running units of the sorted tokens
+  uint16_t start[kBins + 1], stop[kBins + 1];  // a bin's sorted tokens
   uint32_t wanted[kBins / 32];
   u64 red[kSampleWaves];
-  double table[32];
+  int red_n[kSampleWaves];
+  double table[kPerOctave];
   int pick[4];
 };
 
@@ -312,29 +370,81 @@ __device__ __forceinline__ int first_of(int lo, int hi, F f) {
   return hit ? lo + __builtin_ctzll(hit) : hi;
 }
 
-// Inclusive running sums over n values of LDS, in place.
 template <typename T>
-__device__ void run_sums(T *x, int n, Shared &s) {
+__device__ __forceinline__ T wave_run(T v) {   // inclusive running sum over the lanes
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const T y = __shfl_up(v, o, 64);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
+
+// Running sums of the bins' weights and (HAS_K) counts: a thread has four bins.
+static_assert(4 * kThreads == kBins);
+template <bool HAS_K>
+__device__ __forceinline__ void run_bins(const u64 *gw, const int *gc, Shared &s) {
+  const int i = 4 * threadIdx.x, wave = threadIdx.x >> 6;
+  u64 w[4];
+  int c[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    w[e] = gw[i + e];
+    c[e] = HAS_K ? gc[i + e] : 0;
+  }
+  const u64 w_rest = gw[kBins];
+  const int c_rest = HAS_K ? gc[kBins] : 0;
+#pragma unroll
+  for (int e = 1; e < 4; ++e) {
+    w[e] += w[e - 1];
+    c[e] += c[e - 1];
+  }
+  const u64 w_run = wave_run(w[3]);
+  const int c_run = HAS_K ? wave_run(c[3]) : 0;
+  if ((threadIdx.x & 63) == 63) {
+    s.red[wave] = w_run;
+    s.red_n[wave] = c_run;
+  }
+  __syncthreads();
+  u64 w_at = w_run - w[3], w_all = 0;
+  int c_at = c_run - c[3], c_all = 0;
+  for (int v = 0; v < kSampleWaves; ++v) {
+    if (v < wave) {
+      w_at += s.red[v];
+      c_at += s.red_n[v];
+    }
+    w_all += s.red[v];
+    c_all += s.red_n[v];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    s.weight[i + e] = w_at + w[e];
+    if (HAS_K) s.count[i + e] = c_at + c[e];
+  }
+  if (threadIdx.x == 0) {
+    s.weight[kBins] = w_all + w_rest;
+    s.count[kBins] = c_all + c_rest;
+  }
+  __syncthreads();
+}
+
+// Inclusive running sums over n values of LDS, in place.
+__device__ __forceinline__ void run_sums(u64 *x, int n, Shared &s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   u64 before = 0;
   for (int base = 0; base < n; base += kThreads) {
     const int i = base + threadIdx.x;
-    T v = i < n ? x[i] : T(0);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const T y = __shfl_up(v, o, 64);
-      if (lane >= o) v += y;
-    }
+    const u64 v = wave_run(i < n ? x[i] : 0);
     __syncthreads();
-    if (lane == 63) s.red[wave] = (u64)v;
+    if (lane == 63) s.red[wave] = v;
     __syncthreads();
-    u64 add = before, all = 0;
+    u64 add = before;
     for (int w = 0; w < kSampleWaves; ++w) {
       if (w < wave) add += s.red[w];
-      all += s.red[w];
+      before += s.red[w];
     }
-    if (i < n) x[i] = v + (T)add;
-    before += all;
+    if (i < n) x[i] = v + add;
   }
   __syncthreads();
 }
@@ -362,12 +472,15 @@ __device__ Place descend(const Row<F32> &row, const Weights &wt, Shared &s, Cros
       s.count[i] = 0;
     }
     __syncthreads();
-    row.each(0, 1, [&](float x, int) {
-      const uint32_t k = order_key(x);
-      if (shift < 24 && (k >> (shift + 8)) != (p.key >> (shift + 8))) return;
-      const int bin = (k >> shift) & (kDigits - 1);
-      atomicAdd(&s.count[bin], 1);
-      atomicAdd(&s.weight[bin], wt.units(wt.of(k)));
+    row.each(0, 1, [&](const auto &x, int) {
+#pragma unroll 1
+      for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
+        const uint32_t k = order_key(x[e]);
+        if (shift < 24 && (k >> (shift + 8)) != (p.key >> (shift + 8))) continue;
+        const int bin = (k >> shift) & (kDigits - 1);
+        atomicAdd(&s.count[bin], 1);
+        atomicAdd(&s.weight[bin], wt.units(wt.of(k)));
+      }
     });
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -451,9 +564,12 @@ __device__ void whole_row(const SampleArgs &a, int r, const Row<F32> &row, const
     if (threadIdx.x == 0) s.weight[0] = 0;
     __syncthreads();
     u64 sum = 0;
-    row.each(0, 1, [&](float x, int) {
-      const double w = wt.of(order_key(x));
-      if (w >= want.q) sum += wt.units(w);
+    row.each(0, 1, [&](const auto &x, int) {
+#pragma unroll 1
+      for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
+        const double w = wt.of(order_key(x[e]));
+        if (w >= want.q) sum += wt.units(w);
+      }
     });
     if (sum) atomicAdd(&s.weight[0], sum);
     __syncthreads();
@@ -470,42 +586,62 @@ __device__ void whole_row(const SampleArgs &a, int r, const Row<F32> &row, const
 
 // ---- by bins ------------------------------------------------------------------
 
-// Sorts n tokens of LDS in descending order (n rounded up to a power of two).
-__device__ void sort_tokens(u64 *x, int n) {
-  int m = 2;
-  while (m < n) m *= 2;
-  for (int i = n + threadIdx.x; i < m; i += kThreads) x[i] = 0;
-  __syncthreads();
-  for (int size = 2; size <= m; size *= 2)
-    for (int gap = size / 2; gap >= 1; gap /= 2) {
-      for (int i = threadIdx.x; i < m / 2; i += kThreads) {
-        const int lo = 2 * i - (i & (gap - 1)), hi = lo + gap;
-        const u64 p = x[lo], q = x[hi];
-        if ((p < q) == ((lo & size) == 0)) {
-          x[lo] = q;
-          x[hi] = p;
-        }
+// Sorts n <= kMost distinct tokens of s.token[0] in descending order into
+// s.token[1]: 64 at a time within a wavefront, then every token is placed by its
+// rank in the other lists of 64.
+__device__ __forceinline__ void sort_tokens(int n, Shared &s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lists = (n + 63) / 64;
+  constexpr int kOwn = kMost / kThreads;       // lists of a wavefront
+  u64 x[kOwn];
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o) {
+    const int l = wave + o * kSampleWaves;
+    x[o] = l < lists && 64 * l + lane < n ? s.token[0][64 * l + lane] : 0;
+    if (l >= lists) continue;
+    for (int size = 2; size <= 64; size *= 2)
+      for (int gap = size / 2; gap >= 1; gap /= 2) {
+        const u64 y = __shfl_xor(x[o], gap, 64);
+        const bool first = (lane & gap) == 0, down = (lane & size) == 0;
+        x[o] = (x[o] > y) == (first == down) ? x[o] : y;
       }
-      __syncthreads();
+    (lists == 1 ? s.token[1] : s.token[0])[64 * l + lane] = x[o];
+  }
+  __syncthreads();
+  if (lists == 1) return;
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o) {
+    const int l = wave + o * kSampleWaves;
+    if (l >= lists || x[o] == 0) continue;
+    int rank = lane;
+#pragma unroll 4
+    for (int m = 0; m < lists; ++m) {
+      const u64 *list = s.token[0] + 64 * m;
+      int at = 0;                              // tokens of the list before x
+#pragma unroll
+      for (int step = 32; step >= 1; step /= 2) at += list[at + step - 1] > x[o] ? step : 0;
+      at += list[at] > x[o];
+      rank += m == l ? 0 : at;
     }
+    s.token[1][rank] = x[o];
+  }
+  __syncthreads();
 }
 
 // Whether the workgroup is to go over the whole row: the bins do not answer.
 template <int F32>
 __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chunk,
-                                             const Row<F32> &row, const Wants &want, uint32_t top,
-                                             float t, const Weights &wt, Shared &s) {
-  const FastWeights fw = fast_weights(key_value(top), t, a.bits, s.table);
+                                             const Row<F32> &row, const Wants &want,
+                                             const Ends &ends, float t, const Weights &wt,
+                                             Shared &s) {
+  const float top = wt.top;
+  const FastWeights fw = fast_weights(top, ends.low, t, a.bits, s.table);
   const u64 *gw = a.weight + (size_t)r * (kBins + 1);
   const int *gc = a.count + (size_t)r * (kBins + 1);
-  for (int i = threadIdx.x; i <= kBins; i += kThreads) {
-    s.weight[i] = gw[i];
-    s.count[i] = gc[i];
-  }
   if (threadIdx.x < kBins / 32) s.wanted[threadIdx.x] = 0;
-  __syncthreads();
-  run_sums(s.weight, kBins + 1, s);
-  if (want.k < a.vocab) run_sums(s.count, kBins + 1, s);
+  if (threadIdx.x == 0) s.pick[0] = 0;
+  if (want.k < a.vocab) run_bins<true>(gw, gc, s);
+  else run_bins<false>(gw, gc, s);
 
   // Each filter leaves a weight W; the smallest of the three is drawn from. What
   // the sums of the bins leave open of it, and the bins in which the answers lie
@@ -530,8 +666,8 @@ __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chu
     p1 = reaches(want.p * (double)k1);
   }
   if (has_q) {
-    // the bin of weight q is -32 log2 q, rounded; its neighbours cover the roundings
-    const double y = -kPerOctave * log2(want.q);
+    // the bin of weight q is y below, rounded; its neighbours cover the roundings
+    const double y = -kPerOctave * fw.fine * log2(want.q);
     q0 = y > kBins ? kBins : max(0, (int)y - 1);
     q1 = min(kBins, q0 + 3);
   }
@@ -555,111 +691,139 @@ __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chu
   want_bins(d0, d1);
 
   // The tokens of those bins. (A logit below `least` is in none of them.)
-  const float least =
-      key_value(top) - (float)((last + 2) * (double)t / (kPerOctave * 1.4426950408889634074)) * 1.0001f -
-      1e-5f * __builtin_fabsf(key_value(top));
-  if (threadIdx.x == 0) s.pick[0] = 0;
+  const float least = top - (float)((last + 2) / (fw.fine * fw.slope)) * 1.0001f -
+                      1e-5f * __builtin_fabsf(top);
   __syncthreads();
-  row.each(chunk, a.chunks, [&](float x, int i) {
-    if (!(x >= least)) return;
-    const double sh = fw.shifted(x);
-    const int b = FastWeights::bin(sh);
-    if (!FastWeights::binned(sh) || b > last || !(s.wanted[b >> 5] >> (b & 31) & 1)) return;
-    const int at = atomicAdd(&s.pick[0], 1);
-    if (at < kMost) s.token[at] = token_of(order_key(x), i);
+  row.each(chunk, a.draws, [&](const auto &x, int i) {
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) any |= x[e] >= least;
+    if (!any) return;
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
+      if (!(x[e] >= least)) continue;
+      const int b = fw.bin_of(x[e]);
+      if (b > last || !(s.wanted[b >> 5] >> (b & 31) & 1)) continue;
+      const int at = atomicAdd(&s.pick[0], 1);
+      if (at < kMost) s.token[0][at] = token_of(order_key(x[e]), i + e);
+    }
   });
   __syncthreads();
-  const int mine = s.pick[0];
-  u64 *list = a.list + (size_t)r * kMost;
-  if (a.chunks > 1) {
-    int *state = a.state + 2 * r;              // tokens collected, workgroups done
-    if (threadIdx.x == 0 && mine)
-      s.pick[1] = __hip_atomic_fetch_add(state, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (mine) {
+  int n = s.pick[0];
+  if (a.draws > 1) {
+    // collected so far in the lower 20 bits of the row's state (a workgroup adds
+    // kMost + 1 at most), workgroups done above
+    constexpr int kDone = 1 << 20;
+    u64 *list = a.list + (size_t)r * kMost;
+    if (n) {
+      if (threadIdx.x == 0)
+        s.pick[1] = __hip_atomic_fetch_add(a.state + r, min(n, kMost + 1), __ATOMIC_RELAXED,
+                                           __HIP_MEMORY_SCOPE_AGENT) & (kDone - 1);
+      __syncthreads();
       const int at = s.pick[1];
-      for (int i = threadIdx.x; i < mine; i += kThreads)
-        if (i < kMost && at + i < kMost)
-          __hip_atomic_store(list + at + i, s.token[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int i = threadIdx.x; i < min(n, kMost); i += kThreads)
+        if (at + i < kMost)
+          __hip_atomic_store(list + at + i, s.token[0][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (!last_arrival_of(state + 1, a.chunks, &s.pick[3])) return false;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): this wave's stores are complete
+    asm volatile("" ::: "memory");
+    __syncthreads();
     if (threadIdx.x == 0)
-      s.pick[0] = __hip_atomic_load(state, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      s.pick[1] = __hip_atomic_fetch_add(a.state + r, kDone, __ATOMIC_RELAXED,
+                                         __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (s.pick[1] / kDone != a.draws - 1) return false;
+    n = s.pick[1] & (kDone - 1);
+    if (n <= kMost)
+      for (int i = threadIdx.x; i < n; i += kThreads)
+        s.token[0][i] = __hip_atomic_load(list + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
   }
-  const int n = s.pick[0];
-  if (n > kMost) {
-    return true;
+  if (n > kMost) return true;
+  sort_tokens(n, s);
+  const u64 *token = s.token[1];
+  u64 *sum = s.token[0];
+  auto value_at = [&](int i) { return key_value((uint32_t)(token[i] >> 32)); };
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const float x = value_at(i);
+    sum[i] = fw.units_of(x);
+    const int b = fw.bin_of(x);
+    if (i == 0 || fw.bin_of(value_at(i - 1)) != b) s.start[b] = (uint16_t)i;
+    if (i == n - 1 || fw.bin_of(value_at(i + 1)) != b) s.stop[b] = (uint16_t)(i + 1);
   }
-  if (a.chunks > 1)
-    for (int i = threadIdx.x; i < n; i += kThreads)
-      s.token[i] = __hip_atomic_load(list + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   __syncthreads();
-  sort_tokens(s.token, n);
-  auto value_at = [&](int i) { return key_value((uint32_t)(s.token[i] >> 32)); };
-  auto bin_at = [&](int i) { return FastWeights::bin(fw.shifted(value_at(i))); };
-  for (int i = threadIdx.x; i < n; i += kThreads) s.sum[i] = fw.units(value_at(i), fw.shifted(value_at(i)));
-  __syncthreads();
-  run_sums(s.sum, n, s);
-
+  run_sums(sum, n, s);
   // running weight up to and with sorted token i of bin b, whose tokens start at i0
-  auto start_of = [&](int b) { return first_of(0, n, [&](int i) { return bin_at(i) >= b; }); };
   auto weight_at = [&](int i, int b, int i0) -> u64 {
-    return weight_to(b - 1) + s.sum[i] - (i0 > 0 ? s.sum[i0 - 1] : 0);
+    return weight_to(b - 1) + sum[i] - (i0 > 0 ? sum[i0 - 1] : 0);
   };
   // the first sorted token of bin b whose running weight passes, and that weight
   auto place = [&](int b, u64 &weight, auto passes) {
-    const int i0 = start_of(b), i1 = start_of(b + 1);
+    const int i0 = min((int)s.start[b], n - 1), i1 = min((int)s.stop[b], n);
     const int i = min(first_of(i0, i1, [&](int j) { return passes(weight_at(j, b, i0)); }),
                       max(i0, i1 - 1));
     weight = weight_at(i, b, i0);
     return i;
   };
-  if (get_k) {
-    const int i0 = start_of(bk);
-    const int i = min(n - 1, i0 + want.k - (bk > 0 ? s.count[bk - 1] : 0) - 1);
-    k0 = k1 = weight_at(i, bk, i0);
-  }
-  u64 w0 = k0, w1 = k1;
-  if (has_p) {
-    auto run = [&](double goal, u64 least) {
-      const int b = reaches(goal);
-      u64 w = b < kBins ? weight_to(b) : least;
-      if (b <= pe) place(b, w, [&](u64 x) { return (double)x >= goal; });
-      return w;
-    };
-    w0 = min(w0, run(want.p * (double)k0, weight_to(kBins - 1)));
-    w1 = min(w1, run(want.p * (double)k1, weight_to(kBins)));
-  }
-  if (has_q) {
-    const int i0 = start_of(q0), i1 = start_of(qe + 1);
-    const int i = first_of(i0, i1, [&](int j) { return wt.of((uint32_t)(s.token[j] >> 32)) < want.q; });
-    if (i < i1) {
-      const int b = bin_at(i), ib = start_of(b);
-      const u64 w = i > ib ? weight_at(i - 1, b, ib) : weight_to(b - 1);
-      w0 = min(w0, w);
-      w1 = min(w1, w);
-    } else {
-      w0 = min(w0, weight_to(qe));
-      w1 = min(w1, weight_to(q1 < kBins ? qe : kBins));
+  // false: the bins do not answer
+  auto answer = [&]() {
+    u64 w0 = k0, w1 = k1;
+    if (get_k) {
+      const int i0 = min((int)s.start[bk], n - 1);
+      const int i = min(n - 1, i0 + want.k - (bk > 0 ? s.count[bk - 1] : 0) - 1);
+      w0 = w1 = weight_at(i, bk, i0);
     }
-  }
-  auto draw = [&](u64 total) {
-    const double goal = want.u * (double)total;
-    u64 w;
-    return place(exceeds(goal), w, [&](u64 x) { return (double)x > goal; });
-  };
-  // What lies below 2^-32 may leave the weight open: not if it does not matter.
-  const int i = draw(w0);
-  if (w0 != w1 && ((double)(w1 - w0) > 0x1p-26 * (double)w0 || draw(w1) != i)) {
+    if (has_p) {
+      auto run = [&](double goal, u64 least) {
+        const int b = reaches(goal);
+        u64 w = b < kBins ? weight_to(b) : least;
+        if (b <= pe) place(b, w, [&](u64 x) { return (double)x >= goal; });
+        return w;
+      };
+      const u64 p_low = run(want.p * (double)w0, weight_to(kBins - 1));
+      const u64 p_high = w0 == w1 && p1 < kBins ? p_low : run(want.p * (double)w1, weight_to(kBins));
+      w0 = min(w0, p_low);
+      w1 = min(w1, p_high);
+    }
+    if (has_q) {
+      // the first token of the bins around q that does not reach it
+      const int i = first_of(0, n, [&](int j) {
+        const int b = fw.bin_of(value_at(j));
+        return b > qe || (b >= q0 && wt.of((uint32_t)(token[j] >> 32)) < want.q);
+      });
+      const int b = i < n ? fw.bin_of(value_at(i)) : kBins;
+      if (b <= qe) {
+        const int i0 = min((int)s.start[b], n - 1);
+        const u64 w = i > i0 ? weight_at(i - 1, b, i0) : weight_to(b - 1);
+        w0 = min(w0, w);
+        w1 = min(w1, w);
+      } else {
+        w0 = min(w0, weight_to(qe));
+        w1 = min(w1, weight_to(q1 < kBins ? qe : kBins));
+      }
+    }
+    auto draw = [&](u64 total) {
+      const double goal = want.u * (double)total;
+      u64 w;
+      return place(exceeds(goal), w, [&](u64 x) { return (double)x > goal; });
+    };
+    // What lies below 2^-32 may leave the weight open: not if it does not matter.
+    const int i = draw(w0);
+    if (w0 != w1 && ((double)(w1 - w0) > 0x1p-26 * (double)w0 || draw(w1) != i)) return false;
+    if (threadIdx.x == 0) {
+      a.token[r] = index_of(token[i]);
+      if (a.prob)
+        a.prob[r] = (float)(ldexp(wt.of((uint32_t)(token[i] >> 32)), a.bits) / (double)w1);
+    }
     return true;
+  };
+  if (threadIdx.x < 64) {
+    const bool answered = answer();
+    if (threadIdx.x == 0) s.pick[2] = !answered;
   }
-  if (threadIdx.x == 0) {
-    const u64 token = s.token[i];
-    a.token[r] = index_of(token);
-    if (a.prob) a.prob[r] = (float)(ldexp(wt.of((uint32_t)(token >> 32)), a.bits) / (double)w1);
-  }
-  return false;
+  __syncthreads();
+  return s.pick[2] != 0;
 }
 
 template <int F32>
@@ -668,18 +832,18 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a) {
   const int chunk = blockIdx.x, r = blockIdx.y;
   const Row<F32> row(a, r);
   const Wants want = wants_of(a, r);
-  const u64 best = row_top(a, r);
-  const uint32_t top = (uint32_t)(best >> 32);
+  const Ends ends = row_ends(a, r);
+  const uint32_t top = (uint32_t)(ends.best >> 32);
   const float t = a.temperature ? a.temperature[r] : 1.f;
   if (top == 0 || want.greedy) {               // nothing above -inf, or no draw
     if (chunk == 0 && threadIdx.x == 0) {
-      a.token[r] = top == 0 ? -1 : index_of(best);
+      a.token[r] = top == 0 ? -1 : index_of(ends.best);
       if (a.prob) a.prob[r] = top == 0 ? 0.f : 1.f;
     }
     return;
   }
   const Weights wt{key_value(top), 1.4426950408889634074 / (double)t, a.bits};
-  const bool whole = by_bins(want, top, t) ? draw_by_bins(a, r, chunk, row, want, top, t, wt, s)
+  const bool whole = by_bins(want, top, t) ? draw_by_bins(a, r, chunk, row, want, ends, t, wt, s)
                                            : chunk == 0;
   if (whole) whole_row(a, r, row, want, wt, s);
 }
@@ -689,24 +853,28 @@ void launch(const SampleArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)a.chunks, (unsigned)a.rows);
   hipLaunchKernelGGL(sample_top_kernel<F32>, grid, dim3(kThreads), 0, s, a);
   hipLaunchKernelGGL(sample_bins_kernel<F32>, grid, dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL(sample_draw_kernel<F32>, grid, dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(sample_draw_kernel<F32>, dim3((unsigned)a.draws, (unsigned)a.rows),
+                     dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
 
-// Workspace: [tops][weights][counts][lists][states].
+// Workspace: [tops][lows][weights][counts][lists][states].
 SampleLayout sample_layout(int rows, int vocab, int cus) {
   SampleLayout l;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  // about two workgroups per CU, of at least a load per thread (of bf16 logits)
+  // About four workgroups per CU for the sums, one for the draws, of at least a
+  // load per thread (of bf16 logits).
   const int most = std::max(1, vocab / (8 * kThreads));
-  l.chunks = std::max(1, std::min(most, 2 * cus / rows));
+  l.chunks = std::max(1, std::min(most, 4 * cus / rows));
+  l.draws = std::max(1, std::min(most, cus / rows));
   const size_t n = (size_t)rows;
-  l.weight = up(n * l.chunks * sizeof(u64));
+  l.lows = up(n * l.chunks * sizeof(u64));
+  l.weight = l.lows + up(n * l.chunks * sizeof(float));
   l.count = l.weight + up(n * (kBins + 1) * sizeof(u64));
   l.list = l.count + up(n * (kBins + 1) * sizeof(int32_t));
   l.state = l.list + up(n * kMost * sizeof(u64));
-  l.total = l.state + up(n * 2 * sizeof(int32_t));
+  l.total = l.state + up(n * sizeof(int32_t));
   return l;
 }
 
