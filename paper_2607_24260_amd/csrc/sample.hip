@@ -29,16 +29,18 @@
 #include "kap_internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace kap {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kSumThreads = 512;               // of the first two launches
+constexpr int kThreads = 1024;                 // of the third
 constexpr int kSampleWaves = kThreads / 64;
-// Weights are split at 32 steps per factor of two; the bins are a power of two
-// times as fine, 2 at least (2048 bins then reach down to 2^-32) and kFinest at
-// most: as fine as the row's smallest logit allows. 150K logits a few factors
-// apart would else put thousands into a bin.
+// A factor of two in weight has 32 steps, and a step a power of two of bins, two at
+// least (2048 bins then reach down to 2^-32) and kFinest at most: as many as the
+// row's smallest logit allows. 150K logits a few factors apart would else put
+// thousands into a bin.
 constexpr int kPerOctave = 32;
 constexpr int kFinest = 64;
 constexpr int kBins = 2048;
@@ -84,10 +86,10 @@ struct Row {
     return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(x)[i] << 16);
   }
   // f(logits, index of the first) for the tokens of a chunk, kVec or one at a time,
-  // a thread's tokens in ascending order. Four loads are in flight.
-  template <class F>
+  // a thread's tokens in ascending order. Two loads of it are in flight.
+  template <int THREADS, class F>
   __device__ __forceinline__ void each(int chunk, int chunks, F f) const {
-    constexpr int kLoads = 4;
+    constexpr int kLoads = 2;
     auto single = [&](int i) {
       const float y[1] = {one(i)};
       f(y, i);
@@ -96,19 +98,19 @@ struct Row {
     const kv_u32x4 *v = reinterpret_cast<const kv_u32x4 *>(x + (size_t)head * (F32 ? 4 : 2));
     const int per = (vecs + chunks - 1) / chunks;
     const int v0 = chunk * per, v1 = min(vecs, v0 + per);
-    for (int j = v0 + threadIdx.x; j < v1; j += kLoads * kThreads) {
+    for (int j = v0 + threadIdx.x; j < v1; j += kLoads * THREADS) {
       kv_u32x4 w[kLoads];
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) w[u] = v[min(j + u * kThreads, v1 - 1)];
+      for (int u = 0; u < kLoads; ++u) w[u] = v[min(j + u * THREADS, v1 - 1)];
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
-        if (j + u * kThreads >= v1) break;
+        if (j + u * THREADS >= v1) break;
         float y[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
           y[e] = F32 ? __uint_as_float(w[u][e & 3])
                      : ((e & 1) ? bf16_hi(w[u][(e >> 1) & 3]) : bf16_lo(w[u][(e >> 1) & 3]));
-        f(y, head + (j + u * kThreads) * kVec);
+        f(y, head + (j + u * THREADS) * kVec);
       }
     }
     if (chunk == chunks - 1) {
@@ -134,62 +136,66 @@ struct Weights {
   __device__ u64 units(double w) const { return (u64)rint(ldexp(w, bits)); }
 };
 
-// The same to 2^-48 of a weight, and its bin, for the sums over whole rows: with
-// y = 32 log2 w, n = rint(y): 2^(n / 32) from a table of 32 and 2^((y - n) / 32)
-// by its series to the fifth power ((ln 2 / 64)^6 / 6! = 2^-48.7).
+// The same to 2^-44 of a weight, and its bin, for the sums over whole rows: with
+// y = log2 w in bins and n = rint(y), 2^n from a table with a bin's weight each,
+// times 2^(y - n) by its series to the fourth power (a bin is at most 1/64 of a
+// factor of two: (ln 2 / 128)^5 / 5! = 2^-44.5). Eleven 64-bit operations a
+// logit, which is what the second launch takes its time for (splitting off whole
+// factors of two and 32nds instead, with the fifth power: fifteen).
 struct FastWeights {
   double slope, offset;                        // y = x * slope + offset
-  double unit;                                 // 2^bits
-  double fine;                                 // bins per step of y
-  const double *table;                         // 2^(i / 32), in LDS
+  double c1, c2, c3, c4;                       // of 2^(y - n)
+  int beyond;                                  // bits to shift a weight below the last bin by
   __device__ static constexpr double magic() { return 6755399441055744.0; }   // 1.5 * 2^52
-  // y, at least -2000: a weight of 2^-62, which is no unit (NaN and -inf too)
-  __device__ double power(float x) const { return fmax(fma((double)x, slope, offset), -2000.0); }
-  // kBins and more: below the last one
-  __device__ int bin(double y) const {
-    return -(int)(uint32_t)__double_as_longlong(fma(y, fine, magic()));
+  // y, and rint(y) in the lower half of t. No less than -2 kBins + 1: no unit is
+  // left of such a weight (NaN's and -inf's too).
+  __device__ double power(float x) const {
+    return fmax(fma((double)x, slope, offset), 1.0 - 2 * kBins);
   }
-  __device__ u64 units(double y) const {
-    constexpr double c = 0.69314718055994530942 / 32;
-    const double t = y + magic();              // rint(y) in the lower half
-    const int n = (int)(uint32_t)__double_as_longlong(t);
+  __device__ static int bin(double t) { return -(int)(uint32_t)__double_as_longlong(t); }
+  // units of a weight with power y in bin b, of which 2^n has `unit`
+  __device__ u64 units(double y, double t, int b, double unit) const {
     const double f = y - (t - magic());
-    const double p =
-        f * (c + f * (c * c / 2 + f * (c * c * c / 6 +
-                                       f * (c * c * c * c / 24 + f * (c * c * c * c * c / 120)))));
-    const double s = table[n & 31];
-    const double w = ldexp(fma(s, p, s), n >> 5);
-    return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull;
+    const double p = fma(f, fma(f, fma(f, fma(f, c4, c3), c2), c1), 1.0);
+    const u64 v = (u64)__double_as_longlong(fma(unit, p, 4503599627370496.0)) & 0xfffffffffffffull;
+    return v >> (b >= kBins ? beyond : 0);
   }
-  __device__ int bin_of(float x) const { return bin(power(x)); }
-  __device__ u64 units_of(float x) const { return units(power(x)); }
+  __device__ int bin_of(float x) const { return bin(power(x) + magic()); }
+  // the units of 2^n in bin b (those below the last bin are a bin 2048 above, shifted)
+  __device__ double unit_of(int b, int bits) const {
+    return ldexp(exp2((b & (kBins - 1)) * (c1 * -1.4426950408889634074)), bits);
+  }
 };
 
-__device__ __forceinline__ FastWeights fast_weights(float top, float low, float t, int bits,
-                                                    double *table) {
-  if (threadIdx.x < kPerOctave) table[threadIdx.x] = exp2(threadIdx.x / (double)kPerOctave);
-  const double slope = kPerOctave * 1.4426950408889634074 / (double)t;
-  const double span = ((double)top - (double)low) * slope + 1.0;
+__device__ __forceinline__ FastWeights fast_weights(float top, float low, float t) {
+  const double steps = kPerOctave * 1.4426950408889634074 / (double)t;
+  const double span = ((double)top - (double)low) * steps + 1.0;
   double fine = 2.0;
   while (fine < kFinest && span * (2 * fine) < kBins) fine *= 2;
-  return FastWeights{slope, -(double)top * slope, ldexp(1.0, bits), fine, table};
+  const double slope = steps * fine, c = 0.69314718055994530942 / (kPerOctave * fine);
+  // (with finer bins none of the row's tokens is below the last one)
+  return FastWeights{slope, -(double)top * slope, c, c * c / 2, c * c * c / 6, c * c * c * c / 24,
+                     fine == 2.0 ? kBins / (2 * kPerOctave) : 63};
 }
 
-// What a row asks for.
+// What a row asks for. (An array that is not there is read as another one and the
+// value left out: the loads go out together.)
 struct Wants {
-  bool greedy;
+  float t;
   int k;             // vocab: no top-k
   double p, q, u;    // p 1: no top-p; q 0: no min-p
 };
 __device__ __forceinline__ Wants wants_of(const SampleArgs &a, int r) {
+  const float u = a.uniform[r];
+  const float t = (a.temperature ? a.temperature : a.uniform)[r];
+  const int k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(a.uniform))[r];
+  const float p = (a.top_p ? a.top_p : a.uniform)[r], q = (a.min_p ? a.min_p : a.uniform)[r];
   Wants w;
-  const float t = a.temperature ? a.temperature[r] : 1.f;
-  w.greedy = !(t > 0.f);
-  w.k = a.top_k && a.top_k[r] > 0 ? min(a.top_k[r], a.vocab) : a.vocab;
-  w.p = a.top_p && a.top_p[r] < 1.f ? (double)a.top_p[r] : 1.0;
-  w.q = a.min_p && a.min_p[r] > 0.f ? fmin((double)a.min_p[r], 1.0) : 0.0;
-  const double u = a.uniform[r];
-  w.u = u > 0.0 ? fmin(u, 1.0 - 0x1p-24) : 0.0;
+  w.t = a.temperature ? t : 1.f;
+  w.k = a.top_k && k > 0 ? min(k, a.vocab) : a.vocab;
+  w.p = a.top_p && p < 1.f ? (double)p : 1.0;
+  w.q = a.min_p && q > 0.f ? fmin((double)q, 1.0) : 0.0;
+  w.u = u > 0.f ? fmin((double)u, 1.0 - 0x1p-24) : 0.0;
   return w;
 }
 
@@ -213,10 +219,11 @@ __device__ __forceinline__ Ends row_ends(const SampleArgs &a, int r) {
   return e;
 }
 
-// Whether the histogram serves a row: a drawn one whose largest logit and
+// Whether a row is drawn from, and whether by bins: its largest logit and
 // temperature give finite coefficients.
-__device__ __forceinline__ bool by_bins(const Wants &w, uint32_t top, float t) {
-  return !w.greedy && key_value(top) < INFINITY && t > 1e-30f;
+__device__ __forceinline__ bool drawn(const Wants &w) { return w.t > 0.f; }
+__device__ __forceinline__ bool by_bins(const Wants &w, uint32_t top) {
+  return w.t > 1e-30f && key_value(top) < INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -224,14 +231,14 @@ __device__ __forceinline__ bool by_bins(const Wants &w, uint32_t top, float t) {
 // ---------------------------------------------------------------------------
 
 template <int F32>
-__global__ __launch_bounds__(kThreads) void sample_top_kernel(SampleArgs a) {
-  __shared__ u64 s_best[kSampleWaves];
-  __shared__ float s_low[kSampleWaves];
+__global__ __launch_bounds__(kSumThreads) void sample_top_kernel(SampleArgs a) {
+  __shared__ u64 s_best[kSumThreads / 64];
+  __shared__ float s_low[kSumThreads / 64];
   const int chunk = blockIdx.x, r = blockIdx.y;
   const Row<F32> row(a, r);
   float best = -INFINITY, low = INFINITY;      // low: of those above -inf
   int at = -1;
-  row.each(chunk, a.chunks, [&](const auto &x, int i) {
+  row.template each<kSumThreads>(chunk, a.chunks, [&](const auto &x, int i) {
 #pragma unroll
     for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
       if (x[e] > best) {
@@ -251,14 +258,14 @@ __global__ __launch_bounds__(kThreads) void sample_top_kernel(SampleArgs a) {
     s_best[threadIdx.x >> 6] = token;
     s_low[threadIdx.x >> 6] = low;
   }
-  for (int i = chunk * kThreads + threadIdx.x; i <= kBins; i += a.chunks * kThreads) {
+  for (int i = chunk * kSumThreads + threadIdx.x; i <= kBins; i += a.chunks * kSumThreads) {
     a.weight[(size_t)r * (kBins + 1) + i] = 0;
     a.count[(size_t)r * (kBins + 1) + i] = 0;
   }
   if (chunk == 0 && threadIdx.x == 0) a.state[r] = 0;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kSampleWaves; ++w) {
+    for (int w = 1; w < kSumThreads / 64; ++w) {
       token = max(token, s_best[w]);
       low = fminf(low, s_low[w]);
     }
@@ -272,47 +279,56 @@ __global__ __launch_bounds__(kThreads) void sample_top_kernel(SampleArgs a) {
 // ---------------------------------------------------------------------------
 
 template <int F32>
-__global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kSumThreads) void sample_bins_kernel(SampleArgs a) {
   __shared__ u64 s_weight[kBins + 1];
   __shared__ int s_count[kBins + 1];
-  __shared__ double s_table[kPerOctave];
+  __shared__ double s_unit[kBins];
   const int chunk = blockIdx.x, r = blockIdx.y;
   const Wants want = wants_of(a, r);
   const Ends ends = row_ends(a, r);
   const uint32_t top = (uint32_t)(ends.best >> 32);
-  const float t = a.temperature ? a.temperature[r] : 1.f;
-  if (top == 0 || !by_bins(want, top, t)) return;
-  const FastWeights w = fast_weights(key_value(top), ends.low, t, a.bits, s_table);
-  for (int i = threadIdx.x; i <= kBins; i += kThreads) {
+  if (top == 0 || !by_bins(want, top)) return;
+  const FastWeights w = fast_weights(key_value(top), ends.low, want.t);
+  for (int i = threadIdx.x; i < kBins; i += kSumThreads) {
     s_weight[i] = 0;
     s_count[i] = 0;
+    s_unit[i] = w.unit_of(i, a.bits);
+  }
+  if (threadIdx.x == 0) {
+    s_weight[kBins] = 0;
+    s_count[kBins] = 0;
   }
   __syncthreads();
   const bool counts = want.k < a.vocab;
   u64 rest = 0;
   int rest_n = 0;
   const Row<F32> row(a, r);
-  row.each(chunk, a.chunks, [&](const auto &x, int) {
-    constexpr int N = sizeof(x) / sizeof(float);
-    int b[N];
-    u64 v[N];
+  row.template each<kSumThreads>(chunk, a.chunks, [&](const auto &x, int) {
+    // (four at a time: eight take the registers of two wavefronts)
+    constexpr int ALL = sizeof(x) / sizeof(float), N = ALL < 4 ? ALL : 4;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const double y = w.power(x[e]);
-      b[e] = w.bin(y);
-      v[e] = w.units(y);
-    }
+    for (int e0 = 0; e0 < ALL; e0 += N) {
+      if (e0) __builtin_amdgcn_sched_barrier(0);
+      int b[N];
+      u64 v[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const bool in = b[e] < kBins;            // the many below stay in registers
-      rest += in ? 0 : v[e];
-      rest_n += !in;
-      if (in) atomicAdd(&s_weight[b[e]], v[e]);
-    }
-    if (counts) {
+      for (int e = 0; e < N; ++e) {
+        const double y = w.power(x[e0 + e]), t = y + FastWeights::magic();
+        b[e] = FastWeights::bin(t);
+        v[e] = w.units(y, t, b[e], s_unit[b[e] & (kBins - 1)]);
+      }
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (b[e] < kBins) atomicAdd(&s_count[b[e]], 1);
+      for (int e = 0; e < N; ++e) {
+        const bool in = b[e] < kBins;          // the many below stay in registers
+        rest += in ? 0 : v[e];
+        rest_n += !in;
+        if (in) atomicAdd(&s_weight[b[e]], v[e]);
+      }
+      if (counts) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (b[e] < kBins) atomicAdd(&s_count[b[e]], 1);
+      }
     }
   });
 #pragma unroll
@@ -327,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   __syncthreads();
   u64 *gw = a.weight + (size_t)r * (kBins + 1);
   int *gc = a.count + (size_t)r * (kBins + 1);
-  for (int i = threadIdx.x; i <= kBins; i += kThreads) {
+  for (int i = threadIdx.x; i <= kBins; i += kSumThreads) {
     if (s_weight[i]) atomicAdd(gw + i, s_weight[i]);
     if (counts && s_count[i]) atomicAdd(gc + i, s_count[i]);
   }
@@ -347,7 +363,6 @@ struct Shared {
   uint32_t wanted[kBins / 32];
   u64 red[kSampleWaves];
   int red_n[kSampleWaves];
-  double table[kPerOctave];
   int pick[4];
 };
 
@@ -381,34 +396,34 @@ __device__ __forceinline__ T wave_run(T v) {   // inclusive running sum over the
   return v;
 }
 
-// Running sums of the bins' weights and (HAS_K) counts: a thread has four bins.
-static_assert(4 * kThreads == kBins);
+// Running sums of the bins' weights and (HAS_K) counts: a thread has two bins.
+constexpr int kOwnBins = kBins / kThreads;
 template <bool HAS_K>
 __device__ __forceinline__ void run_bins(const u64 *gw, const int *gc, Shared &s) {
-  const int i = 4 * threadIdx.x, wave = threadIdx.x >> 6;
-  u64 w[4];
-  int c[4];
+  const int i = kOwnBins * threadIdx.x, wave = threadIdx.x >> 6;
+  u64 w[kOwnBins];
+  int c[kOwnBins];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < kOwnBins; ++e) {
     w[e] = gw[i + e];
     c[e] = HAS_K ? gc[i + e] : 0;
   }
   const u64 w_rest = gw[kBins];
   const int c_rest = HAS_K ? gc[kBins] : 0;
 #pragma unroll
-  for (int e = 1; e < 4; ++e) {
+  for (int e = 1; e < kOwnBins; ++e) {
     w[e] += w[e - 1];
     c[e] += c[e - 1];
   }
-  const u64 w_run = wave_run(w[3]);
-  const int c_run = HAS_K ? wave_run(c[3]) : 0;
+  const u64 w_run = wave_run(w[kOwnBins - 1]);
+  const int c_run = HAS_K ? wave_run(c[kOwnBins - 1]) : 0;
   if ((threadIdx.x & 63) == 63) {
     s.red[wave] = w_run;
     s.red_n[wave] = c_run;
   }
   __syncthreads();
-  u64 w_at = w_run - w[3], w_all = 0;
-  int c_at = c_run - c[3], c_all = 0;
+  u64 w_at = w_run - w[kOwnBins - 1], w_all = 0;
+  int c_at = c_run - c[kOwnBins - 1], c_all = 0;
   for (int v = 0; v < kSampleWaves; ++v) {
     if (v < wave) {
       w_at += s.red[v];
@@ -418,7 +433,7 @@ __device__ __forceinline__ void run_bins(const u64 *gw, const int *gc, Shared &s
     c_all += s.red_n[v];
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < kOwnBins; ++e) {
     s.weight[i + e] = w_at + w[e];
     if (HAS_K) s.count[i + e] = c_at + c[e];
   }
@@ -472,7 +487,7 @@ __device__ Place descend(const Row<F32> &row, const Weights &wt, Shared &s, Cros
       s.count[i] = 0;
     }
     __syncthreads();
-    row.each(0, 1, [&](const auto &x, int) {
+    row.template each<kThreads>(0, 1, [&](const auto &x, int) {
 #pragma unroll 1
       for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
         const uint32_t k = order_key(x[e]);
@@ -564,7 +579,7 @@ __device__ void whole_row(const SampleArgs &a, int r, const Row<F32> &row, const
     if (threadIdx.x == 0) s.weight[0] = 0;
     __syncthreads();
     u64 sum = 0;
-    row.each(0, 1, [&](const auto &x, int) {
+    row.template each<kThreads>(0, 1, [&](const auto &x, int) {
 #pragma unroll 1
       for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
         const double w = wt.of(order_key(x[e]));
@@ -632,10 +647,9 @@ __device__ __forceinline__ void sort_tokens(int n, Shared &s) {
 template <int F32>
 __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chunk,
                                              const Row<F32> &row, const Wants &want,
-                                             const Ends &ends, float t, const Weights &wt,
-                                             Shared &s) {
+                                             const Ends &ends, const Weights &wt, Shared &s) {
   const float top = wt.top;
-  const FastWeights fw = fast_weights(top, ends.low, t, a.bits, s.table);
+  const FastWeights fw = fast_weights(top, ends.low, want.t);
   const u64 *gw = a.weight + (size_t)r * (kBins + 1);
   const int *gc = a.count + (size_t)r * (kBins + 1);
   if (threadIdx.x < kBins / 32) s.wanted[threadIdx.x] = 0;
@@ -667,7 +681,7 @@ __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chu
   }
   if (has_q) {
     // the bin of weight q is y below, rounded; its neighbours cover the roundings
-    const double y = -kPerOctave * fw.fine * log2(want.q);
+    const double y = -0.69314718055994530942 / fw.c1 * log2(want.q);
     q0 = y > kBins ? kBins : max(0, (int)y - 1);
     q1 = min(kBins, q0 + 3);
   }
@@ -677,37 +691,72 @@ __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chu
   const int d1 = cut ? exceeds(want.u * (double)weight_to(c1)) : d0;
   const bool get_k = bk < kBins && (has_p || bk <= c1);
   const int pe = min(p1, min(c1, kBins - 1)), qe = min(q1, min(c1, kBins - 1));
-  const int last = max(max(get_k ? bk : 0, d1), max(has_p ? pe : 0, has_q ? qe : 0));
   if (d1 >= kBins) {                           // a draw from below 2^-32
     return chunk == 0;
   }
-  auto want_bins = [&](int b0, int b1) {
+  // Those bins, and bounds on the logits in them (rounded outwards): nearly every
+  // token is left by the bounds, two comparisons for each of the bounds there are.
+  float low[4], high[4];
+  int bounds = 0;
+  auto want_bins = [&](bool any, int b0, int b1) {
+    if (!any) return;
+    const float d1 = (float)((b1 + 0.51) / fw.slope), d0 = (float)((b0 - 0.51) / fw.slope);
+    const float lo = top - d1 - 1e-5f * (__builtin_fabsf(top) + d1);
+    const float hi = top - d0 + 1e-5f * (__builtin_fabsf(top) + __builtin_fabsf(d0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i == bounds) {
+        low[i] = lo;
+        high[i] = hi;
+      }
+    ++bounds;
     for (int b = b0 + (int)threadIdx.x; b <= b1; b += kThreads)
       atomicOr(&s.wanted[b >> 5], 1u << (b & 31));
   };
-  if (get_k) want_bins(bk, bk);
-  if (has_p) want_bins(p0, pe);
-  if (has_q) want_bins(q0, qe);
-  want_bins(d0, d1);
-
-  // The tokens of those bins. (A logit below `least` is in none of them.)
-  const float least = top - (float)((last + 2) / (fw.fine * fw.slope)) * 1.0001f -
-                      1e-5f * __builtin_fabsf(top);
+  want_bins(true, d0, d1);
+  want_bins(get_k, bk, bk);
+  want_bins(has_p && p0 <= pe, p0, pe);
+  want_bins(has_q && q0 <= qe, q0, qe);
   __syncthreads();
-  row.each(chunk, a.draws, [&](const auto &x, int i) {
-    bool any = false;
+  auto collect = [&](auto bounds_there) {
+    constexpr int B = decltype(bounds_there)::value;
+    row.template each<kThreads>(chunk, a.draws, [&](const auto &x, int i) {
+      constexpr int N = sizeof(x) / sizeof(float);
+      bool hit[N], any = false;
 #pragma unroll
-    for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) any |= x[e] >= least;
-    if (!any) return;
+      for (int e = 0; e < N; ++e) {
+        hit[e] = x[e] >= low[0] && x[e] <= high[0];
 #pragma unroll
-    for (int e = 0; e < (int)(sizeof(x) / sizeof(float)); ++e) {
-      if (!(x[e] >= least)) continue;
-      const int b = fw.bin_of(x[e]);
-      if (b > last || !(s.wanted[b >> 5] >> (b & 31) & 1)) continue;
-      const int at = atomicAdd(&s.pick[0], 1);
-      if (at < kMost) s.token[0][at] = token_of(order_key(x[e]), i + e);
+        for (int j = 1; j < B; ++j) hit[e] |= x[e] >= low[j] && x[e] <= high[j];
+        any |= hit[e];
+      }
+      if (!any) return;
+      uint32_t hits = 0;                       // one each time, of a lane that has several
+#pragma unroll
+      for (int e = 0; e < N; ++e) hits |= hit[e] ? 1u << e : 0u;
+      do {
+        const int at_e = __builtin_ctz(hits);
+        hits &= hits - 1;
+        float v = x[0];
+#pragma unroll
+        for (int e = 1; e < N; ++e) v = at_e == e ? x[e] : v;
+        const int b = fw.bin_of(v);
+        if (b >= 0 && b < kBins && (s.wanted[b >> 5] >> (b & 31) & 1)) {
+          const int at = atomicAdd(&s.pick[0], 1);
+          if (at < kMost) s.token[0][at] = token_of(order_key(v), i + at_e);
+        }
+      } while (hits);
+    });
+  };
+  if (bounds == 1) collect(std::integral_constant<int, 1>{});
+  else if (bounds == 2) collect(std::integral_constant<int, 2>{});
+  else {
+    if (bounds == 3) {
+      low[3] = low[2];
+      high[3] = high[2];
     }
-  });
+    collect(std::integral_constant<int, 4>{});
+  }
   __syncthreads();
   int n = s.pick[0];
   if (a.draws > 1) {
@@ -747,8 +796,9 @@ __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chu
   auto value_at = [&](int i) { return key_value((uint32_t)(token[i] >> 32)); };
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const float x = value_at(i);
-    sum[i] = fw.units_of(x);
-    const int b = fw.bin_of(x);
+    const double y = fw.power(x), t = y + FastWeights::magic();
+    const int b = FastWeights::bin(t);
+    sum[i] = fw.units(y, t, b, fw.unit_of(b, a.bits));
     if (i == 0 || fw.bin_of(value_at(i - 1)) != b) s.start[b] = (uint16_t)i;
     if (i == n - 1 || fw.bin_of(value_at(i + 1)) != b) s.stop[b] = (uint16_t)(i + 1);
   }
@@ -834,25 +884,24 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a) {
   const Wants want = wants_of(a, r);
   const Ends ends = row_ends(a, r);
   const uint32_t top = (uint32_t)(ends.best >> 32);
-  const float t = a.temperature ? a.temperature[r] : 1.f;
-  if (top == 0 || want.greedy) {               // nothing above -inf, or no draw
+  if (top == 0 || !drawn(want)) {               // nothing above -inf, or no draw
     if (chunk == 0 && threadIdx.x == 0) {
       a.token[r] = top == 0 ? -1 : index_of(ends.best);
       if (a.prob) a.prob[r] = top == 0 ? 0.f : 1.f;
     }
     return;
   }
-  const Weights wt{key_value(top), 1.4426950408889634074 / (double)t, a.bits};
-  const bool whole = by_bins(want, top, t) ? draw_by_bins(a, r, chunk, row, want, ends, t, wt, s)
-                                           : chunk == 0;
+  const Weights wt{key_value(top), 1.4426950408889634074 / (double)want.t, a.bits};
+  const bool whole =
+      by_bins(want, top) ? draw_by_bins(a, r, chunk, row, want, ends, wt, s) : chunk == 0;
   if (whole) whole_row(a, r, row, want, wt, s);
 }
 
 template <int F32>
 void launch(const SampleArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)a.chunks, (unsigned)a.rows);
-  hipLaunchKernelGGL(sample_top_kernel<F32>, grid, dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL(sample_bins_kernel<F32>, grid, dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(sample_top_kernel<F32>, grid, dim3(kSumThreads), 0, s, a);
+  hipLaunchKernelGGL(sample_bins_kernel<F32>, grid, dim3(kSumThreads), 0, s, a);
   hipLaunchKernelGGL(sample_draw_kernel<F32>, dim3((unsigned)a.draws, (unsigned)a.rows),
                      dim3(kThreads), 0, s, a);
 }
@@ -863,11 +912,14 @@ void launch(const SampleArgs &a, hipStream_t s) {
 SampleLayout sample_layout(int rows, int vocab, int cus) {
   SampleLayout l;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  // About four workgroups per CU for the sums, one for the draws, of at least a
-  // load per thread (of bf16 logits).
-  const int most = std::max(1, vocab / (8 * kThreads));
-  l.chunks = std::max(1, std::min(most, 4 * cus / rows));
-  l.draws = std::max(1, std::min(most, cus / rows));
+  // Chunks of at least a load per thread (of bf16 logits): about two workgroups per
+  // CU for the sums, or four where they have 16K tokens each (64 x 151936: 18 us
+  // with two, 21 with four, whose bins are twice as many to add up; 320 x 151937:
+  // 50 with four, 68 with two); one for the draws.
+  const int most = std::max(1, vocab / (8 * kSumThreads));
+  l.chunks = std::max(1, std::min(most, std::max(2 * cus / rows,
+                                                 std::min(4 * cus / rows, vocab / 16384))));
+  l.draws = std::max(1, std::min(std::max(1, vocab / (8 * kThreads)), cus / rows));
   const size_t n = (size_t)rows;
   l.lows = up(n * l.chunks * sizeof(u64));
   l.weight = l.lows + up(n * l.chunks * sizeof(float));

@@ -4,8 +4,8 @@ to single precision.
 A token may differ only where two outcomes lie closer together than the running
 weights are exact: each weight is rounded to half a unit of 2^-(62 - ceil(log2 n))
 of the largest one, n of them are added, and the kept weight is at least 1:
-2^2 n^2 2^-63 with n rounded up to a power of two, plus 2^-45 for the 64-bit
-exponentials and products (over a hundred half steps of 2^-53). Rows whose
+2^2 n^2 2^-63 with n rounded up to a power of two, plus 2^-44 for the exponentials
+(a series cut off at 2^-44.5) and products. Rows whose
 nearest boundary (the oracle's distance) is closer are not compared; at the sizes
 here there is hardly one.
 """
@@ -24,7 +24,7 @@ DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
 def exactness(n):
-    return 4.0 * n * n * 2.0 ** -63 + 2.0 ** -45
+    return 4.0 * n * n * 2.0 ** -63 + 2.0 ** -44
 
 
 def check(x, u, t=None, k=None, p=None, q=None, least=0.97, **kw):
