@@ -3,9 +3,8 @@
 // the query rows of all the group's sequences, then every sequence's own pages
 // with its own rows, and the parts are merged by their log-sum-exp.
 //
-// A unit is (rows, pages): a group's rows over its shared pages, or a
-// sequence's q_len * G rows over its own. A workgroup owns (unit, block of rows,
-// KV head, split of the pages). A wavefront holds 32 rows and walks 32 keys (two
+// A unit is (rows, pages): a group's rows over its shared pages, or a sequence's
+// q_len * G rows over its own. A wavefront holds 32 rows and walks 32 keys (two
 // pages) a step:
 //   S^T[key][row] = K . Q^T       v_mfma_f32_32x32x16_bf16, or
 //   O^T[dim][row] += V^T P^T      v_mfma_f32_32x32x2_f32 for float32 KV
@@ -13,6 +12,15 @@
 // lane of that row the rest; with the keys of K's operand in the order of
 // key_of_row() those are eight neighbouring keys of either page, which is the
 // layout P^T's operand needs: weights never leave their lane.
+//
+// A workgroup takes a split of a group's shared pages with up to 32 WR rows: WR
+// wavefronts with 32 rows each, as many wavefronts as that leaves by different
+// keys. From WR = 2 on the pages go through LDS, so that each is read once per
+// workgroup, in operand blocks of 1 KB laid out as the lanes multiply them; fp8
+// codes are widened on the way in. With WR = 1, and for a sequence's own pages (a
+// wavefront by itself: unit, row block, KV head and split), operands go straight
+// from memory to the lane's registers, the next step's on the way while this one
+// is multiplied.
 //
 // Weights are float32, split into bf16 hi + lo for 16-bit V, both rounded to
 // nearest (what is left out is at most 2^-18 of a weight; with hi truncated
@@ -33,9 +41,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kWaves = 4;
 constexpr int kRows = 32;                      // of a wavefront
 constexpr int kKeys = 32;                      // of a step
+// Wavefronts of a workgroup: two per SIMD, or one where accumulators, queries and
+// a step's operands leave no room for a second.
+constexpr int waves_of(int kv, int D) { return D == 256 || (kv == kF32 && D == 128) ? 4 : 8; }
 
 __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
@@ -119,12 +129,15 @@ __device__ __forceinline__ long long wave_sum(long long x) {
   return x;
 }
 
-// Work item of workgroup w. A unit's cost is its steps times its row blocks and
-// heads; a unit is split into ceil(steps / C) parts, where C, the cost of all
-// units over the workgroups wanted, is the most a workgroup gets. Parts are
-// numbered group by group, then sequence by sequence, so at most `target` plus
-// one per (unit, row block, head) of them exist: the grid.
-__device__ bool shared_map(const SharedArgs &a, int w, Item &it) {
+// Work item of a wavefront. The cost of a step is that of its pages' bytes, the
+// same for either kind of unit. C, the cost of all units over the workgroups
+// wanted, is what a workgroup gets: a group's shared pages are split into
+// ceil(steps / C) parts, a workgroup each; a sequence's own into parts of C over
+// the wavefronts of a workgroup, a wavefront each. Parts are numbered group by
+// group, then sequence by sequence, so there are at most `target` workgroups plus
+// one part per (unit, row block, head): the grid.
+template <int WAVES>
+__device__ bool shared_map(const SharedArgs &a, int w, int wave, Item &it) {
   const int lane = threadIdx.x & 63;
   auto steps_of = [](const Unit &u) { return (u.pages + 1) / 2; };
   auto blocks_of = [&](const Unit &u, bool shared) {
@@ -137,27 +150,34 @@ __device__ bool shared_map(const SharedArgs &a, int w, Item &it) {
     return shared ? group_unit(a, i) : seq_unit(a, i);
   };
   long long total = 0;
+  Unit first[2];                               // of the first 64, kept for the second pass
   for (int kind = 0; kind < 2; ++kind) {
     const int n = kind == 0 ? a.num_groups : a.batch;
-    for (int i0 = 0; i0 < n; i0 += 64) {
+    first[kind] = unit_of(kind == 0, lane);
+    total += (long long)steps_of(first[kind]) * blocks_of(first[kind], kind == 0);
+    for (int i0 = 64; i0 < n; i0 += 64) {
       const Unit u = unit_of(kind == 0, i0 + lane);
-      total += wave_sum((long long)steps_of(u) * blocks_of(u, kind == 0) *
-                        (kind == 0 ? a.shared_cost : a.own_cost));
+      total += (long long)steps_of(u) * blocks_of(u, kind == 0);
     }
   }
-  total *= a.Hkv;
-  const long long most = max((total + a.target - 1) / a.target, (long long)a.least);
+  total = wave_sum(total) * a.Hkv;
+  const int most =
+      (int)min(max((total + a.target - 1) / a.target, (long long)a.least), 0x3fffffffll);
   int base = 0;
-  int64_t row = 0;
   for (int kind = 0; kind < 2; ++kind) {
     const bool shared = kind == 0;
     const int n = shared ? a.num_groups : a.batch;
     const int slot_rows = shared ? a.shared_rows : a.own_rows;
+    const int len = shared ? most : max((most + WAVES - 1) / WAVES, a.own_least);
+    const int64_t start = shared ? 0 : a.own_base;
+    if (!shared) {                             // parts are wavefronts' from here on
+      w = (w - base) * WAVES + wave;
+      base = 0;
+    }
     for (int i0 = 0; i0 < n; i0 += 64) {
-      const Unit u = unit_of(shared, i0 + lane);
+      const Unit u = i0 == 0 ? first[kind] : unit_of(shared, i0 + lane);
       const int rb = blocks_of(u, shared);
-      const int parts =
-          (int)ceil((double)steps_of(u) * (shared ? a.shared_cost : a.own_cost) / (double)most);
+      const int parts = div_small(steps_of(u) + len - 1, len);
       const int cnt = parts * rb * a.Hkv;
       const int incl = wave_scan_add(cnt), excl = incl - cnt;
       const unsigned long long hit = __ballot(w >= base + excl && w < base + incl);
@@ -170,18 +190,16 @@ __device__ bool shared_map(const SharedArgs &a, int w, Item &it) {
         it.page0 = __builtin_amdgcn_readlane(u.page0, l);
         it.pages = __builtin_amdgcn_readlane(u.pages, l);
         it.n_split = __builtin_amdgcn_readlane(parts, l);
-        const int e = __builtin_amdgcn_readlane(excl, l);
-        it.row0 = row + (int64_t)e * slot_rows;
-        const int off = w - base - e;
-        const int block = off / it.n_split;
+        const int e = base + __builtin_amdgcn_readlane(excl, l);
+        it.row0 = start + (int64_t)e * slot_rows;
+        const int off = w - e;
+        const int block = div_small(off, it.n_split);
         it.split = off - block * it.n_split;
-        it.rb = block / a.Hkv;
+        it.rb = div_small(block, a.Hkv);
         it.g = block - it.rb * a.Hkv;
         return true;
       }
-      const int all = lane63(incl);
-      base += all;
-      row += (int64_t)all * slot_rows;
+      base += lane63(incl);
     }
   }
   return false;
@@ -191,20 +209,21 @@ __device__ bool shared_map(const SharedArgs &a, int w, Item &it) {
 // operands
 // ---------------------------------------------------------------------------
 
-// K and V^T operands as loaded (fp8: codes, widened at use): a K operand serves
-// 16 dims (float32: 8) of the step's 32 keys, a V operand 32 dims of a page's 16
-// keys (float32: of eight of them).
-template <int KV> struct KOperand { u32x4 x; };
-template <> struct KOperand<kFP8> { u32x2 x; };
-template <int KV> using VOperand = KOperand<KV>;
+// An operand as loaded (fp8: codes, widened at use). A K operand serves 16 dims
+// (float32: 8) of a step's 32 keys, a V operand 32 dims of a page's 16 keys
+// (float32: of eight of them).
+template <int KV> struct Operand { u32x4 x; };
+template <> struct Operand<kFP8> { u32x2 x; };
+
+// K operands of a step, as many as V operands; V operands per 32 dims.
+template <int KV, int D> constexpr int operands() { return KV == kF32 ? D / 8 : D / 16; }
+template <int KV> constexpr int v_parts() { return KV == kF32 ? 4 : 2; }
 
 // Q^T, the operand K meets: 16-bit dims 16 c + 8 hb .., float32 8 c + 4 hb .. In
-// registers, except where they are 128 of them: 256-dim float32 heads keep it in
-// LDS, lane for lane.
-template <int KV, int D> constexpr int q_operands() { return KV == kF32 ? D / 8 : D / 16; }
+// registers, except 256-dim float32 heads' (128 of them): in LDS, lane for lane.
 template <int KV, int D> constexpr bool q_in_lds() { return KV == kF32 && D == 256; }
 template <int KV, int D> struct Queries {
-  u32x4 q[q_in_lds<KV, D>() ? 1 : q_operands<KV, D>()];
+  u32x4 q[q_in_lds<KV, D>() ? 1 : operands<KV, D>()];
   const u32x4 *lds;
   __device__ u32x4 at(int c) const {
     if constexpr (q_in_lds<KV, D>()) return lds[c * 64];
@@ -216,69 +235,96 @@ __device__ __forceinline__ u32x4 widen8(u32x2 x) {
   const u32x2 lo = fp8x4_to_bf16x4(x[0]), hi = fp8x4_to_bf16x4(x[1]);
   return u32x4{lo[0], lo[1], hi[0], hi[1]};
 }
-__device__ __forceinline__ u32x4 wide(const KOperand<kBF16> &r) { return r.x; }
-__device__ __forceinline__ u32x4 wide(const KOperand<kF32> &r) { return r.x; }
-__device__ __forceinline__ u32x4 wide(const KOperand<kFP8> &r) { return widen8(r.x); }
+__device__ __forceinline__ u32x4 wide(const Operand<kBF16> &r) { return r.x; }
+__device__ __forceinline__ u32x4 wide(const Operand<kF32> &r) { return r.x; }
+__device__ __forceinline__ u32x4 wide(const Operand<kFP8> &r) { return widen8(r.x); }
 
-// The two pages of a step: ids (0 where there is none) and what is visible.
+// The two pages of a step: ids (0 where there is none) and whether they are there.
 struct Step {
   int id[2];
   bool ok[2];
-  int pos;           // of its first key
 };
 
-// Operands of a step from memory, in the lane that multiplies them.
+// Operands of a step in memory, for the lane that multiplies them.
 template <int KV, int D>
 struct Pages {
-  static constexpr int kK = KV == kF32 ? D / 8 : D / 16;   // K operands
-  static constexpr int kV = KV == kF32 ? 4 : 2;            // V operands per 32 dims
+  static constexpr size_t kTile = (size_t)kPage * D * elem_bytes(KV);
   const char *k, *v[2];
-  __device__ Pages(const SharedArgs &a, const Step &s, int g, int lane) {
-    constexpr size_t kTile = (size_t)kPage * D * elem_bytes(KV);
+  __device__ Pages(const SharedArgs &a, const int (&id)[2], int g, int lane) {
     const int i = lane & 31, hb = lane >> 5, tok = key_of_row<KV>(i) & 15;
     k = static_cast<const char *>(a.k_pages) +
-        ((size_t)(i < 16 ? s.id[0] : s.id[1]) * a.Hkv + g) * kTile +
+        ((size_t)(i < 16 ? id[0] : id[1]) * a.Hkv + g) * kTile +
         tok * 8 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 128 * elem_bytes(KV));
 #pragma unroll
     for (int pg = 0; pg < 2; ++pg)
-      v[pg] = static_cast<const char *>(a.v_pages) + ((size_t)s.id[pg] * a.Hkv + g) * kTile +
+      v[pg] = static_cast<const char *>(a.v_pages) + ((size_t)id[pg] * a.Hkv + g) * kTile +
               i * 16 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 8 * elem_bytes(KV));
   }
-  __device__ KOperand<KV> key(int c) const {
-    return *reinterpret_cast<const KOperand<KV> *>(k + c * (KV == kF32 ? 512 : 256 * elem_bytes(KV)));
+  __device__ Operand<KV> raw_key(int c) const {
+    return *reinterpret_cast<const Operand<KV> *>(k + c * (KV == kF32 ? 512 : 256 * elem_bytes(KV)));
   }
-  __device__ VOperand<KV> value(int y, int db) const {
+  __device__ Operand<KV> raw_value(int y, int db) const {
     if constexpr (KV == kF32)
-      return *reinterpret_cast<const VOperand<KV> *>(v[y >> 1] + db * 2048 + (y & 1) * 32);
+      return *reinterpret_cast<const Operand<KV> *>((y >> 1 ? v[1] : v[0]) + db * 2048 + (y & 1) * 32);
     else
-      return *reinterpret_cast<const VOperand<KV> *>(v[y] + db * 512 * elem_bytes(KV));
+      return *reinterpret_cast<const Operand<KV> *>((y ? v[1] : v[0]) + db * 512 * elem_bytes(KV));
+  }
+  __device__ u32x4 key(int c) const { return wide(raw_key(c)); }
+  __device__ u32x4 value(int y, int db) const { return wide(raw_value(y, db)); }
+};
+
+// The same in registers ...
+template <int KV, int D>
+struct Held {
+  Operand<KV> k[operands<KV, D>()], v[v_parts<KV>()][D / 32];
+  __device__ __forceinline__ void load_k(const Pages<KV, D> &p) {
+#pragma unroll
+    for (int c = 0; c < operands<KV, D>(); ++c) k[c] = p.raw_key(c);
+  }
+  __device__ __forceinline__ void load_v(const Pages<KV, D> &p) {
+#pragma unroll
+    for (int y = 0; y < v_parts<KV>(); ++y)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) v[y][db] = p.raw_value(y, db);
+  }
+  __device__ u32x4 key(int c) const { return wide(k[c]); }
+  __device__ u32x4 value(int y, int db) const { return wide(v[y][db]); }
+};
+
+// ... and in LDS: blocks of 64 lanes' 16 bytes, K's and then V's.
+template <int KV, int D>
+struct Tile {
+  static constexpr int kBytes = 2 * operands<KV, D>() * 1024;
+  const u32x4 *at;                             // of this lane
+  __device__ u32x4 key(int c) const { return at[c * 64]; }
+  __device__ u32x4 value(int y, int db) const {
+    return at[(operands<KV, D>() + y * (D / 32) + db) * 64];
   }
 };
 
 template <int KV, int D, class Source>
 __device__ __forceinline__ f32x16 logits(const Source &src, const Queries<KV, D> &q) {
-  // operands whose loads the compiler may have in flight together (more spill
-  // with 256-dim float32 heads)
-  constexpr int kTogether = KV == kF32 ? 8 : 16;
+  // operands whose loads the compiler may have in flight together
+  constexpr int kTogether = 8, K = operands<KV, D>();
   f32x16 s = zero16();
 #pragma unroll
-  for (int c0 = 0; c0 < Source::kK; c0 += kTogether) {
-    KOperand<KV> k[kTogether];
+  for (int c0 = 0; c0 < K; c0 += kTogether) {
+    u32x4 k[kTogether];
 #pragma unroll
     for (int c = 0; c < kTogether; ++c)
-      if (c0 + c < Source::kK) k[c] = src.key(c0 + c);
+      if (c0 + c < K) k[c] = src.key(c0 + c);
 #pragma unroll
     for (int c = 0; c < kTogether; ++c) {
-      if (c0 + c >= Source::kK) continue;
-      const u32x4 kk = wide(k[c]), qq = q.at(c0 + c);
+      if (c0 + c >= K) continue;
+      const u32x4 qq = q.at(c0 + c);
       if constexpr (KV == kF32) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = mfma(__uint_as_float(kk[e]), __uint_as_float(qq[e]), s);
+        for (int e = 0; e < 4; ++e) s = mfma(__uint_as_float(k[c][e]), __uint_as_float(qq[e]), s);
       } else {
-        s = mfma(kk, qq, s);
+        s = mfma(k[c], qq, s);
       }
     }
-    if (Source::kK > kTogether) __builtin_amdgcn_sched_barrier(0);
+    if (K > kTogether) __builtin_amdgcn_sched_barrier(0);
   }
   return s;
 }
@@ -385,7 +431,7 @@ __device__ __forceinline__ void add_values(State<D> &st, const Source &src, cons
                                            uint32_t seen, const float (&vs)[2]) {
   uint32_t wild = 0;
 #pragma unroll
-  for (int y = 0; y < Source::kV; ++y) {
+  for (int y = 0; y < v_parts<KV>(); ++y) {
     u32x4 hi, lo, sees;
     if constexpr (KV != kF32) {
       float p[8];
@@ -394,12 +440,9 @@ __device__ __forceinline__ void add_values(State<D> &st, const Source &src, cons
       split8(p, hi, lo);
     }
     if constexpr (MASKED) sees = seen_words<KV>(seen, y);
-    VOperand<KV> r[D / 32];
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) r[db] = src.value(y, db);
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) {
-      u32x4 v = wide(r[db]);
+      u32x4 v = src.value(y, db);
       if constexpr (MASKED) {
         v &= sees;
         const u32x4 m = wild_words<KV>(v);
@@ -414,7 +457,7 @@ __device__ __forceinline__ void add_values(State<D> &st, const Source &src, cons
         st.o[db] = mfma(v, lo, st.o[db]);
       }
     }
-    if (MASKED || Source::kV > 2) __builtin_amdgcn_sched_barrier(0);
+    if (MASKED || KV == kF32) __builtin_amdgcn_sched_barrier(0);
   }
   if constexpr (MASKED) {
     if (!__any(wild != 0u)) return;
@@ -424,8 +467,8 @@ __device__ __forceinline__ void add_values(State<D> &st, const Source &src, cons
       for (int db = 0; db < D / 32; ++db) {
         f32x16 hits = zero16();
 #pragma unroll
-        for (int y = 0; y < Source::kV; ++y) {
-          const u32x4 one = class_words<KV>(wide(src.value(y, db)) & seen_words<KV>(seen, y), cls);
+        for (int y = 0; y < v_parts<KV>(); ++y) {
+          const u32x4 one = class_words<KV>(src.value(y, db) & seen_words<KV>(seen, y), cls);
           if constexpr (KV == kF32) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -461,150 +504,449 @@ __device__ __forceinline__ RowOf row_of(const SharedArgs &a, const Item &it, int
                max(0, min(a.seq_lens[b], a.max_pages * kPage) - a.q_len + i + 1)};
 }
 
+// What a wavefront (or workgroup) walks: steps of table row `table`, whose first
+// page is page `page0` of the sequence.
+struct Walk {
+  const int32_t *table;
+  int page0, pages;
+  int all, some;     // keys that every row, that some row sees
+  int s0, s1;        // steps
+  int plain;         // steps below this are there and seen by every row
+};
+
+__device__ __forceinline__ bool in_pool(const SharedArgs &a, int id) {
+  return id >= 0 && (int64_t)id < a.num_pages;
+}
+__device__ __forceinline__ Step step_at(const SharedArgs &a, const Walk &w, int s) {
+  Step x;
+#pragma unroll
+  for (int pg = 0; pg < 2; ++pg) {
+    const int id = s < w.s1 && 2 * s + pg < w.pages ? w.table[2 * s + pg] : -1;
+    x.ok[pg] = in_pool(a, id);
+    x.id[pg] = x.ok[pg] ? id : 0;
+  }
+  return x;
+}
+// plain: what positions allow, if all the pages up to there are in the pool (the
+// lanes of `n` threads look at them).
+__device__ __forceinline__ bool pages_fine(const SharedArgs &a, const Walk &w, int thread, int n) {
+  bool fine = true;
+  for (int i = 2 * w.s0 + thread; i < 2 * w.plain; i += n) fine &= in_pool(a, w.table[i]);
+  return fine;
+}
+__device__ __forceinline__ int plain_by_position(const Walk &w) {
+  return max(w.s0, min(min(w.s1, w.pages / 2), (w.all / kPage - w.page0) / 2));
+}
+
+// One step with its operands; ks, vs: the pages' scales (fp8).
+template <int KV, int D, bool MASKED, class Source>
+__device__ __forceinline__ void take_step(State<D> &st, const SharedArgs &a, const Walk &w,
+                                          const Queries<KV, D> &q, const Source &src, int s,
+                                          const bool (&ok)[2], int limit, const float (&ks)[2],
+                                          const float (&vs)[2]) {
+  const int hb = (threadIdx.x & 63) >> 5;
+  f32x16 z = logits<KV, D>(src, q);
+  uint32_t seen = 0xffffu;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    z[i] *= KV == kFP8 ? a.scale_log2 * ks[i >> 3] : a.scale_log2;
+    if constexpr (MASKED) {
+      const int pos = (w.page0 + 2 * s + (i >> 3)) * kPage + key_of_reg<KV>(i & 7, hb);
+      if (!(ok[i >> 3] && pos < limit)) z[i] = -INFINITY;
+      if (!(ok[i >> 3] && pos < w.some)) seen &= ~(1u << i);
+    }
+  }
+  weigh(st, z);
+  add_values<KV, D, MASKED>(st, src, z, seen, vs);
+}
+
+template <int KV>
+__device__ __forceinline__ void scales_of(const SharedArgs &a, const int (&id)[2], float (&ks)[2],
+                                          float (&vs)[2]) {
+  if constexpr (KV == kFP8) {
+#pragma unroll
+    for (int pg = 0; pg < 2; ++pg) {
+      ks[pg] = a.kv_scales[2 * (size_t)id[pg]];
+      vs[pg] = a.kv_scales[2 * (size_t)id[pg] + 1];
+    }
+  }
+}
+
+// Steps first, first + stride, .. below w.s1, operands from memory.
 template <int KV, int D>
-__global__ __launch_bounds__(64 * kWaves)
+__device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, const Walk &w,
+                                            const Queries<KV, D> &q, int g, int first, int stride,
+                                            int limit) {
+  const int lane = threadIdx.x & 63;
+  const bool fine[2] = {true, true};
+  int s = first;
+  if constexpr (KV != kF32 || D < 256) {
+    // the next step's K is fetched as soon as this one's has been multiplied, and
+    // so is V; the page ids two steps ahead
+    auto ids = [&](int t, int (&id)[2]) {
+      t = min(t, w.plain - 1);
+      id[0] = w.table[2 * t];
+      id[1] = w.table[2 * t + 1];
+    };
+    if (s < w.plain) {
+      int id[2], id1[2], id2[2];
+      float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f}, ks1[2] = {1.f, 1.f}, vs1[2] = {1.f, 1.f};
+      ids(s, id);
+      ids(s + stride, id1);
+      Held<KV, D> r;
+      {
+        const Pages<KV, D> p(a, id, g, lane);
+        r.load_k(p);
+        r.load_v(p);
+        scales_of<KV>(a, id, ks, vs);
+      }
+      for (;;) {
+        const bool more = s + stride < w.plain;
+        const Pages<KV, D> p(a, id1, g, lane);
+        ids(s + 2 * stride, id2);
+        scales_of<KV>(a, id1, ks1, vs1);
+        f32x16 z = logits<KV, D>(r, q);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) r.load_k(p);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] *= KV == kFP8 ? a.scale_log2 * ks[i >> 3] : a.scale_log2;
+        weigh(st, z);
+        add_values<KV, D, false>(st, r, z, 0xffffu, vs);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) r.load_v(p);
+        s += stride;
+        if (!more) break;
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+          id1[pg] = id2[pg];
+          ks[pg] = ks1[pg];
+          vs[pg] = vs1[pg];
+        }
+      }
+    }
+  } else {
+    for (; s < w.plain; s += stride) {
+      const Step x = step_at(a, w, s);
+      const float one[2] = {1.f, 1.f};
+      take_step<KV, D, false>(st, a, w, q, Pages<KV, D>(a, x.id, g, lane), s, fine, limit, one, one);
+    }
+  }
+  for (; s < w.s1; s += stride) {
+    const Step x = step_at(a, w, s);
+    float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
+    scales_of<KV>(a, x.id, ks, vs);
+    take_step<KV, D, true>(st, a, w, q, Pages<KV, D>(a, x.id, g, lane), s, x.ok, limit, ks, vs);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// shared pages through LDS
+// ---------------------------------------------------------------------------
+
+// A stage is WK = WAVES / WR tiles of 32 keys. Half of the wavefronts fetch K,
+// half V: each a run of one tile's blocks, into registers, several stages ahead of
+// the LDS buffer they go to. Two buffers, one barrier a stage: a buffer is written
+// again only after all wavefronts have passed the barrier of the stage between.
+template <int KV, int D, int WR>
+struct Staging {
+  static constexpr int kWaves = waves_of(KV, D), kTiles = kWaves / WR, kHalf = kWaves / 2;
+  // 1 KB loads of a tile's K (or V), and of a wavefront in a stage
+  static constexpr int kLoads = KV == kFP8 ? operands<KV, D>() / 2 : operands<KV, D>();
+  static constexpr int kMine = kLoads * kTiles < kHalf ? 1 : kLoads * kTiles / kHalf;
+  static constexpr int kBusy = kLoads * kTiles / kMine;        // wavefronts of a half that fetch
+  static constexpr int kAhead = kMine >= 8 ? 1 : (kMine >= 4 ? 2 : 4);   // stages
+  static constexpr int kStage = kTiles * Tile<KV, D>::kBytes;
+  static constexpr int kScales = KV == kFP8 ? 2 * kTiles * 4 * 4 : 0;   // bytes
+  static constexpr int kBytes = 2 * kStage + kScales;
+};
+
+template <int KV, int D, int WR>
+__device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, const Walk &w,
+                                            const Queries<KV, D> &q, int g, int limit, bool idle,
+                                            char *smem) {
+  using S = Staging<KV, D, WR>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kw = wave / WR;                    // tile of a stage this wavefront multiplies
+  // what it fetches
+  const bool is_v = wave >= S::kHalf, busy = wave % S::kHalf < S::kBusy;
+  const int load0 = wave % S::kHalf * S::kMine, tile = load0 / S::kLoads, c0 = load0 % S::kLoads;
+  const bool has_scales = KV == kFP8 && !is_v && busy && c0 == 0;
+  constexpr size_t kPageTile = Pages<KV, D>::kTile;
+  u32x4 raw[S::kAhead][S::kMine];
+  float raw_scale[S::kAhead];
+  const int stages = (w.s1 - w.s0 + S::kTiles - 1) / S::kTiles;
+  const int plain = (w.plain - w.s0) / S::kTiles;
+
+  auto fetch = [&](int stage, int slot) {
+    if (!busy) return;
+    const Step x = step_at(a, w, w.s0 + stage * S::kTiles + tile);
+    if constexpr (KV == kFP8) {
+      const char *base = static_cast<const char *>(is_v ? a.v_pages : a.k_pages);
+#pragma unroll
+      for (int t = 0; t < S::kMine; ++t) {
+        const int c = c0 + t, pg = c / (D / 64), part = c % (D / 64);
+        raw[slot][t] = *reinterpret_cast<const u32x4 *>(
+            base + ((size_t)(pg ? x.id[1] : x.id[0]) * a.Hkv + g) * kPageTile + part * 1024 + lane * 16);
+      }
+      if (has_scales)
+        raw_scale[slot] =
+            lane < 4 ? a.kv_scales[2 * (size_t)(lane < 2 ? x.id[0] : x.id[1]) + (lane & 1)] : 0.f;
+    } else {
+      const Pages<KV, D> p(a, x.id, g, lane);
+#pragma unroll
+      for (int t = 0; t < S::kMine; ++t) {
+        const int c = c0 + t;
+        raw[slot][t] = is_v ? p.raw_value(c / (D / 32), c % (D / 32)).x : p.raw_key(c).x;
+      }
+    }
+  };
+  auto place = [&](int buffer, int slot) {
+    if (!busy) return;
+    u32x4 *to = reinterpret_cast<u32x4 *>(smem + buffer * S::kStage + tile * Tile<KV, D>::kBytes) +
+                (is_v ? operands<KV, D>() * 64 : 0);
+#pragma unroll
+    for (int t = 0; t < S::kMine; ++t) {
+      const int c = c0 + t;
+      if constexpr (KV == kFP8) {
+        const int pg = c / (D / 64), part = c % (D / 64);
+        const u32x4 lo = widen8(u32x2{raw[slot][t][0], raw[slot][t][1]});
+        const u32x4 hi = widen8(u32x2{raw[slot][t][2], raw[slot][t][3]});
+        if (is_v) {                            // dim 64 part + lane: its keys 0..7 and 8..15
+          u32x4 *at = to + (pg * (D / 32) + 2 * part + (lane >> 5)) * 64 + (lane & 31);
+          at[0] = lo;
+          at[32] = hi;
+        } else {                               // chunk 8 part + lane / 8, two tokens
+          const int chunk = 8 * part + (lane >> 3), tok = 2 * (lane & 7);
+          u32x4 *at = to + (chunk >> 1) * 64 + (chunk & 1) * 32 + 16 * pg;
+          at[key_of_row<KV>(tok)] = lo;
+          at[key_of_row<KV>(tok + 1)] = hi;
+        }
+      } else {
+        to[c * 64 + lane] = raw[slot][t];
+      }
+    }
+    if (has_scales && lane < 4)
+      reinterpret_cast<float *>(smem + 2 * S::kStage)[(buffer * S::kTiles + tile) * 4 + lane] =
+          raw_scale[slot];
+  };
+
+#pragma unroll
+  for (int u = 0; u < S::kAhead; ++u)
+    if (u < stages) fetch(u, u);
+  int stage0 = 0;
+  auto walk = [&](auto masked, int end) {
+    constexpr bool kMasked = decltype(masked)::value;
+    // (slots are numbered from the walk's first stage on, which is a multiple of kAhead)
+    for (; stage0 < end; stage0 += S::kAhead) {
+#pragma unroll
+      for (int u = 0; u < S::kAhead; ++u) {
+        const int stage = stage0 + u;
+        if (kMasked && stage >= end) break;
+        const int buffer = stage & 1;
+        place(buffer, u);
+        __syncthreads();
+        if (stage + S::kAhead < stages) fetch(stage + S::kAhead, u);
+        if (idle) continue;
+        const Tile<KV, D> src{reinterpret_cast<const u32x4 *>(smem + buffer * S::kStage +
+                                                              kw * Tile<KV, D>::kBytes) + lane};
+        float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
+        if constexpr (KV == kFP8) {
+          const float *sc = reinterpret_cast<const float *>(smem + 2 * S::kStage) +
+                            (buffer * S::kTiles + kw) * 4;
+          ks[0] = sc[0];
+          vs[0] = sc[1];
+          ks[1] = sc[2];
+          vs[1] = sc[3];
+        }
+        const int s = w.s0 + stage * S::kTiles + kw;
+        bool ok[2] = {true, true};
+        if constexpr (kMasked) {
+          const Step x = step_at(a, w, s);
+          ok[0] = x.ok[0];
+          ok[1] = x.ok[1];
+        }
+        take_step<KV, D, kMasked>(st, a, w, q, src, s, ok, limit, ks, vs);
+      }
+    }
+  };
+  walk(std::false_type{}, plain / S::kAhead * S::kAhead);
+  walk(std::true_type{}, stages);
+  __syncthreads();
+}
+
+// ---------------------------------------------------------------------------
+// the kernel
+// ---------------------------------------------------------------------------
+
+template <int KV, int D, int WR>
+struct Layout {
+  static constexpr int kWaves = waves_of(KV, D);
+  // the wavefronts' parts, 32 dims at a time: [wave][row][32 dims + 4]
+  static constexpr int kPart = kRows * 36 * 4;
+  static constexpr int kStaged = [] {
+    if constexpr (WR > 1) return Staging<KV, D, WR>::kBytes;
+    else return 0;
+  }();
+  static constexpr int kWalk = kStaged > kWaves * kPart ? kStaged : kWaves * kPart;
+  static constexpr int kBytes =
+      kWalk + (q_in_lds<KV, D>() ? kWaves * operands<KV, D>() * 1024 : 0);
+};
+
+template <int KV, int D, int WR>
+__global__ __launch_bounds__(64 * waves_of(KV, D))
+__attribute__((amdgpu_waves_per_eu(waves_of(KV, D) / 4)))
 void attn_shared_kernel(SharedArgs a) {
-  constexpr int DC = D < 128 ? D : 128;        // dims combined through LDS at a time
-  __shared__ float s_o[kWaves][kRows][DC + 4];
+  constexpr int kWaves = waves_of(KV, D), kTiles = kWaves / WR;
+  __shared__ __align__(16) char smem[Layout<KV, D, WR>::kBytes];
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  __shared__ int s_all, s_some, s_bad;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hb = lane >> 5;
+  if (threadIdx.x == 0) {
+    s_all = 0x7fffffff;
+    s_some = 0;
+    s_bad = 0;
+  }
   Item it;
-  if (!shared_map(a, blockIdx.x, it)) return;
+  if (!shared_map<kWaves>(a, blockIdx.x, wave, it)) return;   // (a shared part: all wavefronts)
   const int slot_rows = it.shared ? a.shared_rows : a.own_rows;
   const int64_t part0 =
       it.row0 + ((int64_t)(it.rb * a.Hkv + it.g) * it.n_split + it.split) * slot_rows;
-  if (part0 + slot_rows > a.part_rows) return;   // group offsets that do not ascend
-  if (it.rb == 0 && it.g == 0 && it.split == 0 && threadIdx.x == 0)
+  // (group offsets that do not ascend)
+  if (part0 + slot_rows > (it.shared ? a.own_base : a.part_rows)) return;
+  if (it.rb == 0 && it.g == 0 && it.split == 0 && (it.shared ? threadIdx.x == 0 : lane == 0))
     (it.shared ? a.group_parts : a.seq_parts)[it.unit] = PartsOf{it.row0, it.n_split, 0};
 
-  const int r0 = it.rb * slot_rows;
-  const RowOf row = row_of(a, it, (lane & 31) < slot_rows ? r0 + (lane & 31) : it.rows);
+  // ---- rows ---------------------------------------------------------------------
+  const int rw = it.shared ? wave % WR : 0;
+  const int r0 = it.rb * slot_rows + rw * kRows;        // of the unit
+  const int in_block = rw * kRows + (lane & 31);
+  const RowOf row = row_of(a, it, in_block < slot_rows ? it.rb * slot_rows + in_block : it.rows);
   Queries<KV, D> q;
   {
     constexpr int kBytes = KV == kF32 ? 4 : 2;
     const char *p = static_cast<const char *>(a.q) + (row.q < 0 ? 0 : row.q) * D * kBytes + hb * 16;
-    __shared__ u32x4 s_q[q_in_lds<KV, D>() ? q_operands<KV, D>() * 64 : 1];
-    q.lds = s_q + lane;
+    u32x4 *lds = reinterpret_cast<u32x4 *>(smem + Layout<KV, D, WR>::kWalk) +
+                 wave * operands<KV, D>() * 64 + lane;
+    q.lds = lds;
 #pragma unroll
-    for (int c = 0; c < q_operands<KV, D>(); ++c) {
+    for (int c = 0; c < operands<KV, D>(); ++c) {
       const u32x4 x = row.q < 0 ? u32x4{0, 0, 0, 0} : *reinterpret_cast<const u32x4 *>(p + c * 32);
-      if constexpr (q_in_lds<KV, D>()) {
-        if (wave == 0) s_q[c * 64 + lane] = x;
-      } else {
-        q.q[c] = x;
-      }
+      if constexpr (q_in_lds<KV, D>()) lds[c * 64] = x;   // read by this lane alone
+      else q.q[c] = x;
     }
-    if constexpr (q_in_lds<KV, D>()) __syncthreads();
   }
-  // keys that every row, and that some row of the block sees
+  Walk w;
+  w.table = a.table + (size_t)it.seq0 * a.stride + it.page0;
+  w.page0 = it.page0;
+  w.pages = it.pages;
+  const int steps = (it.pages + 1) / 2;
+  w.s0 = (int)((long long)steps * it.split / it.n_split);
+  w.s1 = (int)((long long)steps * (it.split + 1) / it.n_split);
   int all = row.q < 0 ? 0x7fffffff : row.limit, some = row.limit;
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
     all = min(all, __shfl_xor(all, o, 64));
     some = max(some, __shfl_xor(some, o, 64));
   }
-  all = __builtin_amdgcn_readfirstlane(all);
-  some = __builtin_amdgcn_readfirstlane(some);
-
-  const int steps = (it.pages + 1) / 2;
-  const int s0 = (int)((long long)steps * it.split / it.n_split);
-  const int s1 = (int)((long long)steps * (it.split + 1) / it.n_split);
-  const int32_t *table = a.table + (size_t)it.seq0 * a.stride + it.page0;
-  auto step_at = [&](int s) {
-    Step x;
-    x.pos = (it.page0 + 2 * s) * kPage;
-#pragma unroll
-    for (int pg = 0; pg < 2; ++pg) {
-      const int id = 2 * s + pg < it.pages ? table[2 * s + pg] : -1;
-      x.ok[pg] = id >= 0 && (int64_t)id < a.num_pages;
-      x.id[pg] = x.ok[pg] ? id : 0;
-    }
-    return x;
-  };
-
   State<D> st;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
   st.ref = kNoMax;
   st.sum = 0.f;
-  // Steps whose keys every row sees, then the rest: those at the end of a
-  // sequence, and from the first page on that is not there.
-  int s = s0 + wave;
-  auto walk = [&](auto masked) {
-    constexpr bool kMasked = decltype(masked)::value;
-    for (; s < s1; s += kWaves) {
-      const Step x = step_at(s);
-      if (!kMasked && !(x.ok[0] && x.ok[1] && x.pos + kKeys <= all)) break;
-      const Pages<KV, D> r(a, x, it.g, lane);
-      float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
-      if constexpr (KV == kFP8) {
-#pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-          ks[pg] = a.kv_scales[2 * (size_t)x.id[pg]];
-          vs[pg] = a.kv_scales[2 * (size_t)x.id[pg] + 1];
-        }
-      }
-      f32x16 z = logits<KV, D>(r, q);
-      uint32_t seen = 0xffffu;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        z[i] *= a.scale_log2 * ks[i >> 3];
-        if constexpr (kMasked) {
-          const int pos = x.pos + 16 * (i >> 3) + key_of_reg<KV>(i & 7, hb);
-          if (!(x.ok[i >> 3] && pos < row.limit)) z[i] = -INFINITY;
-          if (!(x.ok[i >> 3] && pos < some)) seen &= ~(1u << i);
-        }
-      }
-      weigh(st, z);
-      add_values<KV, D, kMasked>(st, r, z, seen, vs);
-    }
-  };
-  walk(std::false_type{});
-  walk(std::true_type{});
 
-  // ---- the four wavefronts' parts into one ------------------------------------
+  if (!it.shared) {
+    // ---- a wavefront by itself ----------------------------------------------------
+    w.all = __builtin_amdgcn_readfirstlane(all);
+    w.some = __builtin_amdgcn_readfirstlane(some);
+    w.plain = plain_by_position(w);
+    if (__any(!pages_fine(a, w, lane, 64))) w.plain = w.s0;
+    walk_memory<KV, D>(st, a, w, q, it.g, w.s0, 1, row.limit);
+    st.sum += other_half(st.sum);
+    const int rr = lane & 31;
+    if (rr >= slot_rows || r0 + rr >= it.rows) return;
+    const float inv = st.sum == 0.f ? 0.f : 1.f / st.sum;
+    float *o = a.part_o + (part0 + rr) * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = st.sum == 0.f ? 0.f : st.o[db][4 * y + e] * inv;
+        *reinterpret_cast<f32x4 *>(o + 32 * db + 8 * y + 4 * hb) = v;
+      }
+    if (hb == 0) a.part_lse[part0 + rr] = st.sum == 0.f ? -INFINITY : st.ref + log2f(st.sum);
+    return;
+  }
+
+  // ---- a workgroup --------------------------------------------------------------
+  __syncthreads();
+  if (lane == 0) {
+    atomicMin(&s_all, all);
+    atomicMax(&s_some, some);
+  }
+  __syncthreads();
+  w.all = __builtin_amdgcn_readfirstlane(s_all);
+  w.some = __builtin_amdgcn_readfirstlane(s_some);
+  w.plain = plain_by_position(w);
+  if (!pages_fine(a, w, threadIdx.x, 64 * kWaves)) s_bad = 1;
+  __syncthreads();
+  if (__builtin_amdgcn_readfirstlane(s_bad)) w.plain = w.s0;
+  if constexpr (WR == 1) {
+    walk_memory<KV, D>(st, a, w, q, it.g, w.s0 + wave, kWaves, row.limit);
+  } else {
+    walk_staged<KV, D, WR>(st, a, w, q, it.g, row.limit, r0 >= it.rows, smem);
+  }
   st.sum += other_half(st.sum);
   if (lane < kRows) {
     s_m[wave][lane] = st.ref;
     s_l[wave][lane] = st.sum;
   }
   __syncthreads();
-  for (int d0 = 0; d0 < D; d0 += DC) {
-    if (d0) __syncthreads();
-    float m = s_m[0][lane & 31];
+  // the wavefronts with other keys of the same rows: wave % WR + WR t
+  float *part = reinterpret_cast<float *>(smem);
+  float m = s_m[rw][lane & 31];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = max_f(m, s_m[w][lane & 31]);
-    const float f = exp2_fast(st.ref - m);
+  for (int t = 1; t < kTiles; ++t) m = max_f(m, s_m[rw + WR * t][lane & 31]);
+  const float f = exp2_fast(st.ref - m);
+  for (int db = 0; db < D / 32; ++db) {
+    if (db) __syncthreads();
 #pragma unroll
-    for (int db = 0; db < DC / 32; ++db)
+    for (int d = 0; d < D / 32; ++d)           // (registers are not indexed)
+      if (d == db) {
 #pragma unroll
-      for (int y = 0; y < 4; ++y)
+        for (int y = 0; y < 4; ++y) {
+          f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          s_o[wave][lane & 31][32 * db + 8 * y + 4 * hb + e] = st.o[d0 / 32 + db][4 * y + e] * f;
+          for (int e = 0; e < 4; ++e) v[e] = st.o[d][4 * y + e] * f;
+          *reinterpret_cast<f32x4 *>(part + (wave * kRows + (lane & 31)) * 36 + 8 * y + 4 * hb) = v;
+        }
+      }
     __syncthreads();
-    for (int i = threadIdx.x; i < kRows * (DC / 4); i += 64 * kWaves) {
-      const int rr = i / (DC / 4), d = i % (DC / 4) * 4;
-      if (rr >= slot_rows || r0 + rr >= it.rows) continue;
-      float mm = s_m[0][rr];
+    for (int i = threadIdx.x; i < WR * kRows * 8; i += 64 * kWaves) {
+      const int rr = i >> 3, d = (i & 7) * 4, rg = rr / kRows, rl = rr % kRows;
+      if (rr >= slot_rows || it.rb * slot_rows + rr >= it.rows) continue;
+      float mm = s_m[rg][rl];
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) mm = max_f(mm, s_m[w][rr]);
+      for (int t = 1; t < kTiles; ++t) mm = max_f(mm, s_m[rg + WR * t][rl]);
       float l = 0.f;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        l += s_l[w][rr] * exp2_fast(s_m[w][rr] - mm);
+      for (int t = 0; t < kTiles; ++t) {
+        const int v = rg + WR * t;
+        l += s_l[v][rl] * exp2_fast(s_m[v][rl] - mm);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (v * kRows + rl) * 36 + d);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += s_o[w][rr][d + e];
+        for (int e = 0; e < 4; ++e) o[e] += x[e];
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int64_t at = part0 + rr;
       f32x4 res;
 #pragma unroll
       for (int e = 0; e < 4; ++e) res[e] = l == 0.f ? 0.f : o[e] * inv;
-      *reinterpret_cast<f32x4 *>(a.part_o + at * D + d0 + d) = res;
-      if (d0 + d == 0) a.part_lse[at] = l == 0.f ? -INFINITY : mm + log2f(l);
+      *reinterpret_cast<f32x4 *>(a.part_o + (part0 + rr) * D + 32 * db + d) = res;
+      if (db == 0 && d == 0) a.part_lse[part0 + rr] = l == 0.f ? -INFINITY : mm + log2f(l);
     }
   }
 }
@@ -613,9 +955,13 @@ void attn_shared_kernel(SharedArgs a) {
 // merge: rows of (sequence, KV head) over the parts of its group and its own
 // ---------------------------------------------------------------------------
 
+constexpr int kItems = 128, kShares = 8;       // (row, four dims) items; threads an item
+
 template <int D>
-__global__ __launch_bounds__(256) void merge_shared_kernel(SharedArgs a) {
-  constexpr int D4 = D / 4;
+__global__ __launch_bounds__(kItems * kShares) void merge_shared_kernel(SharedArgs a) {
+  constexpr int D4 = D / 4, kBatch = 4;
+  __shared__ f32x4 s_o[kShares][kItems];
+  __shared__ float s_m[kShares][kItems], s_l[kShares][kItems];
   const int g = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
   const int grp = group_of(a, b);
   const Unit own = seq_unit(a, b);
@@ -624,45 +970,83 @@ __global__ __launch_bounds__(256) void merge_shared_kernel(SharedArgs a) {
   const PartsOf po = own.pages > 0 ? a.seq_parts[b] : PartsOf{0, 0, 0};
   const PartsOf pp = pre.pages > 0 ? a.group_parts[grp] : PartsOf{0, 0, 0};
   const int per = a.q_len * a.G;
-  for (int i = threadIdx.x; i < per * D4; i += 256) {
-    const int r = i / D4, d = i % D4 * 4;
-    float m = kNoMax, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    auto add = [&](int64_t row0, int n, int rows, int rr) {
-      const int rb = rr / rows;
-      const int64_t at0 = row0 + (int64_t)(rb * a.Hkv + g) * n * rows + (rr - rb * rows);
-      // (only with group offsets that do not ascend)
-      if (row0 < 0 || n > a.grid || rr < 0 || at0 + (int64_t)(n - 1) * rows >= a.part_rows) return;
-      for (int s = 0; s < n; ++s) {
-        const int64_t at = at0 + (int64_t)s * rows;
-        const float lse = a.part_lse[at];
-        if (lse == -INFINITY) continue;              // no key seen
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + d);
-        const float mm = max_f(m, lse);
-        const float f = exp2_fast(m - mm), w = exp2_fast(lse - mm);
-        m = mm;
-        l = l * f + w;
+  const int item = threadIdx.x % kItems, share = threadIdx.x / kItems;
+  const int i = min((int)blockIdx.y * kItems + item, per * D4 - 1);
+  const int r = i / D4, d = i % D4 * 4;
+  float m = kNoMax, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  auto fold = [&](float lse, f32x4 v) {
+    if (lse == -INFINITY) return;              // no key seen
+    const float mm = max_f(m, lse);
+    const float f = exp2_fast(m - mm), w = exp2_fast(lse - mm);
+    m = mm;
+    l = l * f + w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o[e] = (f == 0.f ? 0.f : o[e] * f) + (w == 0.f ? 0.f : v[e] * w);
+    for (int e = 0; e < 4; ++e) o[e] = (f == 0.f ? 0.f : o[e] * f) + (w == 0.f ? 0.f : v[e] * w);
+  };
+  auto add = [&](int64_t row0, int n, int rows, int rr) {
+    if (n <= 0) return;
+    const int rb = rr / rows;
+    const int64_t at0 = row0 + (int64_t)(rb * a.Hkv + g) * n * rows + (rr - rb * rows);
+    // (only with group offsets that do not ascend)
+    if (row0 < 0 || n > a.most_parts || rr < 0 || at0 + (int64_t)(n - 1) * rows >= a.part_rows) return;
+    for (int s = share; s < n; s += kShares * kBatch) {
+      float lse[kBatch];
+      f32x4 v[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int64_t at = at0 + (int64_t)min(s + kShares * j, n - 1) * rows;
+        lse[j] = s + kShares * j < n ? a.part_lse[at] : -INFINITY;
+        v[j] = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + d);
       }
-    };
-    add(pp.row0, pp.n, a.shared_rows, (b - pre.seq0) * per + r);
-    add(po.row0, po.n, a.own_rows, r);
-    const int q = r / a.G;
-    const int64_t row = ((int64_t)b * a.q_len + q) * a.Hq + g * a.G + (r - q * a.G);
-    f32x4 res;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) res[e] = l == 0.f ? 0.f : o[e] / l;
-    *reinterpret_cast<f32x4 *>(a.out + row * D + d) = res;
-    if (d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      for (int j = 0; j < kBatch; ++j) fold(lse[j], v[j]);
+    }
+  };
+  add(pp.row0, pp.n, a.shared_rows, (b - pre.seq0) * per + r);
+  add(po.row0, po.n, a.own_rows, r);
+  s_o[share][item] = o;
+  s_m[share][item] = m;
+  s_l[share][item] = l;
+  __syncthreads();
+  if (share != 0 || (int)blockIdx.y * kItems + item >= per * D4) return;
+#pragma unroll
+  for (int t = 1; t < kShares; ++t) {
+    const float lt = s_l[t][item];
+    if (lt == 0.f) continue;                   // nothing there (a sum is 0 only then; NaN is not)
+    const float mt = s_m[t][item], mm = max_f(m, mt);
+    const float f = exp2_fast(m - mm), w = exp2_fast(mt - mm);
+    const f32x4 v = s_o[t][item];
+    m = mm;
+    l = l * f + lt * w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (f == 0.f ? 0.f : o[e] * f) + (w == 0.f ? 0.f : v[e] * w);
   }
+  const int qi = r / a.G;
+  const int64_t row = ((int64_t)b * a.q_len + qi) * a.Hq + g * a.G + (r - qi * a.G);
+  f32x4 res;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) res[e] = l == 0.f ? 0.f : o[e] / l;
+  *reinterpret_cast<f32x4 *>(a.out + row * D + d) = res;
+  if (d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 template <int KV, int D>
 void launch_d(const SharedArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((attn_shared_kernel<KV, D>), dim3((unsigned)a.grid), dim3(64 * kWaves), 0, s, a);
-  hipLaunchKernelGGL(merge_shared_kernel<D>, dim3((unsigned)(a.batch * a.Hkv)), dim3(256), 0, s, a);
+  constexpr int kWaves = waves_of(KV, D);
+  const dim3 grid((unsigned)a.grid), block(64 * kWaves);
+  const int wr = a.shared_rows / kRows;
+  if (wr == 1) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 1>), grid, block, 0, s, a);
+  if constexpr (KV != kF32) {
+    if (wr == 2) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 2>), grid, block, 0, s, a);
+    if (wr == 4) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 4>), grid, block, 0, s, a);
+    if constexpr (kWaves == 8)
+      if (wr == 8) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 8>), grid, block, 0, s, a);
+  }
+  const int items = a.q_len * a.G * (D / 4);
+  hipLaunchKernelGGL(merge_shared_kernel<D>,
+                     dim3((unsigned)(a.batch * a.Hkv), (unsigned)((items + kItems - 1) / kItems)),
+                     dim3(kItems * kShares), 0, s, a);
 }
 
 template <int KV>
@@ -673,6 +1057,18 @@ void launch_kv(const SharedArgs &a, hipStream_t s) {
 }
 
 }  // namespace
+
+// Wavefronts with rows of their own: enough for a group's rows, of the numbers
+// there are kernels for. float32 takes one: its matrix instructions are what such
+// a call waits for (32 rows and keys of 128 dims: 8192 cycles of them for 32 KB),
+// and row blocks that read the same pages again get them from the caches.
+int shared_row_waves(int kv_type, int D, long long rows) {
+  if (kv_type == kF32) return 1;
+  int wr = 1;
+  while (wr < waves_of(kv_type, D) && rows > (long long)wr * kRows) wr *= 2;
+  return wr;
+}
+int shared_waves(int kv_type, int D) { return waves_of(kv_type, D); }
 
 hipError_t launch_attn_shared(const SharedArgs &a, hipStream_t s) {
   if (a.kv_type == kF32) launch_kv<kF32>(a, s);

@@ -848,29 +848,37 @@ kap_status kap_verify(const kap_kv_cache *kv, int32_t batch, int32_t q_len, cons
 // Sizes of a call's work map and workspace: [parts of groups][parts of
 // sequences][partial o][partial lse].
 struct SharedPlan {
-  int shared_rows, own_rows, target, least;
-  long long slots_shared, slots_own;           // bounds on the parts of either kind
-  long long part_rows;
+  int shared_rows, own_rows, target, least, own_least;
+  long long grid, most_parts, own_base, part_rows;
   size_t seq_parts, part_o, part_lse, total;
 };
 
+// The work is spread over one workgroup per CU; the rows of an average group say
+// how many of its wavefronts take rows of their own.
 static SharedPlan plan_shared(const kap_kv_cache *kv, int batch, int q_len, int num_groups) {
   SharedPlan p;
   const long long per = (long long)q_len * (kv->num_q_heads / kv->num_kv_heads);
   const long long rows = per * batch;
-  p.shared_rows = 32;
+  const int waves = kap::shared_waves(kv->kv_dtype, kv->head_dim);
+  p.shared_rows = 32 * kap::shared_row_waves(kv->kv_dtype, kv->head_dim,
+                                             num_groups > 0 ? rows / num_groups : 1);
   p.own_rows = (int)std::min<long long>(32, per);
-  p.target = 2 * device_cus();
-  p.least = 8;
-  const long long blocks = rows / p.shared_rows + num_groups;
-  p.slots_shared = num_groups ? p.target + blocks * kv->num_kv_heads : 0;
-  p.slots_own = p.target + (long long)batch * cdiv(per, p.own_rows) * kv->num_kv_heads;
-  p.part_rows = p.slots_shared * p.shared_rows + p.slots_own * p.own_rows;
-  const size_t part_rows = (size_t)p.part_rows;
+  p.target = device_cus();
+  p.least = 16;
+  p.own_least = 2;
+  // parts of groups (workgroups), and of sequences (wavefronts)
+  const long long shared =
+      num_groups ? p.target + (rows / p.shared_rows + num_groups) * kv->num_kv_heads : 0;
+  const long long own = (long long)p.target * waves +
+                        (long long)batch * cdiv(per, p.own_rows) * kv->num_kv_heads;
+  p.grid = shared + (own + waves - 1) / waves;
+  p.most_parts = (long long)(p.target + 1) * waves;
+  p.own_base = shared * p.shared_rows;
+  p.part_rows = p.own_base + own * p.own_rows;
   p.seq_parts = round_up((size_t)num_groups * sizeof(kap::PartsOf), 256);
   p.part_o = p.seq_parts + round_up((size_t)batch * sizeof(kap::PartsOf), 256);
-  p.part_lse = p.part_o + round_up(part_rows * kv->head_dim * sizeof(float), 256);
-  p.total = p.part_lse + round_up(part_rows * sizeof(float), 256);
+  p.part_lse = p.part_o + round_up((size_t)p.part_rows * kv->head_dim * sizeof(float), 256);
+  p.total = p.part_lse + round_up((size_t)p.part_rows * sizeof(float), 256);
   return p;
 }
 
@@ -942,11 +950,12 @@ kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_le
   a.scale_log2 = sm_scale * kap::kLog2e;
   a.shared_rows = p.shared_rows;
   a.own_rows = p.own_rows;
-  a.shared_cost = 1;
-  a.own_cost = 1;
   a.target = p.target;
   a.least = p.least;
-  a.grid = p.slots_shared + p.slots_own - (num_groups ? p.target : 0);
+  a.own_least = p.own_least;
+  a.grid = p.grid;
+  a.most_parts = p.most_parts;
+  a.own_base = p.own_base;
   a.part_rows = p.part_rows;
   a.group_parts = reinterpret_cast<kap::PartsOf *>(base);
   a.seq_parts = reinterpret_cast<kap::PartsOf *>(base + p.seq_parts);

@@ -207,9 +207,10 @@ struct SharedArgs {
   const int32_t *shared;         // [num_groups] shared pages
   float scale_log2;              // sm_scale * log2(e)
   int shared_rows, own_rows;     // rows of a block
-  int shared_cost, own_cost;     // of a step
-  int target, least;             // workgroups the work is spread over; least cost of one
-  int64_t grid, part_rows;       // workgroups; rows of the partials
+  int target;                    // workgroups the work is spread over
+  int least, own_least;          // least steps of a workgroup, of a wavefront by itself
+  int64_t grid, most_parts;      // workgroups; most parts of a unit
+  int64_t own_base, part_rows;   // rows of the partials: sequences' own from own_base on
   PartsOf *group_parts, *seq_parts;
   float *part_o, *part_lse;      // [rows][D], [rows]: normalised, log2 domain
   float *out, *lse;
@@ -243,6 +244,8 @@ SampleLayout sample_layout(int rows, int vocab, int cus);
 
 hipError_t launch_compile_plan(const PlanArgs &a, hipStream_t s);
 hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);
+int shared_row_waves(int kv_type, int D, long long rows);
+int shared_waves(int kv_type, int D);
 hipError_t launch_attn_shared(const SharedArgs &a, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
 hipError_t launch_fallback_update(const FallbackArgs &a, hipStream_t s);
