@@ -338,12 +338,14 @@ template <int D> struct State {
   float ref, sum;    // reference (powers of two), and this lane's half of the sum
 };
 
-// Weights of a step's logits (z: in powers of two), in place; moves the reference.
+// Weights of a step's logits (c z: in powers of two, c >= 0), in place; moves the
+// reference.
 template <int D>
-__device__ __forceinline__ void weigh(State<D> &st, f32x16 &z) {
+__device__ __forceinline__ void weigh(State<D> &st, f32x16 &z, float c) {
   float top = max_f(z[0], z[1]);
 #pragma unroll
   for (int i = 2; i < 16; ++i) top = max_f(top, z[i]);
+  top *= c;
   if (__any(top > st.ref)) {
     top = max_f(top, other_half(top));
     const float ref = top > st.ref ? top + kDefer : st.ref;
@@ -357,7 +359,7 @@ __device__ __forceinline__ void weigh(State<D> &st, f32x16 &z) {
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    z[i] = exp2_fast(z[i] - st.ref);
+    z[i] = exp2_fast(fmaf(z[i], c, -st.ref));
     st.sum += z[i];
   }
 }
@@ -517,16 +519,37 @@ struct Walk {
 __device__ __forceinline__ bool in_pool(const SharedArgs &a, int id) {
   return id >= 0 && (int64_t)id < a.num_pages;
 }
-__device__ __forceinline__ Step step_at(const SharedArgs &a, const Walk &w, int s) {
-  Step x;
-#pragma unroll
-  for (int pg = 0; pg < 2; ++pg) {
-    const int id = s < w.s1 && 2 * s + pg < w.pages ? w.table[2 * s + pg] : -1;
-    x.ok[pg] = in_pool(a, id);
-    x.id[pg] = x.ok[pg] ? id : 0;
+// Page ids of a wavefront's steps first, first + stride, ..: 32 steps' in the lanes
+// of one register, the next 32 steps' on the way. (A load of an id right before
+// it is needed would be waited for with everything that is in flight.)
+struct PageIds {
+  int cur, next, k0, first, stride;
+  __device__ int fetch(const Walk &w, int k) const {
+    const int lane = threadIdx.x & 63, e = 2 * (first + (k + (lane >> 1)) * stride) + (lane & 1);
+    return w.table[min(e, max(w.pages - 1, 0))];
   }
-  return x;
-}
+  __device__ PageIds(const Walk &w, int first_, int stride_) : k0(0), first(first_), stride(stride_) {
+    cur = fetch(w, 0);
+    next = fetch(w, 32);
+  }
+  // of the k-th step; k never goes back
+  __device__ Step at(const SharedArgs &a, const Walk &w, int k) {
+    if (k - k0 >= 32) {
+      k0 += 32;
+      cur = next;
+      next = fetch(w, k0 + 32);
+    }
+    const int s = first + k * stride;
+    Step x;
+#pragma unroll
+    for (int pg = 0; pg < 2; ++pg) {
+      const int id = __builtin_amdgcn_readlane(cur, 2 * (k - k0) + pg);
+      x.ok[pg] = s < w.s1 && 2 * s + pg < w.pages && in_pool(a, id);
+      x.id[pg] = x.ok[pg] ? id : 0;
+    }
+    return x;
+  }
+};
 // plain: what positions allow, if all the pages up to there are in the pool (the
 // lanes of `n` threads look at them).
 __device__ __forceinline__ bool pages_fine(const SharedArgs &a, const Walk &w, int thread, int n) {
@@ -538,15 +561,15 @@ __device__ __forceinline__ int plain_by_position(const Walk &w) {
   return max(w.s0, min(min(w.s1, w.pages / 2), (w.all / kPage - w.page0) / 2));
 }
 
-// One step with its operands; ks, vs: the pages' scales (fp8).
-template <int KV, int D, bool MASKED, class Source>
-__device__ __forceinline__ void take_step(State<D> &st, const SharedArgs &a, const Walk &w,
-                                          const Queries<KV, D> &q, const Source &src, int s,
-                                          const bool (&ok)[2], int limit, const float (&ks)[2],
-                                          const float (&vs)[2]) {
+// Raw logits to powers of two, up to the factor that is returned (not negative:
+// the sign of sm_scale is in Q). MASKED: keys that a row does not see to -inf.
+template <int KV, bool MASKED>
+__device__ __forceinline__ float scale_logits(const SharedArgs &a, const Walk &w, f32x16 &z,
+                                              uint32_t &seen, int s, const bool (&ok)[2], int limit,
+                                              const float (&ks)[2]) {
   const int hb = (threadIdx.x & 63) >> 5;
-  f32x16 z = logits<KV, D>(src, q);
-  uint32_t seen = 0xffffu;
+  seen = 0xffffu;
+  if constexpr (KV != kFP8 && !MASKED) return a.scale_log2;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     z[i] *= KV == kFP8 ? a.scale_log2 * ks[i >> 3] : a.scale_log2;
@@ -556,7 +579,19 @@ __device__ __forceinline__ void take_step(State<D> &st, const SharedArgs &a, con
       if (!(ok[i >> 3] && pos < w.some)) seen &= ~(1u << i);
     }
   }
-  weigh(st, z);
+  return 1.f;
+}
+
+// One step with its operands; ks, vs: the pages' scales (fp8).
+template <int KV, int D, bool MASKED, class Source>
+__device__ __forceinline__ void take_step(State<D> &st, const SharedArgs &a, const Walk &w,
+                                          const Queries<KV, D> &q, const Source &src, int s,
+                                          const bool (&ok)[2], int limit, const float (&ks)[2],
+                                          const float (&vs)[2]) {
+  f32x16 z = logits<KV, D>(src, q);
+  uint32_t seen;
+  const float c = scale_logits<KV, MASKED>(a, w, z, seen, s, ok, limit, ks);
+  weigh(st, z, c);
   add_values<KV, D, MASKED>(st, src, z, seen, vs);
 }
 
@@ -578,65 +613,54 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
                                             const Queries<KV, D> &q, int g, int first, int stride,
                                             int limit) {
   const int lane = threadIdx.x & 63;
-  const bool fine[2] = {true, true};
-  int s = first;
+  if (first >= w.s1) return;
+  PageIds ids(w, first, stride);
+  int k = 0;
+  auto step = [&](int i) { return first + i * stride; };
   if constexpr (KV != kF32 || D < 256) {
     // the next step's K is fetched as soon as this one's has been multiplied, and
-    // so is V; the page ids two steps ahead
-    auto ids = [&](int t, int (&id)[2]) {
-      t = min(t, w.plain - 1);
-      id[0] = w.table[2 * t];
-      id[1] = w.table[2 * t + 1];
-    };
-    if (s < w.plain) {
-      int id[2], id1[2], id2[2];
+    // so is V
+    if (first < w.plain) {
+      const bool fine[2] = {true, true};
       float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f}, ks1[2] = {1.f, 1.f}, vs1[2] = {1.f, 1.f};
-      ids(s, id);
-      ids(s + stride, id1);
       Held<KV, D> r;
       {
-        const Pages<KV, D> p(a, id, g, lane);
+        const Step x = ids.at(a, w, 0);
+        const Pages<KV, D> p(a, x.id, g, lane);
         r.load_k(p);
         r.load_v(p);
-        scales_of<KV>(a, id, ks, vs);
+        scales_of<KV>(a, x.id, ks, vs);
       }
       for (;;) {
-        const bool more = s + stride < w.plain;
-        const Pages<KV, D> p(a, id1, g, lane);
-        ids(s + 2 * stride, id2);
-        scales_of<KV>(a, id1, ks1, vs1);
+        const bool more = step(k + 1) < w.plain;
+        const Step x = ids.at(a, w, k + 1);
+        const Pages<KV, D> p(a, x.id, g, lane);
+        scales_of<KV>(a, x.id, ks1, vs1);
         f32x16 z = logits<KV, D>(r, q);
         __builtin_amdgcn_sched_barrier(0);
         if (more) r.load_k(p);
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] *= KV == kFP8 ? a.scale_log2 * ks[i >> 3] : a.scale_log2;
-        weigh(st, z);
-        add_values<KV, D, false>(st, r, z, 0xffffu, vs);
+        uint32_t seen;
+        const float c = scale_logits<KV, false>(a, w, z, seen, step(k), fine, limit, ks);
+        weigh(st, z, c);
+        add_values<KV, D, false>(st, r, z, seen, vs);
         __builtin_amdgcn_sched_barrier(0);
         if (more) r.load_v(p);
-        s += stride;
+        ++k;
         if (!more) break;
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
-          id1[pg] = id2[pg];
           ks[pg] = ks1[pg];
           vs[pg] = vs1[pg];
         }
       }
     }
-  } else {
-    for (; s < w.plain; s += stride) {
-      const Step x = step_at(a, w, s);
-      const float one[2] = {1.f, 1.f};
-      take_step<KV, D, false>(st, a, w, q, Pages<KV, D>(a, x.id, g, lane), s, fine, limit, one, one);
-    }
   }
-  for (; s < w.s1; s += stride) {
-    const Step x = step_at(a, w, s);
+  for (; step(k) < w.s1; ++k) {
+    const Step x = ids.at(a, w, k);
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
     scales_of<KV>(a, x.id, ks, vs);
-    take_step<KV, D, true>(st, a, w, q, Pages<KV, D>(a, x.id, g, lane), s, x.ok, limit, ks, vs);
+    take_step<KV, D, true>(st, a, w, q, Pages<KV, D>(a, x.id, g, lane), step(k), x.ok, limit, ks, vs);
   }
 }
 
@@ -675,12 +699,13 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
   constexpr size_t kPageTile = Pages<KV, D>::kTile;
   u32x4 raw[S::kAhead][S::kMine];
   float raw_scale[S::kAhead];
+  PageIds ids(w, w.s0 + tile, S::kTiles);
   const int stages = (w.s1 - w.s0 + S::kTiles - 1) / S::kTiles;
   const int plain = (w.plain - w.s0) / S::kTiles;
 
   auto fetch = [&](int stage, int slot) {
     if (!busy) return;
-    const Step x = step_at(a, w, w.s0 + stage * S::kTiles + tile);
+    const Step x = ids.at(a, w, stage);
     if constexpr (KV == kFP8) {
       const char *base = static_cast<const char *>(is_v ? a.v_pages : a.k_pages);
 #pragma unroll
@@ -761,10 +786,10 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
         }
         const int s = w.s0 + stage * S::kTiles + kw;
         bool ok[2] = {true, true};
-        if constexpr (kMasked) {
-          const Step x = step_at(a, w, s);
-          ok[0] = x.ok[0];
-          ok[1] = x.ok[1];
+        if constexpr (kMasked) {               // (few stages: ids are read again)
+#pragma unroll
+          for (int pg = 0; pg < 2; ++pg)
+            ok[pg] = s < w.s1 && 2 * s + pg < w.pages && in_pool(a, w.table[2 * s + pg]);
         }
         take_step<KV, D, kMasked>(st, a, w, q, src, s, ok, limit, ks, vs);
       }
@@ -832,7 +857,8 @@ void attn_shared_kernel(SharedArgs a) {
     q.lds = lds;
 #pragma unroll
     for (int c = 0; c < operands<KV, D>(); ++c) {
-      const u32x4 x = row.q < 0 ? u32x4{0, 0, 0, 0} : *reinterpret_cast<const u32x4 *>(p + c * 32);
+      u32x4 x = row.q < 0 ? u32x4{0, 0, 0, 0} : *reinterpret_cast<const u32x4 *>(p + c * 32);
+      x ^= a.q_sign;
       if constexpr (q_in_lds<KV, D>()) lds[c * 64] = x;   // read by this lane alone
       else q.q[c] = x;
     }

@@ -947,7 +947,8 @@ kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_le
   a.num_groups = num_groups;
   a.offsets = group_offsets;
   a.shared = shared_blocks;
-  a.scale_log2 = sm_scale * kap::kLog2e;
+  a.scale_log2 = (sm_scale < 0 ? -sm_scale : sm_scale) * kap::kLog2e;
+  a.q_sign = sm_scale < 0 ? (kv->q_dtype == KAP_DT_F32 ? 0x80000000u : 0x80008000u) : 0;
   a.shared_rows = p.shared_rows;
   a.own_rows = p.own_rows;
   a.target = p.target;

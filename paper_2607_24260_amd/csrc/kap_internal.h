@@ -205,7 +205,8 @@ struct SharedArgs {
   int num_groups;
   const int32_t *offsets;        // [num_groups + 1]
   const int32_t *shared;         // [num_groups] shared pages
-  float scale_log2;              // sm_scale * log2(e)
+  float scale_log2;              // |sm_scale| * log2(e)
+  uint32_t q_sign;               // flips the sign of a word of q if sm_scale < 0
   int shared_rows, own_rows;     // rows of a block
   int target;                    // workgroups the work is spread over
   int least, own_least;          // least steps of a workgroup, of a wavefront by itself
