@@ -338,10 +338,9 @@ template <int D> struct State {
   float ref, sum;    // reference (powers of two), and this lane's half of the sum
 };
 
-// Weights of a step's logits (c z: in powers of two, c >= 0), in place; moves the
-// reference.
+// Moves the reference above a step's logits (c z: in powers of two, c >= 0).
 template <int D>
-__device__ __forceinline__ void weigh(State<D> &st, f32x16 &z, float c) {
+__device__ __forceinline__ void move_reference(State<D> &st, const f32x16 &z, float c) {
   float top = max_f(z[0], z[1]);
 #pragma unroll
   for (int i = 2; i < 16; ++i) top = max_f(top, z[i]);
@@ -357,6 +356,10 @@ __device__ __forceinline__ void weigh(State<D> &st, f32x16 &z, float c) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) st.o[db][i] *= f;
   }
+}
+// Weights in the place of the logits.
+template <int D>
+__device__ __forceinline__ void weigh(State<D> &st, f32x16 &z, float c) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     z[i] = exp2_fast(fmaf(z[i], c, -st.ref));
@@ -591,6 +594,7 @@ __device__ __forceinline__ void take_step(State<D> &st, const SharedArgs &a, con
   f32x16 z = logits<KV, D>(src, q);
   uint32_t seen;
   const float c = scale_logits<KV, MASKED>(a, w, z, seen, s, ok, limit, ks);
+  move_reference(st, z, c);
   weigh(st, z, c);
   add_values<KV, D, MASKED>(st, src, z, seen, vs);
 }
@@ -642,6 +646,7 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
         __builtin_amdgcn_sched_barrier(0);
         uint32_t seen;
         const float c = scale_logits<KV, false>(a, w, z, seen, step(k), fine, limit, ks);
+        move_reference(st, z, c);
         weigh(st, z, c);
         add_values<KV, D, false>(st, r, z, seen, vs);
         __builtin_amdgcn_sched_barrier(0);
@@ -670,8 +675,13 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
 
 // A stage is WK = WAVES / WR tiles of 32 keys. Half of the wavefronts fetch K,
 // half V: each a run of one tile's blocks, into registers, several stages ahead of
-// the LDS buffer they go to. Two buffers, one barrier a stage: a buffer is written
-// again only after all wavefronts have passed the barrier of the stage between.
+// the LDS buffer they go to. Stage i multiplies K of i + 1 and V of i, so that the
+// matrix unit has the next logits to work on while the vector unit turns these
+// into weights (all wavefronts do the same between two barriers: without that a
+// stage of 256 rows took 3500 cycles, 1536 of them matrix instructions and about as
+// many vector instructions). Of K and of V there are two buffers, and one barrier a
+// stage: a buffer is written again only after all wavefronts have passed the
+// barrier that follows its last use.
 template <int KV, int D, int WR>
 struct Staging {
   static constexpr int kWaves = waves_of(KV, D), kTiles = kWaves / WR, kHalf = kWaves / 2;
@@ -681,7 +691,7 @@ struct Staging {
   static constexpr int kBusy = kLoads * kTiles / kMine;        // wavefronts of a half that fetch
   static constexpr int kAhead = kMine >= 8 ? 1 : (kMine >= 4 ? 2 : 4);   // stages
   static constexpr int kStage = kTiles * Tile<KV, D>::kBytes;
-  static constexpr int kScales = KV == kFP8 ? 2 * kTiles * 4 * 4 : 0;   // bytes
+  static constexpr int kScales = KV == kFP8 ? 4 * kTiles * 4 * 4 : 0;   // of four stages
   static constexpr int kBytes = 2 * kStage + kScales;
 };
 
@@ -697,26 +707,30 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
   const int load0 = wave % S::kHalf * S::kMine, tile = load0 / S::kLoads, c0 = load0 % S::kLoads;
   const bool has_scales = KV == kFP8 && !is_v && busy && c0 == 0;
   constexpr size_t kPageTile = Pages<KV, D>::kTile;
+  const char *const k_pages = static_cast<const char *>(a.k_pages);
+  const char *const v_pages = static_cast<const char *>(a.v_pages);
+  const char *const pages = is_v ? v_pages : k_pages;
   u32x4 raw[S::kAhead][S::kMine];
   float raw_scale[S::kAhead];
   PageIds ids(w, w.s0 + tile, S::kTiles);
   const int stages = (w.s1 - w.s0 + S::kTiles - 1) / S::kTiles;
   const int plain = (w.plain - w.s0) / S::kTiles;
 
-  auto fetch = [&](int stage, int slot) {
+  auto fetch = [&](int stage, int slot) __attribute__((always_inline)) {
     if (!busy) return;
     const Step x = ids.at(a, w, stage);
+    const int id0 = x.id[0], id1 = x.id[1];
     if constexpr (KV == kFP8) {
-      const char *base = static_cast<const char *>(is_v ? a.v_pages : a.k_pages);
 #pragma unroll
       for (int t = 0; t < S::kMine; ++t) {
         const int c = c0 + t, pg = c / (D / 64), part = c % (D / 64);
+        const int id = pg ? id1 : id0;
         raw[slot][t] = *reinterpret_cast<const u32x4 *>(
-            base + ((size_t)(pg ? x.id[1] : x.id[0]) * a.Hkv + g) * kPageTile + part * 1024 + lane * 16);
+            pages + ((size_t)id * a.Hkv + g) * kPageTile + part * 1024 + lane * 16);
       }
       if (has_scales)
         raw_scale[slot] =
-            lane < 4 ? a.kv_scales[2 * (size_t)(lane < 2 ? x.id[0] : x.id[1]) + (lane & 1)] : 0.f;
+            lane < 4 ? a.kv_scales[2 * (size_t)(lane < 2 ? id0 : id1) + (lane & 1)] : 0.f;
     } else {
       const Pages<KV, D> p(a, x.id, g, lane);
 #pragma unroll
@@ -726,9 +740,9 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
       }
     }
   };
-  auto place = [&](int buffer, int slot) {
+  auto place = [&](int stage, int slot) __attribute__((always_inline)) {
     if (!busy) return;
-    u32x4 *to = reinterpret_cast<u32x4 *>(smem + buffer * S::kStage + tile * Tile<KV, D>::kBytes) +
+    u32x4 *to = reinterpret_cast<u32x4 *>(smem + (stage & 1) * S::kStage + tile * Tile<KV, D>::kBytes) +
                 (is_v ? operands<KV, D>() * 64 : 0);
 #pragma unroll
     for (int t = 0; t < S::kMine; ++t) {
@@ -752,15 +766,28 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
       }
     }
     if (has_scales && lane < 4)
-      reinterpret_cast<float *>(smem + 2 * S::kStage)[(buffer * S::kTiles + tile) * 4 + lane] =
+      reinterpret_cast<float *>(smem + 2 * S::kStage)[((stage & 3) * S::kTiles + tile) * 4 + lane] =
           raw_scale[slot];
   };
 
+  // K runs a stage ahead of V: its wavefronts' slot of stage i holds stage i + 1.
+  const int lead = is_v ? 0 : 1;
+  auto tile_at = [&](int stage) {
+    return Tile<KV, D>{reinterpret_cast<const u32x4 *>(smem + (stage & 1) * S::kStage +
+                                                       kw * Tile<KV, D>::kBytes) + lane};
+  };
+  if (lead) {
+    fetch(0, 0);
+    place(0, 0);
+  }
 #pragma unroll
   for (int u = 0; u < S::kAhead; ++u)
-    if (u < stages) fetch(u, u);
+    if (u + lead < stages) fetch(u + lead, u);
+  __syncthreads();
+  f32x16 z = zero16();
+  if (!idle) z = logits<KV, D>(tile_at(0), q);
   int stage0 = 0;
-  auto walk = [&](auto masked, int end) {
+  auto walk = [&](auto masked, int end) __attribute__((always_inline)) {
     constexpr bool kMasked = decltype(masked)::value;
     // (slots are numbered from the walk's first stage on, which is a multiple of kAhead)
     for (; stage0 < end; stage0 += S::kAhead) {
@@ -768,17 +795,14 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
       for (int u = 0; u < S::kAhead; ++u) {
         const int stage = stage0 + u;
         if (kMasked && stage >= end) break;
-        const int buffer = stage & 1;
-        place(buffer, u);
+        if (stage + lead < stages) place(stage + lead, u);
         __syncthreads();
-        if (stage + S::kAhead < stages) fetch(stage + S::kAhead, u);
+        if (stage + lead + S::kAhead < stages) fetch(stage + lead + S::kAhead, u);
         if (idle) continue;
-        const Tile<KV, D> src{reinterpret_cast<const u32x4 *>(smem + buffer * S::kStage +
-                                                              kw * Tile<KV, D>::kBytes) + lane};
         float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
         if constexpr (KV == kFP8) {
-          const float *sc = reinterpret_cast<const float *>(smem + 2 * S::kStage) +
-                            (buffer * S::kTiles + kw) * 4;
+          const f32x4 sc = *reinterpret_cast<const f32x4 *>(
+              smem + 2 * S::kStage + ((stage & 3) * S::kTiles + kw) * 16);
           ks[0] = sc[0];
           vs[0] = sc[1];
           ks[1] = sc[2];
@@ -791,7 +815,14 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
           for (int pg = 0; pg < 2; ++pg)
             ok[pg] = s < w.s1 && 2 * s + pg < w.pages && in_pool(a, w.table[2 * s + pg]);
         }
-        take_step<KV, D, kMasked>(st, a, w, q, src, s, ok, limit, ks, vs);
+        uint32_t seen;
+        const float c = scale_logits<KV, kMasked>(a, w, z, seen, s, ok, limit, ks);
+        move_reference(st, z, c);
+        // (past the last stage: what the buffer holds, for nothing)
+        const f32x16 z1 = logits<KV, D>(tile_at(stage + 1), q);
+        weigh(st, z, c);
+        add_values<KV, D, kMasked>(st, tile_at(stage), z, seen, vs);
+        z = z1;
       }
     }
   };
