@@ -123,52 +123,66 @@ __device__ __forceinline__ Unit seq_unit(const SharedArgs &a, int b) {
   return Unit{b, a.q_len * a.G, sh, max(0, np - sh)};
 }
 
-__device__ __forceinline__ long long wave_sum(long long x) {
+__device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
   return x;
 }
 
-// Work item of a wavefront. The cost of a step is that of its pages' bytes, the
-// same for either kind of unit. C, the cost of all units over the workgroups
-// wanted, is what a workgroup gets: a group's shared pages are split into
-// ceil(steps / C) parts, a workgroup each; a sequence's own into parts of C over
-// the wavefronts of a workgroup, a wavefront each. Parts are numbered group by
-// group, then sequence by sequence, so there are at most `target` workgroups plus
-// one part per (unit, row block, head): the grid.
+// Work item of a wavefront. A step of a group's shared pages costs a.shared_cost, one
+// of a sequence's own a.own_cost (a wavefront's share of a workgroup's time). C is
+// what a workgroup gets; shared pages are split into parts of up to C, a workgroup
+// each, a sequence's own into parts of up to C over the wavefronts of a workgroup, a
+// wavefront each. The last part of a unit is not full, by one half on average and by
+// more in a unit shorter than C: C is the cost of all units over the workgroups
+// wanted less those, so that what runs at once is filled and no few parts are left to
+// run after it. Parts are numbered group by group, then sequence by sequence. There
+// are at most total / C, so at most `target`, workgroups plus one part per (unit, row
+// block, head): the grid. The sums are float32, their rounding well inside the slack
+// taken of C: every wavefront of the launch finds the same C, from the same operations.
 template <int WAVES>
 __device__ bool shared_map(const SharedArgs &a, int w, int wave, Item &it) {
   const int lane = threadIdx.x & 63;
   auto steps_of = [](const Unit &u) { return (u.pages + 1) / 2; };
   auto blocks_of = [&](const Unit &u, bool shared) {
     const int br = shared ? a.shared_rows : a.own_rows;
-    return (u.rows + br - 1) / br;
+    return div_small(u.rows + br - 1, br);
   };
   auto unit_of = [&](bool shared, int i) {
     const int n = shared ? a.num_groups : a.batch;
     if (i >= n) return Unit{0, 0, 0, 0};
     return shared ? group_unit(a, i) : seq_unit(a, i);
   };
-  long long total = 0;
-  Unit first[2];                               // of the first 64, kept for the second pass
-  for (int kind = 0; kind < 2; ++kind) {
-    const int n = kind == 0 ? a.num_groups : a.batch;
-    first[kind] = unit_of(kind == 0, lane);
-    total += (long long)steps_of(first[kind]) * blocks_of(first[kind], kind == 0);
-    for (int i0 = 64; i0 < n; i0 += 64) {
-      const Unit u = unit_of(kind == 0, i0 + lane);
-      total += (long long)steps_of(u) * blocks_of(u, kind == 0);
-    }
-  }
-  total = wave_sum(total) * a.Hkv;
-  const int most =
-      (int)min(max((total + a.target - 1) / a.target, (long long)a.least), 0x3fffffffll);
+  Unit first[2];                               // of the first 64, kept for the later passes
+  first[0] = unit_of(true, lane);
+  first[1] = unit_of(false, lane);
+  // f(cost, row blocks, shared) of all units, the sum over the lanes
+  auto sum = [&](auto f) {
+    auto of = [&](const Unit &u, bool shared) {
+      return f((float)steps_of(u) * (float)(shared ? a.shared_cost : a.own_cost),
+               (float)(u.pages > 0 ? blocks_of(u, shared) : 0), shared);
+    };
+    float x = of(first[0], true) + of(first[1], false);
+    for (int i0 = 64; i0 < a.num_groups; i0 += 64) x += of(unit_of(true, i0 + lane), true);
+    for (int i0 = 64; i0 < a.batch; i0 += 64) x += of(unit_of(false, i0 + lane), false);
+    return wave_sum(x) * (float)a.Hkv;
+  };
+  const float total = sum([](float cost, float blocks, bool) { return cost * blocks; });
+  const float per = (float)a.target / fmaxf(total, 1.f);
+  const float unfilled = sum([&](float cost, float blocks, bool shared) {
+    const float full = cost * per * (shared ? 1.f : (float)WAVES);   // parts, were they all full
+    return fmaxf(0.5f, 1.f - full) * blocks * (shared ? 1.f : 1.f / WAVES);
+  });
+  const float wanted = fmaxf((float)a.target - unfilled, 0.5f * a.target);
+  const float most = fmaxf(total * 1.0001f / wanted, (float)a.least);
+  const int len[2] = {                         // steps of a part
+      (int)fminf(ceilf(most / a.shared_cost), 1e9f),
+      max((int)fminf(ceilf(most / (a.own_cost * WAVES)), 1e9f), a.own_least)};
   int base = 0;
   for (int kind = 0; kind < 2; ++kind) {
     const bool shared = kind == 0;
     const int n = shared ? a.num_groups : a.batch;
     const int slot_rows = shared ? a.shared_rows : a.own_rows;
-    const int len = shared ? most : max((most + WAVES - 1) / WAVES, a.own_least);
     const int64_t start = shared ? 0 : a.own_base;
     if (!shared) {                             // parts are wavefronts' from here on
       w = (w - base) * WAVES + wave;
@@ -177,7 +191,7 @@ __device__ bool shared_map(const SharedArgs &a, int w, int wave, Item &it) {
     for (int i0 = 0; i0 < n; i0 += 64) {
       const Unit u = i0 == 0 ? first[kind] : unit_of(shared, i0 + lane);
       const int rb = blocks_of(u, shared);
-      const int parts = div_small(steps_of(u) + len - 1, len);
+      const int parts = div_small(steps_of(u) + len[kind] - 1, len[kind]);
       const int cnt = parts * rb * a.Hkv;
       const int incl = wave_scan_add(cnt), excl = incl - cnt;
       const unsigned long long hit = __ballot(w >= base + excl && w < base + incl);
@@ -250,15 +264,19 @@ template <int KV, int D>
 struct Pages {
   static constexpr size_t kTile = (size_t)kPage * D * elem_bytes(KV);
   const char *k, *v[2];
-  __device__ Pages(const SharedArgs &a, const int (&id)[2], int g, int lane) {
+  // not live: the loads are issued all the same, all lanes' from one place (a branch
+  // around them would leave the compiler no count of what is in flight, and make
+  // every wait one for everything)
+  __device__ Pages(const SharedArgs &a, const int (&id)[2], int g, int lane, bool live = true) {
     const int i = lane & 31, hb = lane >> 5, tok = key_of_row<KV>(i) & 15;
+    const int k_at = tok * 8 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 128 * elem_bytes(KV));
+    const int v_at = i * 16 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 8 * elem_bytes(KV));
     k = static_cast<const char *>(a.k_pages) +
-        ((size_t)(i < 16 ? id[0] : id[1]) * a.Hkv + g) * kTile +
-        tok * 8 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 128 * elem_bytes(KV));
+        ((size_t)(i < 16 && live ? id[0] : id[1]) * a.Hkv + g) * kTile + (live ? k_at : 0);
 #pragma unroll
     for (int pg = 0; pg < 2; ++pg)
       v[pg] = static_cast<const char *>(a.v_pages) + ((size_t)id[pg] * a.Hkv + g) * kTile +
-              i * 16 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 8 * elem_bytes(KV));
+              (live ? v_at : 0);
   }
   __device__ Operand<KV> raw_key(int c) const {
     return *reinterpret_cast<const Operand<KV> *>(k + c * (KV == kF32 ? 512 : 256 * elem_bytes(KV)));
@@ -427,6 +445,40 @@ __device__ __forceinline__ u32x4 class_words(u32x4 v, int cls) {
   return m;
 }
 
+// Infinities and NaNs of V that were kept out of the products: added by class to
+// the rows that give them a weight.
+template <int KV, int D, class Source>
+__device__ __forceinline__ void add_classes(State<D> &st, const Source &src, const f32x16 &w,
+                                            uint32_t seen) {
+  for (int cls = 0; cls < 3; ++cls) {
+    const float what = cls == 0 ? INFINITY : (cls == 1 ? -INFINITY : __builtin_nanf(""));
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      f32x16 hits = zero16();
+#pragma unroll
+      for (int y = 0; y < v_parts<KV>(); ++y) {
+        const u32x4 one = class_words<KV>(src.value(y, db) & seen_words<KV>(seen, y), cls);
+        if constexpr (KV == kF32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            hits = mfma(__uint_as_float(one[e]), w[4 * y + e] != 0.f ? 1.f : 0.f, hits);
+        } else {
+          u32x4 nz;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            nz[i] = (w[8 * y + 2 * i] != 0.f ? 0x3f80u : 0u) |
+                    (w[8 * y + 2 * i + 1] != 0.f ? 0x3f800000u : 0u);
+          hits = mfma(one, nz, hits);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        st.o[db][i] += hits[i] != 0.f ? what : 0.f;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
 // O += V^T P^T for a step's weights w. MASKED: some key of the step is hidden
 // from some row. V of keys that no row sees is cleared, and infinities and NaNs
 // of the others are kept out of the products, where a weight of zero would spread
@@ -464,36 +516,8 @@ __device__ __forceinline__ void add_values(State<D> &st, const Source &src, cons
     }
     if (MASKED || KV == kF32) __builtin_amdgcn_sched_barrier(0);
   }
-  if constexpr (MASKED) {
-    if (!__any(wild != 0u)) return;
-    for (int cls = 0; cls < 3; ++cls) {
-      const float what = cls == 0 ? INFINITY : (cls == 1 ? -INFINITY : __builtin_nanf(""));
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        f32x16 hits = zero16();
-#pragma unroll
-        for (int y = 0; y < v_parts<KV>(); ++y) {
-          const u32x4 one = class_words<KV>(src.value(y, db) & seen_words<KV>(seen, y), cls);
-          if constexpr (KV == kF32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              hits = mfma(__uint_as_float(one[e]), w[4 * y + e] != 0.f ? 1.f : 0.f, hits);
-          } else {
-            u32x4 nz;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              nz[i] = (w[8 * y + 2 * i] != 0.f ? 0x3f80u : 0u) |
-                      (w[8 * y + 2 * i + 1] != 0.f ? 0x3f800000u : 0u);
-            hits = mfma(one, nz, hits);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          st.o[db][i] += hits[i] != 0.f ? what : 0.f;
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  }
+  if constexpr (MASKED)
+    if (__any(wild != 0u)) add_classes<KV, D>(st, src, w, seen);
 }
 
 // The rows of a block that a lane serves.
@@ -638,11 +662,11 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
       for (;;) {
         const bool more = step(k + 1) < w.plain;
         const Step x = ids.at(a, w, k + 1);
-        const Pages<KV, D> p(a, x.id, g, lane);
+        const Pages<KV, D> p(a, x.id, g, lane, more);
         scales_of<KV>(a, x.id, ks1, vs1);
         f32x16 z = logits<KV, D>(r, q);
         __builtin_amdgcn_sched_barrier(0);
-        if (more) r.load_k(p);
+        r.load_k(p);
         __builtin_amdgcn_sched_barrier(0);
         uint32_t seen;
         const float c = scale_logits<KV, false>(a, w, z, seen, step(k), fine, limit, ks);
@@ -650,7 +674,7 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
         weigh(st, z, c);
         add_values<KV, D, false>(st, r, z, seen, vs);
         __builtin_amdgcn_sched_barrier(0);
-        if (more) r.load_v(p);
+        r.load_v(p);
         ++k;
         if (!more) break;
 #pragma unroll
@@ -688,12 +712,92 @@ struct Staging {
   // 1 KB loads of a tile's K (or V), and of a wavefront in a stage
   static constexpr int kLoads = KV == kFP8 ? operands<KV, D>() / 2 : operands<KV, D>();
   static constexpr int kMine = kLoads * kTiles < kHalf ? 1 : kLoads * kTiles / kHalf;
-  static constexpr int kBusy = kLoads * kTiles / kMine;        // wavefronts of a half that fetch
+  static constexpr int kBusy = kLoads * kTiles / kMine;   // of a half; any others fetch the same
   static constexpr int kAhead = kMine >= 8 ? 1 : (kMine >= 4 ? 2 : 4);   // stages
   static constexpr int kStage = kTiles * Tile<KV, D>::kBytes;
   static constexpr int kScales = KV == kFP8 ? 4 * kTiles * 4 * 4 : 0;   // of four stages
   static constexpr int kBytes = 2 * kStage + kScales;
 };
+
+// A stage of one wavefront: weights of the logits z of tile `now` and its values,
+// and z of tile `next`. Operands are read from LDS a group of four ahead of the
+// matrix instructions that take them, in regions that the scheduler may not cross
+// (left alone, it reads each operand right before it is multiplied: most of a stage
+// was waiting for LDS), and the vector instructions are shared out over them.
+template <int KV, int D, bool MASKED>
+__device__ __forceinline__ void staged_step(State<D> &st, f32x16 &z, const SharedArgs &a,
+                                            const Walk &walk, const Queries<KV, D> &q,
+                                            const Tile<KV, D> &now, const Tile<KV, D> &next, int s,
+                                            const bool (&ok)[2], int limit, const float (&ks)[2],
+                                            const float (&vs)[2]) {
+  constexpr int K = operands<KV, D>(), DB = D / 32;
+  constexpr int kGroup = DB < 4 ? DB : 4;                  // operands of a group
+  constexpr int kQk = K / kGroup, kPv = DB / kGroup;       // groups: K's, V's of a page
+  constexpr int kGroups = kQk + 2 * kPv;
+  u32x4 op[2][kGroup];
+  auto read = [&](int g, u32x4 (&to)[kGroup]) {
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) {
+      if (g < kQk) to[i] = next.key(g * kGroup + i);
+      else to[i] = now.value((g - kQk) / kPv, (g - kQk) % kPv * kGroup + i);
+    }
+  };
+  read(0, op[0]);
+  __builtin_amdgcn_sched_barrier(0);
+  uint32_t seen, wild = 0;
+  const float c = scale_logits<KV, MASKED>(a, walk, z, seen, s, ok, limit, ks);
+  move_reference(st, z, c);
+  __builtin_amdgcn_sched_barrier(0);
+  f32x16 z1 = zero16();
+  u32x4 hi, lo, sees;
+  auto weigh_page = [&](int y) {
+#pragma unroll
+    for (int i = 8 * y; i < 8 * y + 8; ++i) {
+      z[i] = exp2_fast(fmaf(z[i], c, -st.ref));
+      st.sum += z[i];
+    }
+  };
+  u32x4 hi1, lo1;
+  auto split_page = [&](int y, u32x4 &h, u32x4 &l) {
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = KV == kFP8 ? z[8 * y + i] * vs[y] : z[8 * y + i];
+    split8(p, h, l);
+  };
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    if (g + 1 < kGroups) read(g + 1, op[(g + 1) & 1]);
+    if (g < kQk) {
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) z1 = mfma(op[g & 1][i], q.at(g * kGroup + i), z1);
+      if (g == 0) weigh_page(0);
+      if (g == kQk - 1) {
+        split_page(0, hi, lo);
+        weigh_page(1);
+      }
+    } else {
+      const int y = (g - kQk) / kPv, db0 = (g - kQk) % kPv * kGroup;
+      if constexpr (MASKED) sees = seen_words<KV>(seen, y);
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) {
+        u32x4 v = op[g & 1][i];
+        if constexpr (MASKED) {
+          v &= sees;
+          const u32x4 m = wild_words<KV>(v);
+          wild |= m[0] | m[1] | m[2] | m[3];
+          v &= ~m;
+        }
+        st.o[db0 + i] = mfma(v, y ? hi1 : hi, st.o[db0 + i]);
+        st.o[db0 + i] = mfma(v, y ? lo1 : lo, st.o[db0 + i]);
+      }
+      if (g == kQk) split_page(1, hi1, lo1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if constexpr (MASKED)
+    if (__any(wild != 0u)) add_classes<KV, D>(st, now, z, seen);
+  z = z1;
+}
 
 template <int KV, int D, int WR>
 __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, const Walk &w,
@@ -703,9 +807,9 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kw = wave / WR;                    // tile of a stage this wavefront multiplies
   // what it fetches
-  const bool is_v = wave >= S::kHalf, busy = wave % S::kHalf < S::kBusy;
-  const int load0 = wave % S::kHalf * S::kMine, tile = load0 / S::kLoads, c0 = load0 % S::kLoads;
-  const bool has_scales = KV == kFP8 && !is_v && busy && c0 == 0;
+  const bool is_v = wave >= S::kHalf;
+  const int load0 = wave % S::kBusy * S::kMine, tile = load0 / S::kLoads, c0 = load0 % S::kLoads;
+  const bool has_scales = KV == kFP8 && !is_v && c0 == 0;
   constexpr size_t kPageTile = Pages<KV, D>::kTile;
   const char *const k_pages = static_cast<const char *>(a.k_pages);
   const char *const v_pages = static_cast<const char *>(a.v_pages);
@@ -717,7 +821,7 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
   const int plain = (w.plain - w.s0) / S::kTiles;
 
   auto fetch = [&](int stage, int slot) __attribute__((always_inline)) {
-    if (!busy) return;
+    const bool live = stage < stages;
     const Step x = ids.at(a, w, stage);
     const int id0 = x.id[0], id1 = x.id[1];
     if constexpr (KV == kFP8) {
@@ -726,13 +830,11 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
         const int c = c0 + t, pg = c / (D / 64), part = c % (D / 64);
         const int id = pg ? id1 : id0;
         raw[slot][t] = *reinterpret_cast<const u32x4 *>(
-            pages + ((size_t)id * a.Hkv + g) * kPageTile + part * 1024 + lane * 16);
+            pages + ((size_t)id * a.Hkv + g) * kPageTile + (live ? part * 1024 + lane * 16 : 0));
       }
-      if (has_scales)
-        raw_scale[slot] =
-            lane < 4 ? a.kv_scales[2 * (size_t)(lane < 2 ? id0 : id1) + (lane & 1)] : 0.f;
+      raw_scale[slot] = a.kv_scales[2 * (size_t)(lane & 2 ? id1 : id0) + (lane & 1)];
     } else {
-      const Pages<KV, D> p(a, x.id, g, lane);
+      const Pages<KV, D> p(a, x.id, g, lane, live);
 #pragma unroll
       for (int t = 0; t < S::kMine; ++t) {
         const int c = c0 + t;
@@ -741,7 +843,6 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
     }
   };
   auto place = [&](int stage, int slot) __attribute__((always_inline)) {
-    if (!busy) return;
     u32x4 *to = reinterpret_cast<u32x4 *>(smem + (stage & 1) * S::kStage + tile * Tile<KV, D>::kBytes) +
                 (is_v ? operands<KV, D>() * 64 : 0);
 #pragma unroll
@@ -782,7 +883,7 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
   }
 #pragma unroll
   for (int u = 0; u < S::kAhead; ++u)
-    if (u + lead < stages) fetch(u + lead, u);
+    fetch(u + lead, u);
   __syncthreads();
   f32x16 z = zero16();
   if (!idle) z = logits<KV, D>(tile_at(0), q);
@@ -795,9 +896,9 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
       for (int u = 0; u < S::kAhead; ++u) {
         const int stage = stage0 + u;
         if (kMasked && stage >= end) break;
-        if (stage + lead < stages) place(stage + lead, u);
+        place(stage + lead, u);
         __syncthreads();
-        if (stage + lead + S::kAhead < stages) fetch(stage + lead + S::kAhead, u);
+        fetch(stage + lead + S::kAhead, u);
         if (idle) continue;
         float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
         if constexpr (KV == kFP8) {
@@ -815,14 +916,9 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, c
           for (int pg = 0; pg < 2; ++pg)
             ok[pg] = s < w.s1 && 2 * s + pg < w.pages && in_pool(a, w.table[2 * s + pg]);
         }
-        uint32_t seen;
-        const float c = scale_logits<KV, kMasked>(a, w, z, seen, s, ok, limit, ks);
-        move_reference(st, z, c);
         // (past the last stage: what the buffer holds, for nothing)
-        const f32x16 z1 = logits<KV, D>(tile_at(stage + 1), q);
-        weigh(st, z, c);
-        add_values<KV, D, kMasked>(st, tile_at(stage), z, seen, vs);
-        z = z1;
+        staged_step<KV, D, kMasked>(st, z, a, w, q, tile_at(stage), tile_at(stage + 1), s, ok, limit,
+                                    ks, vs);
       }
     }
   };

@@ -848,13 +848,17 @@ kap_status kap_verify(const kap_kv_cache *kv, int32_t batch, int32_t q_len, cons
 // Sizes of a call's work map and workspace: [parts of groups][parts of
 // sequences][partial o][partial lse].
 struct SharedPlan {
-  int shared_rows, own_rows, target, least, own_least;
+  int shared_rows, own_rows, target, shared_cost, own_cost, least, own_least;
   long long grid, most_parts, own_base, part_rows;
   size_t seq_parts, part_o, part_lse, total;
 };
 
 // The work is spread over one workgroup per CU; the rows of an average group say
-// how many of its wavefronts take rows of their own.
+// how many of its wavefronts take rows of their own, WR. A step of shared pages then
+// keeps the matrix units busy for 0.18 WR us (128 dims, bf16), and one of own pages
+// costs a wavefront's eighth of the time its bytes take, 0.38 us (fp8 0.2): costs of
+// WR : 2 and WR : 1, at least the bytes' own. float32 waits for the matrix units in
+// either.
 static SharedPlan plan_shared(const kap_kv_cache *kv, int batch, int q_len, int num_groups) {
   SharedPlan p;
   const long long per = (long long)q_len * (kv->num_q_heads / kv->num_kv_heads);
@@ -864,7 +868,10 @@ static SharedPlan plan_shared(const kap_kv_cache *kv, int batch, int q_len, int 
                                              num_groups > 0 ? rows / num_groups : 1);
   p.own_rows = (int)std::min<long long>(32, per);
   p.target = device_cus();
-  p.least = 16;
+  const int wr = p.shared_rows / 32;
+  p.own_cost = kv->kv_dtype == KAP_DT_FP8_E4M3FN ? 1 : 2;
+  p.shared_cost = std::max(p.own_cost, wr);
+  p.least = 16 * p.own_cost;
   p.own_least = 2;
   // parts of groups (workgroups), and of sequences (wavefronts)
   const long long shared =
@@ -952,6 +959,8 @@ kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_le
   a.shared_rows = p.shared_rows;
   a.own_rows = p.own_rows;
   a.target = p.target;
+  a.shared_cost = p.shared_cost;
+  a.own_cost = p.own_cost;
   a.least = p.least;
   a.own_least = p.own_least;
   a.grid = p.grid;

@@ -209,7 +209,8 @@ struct SharedArgs {
   uint32_t q_sign;               // flips the sign of a word of q if sm_scale < 0
   int shared_rows, own_rows;     // rows of a block
   int target;                    // workgroups the work is spread over
-  int least, own_least;          // least steps of a workgroup, of a wavefront by itself
+  int shared_cost, own_cost;     // of a step
+  int least, own_least;          // least cost of a workgroup, steps of a wavefront by itself
   int64_t grid, most_parts;      // workgroups; most parts of a unit
   int64_t own_base, part_rows;   // rows of the partials: sequences' own from own_base on
   PartsOf *group_parts, *seq_parts;
