@@ -141,9 +141,9 @@ struct RopeAppendArgs {
   const float *kv_scales;                   // fp8 only
   int64_t num_pages;
   int32_t *bad_slots;                       // may be NULL
-  // set at launch: tokens per workgroup that rotates, workgroups per tile of
-  // tokens for Q and K, workgroups that share a tile's V columns
-  int tile, q_slices, k_slices, v_share;
+  // set at launch: tokens per tile, tiles, workgroups per tile: for Q, for K, that
+  // share a part of its V columns, all; heads of a rotating thread
+  int tile, tiles, q_slices, k_slices, v_share, roles, heads;
 };
 
 // kap_compact_view after host validation.

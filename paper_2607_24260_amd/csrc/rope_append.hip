@@ -10,7 +10,17 @@
 // 32-bit angle is off by up to 2^-7. Sine and cosine of what is left, and the
 // rotation, are 32-bit.
 //
-// Bound by memory: every element is read once and written once.
+// Bound by memory: every element is read once and written once. 8192 tokens of 32
+// query and 8 KV heads of 128 dims, bf16 (201 MB): 42.5 us, 4.7 TB/s, which is what a
+// copy of that size reaches; the angles are not seen in it (42.5 us without them).
+// float32, 3711 tokens of 16 and 8 heads of 64 dims (61 MB): 15.2 us, 4.0 TB/s. A few
+// tokens are bound by the chain of reads from slots to scales to pages and by the
+// launch: 320 tokens with fp8 pages 8.1 us, one token 4.3 us.
+//
+// A workgroup is a role (Q heads, K heads, V columns) of a tile of 16 tokens. The
+// workgroups that an XCD is given one after the other are the roles of one tile: Q's
+// rows are then read and written in one sweep (51 us when a role went over all tiles
+// first, 8192 tokens) and each XCD has as many of each role.
 #include "kap_internal.h"
 
 #include <algorithm>
@@ -20,8 +30,20 @@ namespace kap {
 namespace {
 
 constexpr int kThreads = 256;
+// Rows from here on (more than an L2's 4 MB) are not kept in the caches: 8192 tokens
+// 48.2 -> 42.5 us, 1024 tokens 12.5 -> 10.8 us, 512 tokens 9.4 -> 9.0 us; below there
+// is no difference, and what reads Q next may find it in an L2. float32 rows are kept:
+// a chunk of theirs is two stores, which the caches join (16 -> 25 us without).
+constexpr long long kOnceBytes = 4 << 20;
+// Workgroups to reach before a thread takes more than one head (320 tokens: 9.9 us
+// with four heads a thread, 8.1 us with one; 8192 tokens 62.8 us with two, 61.2 us
+// with four, 59.7 us with eight, then more registers than pay elsewhere).
+constexpr long long kFull = 512;
 // Heads whose loads a thread has in flight.
 constexpr int kHeads = 4;
+// Rows: at any address; 16-byte loads; those, and without a place in the caches kept
+// for what is not used again here.
+constexpr int kUnaligned = 0, kAligned = 1, kOnce = 2;
 
 template <int KV> using In = typename std::conditional<KV == kF32, uint32_t, uint16_t>::type;
 template <int KV>
@@ -32,10 +54,12 @@ using Out = typename std::conditional<
 // is aligned for them).
 template <int KV> struct Raw8 { kv_u32x4 r[KV == kF32 ? 2 : 1]; };
 
-template <int KV, bool ALIGNED>
+template <int KV, int MODE>
 __device__ __forceinline__ Raw8<KV> load8(const In<KV> *p) {
   Raw8<KV> x;
-  if constexpr (ALIGNED) {
+  if constexpr (MODE == kOnce) {
+    x.r[0] = __builtin_nontemporal_load(reinterpret_cast<const kv_u32x4 *>(p));
+  } else if constexpr (MODE == kAligned) {
     x.r[0] = reinterpret_cast<const kv_u32x4 *>(p)[0];
     if constexpr (KV == kF32) x.r[1] = reinterpret_cast<const kv_u32x4 *>(p)[1];
   } else if constexpr (KV == kF32) {
@@ -58,7 +82,7 @@ __device__ __forceinline__ void widen8(const Raw8<KV> &x, float v[8]) {
 }
 
 // In the type they came in, rounded once (nearest even).
-template <int KV>
+template <int KV, int MODE>
 __device__ __forceinline__ void store8(void *p, const float v[8]) {
   kv_u32x4 *d = static_cast<kv_u32x4 *>(p);
   if constexpr (KV == kF32) {
@@ -67,8 +91,10 @@ __device__ __forceinline__ void store8(void *p, const float v[8]) {
     d[1] = kv_u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]),
                     __float_as_uint(v[7])};
   } else {
-    d[0] = kv_u32x4{round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]),
-                    round_bf16x2(v[6], v[7])};
+    const kv_u32x4 x = {round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]),
+                        round_bf16x2(v[4], v[5]), round_bf16x2(v[6], v[7])};
+    if constexpr (MODE == kOnce) __builtin_nontemporal_store(x, d);
+    else *d = x;
   }
 }
 
@@ -83,7 +109,7 @@ __device__ __forceinline__ uint32_t fp8_codes(float x0, float x1, float x2, floa
 }
 
 // Chunk c (eight dims) of KV head g of the token in `off` of a page.
-template <int KV>
+template <int KV, int MODE>
 __device__ __forceinline__ void store_k(const RopeAppendArgs &a, int64_t page, int off, int g,
                                         int c, float scale, const float v[8]) {
   Out<KV> *d = static_cast<Out<KV> *>(a.k_pages) +
@@ -92,7 +118,7 @@ __device__ __forceinline__ void store_k(const RopeAppendArgs &a, int64_t page, i
     *reinterpret_cast<kv_u32x2 *>(d) = kv_u32x2{fp8_codes(v[0], v[1], v[2], v[3], scale),
                                                 fp8_codes(v[4], v[5], v[6], v[7], scale)};
   } else {
-    store8<KV>(d, v);
+    store8<KV, MODE>(d, v);
   }
 }
 
@@ -119,17 +145,17 @@ __device__ __forceinline__ float2 turn_of(int pos, float freq) {
 // row per token), or of K (tokens in neighbouring lanes: a page holds a chunk's
 // 16 tokens side by side). A thread has one chunk pair of one token -- eight
 // frequencies, in registers -- and goes over heads with it.
-template <int KV, bool ALIGNED>
-__device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, bool is_k, int slice,
+template <int KV, int MODE>
+__device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, int bx, bool is_k, int slice,
                                             float2 *s_cs) {
-  const int t0 = blockIdx.x * a.tile, nt = min(a.tile, a.num_tokens - t0);
+  const int t0 = bx * a.tile, nt = min(a.tile, a.num_tokens - t0);
   const int nf = a.rot / 2, P = a.rot / 16;
   const int per_head = P * a.tile, hs_n = kThreads / per_head;
   const int hs = threadIdx.x / per_head, rem = threadIdx.x - hs * per_head;
   const int tok = is_k ? rem % a.tile : rem / P;
   const int c = is_k ? rem / a.tile : rem - tok * P;
   const int H = is_k ? a.Hkv : a.Hq;
-  const int h0 = slice * hs_n * kHeads, h1 = min(H, h0 + hs_n * kHeads);
+  const int h0 = slice * hs_n * a.heads, h1 = min(H, h0 + hs_n * a.heads);
   const In<KV> *src = static_cast<const In<KV> *>(is_k ? a.k_new : a.q_new);
   const size_t stride = (size_t)(is_k ? a.k_stride : a.q_stride);
   const bool mine = hs < hs_n && tok < nt;
@@ -141,8 +167,8 @@ __device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, bool is_k, 
   for (int u = 0; u < kHeads; ++u) {
     const int h = h0 + hs + u * hs_n;
     if (mine && h < h1) {
-      xa[u] = load8<KV, ALIGNED>(row + (size_t)h * a.D + ca * 8);
-      xb[u] = load8<KV, ALIGNED>(row + (size_t)h * a.D + cb * 8);
+      xa[u] = load8<KV, MODE>(row + (size_t)h * a.D + ca * 8);
+      xb[u] = load8<KV, MODE>(row + (size_t)h * a.D + cb * 8);
     }
   }
   const int64_t most = a.num_pages * kPage;
@@ -191,12 +217,12 @@ __device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, bool is_k, 
       if (is_k) {
         const int64_t page = slot / kPage;
         const int off = (int)(slot - page * kPage);
-        store_k<KV>(a, page, off, h, ca, scale, p);
-        store_k<KV>(a, page, off, h, cb, scale, q);
+        store_k<KV, MODE>(a, page, off, h, ca, scale, p);
+        store_k<KV, MODE>(a, page, off, h, cb, scale, q);
       } else {
         In<KV> *dst = static_cast<In<KV> *>(a.q_out) + ((size_t)(t0 + tok) * a.Hq + h) * a.D;
-        store8<KV>(dst + ca * 8, p);
-        store8<KV>(dst + cb * 8, q);
+        store8<KV, MODE>(dst + ca * 8, p);
+        store8<KV, MODE>(dst + cb * 8, q);
       }
     }
   }
@@ -216,15 +242,15 @@ __device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, bool is_k, 
     }
     const int ch = a.rot / 8 + r;
     float x[8];
-    widen8<KV>(load8<KV, ALIGNED>(src + (size_t)(t0 + t) * stride + (size_t)h * a.D + ch * 8), x);
+    widen8<KV>(load8<KV, MODE>(src + (size_t)(t0 + t) * stride + (size_t)h * a.D + ch * 8), x);
     if (is_k) {
       const int64_t s = slot_of(t);
       if (s < 0) continue;
       const int64_t page = s / kPage;
       const float sc = KV == kFP8 ? a.kv_scales[2 * page] : 1.f;
-      store_k<KV>(a, page, (int)(s - page * kPage), h, ch, sc, x);
+      store_k<KV, MODE>(a, page, (int)(s - page * kPage), h, ch, sc, x);
     } else {
-      store8<KV>(static_cast<In<KV> *>(a.q_out) + ((size_t)(t0 + t) * a.Hq + h) * a.D + ch * 8, x);
+      store8<KV, MODE>(static_cast<In<KV> *>(a.q_out) + ((size_t)(t0 + t) * a.Hq + h) * a.D + ch * 8, x);
     }
   }
 }
@@ -232,15 +258,18 @@ __device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, bool is_k, 
 // V, which a page holds transposed. A whole page -- 16 consecutive tokens in its
 // 16 slots -- belongs to the 16 tokens it starts in, wherever in them it starts:
 // a lane reads its 4-byte column of all 16 tokens, turns it around in registers,
-// and a store instruction covers 1 KB (through LDS). Tokens outside whole pages
-// are stored element by element, shared out over a.v_share workgroups.
-template <int KV, bool ALIGNED>
-__device__ __forceinline__ void append_v(const RopeAppendArgs &a, int part, int share,
+// and a store instruction covers 1 KB (through LDS). Outside whole pages (a step's
+// first and last, and any with a padded token in it) four tokens in an aligned four
+// of a page's slots are one store a dim, and what is left is stored element by element
+// (8192 tokens, one in 64 padded: 10 us less than with all of such pages' tokens by
+// element), shared out over a.v_share workgroups.
+template <int KV, int MODE>
+__device__ __forceinline__ void append_v(const RopeAppendArgs &a, int bx, int part, int share,
                                          kv_u32x4 (*s_rows)[256]) {
   constexpr int kColDims = KV == kF32 ? 1 : 2;
   constexpr int kUnits = KV == kFP8 ? 2 : 4;   // 16-byte units of a column's page rows
   const int lane = threadIdx.x & 63;
-  const int t0 = blockIdx.x * kPage;
+  const int t0 = bx * kPage;
   const int row = a.Hkv * a.D, cols = row / kColDims;
   const In<KV> *src = static_cast<const In<KV> *>(a.v_new);
   const size_t stride = (size_t)a.v_stride;
@@ -259,8 +288,12 @@ __device__ __forceinline__ void append_v(const RopeAppendArgs &a, int part, int 
                      ((joined >> first >> 1) & 0x7FFFu) == 0x7FFFu;
   const bool mine = lane >= kPage && lane < 2 * kPage;
   const unsigned long long starts = __ballot(mine && whole && off == 0);   // at most one
-  unsigned single = (unsigned)(__ballot(mine && good && !whole && lane % a.v_share == share) >>
-                               kPage);
+  // likewise four tokens in an aligned four of a page's slots
+  const int four = lane - (off & 3);
+  const bool in_four = good && !whole && four >= 0 && ((joined >> four >> 1) & 7u) == 7u;
+  const bool shared_out = mine && good && !whole && lane % a.v_share == share;
+  unsigned fours = (unsigned)(__ballot(shared_out && in_four && (off & 3) == 0) >> kPage);
+  unsigned single = (unsigned)(__ballot(shared_out && !in_four) >> kPage);
   if (part == 0 && share == 0 && threadIdx.x < 64 && mine && slot >= 0 && !good && a.bad_slots)
     atomicAdd(a.bad_slots, 1);
   auto slot_at = [&](int l) {                  // slot of lane l (the same l in every lane)
@@ -279,7 +312,7 @@ __device__ __forceinline__ void append_v(const RopeAppendArgs &a, int part, int 
 #pragma unroll
       for (int i = 0; i < kPage; ++i) {
         const In<KV> *p = src + (size_t)(token + i) * stride + (size_t)col * kColDims;
-        if constexpr (ALIGNED || KV == kF32) x[i] = *reinterpret_cast<const uint32_t *>(p);
+        if constexpr (MODE != kUnaligned || KV == kF32) x[i] = *reinterpret_cast<const uint32_t *>(p);
         else x[i] = p[0] | (uint32_t)p[1] << 16;
       }
     }
@@ -321,6 +354,50 @@ __device__ __forceinline__ void append_v(const RopeAppendArgs &a, int part, int 
       if (col0 + c < cols) dst[u] = buf[kUnits * c + (((u & (kUnits - 1)) + (c >> 1)) & (kUnits - 1))];
     }
   }
+  // four tokens of a column in a store
+  const int my_col = part * kThreads + threadIdx.x;
+  while (fours) {
+    constexpr int kBatch = 2;
+    int token[kBatch];
+    uint32_t x[kBatch][4] = {};
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      token[i] = fours ? __builtin_ctz(fours) : -1;
+      fours &= fours - 1;
+      if (token[i] < 0 || my_col >= cols) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const In<KV> *p = src + (size_t)(t0 + token[i] + e) * stride + (size_t)my_col * kColDims;
+        if constexpr (MODE != kUnaligned || KV == kF32) x[i][e] = *reinterpret_cast<const uint32_t *>(p);
+        else x[i][e] = p[0] | (uint32_t)p[1] << 16;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (token[i] < 0 || my_col >= cols) continue;
+      const int64_t to = slot_at(kPage + token[i]);
+      const int64_t page = to / kPage;
+      Out<KV> *d = static_cast<Out<KV> *>(a.v_pages) + (size_t)page * row * kPage +
+                   (size_t)my_col * kColDims * kPage + (to & (kPage - 1));
+      if constexpr (KV == kF32) {
+        *reinterpret_cast<kv_u32x4 *>(d) = kv_u32x4{x[i][0], x[i][1], x[i][2], x[i][3]};
+      } else if constexpr (KV == kBF16) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t sel = e ? 0x07060302u : 0x05040100u;
+          *reinterpret_cast<kv_u32x2 *>(d + e * kPage) =
+              kv_u32x2{__builtin_amdgcn_perm(x[i][1], x[i][0], sel),
+                       __builtin_amdgcn_perm(x[i][3], x[i][2], sel)};
+        }
+      } else {
+        const float scale = a.kv_scales[2 * page + 1];
+        *reinterpret_cast<uint32_t *>(d) = fp8_codes(bf16_lo(x[i][0]), bf16_lo(x[i][1]),
+                                                     bf16_lo(x[i][2]), bf16_lo(x[i][3]), scale);
+        *reinterpret_cast<uint32_t *>(d + kPage) = fp8_codes(
+            bf16_hi(x[i][0]), bf16_hi(x[i][1]), bf16_hi(x[i][2]), bf16_hi(x[i][3]), scale);
+      }
+    }
+  }
   // element by element: a store instruction covers 64 neighbouring rows
   const int e0 = part * kThreads * kColDims + threadIdx.x;
   while (single) {
@@ -359,28 +436,33 @@ __device__ __forceinline__ void append_v(const RopeAppendArgs &a, int part, int 
   }
 }
 
-template <int KV, bool ALIGNED>
+template <int KV, int MODE>
 __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeAppendArgs a) {
   __shared__ union {
     float2 cs[kPage * 128];                    // [token][frequency]
     kv_u32x4 rows[kThreads / 64][256];
   } s;
-  const int y = blockIdx.y;
+  const int xcd = blockIdx.x & 7;
+  const int bx = (int)((blockIdx.x >> 3) / a.roles) * 8 + xcd;   // tile
+  const int y = (int)(blockIdx.x >> 3) % a.roles;
+  if (bx >= a.tiles) return;
   if (y < a.q_slices + a.k_slices) {
     const bool is_k = y >= a.q_slices;
-    rotate_rows<KV, ALIGNED>(a, is_k, is_k ? y - a.q_slices : y, s.cs);
+    rotate_rows<KV, MODE>(a, bx, is_k, is_k ? y - a.q_slices : y, s.cs);
   } else {
     const int v = y - a.q_slices - a.k_slices;
-    append_v<KV, ALIGNED>(a, v / a.v_share, v % a.v_share, s.rows);
+    append_v<KV, MODE>(a, bx, v / a.v_share, v % a.v_share, s.rows);
   }
 }
 
 template <int KV>
-void launch_kv(const RopeAppendArgs &a, dim3 grid, bool aligned, hipStream_t s) {
-  if (aligned)
-    hipLaunchKernelGGL((rope_append_kernel<KV, true>), grid, dim3(kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((rope_append_kernel<KV, false>), grid, dim3(kThreads), 0, s, a);
+void launch_kv(const RopeAppendArgs &a, unsigned grid, int mode, hipStream_t s) {
+  if (mode == kUnaligned)
+    hipLaunchKernelGGL((rope_append_kernel<KV, kUnaligned>), grid, dim3(kThreads), 0, s, a);
+  else if (mode == kAligned || KV == kF32)
+    hipLaunchKernelGGL((rope_append_kernel<KV, kAligned>), grid, dim3(kThreads), 0, s, a);
+  else if constexpr (KV != kF32)
+    hipLaunchKernelGGL((rope_append_kernel<KV, kOnce>), grid, dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
@@ -391,24 +473,32 @@ hipError_t launch_rope_append(const RopeAppendArgs &args, hipStream_t s) {
   const auto addr = reinterpret_cast<uintptr_t>(a.q_new) | reinterpret_cast<uintptr_t>(a.k_new) |
                     reinterpret_cast<uintptr_t>(a.v_new) |
                     (uintptr_t)((a.q_new ? a.q_stride : 0) | a.k_stride | a.v_stride) * es;
+  const long long row_bytes = (long long)((a.q_new ? a.Hq : 0) + 2 * a.Hkv) * a.D * es;
+  const int mode = addr % 16 != 0 ? kUnaligned
+                                  : (a.num_tokens * row_bytes >= kOnceBytes ? kOnce : kAligned);
   // Tiles of 16 tokens, or of all of them, so that a few tokens' heads spread
   // over a workgroup.
   a.tile = std::min(a.num_tokens, kPage);
-  const int heads = kHeads * (kThreads / (a.rot / 16 * a.tile));   // of a workgroup
+  a.tiles = (a.num_tokens - 1) / kPage + 1;
+  const int lanes = kThreads / (a.rot / 16 * a.tile);      // heads side by side
+  a.heads = kHeads;
+  while (a.heads > 1 && (long long)a.tiles * ((a.Hq + a.Hkv) / (lanes * a.heads)) < kFull) a.heads /= 2;
+  const int heads = a.heads * lanes;                       // of a workgroup
   a.q_slices = a.q_new ? (a.Hq + heads - 1) / heads : 0;
   a.k_slices = (a.Hkv + heads - 1) / heads;
   const int cols = a.Hkv * a.D / (a.kv_type == kF32 ? 1 : 2);
   const int parts = (cols + kThreads - 1) / kThreads;
-  const long long tiles = ((long long)a.num_tokens + kPage - 1) / kPage;
   // Tokens outside whole pages: one workgroup that moves 16 of them one after
   // the other takes as long, so they are shared out while there are few.
   a.v_share = 1;
-  while (a.v_share < kPage && 2 * tiles * parts * a.v_share <= 1024) a.v_share *= 2;
-  const dim3 grid((unsigned)tiles, (unsigned)(a.q_slices + a.k_slices + parts * a.v_share));
+  while (a.v_share < kPage && 2ll * a.tiles * parts * a.v_share <= 1024) a.v_share *= 2;
+  a.roles = a.q_slices + a.k_slices + parts * a.v_share;
+  const long long grid = ((long long)a.tiles + 7) / 8 * 8 * a.roles;
+  if (grid > 0x7fffffffll) return hipErrorInvalidValue;
   switch (a.kv_type) {
-    case kF32: launch_kv<kF32>(a, grid, addr % 16 == 0, s); break;
-    case kBF16: launch_kv<kBF16>(a, grid, addr % 16 == 0, s); break;
-    default: launch_kv<kFP8>(a, grid, addr % 16 == 0, s); break;
+    case kF32: launch_kv<kF32>(a, (unsigned)grid, mode, s); break;
+    case kBF16: launch_kv<kBF16>(a, (unsigned)grid, mode, s); break;
+    default: launch_kv<kFP8>(a, (unsigned)grid, mode, s); break;
   }
   return hipGetLastError();
 }
