@@ -26,6 +26,14 @@
 // vocab): the sums do not depend on their order, and a running weight is off by
 // less than vocab half units, where 32-bit floats would move the boundaries
 // between tokens by as much as whole tokens.
+//
+// Each launch reads the logits once (the later ones mostly from the caches). It is not
+// bytes that bound it: the first launch goes at 2.7 TB/s for 64 x 151936 bf16 logits
+// (7.3 us), the second computes weights (19.5 us), and the third is a chain of short
+// steps of a row (20.6 us: sums of the bins 3, search 3, collecting 5, then the last
+// workgroup's sort, sums and answers), of which few rows have no others to hide it
+// behind. 46 us in all; 320 x 151937 118 us (0.8 TB/s), 16 x 128000 float32 32 us,
+// 1 x 32000 float32 19 to 24 us (by the draw).
 #include "kap_internal.h"
 
 #include <algorithm>
@@ -86,10 +94,9 @@ struct Row {
     return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(x)[i] << 16);
   }
   // f(logits, index of the first) for the tokens of a chunk, kVec or one at a time,
-  // a thread's tokens in ascending order. Two loads of it are in flight.
+  // a thread's tokens in ascending order. The next load is on its way meanwhile.
   template <int THREADS, class F>
   __device__ __forceinline__ void each(int chunk, int chunks, F f) const {
-    constexpr int kLoads = 2;
     auto single = [&](int i) {
       const float y[1] = {one(i)};
       f(y, i);
@@ -98,19 +105,18 @@ struct Row {
     const kv_u32x4 *v = reinterpret_cast<const kv_u32x4 *>(x + (size_t)head * (F32 ? 4 : 2));
     const int per = (vecs + chunks - 1) / chunks;
     const int v0 = chunk * per, v1 = min(vecs, v0 + per);
-    for (int j = v0 + threadIdx.x; j < v1; j += kLoads * THREADS) {
-      kv_u32x4 w[kLoads];
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) w[u] = v[min(j + u * THREADS, v1 - 1)];
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        if (j + u * THREADS >= v1) break;
+    if (v0 < v1) {
+      int j = v0 + threadIdx.x;
+      kv_u32x4 w = v[min(j, v1 - 1)];
+      for (; j < v1; j += THREADS) {
+        const kv_u32x4 next = v[min(j + THREADS, v1 - 1)];   // (past the end: the last again)
         float y[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
-          y[e] = F32 ? __uint_as_float(w[u][e & 3])
-                     : ((e & 1) ? bf16_hi(w[u][(e >> 1) & 3]) : bf16_lo(w[u][(e >> 1) & 3]));
-        f(y, head + (j + u * THREADS) * kVec);
+          y[e] = F32 ? __uint_as_float(w[e & 3])
+                     : ((e & 1) ? bf16_hi(w[(e >> 1) & 3]) : bf16_lo(w[(e >> 1) & 3]));
+        f(y, head + j * kVec);
+        w = next;
       }
     }
     if (chunk == chunks - 1) {
@@ -139,9 +145,11 @@ struct Weights {
 // The same to 2^-44 of a weight, and its bin, for the sums over whole rows: with
 // y = log2 w in bins and n = rint(y), 2^n from a table with a bin's weight each,
 // times 2^(y - n) by its series to the fourth power (a bin is at most 1/64 of a
-// factor of two: (ln 2 / 128)^5 / 5! = 2^-44.5). Eleven 64-bit operations a
-// logit, which is what the second launch takes its time for (splitting off whole
-// factors of two and 32nds instead, with the fifth power: fifteen).
+// factor of two: (ln 2 / 128)^5 / 5! = 2^-44.5). Eleven 64-bit operations and about
+// thirty others a logit are what the second launch takes its time for: 64 rows of
+// 151936 logits 19.5 us, of which 12.7 us are this loop, and 18.8 us without its LDS
+// additions (splitting off whole factors of two and 32nds instead, with the fifth
+// power: fifteen 64-bit operations).
 struct FastWeights {
   double slope, offset;                        // y = x * slope + offset
   double c1, c2, c3, c4;                       // of 2^(y - n)
