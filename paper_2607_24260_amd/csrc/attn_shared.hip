@@ -13,14 +13,17 @@
 // key_of_row() those are eight neighbouring keys of either page, which is the
 // layout P^T's operand needs: weights never leave their lane.
 //
-// A workgroup takes a split of a group's shared pages with up to 32 WR rows: WR
-// wavefronts with 32 rows each, as many wavefronts as that leaves by different
-// keys. From WR = 2 on the pages go through LDS, so that each is read once per
-// workgroup, in operand blocks of 1 KB laid out as the lanes multiply them; fp8
-// codes are widened on the way in. With WR = 1, and for a sequence's own pages (a
-// wavefront by itself: unit, row block, KV head and split), operands go straight
-// from memory to the lane's registers, the next step's on the way while this one
-// is multiplied.
+// A workgroup takes 32 rows of a group and a split of its shared pages, a step for
+// each of its wavefronts in turn; a wavefront by itself takes up to 32 rows of a
+// sequence and a split of its own pages. Operands go straight from memory (or, where
+// other rows read the same pages, the caches) to the lane's registers, the next
+// step's on the way while this one is multiplied, and no wavefront waits for another
+// before the end: the matrix instructions of one then fall into the vector
+// instructions of the other. (Pages shared out through LDS, read once by wavefronts
+// with up to 256 rows between them, took 88 us where this takes 90 for 256 rows over
+// 32K positions, bf16 and 128 dims, but 56 us where this takes 53 for 128 rows, 56
+// and 45 with fp8 pages, 62 and 48 with 64 dims: barriers, and rows rounded up to a
+// power of two.)
 //
 // Weights are float32, split into bf16 hi + lo for 16-bit V, both rounded to
 // nearest (what is left out is at most 2^-18 of a weight; with hi truncated
@@ -129,23 +132,22 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-// Work item of a wavefront. A step of a group's shared pages costs a.shared_cost, one
-// of a sequence's own a.own_cost (a wavefront's share of a workgroup's time). C is
-// what a workgroup gets; shared pages are split into parts of up to C, a workgroup
-// each, a sequence's own into parts of up to C over the wavefronts of a workgroup, a
-// wavefront each. The last part of a unit is not full, by one half on average and by
-// more in a unit shorter than C: C is the cost of all units over the workgroups
-// wanted less those, so that what runs at once is filled and no few parts are left to
-// run after it. Parts are numbered group by group, then sequence by sequence. There
-// are at most total / C, so at most `target`, workgroups plus one part per (unit, row
-// block, head): the grid. The sums are float32, their rounding well inside the slack
-// taken of C: every wavefront of the launch finds the same C, from the same operations.
+// Work item of a wavefront. C steps are what a workgroup gets; shared pages are
+// split into parts of up to C steps, a workgroup each, a sequence's own into parts of
+// up to C over the wavefronts of a workgroup, a wavefront each. The last part of a
+// unit is not full, by one half on average and by more in a unit shorter than C: C is
+// all units' steps over the workgroups wanted less those, so that what runs at once is
+// filled and no few parts are left to run after it (four groups of 80 rows: 303 ->
+// 284 us). Parts are numbered group by group, then sequence by sequence. There are at
+// most total / C, so at most `target`, workgroups plus one part per (unit, row block,
+// head): the grid. The sums are float32, their rounding well inside the slack taken of
+// C: every wavefront of the launch finds the same C, from the same operations.
 template <int WAVES>
 __device__ bool shared_map(const SharedArgs &a, int w, int wave, Item &it) {
   const int lane = threadIdx.x & 63;
   auto steps_of = [](const Unit &u) { return (u.pages + 1) / 2; };
   auto blocks_of = [&](const Unit &u, bool shared) {
-    const int br = shared ? a.shared_rows : a.own_rows;
+    const int br = shared ? kRows : a.own_rows;
     return div_small(u.rows + br - 1, br);
   };
   auto unit_of = [&](bool shared, int i) {
@@ -159,30 +161,29 @@ __device__ bool shared_map(const SharedArgs &a, int w, int wave, Item &it) {
   // f(cost, row blocks, shared) of all units, the sum over the lanes
   auto sum = [&](auto f) {
     auto of = [&](const Unit &u, bool shared) {
-      return f((float)steps_of(u) * (float)(shared ? a.shared_cost : a.own_cost),
-               (float)(u.pages > 0 ? blocks_of(u, shared) : 0), shared);
+      return f((float)steps_of(u), (float)(u.pages > 0 ? blocks_of(u, shared) : 0), shared);
     };
     float x = of(first[0], true) + of(first[1], false);
     for (int i0 = 64; i0 < a.num_groups; i0 += 64) x += of(unit_of(true, i0 + lane), true);
     for (int i0 = 64; i0 < a.batch; i0 += 64) x += of(unit_of(false, i0 + lane), false);
     return wave_sum(x) * (float)a.Hkv;
   };
-  const float total = sum([](float cost, float blocks, bool) { return cost * blocks; });
+  const float total = sum([](float steps, float blocks, bool) { return steps * blocks; });
   const float per = (float)a.target / fmaxf(total, 1.f);
-  const float unfilled = sum([&](float cost, float blocks, bool shared) {
-    const float full = cost * per * (shared ? 1.f : (float)WAVES);   // parts, were they all full
+  const float unfilled = sum([&](float steps, float blocks, bool shared) {
+    const float full = steps * per * (shared ? 1.f : (float)WAVES);   // parts, were they all full
     return fmaxf(0.5f, 1.f - full) * blocks * (shared ? 1.f : 1.f / WAVES);
   });
   const float wanted = fmaxf((float)a.target - unfilled, 0.5f * a.target);
   const float most = fmaxf(total * 1.0001f / wanted, (float)a.least);
   const int len[2] = {                         // steps of a part
-      (int)fminf(ceilf(most / a.shared_cost), 1e9f),
-      max((int)fminf(ceilf(most / (a.own_cost * WAVES)), 1e9f), a.own_least)};
+      (int)fminf(ceilf(most), 1e9f),
+      max((int)fminf(ceilf(most / WAVES), 1e9f), a.own_least)};
   int base = 0;
   for (int kind = 0; kind < 2; ++kind) {
     const bool shared = kind == 0;
     const int n = shared ? a.num_groups : a.batch;
-    const int slot_rows = shared ? a.shared_rows : a.own_rows;
+    const int slot_rows = shared ? kRows : a.own_rows;
     const int64_t start = shared ? 0 : a.own_base;
     if (!shared) {                             // parts are wavefronts' from here on
       w = (w - base) * WAVES + wave;
@@ -291,7 +292,7 @@ struct Pages {
   __device__ u32x4 value(int y, int db) const { return wide(raw_value(y, db)); }
 };
 
-// The same in registers ...
+// The same in registers.
 template <int KV, int D>
 struct Held {
   Operand<KV> k[operands<KV, D>()], v[v_parts<KV>()][D / 32];
@@ -307,17 +308,6 @@ struct Held {
   }
   __device__ u32x4 key(int c) const { return wide(k[c]); }
   __device__ u32x4 value(int y, int db) const { return wide(v[y][db]); }
-};
-
-// ... and in LDS: blocks of 64 lanes' 16 bytes, K's and then V's.
-template <int KV, int D>
-struct Tile {
-  static constexpr int kBytes = 2 * operands<KV, D>() * 1024;
-  const u32x4 *at;                             // of this lane
-  __device__ u32x4 key(int c) const { return at[c * 64]; }
-  __device__ u32x4 value(int y, int db) const {
-    return at[(operands<KV, D>() + y * (D / 32) + db) * 64];
-  }
 };
 
 template <int KV, int D, class Source>
@@ -577,15 +567,17 @@ struct PageIds {
     return x;
   }
 };
-// plain: what positions allow, if all the pages up to there are in the pool (the
-// lanes of `n` threads look at them).
-__device__ __forceinline__ bool pages_fine(const SharedArgs &a, const Walk &w, int thread, int n) {
+// What positions allow, if the pages of the wavefront's steps up to there are in the
+// pool.
+__device__ __forceinline__ int plain_steps(const SharedArgs &a, const Walk &w, const PageIds &ids) {
+  const int end = max(w.s0, min(min(w.s1, w.pages / 2), (w.all / kPage - w.page0) / 2));
   bool fine = true;
-  for (int i = 2 * w.s0 + thread; i < 2 * w.plain; i += n) fine &= in_pool(a, w.table[i]);
-  return fine;
-}
-__device__ __forceinline__ int plain_by_position(const Walk &w) {
-  return max(w.s0, min(min(w.s1, w.pages / 2), (w.all / kPage - w.page0) / 2));
+  for (int k = 0; ids.first + k * ids.stride < end; k += 32) {
+    const int id = k == 0 ? ids.cur : (k == 32 ? ids.next : ids.fetch(w, k));
+    const int s = ids.first + (k + ((int)(threadIdx.x & 63) >> 1)) * ids.stride;
+    fine &= s >= end || in_pool(a, id);
+  }
+  return __any(!fine) ? w.s0 : end;
 }
 
 // Raw logits to powers of two, up to the factor that is returned (not negative:
@@ -638,11 +630,9 @@ __device__ __forceinline__ void scales_of(const SharedArgs &a, const int (&id)[2
 // Steps first, first + stride, .. below w.s1, operands from memory.
 template <int KV, int D>
 __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, const Walk &w,
-                                            const Queries<KV, D> &q, int g, int first, int stride,
-                                            int limit) {
-  const int lane = threadIdx.x & 63;
+                                            const Queries<KV, D> &q, int g, PageIds ids, int limit) {
+  const int lane = threadIdx.x & 63, first = ids.first, stride = ids.stride;
   if (first >= w.s1) return;
-  PageIds ids(w, first, stride);
   int k = 0;
   auto step = [&](int i) { return first + i * stride; };
   if constexpr (KV != kF32 || D < 256) {
@@ -694,275 +684,30 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
 }
 
 // ---------------------------------------------------------------------------
-// shared pages through LDS
-// ---------------------------------------------------------------------------
-
-// A stage is WK = WAVES / WR tiles of 32 keys. Half of the wavefronts fetch K,
-// half V: each a run of one tile's blocks, into registers, several stages ahead of
-// the LDS buffer they go to. Stage i multiplies K of i + 1 and V of i, so that the
-// matrix unit has the next logits to work on while the vector unit turns these
-// into weights (all wavefronts do the same between two barriers: without that a
-// stage of 256 rows took 3500 cycles, 1536 of them matrix instructions and about as
-// many vector instructions). Of K and of V there are two buffers, and one barrier a
-// stage: a buffer is written again only after all wavefronts have passed the
-// barrier that follows its last use.
-template <int KV, int D, int WR>
-struct Staging {
-  static constexpr int kWaves = waves_of(KV, D), kTiles = kWaves / WR, kHalf = kWaves / 2;
-  // 1 KB loads of a tile's K (or V), and of a wavefront in a stage
-  static constexpr int kLoads = KV == kFP8 ? operands<KV, D>() / 2 : operands<KV, D>();
-  static constexpr int kMine = kLoads * kTiles < kHalf ? 1 : kLoads * kTiles / kHalf;
-  static constexpr int kBusy = kLoads * kTiles / kMine;   // of a half; any others fetch the same
-  static constexpr int kAhead = kMine >= 8 ? 1 : (kMine >= 4 ? 2 : 4);   // stages
-  static constexpr int kStage = kTiles * Tile<KV, D>::kBytes;
-  static constexpr int kScales = KV == kFP8 ? 4 * kTiles * 4 * 4 : 0;   // of four stages
-  static constexpr int kBytes = 2 * kStage + kScales;
-};
-
-// A stage of one wavefront: weights of the logits z of tile `now` and its values,
-// and z of tile `next`. Operands are read from LDS a group of four ahead of the
-// matrix instructions that take them, in regions that the scheduler may not cross
-// (left alone, it reads each operand right before it is multiplied: most of a stage
-// was waiting for LDS), and the vector instructions are shared out over them.
-template <int KV, int D, bool MASKED>
-__device__ __forceinline__ void staged_step(State<D> &st, f32x16 &z, const SharedArgs &a,
-                                            const Walk &walk, const Queries<KV, D> &q,
-                                            const Tile<KV, D> &now, const Tile<KV, D> &next, int s,
-                                            const bool (&ok)[2], int limit, const float (&ks)[2],
-                                            const float (&vs)[2]) {
-  constexpr int K = operands<KV, D>(), DB = D / 32;
-  constexpr int kGroup = DB < 4 ? DB : 4;                  // operands of a group
-  constexpr int kQk = K / kGroup, kPv = DB / kGroup;       // groups: K's, V's of a page
-  constexpr int kGroups = kQk + 2 * kPv;
-  u32x4 op[2][kGroup];
-  auto read = [&](int g, u32x4 (&to)[kGroup]) {
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i) {
-      if (g < kQk) to[i] = next.key(g * kGroup + i);
-      else to[i] = now.value((g - kQk) / kPv, (g - kQk) % kPv * kGroup + i);
-    }
-  };
-  read(0, op[0]);
-  __builtin_amdgcn_sched_barrier(0);
-  uint32_t seen, wild = 0;
-  const float c = scale_logits<KV, MASKED>(a, walk, z, seen, s, ok, limit, ks);
-  move_reference(st, z, c);
-  __builtin_amdgcn_sched_barrier(0);
-  f32x16 z1 = zero16();
-  u32x4 hi, lo, sees;
-  auto weigh_page = [&](int y) {
-#pragma unroll
-    for (int i = 8 * y; i < 8 * y + 8; ++i) {
-      z[i] = exp2_fast(fmaf(z[i], c, -st.ref));
-      st.sum += z[i];
-    }
-  };
-  u32x4 hi1, lo1;
-  auto split_page = [&](int y, u32x4 &h, u32x4 &l) {
-    float p[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = KV == kFP8 ? z[8 * y + i] * vs[y] : z[8 * y + i];
-    split8(p, h, l);
-  };
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    if (g + 1 < kGroups) read(g + 1, op[(g + 1) & 1]);
-    if (g < kQk) {
-#pragma unroll
-      for (int i = 0; i < kGroup; ++i) z1 = mfma(op[g & 1][i], q.at(g * kGroup + i), z1);
-      if (g == 0) weigh_page(0);
-      if (g == kQk - 1) {
-        split_page(0, hi, lo);
-        weigh_page(1);
-      }
-    } else {
-      const int y = (g - kQk) / kPv, db0 = (g - kQk) % kPv * kGroup;
-      if constexpr (MASKED) sees = seen_words<KV>(seen, y);
-#pragma unroll
-      for (int i = 0; i < kGroup; ++i) {
-        u32x4 v = op[g & 1][i];
-        if constexpr (MASKED) {
-          v &= sees;
-          const u32x4 m = wild_words<KV>(v);
-          wild |= m[0] | m[1] | m[2] | m[3];
-          v &= ~m;
-        }
-        st.o[db0 + i] = mfma(v, y ? hi1 : hi, st.o[db0 + i]);
-        st.o[db0 + i] = mfma(v, y ? lo1 : lo, st.o[db0 + i]);
-      }
-      if (g == kQk) split_page(1, hi1, lo1);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  if constexpr (MASKED)
-    if (__any(wild != 0u)) add_classes<KV, D>(st, now, z, seen);
-  z = z1;
-}
-
-template <int KV, int D, int WR>
-__device__ __forceinline__ void walk_staged(State<D> &st, const SharedArgs &a, const Walk &w,
-                                            const Queries<KV, D> &q, int g, int limit, bool idle,
-                                            char *smem) {
-  using S = Staging<KV, D, WR>;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kw = wave / WR;                    // tile of a stage this wavefront multiplies
-  // what it fetches
-  const bool is_v = wave >= S::kHalf;
-  const int load0 = wave % S::kBusy * S::kMine, tile = load0 / S::kLoads, c0 = load0 % S::kLoads;
-  const bool has_scales = KV == kFP8 && !is_v && c0 == 0;
-  constexpr size_t kPageTile = Pages<KV, D>::kTile;
-  const char *const k_pages = static_cast<const char *>(a.k_pages);
-  const char *const v_pages = static_cast<const char *>(a.v_pages);
-  const char *const pages = is_v ? v_pages : k_pages;
-  u32x4 raw[S::kAhead][S::kMine];
-  float raw_scale[S::kAhead];
-  PageIds ids(w, w.s0 + tile, S::kTiles);
-  const int stages = (w.s1 - w.s0 + S::kTiles - 1) / S::kTiles;
-  const int plain = (w.plain - w.s0) / S::kTiles;
-
-  auto fetch = [&](int stage, int slot) __attribute__((always_inline)) {
-    const bool live = stage < stages;
-    const Step x = ids.at(a, w, stage);
-    const int id0 = x.id[0], id1 = x.id[1];
-    if constexpr (KV == kFP8) {
-#pragma unroll
-      for (int t = 0; t < S::kMine; ++t) {
-        const int c = c0 + t, pg = c / (D / 64), part = c % (D / 64);
-        const int id = pg ? id1 : id0;
-        raw[slot][t] = *reinterpret_cast<const u32x4 *>(
-            pages + ((size_t)id * a.Hkv + g) * kPageTile + (live ? part * 1024 + lane * 16 : 0));
-      }
-      raw_scale[slot] = a.kv_scales[2 * (size_t)(lane & 2 ? id1 : id0) + (lane & 1)];
-    } else {
-      const Pages<KV, D> p(a, x.id, g, lane, live);
-#pragma unroll
-      for (int t = 0; t < S::kMine; ++t) {
-        const int c = c0 + t;
-        raw[slot][t] = is_v ? p.raw_value(c / (D / 32), c % (D / 32)).x : p.raw_key(c).x;
-      }
-    }
-  };
-  auto place = [&](int stage, int slot) __attribute__((always_inline)) {
-    u32x4 *to = reinterpret_cast<u32x4 *>(smem + (stage & 1) * S::kStage + tile * Tile<KV, D>::kBytes) +
-                (is_v ? operands<KV, D>() * 64 : 0);
-#pragma unroll
-    for (int t = 0; t < S::kMine; ++t) {
-      const int c = c0 + t;
-      if constexpr (KV == kFP8) {
-        const int pg = c / (D / 64), part = c % (D / 64);
-        const u32x4 lo = widen8(u32x2{raw[slot][t][0], raw[slot][t][1]});
-        const u32x4 hi = widen8(u32x2{raw[slot][t][2], raw[slot][t][3]});
-        if (is_v) {                            // dim 64 part + lane: its keys 0..7 and 8..15
-          u32x4 *at = to + (pg * (D / 32) + 2 * part + (lane >> 5)) * 64 + (lane & 31);
-          at[0] = lo;
-          at[32] = hi;
-        } else {                               // chunk 8 part + lane / 8, two tokens
-          const int chunk = 8 * part + (lane >> 3), tok = 2 * (lane & 7);
-          u32x4 *at = to + (chunk >> 1) * 64 + (chunk & 1) * 32 + 16 * pg;
-          at[key_of_row<KV>(tok)] = lo;
-          at[key_of_row<KV>(tok + 1)] = hi;
-        }
-      } else {
-        to[c * 64 + lane] = raw[slot][t];
-      }
-    }
-    if (has_scales && lane < 4)
-      reinterpret_cast<float *>(smem + 2 * S::kStage)[((stage & 3) * S::kTiles + tile) * 4 + lane] =
-          raw_scale[slot];
-  };
-
-  // K runs a stage ahead of V: its wavefronts' slot of stage i holds stage i + 1.
-  const int lead = is_v ? 0 : 1;
-  auto tile_at = [&](int stage) {
-    return Tile<KV, D>{reinterpret_cast<const u32x4 *>(smem + (stage & 1) * S::kStage +
-                                                       kw * Tile<KV, D>::kBytes) + lane};
-  };
-  if (lead) {
-    fetch(0, 0);
-    place(0, 0);
-  }
-#pragma unroll
-  for (int u = 0; u < S::kAhead; ++u)
-    fetch(u + lead, u);
-  __syncthreads();
-  f32x16 z = zero16();
-  if (!idle) z = logits<KV, D>(tile_at(0), q);
-  int stage0 = 0;
-  auto walk = [&](auto masked, int end) __attribute__((always_inline)) {
-    constexpr bool kMasked = decltype(masked)::value;
-    // (slots are numbered from the walk's first stage on, which is a multiple of kAhead)
-    for (; stage0 < end; stage0 += S::kAhead) {
-#pragma unroll
-      for (int u = 0; u < S::kAhead; ++u) {
-        const int stage = stage0 + u;
-        if (kMasked && stage >= end) break;
-        place(stage + lead, u);
-        __syncthreads();
-        fetch(stage + lead + S::kAhead, u);
-        if (idle) continue;
-        float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
-        if constexpr (KV == kFP8) {
-          const f32x4 sc = *reinterpret_cast<const f32x4 *>(
-              smem + 2 * S::kStage + ((stage & 3) * S::kTiles + kw) * 16);
-          ks[0] = sc[0];
-          vs[0] = sc[1];
-          ks[1] = sc[2];
-          vs[1] = sc[3];
-        }
-        const int s = w.s0 + stage * S::kTiles + kw;
-        bool ok[2] = {true, true};
-        if constexpr (kMasked) {               // (few stages: ids are read again)
-#pragma unroll
-          for (int pg = 0; pg < 2; ++pg)
-            ok[pg] = s < w.s1 && 2 * s + pg < w.pages && in_pool(a, w.table[2 * s + pg]);
-        }
-        // (past the last stage: what the buffer holds, for nothing)
-        staged_step<KV, D, kMasked>(st, z, a, w, q, tile_at(stage), tile_at(stage + 1), s, ok, limit,
-                                    ks, vs);
-      }
-    }
-  };
-  walk(std::false_type{}, plain / S::kAhead * S::kAhead);
-  walk(std::true_type{}, stages);
-  __syncthreads();
-}
-
-// ---------------------------------------------------------------------------
 // the kernel
 // ---------------------------------------------------------------------------
 
-template <int KV, int D, int WR>
+template <int KV, int D>
 struct Layout {
   static constexpr int kWaves = waves_of(KV, D);
   // the wavefronts' parts, 32 dims at a time: [wave][row][32 dims + 4]
   static constexpr int kPart = kRows * 36 * 4;
-  static constexpr int kStaged = [] {
-    if constexpr (WR > 1) return Staging<KV, D, WR>::kBytes;
-    else return 0;
-  }();
-  static constexpr int kWalk = kStaged > kWaves * kPart ? kStaged : kWaves * kPart;
-  static constexpr int kBytes =
-      kWalk + (q_in_lds<KV, D>() ? kWaves * operands<KV, D>() * 1024 : 0);
+  static constexpr int kQ = kWaves * kPart;
+  static constexpr int kBytes = kQ + (q_in_lds<KV, D>() ? kWaves * operands<KV, D>() * 1024 : 0);
 };
 
-template <int KV, int D, int WR>
+template <int KV, int D>
 __global__ __launch_bounds__(64 * waves_of(KV, D))
 __attribute__((amdgpu_waves_per_eu(waves_of(KV, D) / 4)))
 void attn_shared_kernel(SharedArgs a) {
-  constexpr int kWaves = waves_of(KV, D), kTiles = kWaves / WR;
-  __shared__ __align__(16) char smem[Layout<KV, D, WR>::kBytes];
+  constexpr int kWaves = waves_of(KV, D);
+  __shared__ __align__(16) char smem[Layout<KV, D>::kBytes];
   __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
-  __shared__ int s_all, s_some, s_bad;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hb = lane >> 5;
-  if (threadIdx.x == 0) {
-    s_all = 0x7fffffff;
-    s_some = 0;
-    s_bad = 0;
-  }
   Item it;
   if (!shared_map<kWaves>(a, blockIdx.x, wave, it)) return;   // (a shared part: all wavefronts)
-  const int slot_rows = it.shared ? a.shared_rows : a.own_rows;
+  const int slot_rows = it.shared ? kRows : a.own_rows;
   const int64_t part0 =
       it.row0 + ((int64_t)(it.rb * a.Hkv + it.g) * it.n_split + it.split) * slot_rows;
   // (group offsets that do not ascend)
@@ -970,16 +715,24 @@ void attn_shared_kernel(SharedArgs a) {
   if (it.rb == 0 && it.g == 0 && it.split == 0 && (it.shared ? threadIdx.x == 0 : lane == 0))
     (it.shared ? a.group_parts : a.seq_parts)[it.unit] = PartsOf{it.row0, it.n_split, 0};
 
+  // ---- steps, a workgroup's wavefronts in turn ------------------------------------
+  Walk w;
+  w.table = a.table + (size_t)it.seq0 * a.stride + it.page0;
+  w.page0 = it.page0;
+  w.pages = it.pages;
+  const int steps = (it.pages + 1) / 2;
+  w.s0 = (int)((long long)steps * it.split / it.n_split);
+  w.s1 = (int)((long long)steps * (it.split + 1) / it.n_split);
+  const PageIds ids(w, w.s0 + (it.shared ? wave : 0), it.shared ? kWaves : 1);
+
   // ---- rows ---------------------------------------------------------------------
-  const int rw = it.shared ? wave % WR : 0;
-  const int r0 = it.rb * slot_rows + rw * kRows;        // of the unit
-  const int in_block = rw * kRows + (lane & 31);
-  const RowOf row = row_of(a, it, in_block < slot_rows ? it.rb * slot_rows + in_block : it.rows);
+  const int r0 = it.rb * slot_rows, rr = lane & 31;     // of the unit, of the block
+  const RowOf row = row_of(a, it, rr < slot_rows ? r0 + rr : it.rows);
   Queries<KV, D> q;
   {
     constexpr int kBytes = KV == kF32 ? 4 : 2;
     const char *p = static_cast<const char *>(a.q) + (row.q < 0 ? 0 : row.q) * D * kBytes + hb * 16;
-    u32x4 *lds = reinterpret_cast<u32x4 *>(smem + Layout<KV, D, WR>::kWalk) +
+    u32x4 *lds = reinterpret_cast<u32x4 *>(smem + Layout<KV, D>::kQ) +
                  wave * operands<KV, D>() * 64 + lane;
     q.lds = lds;
 #pragma unroll
@@ -990,34 +743,25 @@ void attn_shared_kernel(SharedArgs a) {
       else q.q[c] = x;
     }
   }
-  Walk w;
-  w.table = a.table + (size_t)it.seq0 * a.stride + it.page0;
-  w.page0 = it.page0;
-  w.pages = it.pages;
-  const int steps = (it.pages + 1) / 2;
-  w.s0 = (int)((long long)steps * it.split / it.n_split);
-  w.s1 = (int)((long long)steps * (it.split + 1) / it.n_split);
   int all = row.q < 0 ? 0x7fffffff : row.limit, some = row.limit;
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
     all = min(all, __shfl_xor(all, o, 64));
     some = max(some, __shfl_xor(some, o, 64));
   }
+  w.all = __builtin_amdgcn_readfirstlane(all);
+  w.some = __builtin_amdgcn_readfirstlane(some);
+  w.plain = plain_steps(a, w, ids);
   State<D> st;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
   st.ref = kNoMax;
   st.sum = 0.f;
 
+  walk_memory<KV, D>(st, a, w, q, it.g, ids, row.limit);
+  st.sum += other_half(st.sum);
   if (!it.shared) {
     // ---- a wavefront by itself ----------------------------------------------------
-    w.all = __builtin_amdgcn_readfirstlane(all);
-    w.some = __builtin_amdgcn_readfirstlane(some);
-    w.plain = plain_by_position(w);
-    if (__any(!pages_fine(a, w, lane, 64))) w.plain = w.s0;
-    walk_memory<KV, D>(st, a, w, q, it.g, w.s0, 1, row.limit);
-    st.sum += other_half(st.sum);
-    const int rr = lane & 31;
     if (rr >= slot_rows || r0 + rr >= it.rows) return;
     const float inv = st.sum == 0.f ? 0.f : 1.f / st.sum;
     float *o = a.part_o + (part0 + rr) * D;
@@ -1034,35 +778,16 @@ void attn_shared_kernel(SharedArgs a) {
     return;
   }
 
-  // ---- a workgroup --------------------------------------------------------------
-  __syncthreads();
-  if (lane == 0) {
-    atomicMin(&s_all, all);
-    atomicMax(&s_some, some);
-  }
-  __syncthreads();
-  w.all = __builtin_amdgcn_readfirstlane(s_all);
-  w.some = __builtin_amdgcn_readfirstlane(s_some);
-  w.plain = plain_by_position(w);
-  if (!pages_fine(a, w, threadIdx.x, 64 * kWaves)) s_bad = 1;
-  __syncthreads();
-  if (__builtin_amdgcn_readfirstlane(s_bad)) w.plain = w.s0;
-  if constexpr (WR == 1) {
-    walk_memory<KV, D>(st, a, w, q, it.g, w.s0 + wave, kWaves, row.limit);
-  } else {
-    walk_staged<KV, D, WR>(st, a, w, q, it.g, row.limit, r0 >= it.rows, smem);
-  }
-  st.sum += other_half(st.sum);
+  // ---- a workgroup: its wavefronts' parts, of the same rows ------------------------
   if (lane < kRows) {
     s_m[wave][lane] = st.ref;
     s_l[wave][lane] = st.sum;
   }
   __syncthreads();
-  // the wavefronts with other keys of the same rows: wave % WR + WR t
   float *part = reinterpret_cast<float *>(smem);
-  float m = s_m[rw][lane & 31];
+  float m = s_m[0][rr];
 #pragma unroll
-  for (int t = 1; t < kTiles; ++t) m = max_f(m, s_m[rw + WR * t][lane & 31]);
+  for (int t = 1; t < kWaves; ++t) m = max_f(m, s_m[t][rr]);
   const float f = exp2_fast(st.ref - m);
   for (int db = 0; db < D / 32; ++db) {
     if (db) __syncthreads();
@@ -1074,23 +799,22 @@ void attn_shared_kernel(SharedArgs a) {
           f32x4 v;
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = st.o[d][4 * y + e] * f;
-          *reinterpret_cast<f32x4 *>(part + (wave * kRows + (lane & 31)) * 36 + 8 * y + 4 * hb) = v;
+          *reinterpret_cast<f32x4 *>(part + (wave * kRows + rr) * 36 + 8 * y + 4 * hb) = v;
         }
       }
     __syncthreads();
-    for (int i = threadIdx.x; i < WR * kRows * 8; i += 64 * kWaves) {
-      const int rr = i >> 3, d = (i & 7) * 4, rg = rr / kRows, rl = rr % kRows;
-      if (rr >= slot_rows || it.rb * slot_rows + rr >= it.rows) continue;
-      float mm = s_m[rg][rl];
+    for (int i = threadIdx.x; i < kRows * 8; i += 64 * kWaves) {
+      const int rl = i >> 3, d = (i & 7) * 4;
+      if (rl >= slot_rows || r0 + rl >= it.rows) continue;
+      float mm = s_m[0][rl];
 #pragma unroll
-      for (int t = 1; t < kTiles; ++t) mm = max_f(mm, s_m[rg + WR * t][rl]);
+      for (int t = 1; t < kWaves; ++t) mm = max_f(mm, s_m[t][rl]);
       float l = 0.f;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        const int v = rg + WR * t;
-        l += s_l[v][rl] * exp2_fast(s_m[v][rl] - mm);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (v * kRows + rl) * 36 + d);
+      for (int t = 0; t < kWaves; ++t) {
+        l += s_l[t][rl] * exp2_fast(s_m[t][rl] - mm);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (t * kRows + rl) * 36 + d);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] += x[e];
       }
@@ -1098,8 +822,8 @@ void attn_shared_kernel(SharedArgs a) {
       f32x4 res;
 #pragma unroll
       for (int e = 0; e < 4; ++e) res[e] = l == 0.f ? 0.f : o[e] * inv;
-      *reinterpret_cast<f32x4 *>(a.part_o + (part0 + rr) * D + 32 * db + d) = res;
-      if (db == 0 && d == 0) a.part_lse[part0 + rr] = l == 0.f ? -INFINITY : mm + log2f(l);
+      *reinterpret_cast<f32x4 *>(a.part_o + (part0 + rl) * D + 32 * db + d) = res;
+      if (db == 0 && d == 0) a.part_lse[part0 + rl] = l == 0.f ? -INFINITY : mm + log2f(l);
     }
   }
 }
@@ -1156,7 +880,7 @@ __global__ __launch_bounds__(kItems * kShares) void merge_shared_kernel(SharedAr
       for (int j = 0; j < kBatch; ++j) fold(lse[j], v[j]);
     }
   };
-  add(pp.row0, pp.n, a.shared_rows, (b - pre.seq0) * per + r);
+  add(pp.row0, pp.n, kRows, (b - pre.seq0) * per + r);
   add(po.row0, po.n, a.own_rows, r);
   s_o[share][item] = o;
   s_m[share][item] = m;
@@ -1188,14 +912,7 @@ template <int KV, int D>
 void launch_d(const SharedArgs &a, hipStream_t s) {
   constexpr int kWaves = waves_of(KV, D);
   const dim3 grid((unsigned)a.grid), block(64 * kWaves);
-  const int wr = a.shared_rows / kRows;
-  if (wr == 1) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 1>), grid, block, 0, s, a);
-  if constexpr (KV != kF32) {
-    if (wr == 2) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 2>), grid, block, 0, s, a);
-    if (wr == 4) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 4>), grid, block, 0, s, a);
-    if constexpr (kWaves == 8)
-      if (wr == 8) hipLaunchKernelGGL((attn_shared_kernel<KV, D, 8>), grid, block, 0, s, a);
-  }
+  hipLaunchKernelGGL((attn_shared_kernel<KV, D>), grid, block, 0, s, a);
   const int items = a.q_len * a.G * (D / 4);
   hipLaunchKernelGGL(merge_shared_kernel<D>,
                      dim3((unsigned)(a.batch * a.Hkv), (unsigned)((items + kItems - 1) / kItems)),
@@ -1211,16 +928,6 @@ void launch_kv(const SharedArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Wavefronts with rows of their own: enough for a group's rows, of the numbers
-// there are kernels for. float32 takes one: its matrix instructions are what such
-// a call waits for (32 rows and keys of 128 dims: 8192 cycles of them for 32 KB),
-// and row blocks that read the same pages again get them from the caches.
-int shared_row_waves(int kv_type, int D, long long rows) {
-  if (kv_type == kF32) return 1;
-  int wr = 1;
-  while (wr < waves_of(kv_type, D) && rows > (long long)wr * kRows) wr *= 2;
-  return wr;
-}
 int shared_waves(int kv_type, int D) { return waves_of(kv_type, D); }
 
 hipError_t launch_attn_shared(const SharedArgs &a, hipStream_t s) {

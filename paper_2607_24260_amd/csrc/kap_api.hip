@@ -848,39 +848,29 @@ kap_status kap_verify(const kap_kv_cache *kv, int32_t batch, int32_t q_len, cons
 // Sizes of a call's work map and workspace: [parts of groups][parts of
 // sequences][partial o][partial lse].
 struct SharedPlan {
-  int shared_rows, own_rows, target, shared_cost, own_cost, least, own_least;
+  int own_rows, target, least, own_least;
   long long grid, most_parts, own_base, part_rows;
   size_t seq_parts, part_o, part_lse, total;
 };
 
-// The work is spread over one workgroup per CU; the rows of an average group say
-// how many of its wavefronts take rows of their own, WR. A step of shared pages then
-// keeps the matrix units busy for 0.18 WR us (128 dims, bf16), and one of own pages
-// costs a wavefront's eighth of the time its bytes take, 0.38 us (fp8 0.2): costs of
-// WR : 2 and WR : 1, at least the bytes' own. float32 waits for the matrix units in
-// either.
+// The work is spread over one workgroup per CU.
 static SharedPlan plan_shared(const kap_kv_cache *kv, int batch, int q_len, int num_groups) {
   SharedPlan p;
   const long long per = (long long)q_len * (kv->num_q_heads / kv->num_kv_heads);
   const long long rows = per * batch;
   const int waves = kap::shared_waves(kv->kv_dtype, kv->head_dim);
-  p.shared_rows = 32 * kap::shared_row_waves(kv->kv_dtype, kv->head_dim,
-                                             num_groups > 0 ? rows / num_groups : 1);
   p.own_rows = (int)std::min<long long>(32, per);
   p.target = device_cus();
-  const int wr = p.shared_rows / 32;
-  p.own_cost = kv->kv_dtype == KAP_DT_FP8_E4M3FN ? 1 : 2;
-  p.shared_cost = std::max(p.own_cost, wr);
-  p.least = 16 * p.own_cost;
+  p.least = 16;
   p.own_least = 2;
   // parts of groups (workgroups), and of sequences (wavefronts)
   const long long shared =
-      num_groups ? p.target + (rows / p.shared_rows + num_groups) * kv->num_kv_heads : 0;
+      num_groups ? p.target + (rows / 32 + num_groups) * kv->num_kv_heads : 0;
   const long long own = (long long)p.target * waves +
                         (long long)batch * cdiv(per, p.own_rows) * kv->num_kv_heads;
   p.grid = shared + (own + waves - 1) / waves;
   p.most_parts = (long long)(p.target + 1) * waves;
-  p.own_base = shared * p.shared_rows;
+  p.own_base = shared * 32;
   p.part_rows = p.own_base + own * p.own_rows;
   p.seq_parts = round_up((size_t)num_groups * sizeof(kap::PartsOf), 256);
   p.part_o = p.seq_parts + round_up((size_t)batch * sizeof(kap::PartsOf), 256);
@@ -956,11 +946,8 @@ kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_le
   a.shared = shared_blocks;
   a.scale_log2 = (sm_scale < 0 ? -sm_scale : sm_scale) * kap::kLog2e;
   a.q_sign = sm_scale < 0 ? (kv->q_dtype == KAP_DT_F32 ? 0x80000000u : 0x80008000u) : 0;
-  a.shared_rows = p.shared_rows;
   a.own_rows = p.own_rows;
   a.target = p.target;
-  a.shared_cost = p.shared_cost;
-  a.own_cost = p.own_cost;
   a.least = p.least;
   a.own_least = p.own_least;
   a.grid = p.grid;

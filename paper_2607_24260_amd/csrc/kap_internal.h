@@ -207,10 +207,9 @@ struct SharedArgs {
   const int32_t *shared;         // [num_groups] shared pages
   float scale_log2;              // |sm_scale| * log2(e)
   uint32_t q_sign;               // flips the sign of a word of q if sm_scale < 0
-  int shared_rows, own_rows;     // rows of a block
+  int own_rows;                  // rows of a block of a sequence's own (of a group's: 32)
   int target;                    // workgroups the work is spread over
-  int shared_cost, own_cost;     // of a step
-  int least, own_least;          // least cost of a workgroup, steps of a wavefront by itself
+  int least, own_least;          // least steps of a workgroup, of a wavefront by itself
   int64_t grid, most_parts;      // workgroups; most parts of a unit
   int64_t own_base, part_rows;   // rows of the partials: sequences' own from own_base on
   PartsOf *group_parts, *seq_parts;
@@ -246,7 +245,6 @@ SampleLayout sample_layout(int rows, int vocab, int cus);
 
 hipError_t launch_compile_plan(const PlanArgs &a, hipStream_t s);
 hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);
-int shared_row_waves(int kv_type, int D, long long rows);
 int shared_waves(int kv_type, int D);
 hipError_t launch_attn_shared(const SharedArgs &a, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
