@@ -758,7 +758,9 @@ void attn_shared_kernel(SharedArgs a) {
       else q.q[c] = x;
     }
   }
-  int all = row.q < 0 ? 0x7fffffff : row.limit, some = row.limit;
+  // Rows that see nothing (a padded sequence's) are walked as if they saw everything,
+  // and have no weight afterwards: the other rows' steps stay without masks.
+  int all = row.limit == 0 ? 0x7fffffff : row.limit, some = row.limit;
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
     all = min(all, __shfl_xor(all, o, 64));
@@ -775,6 +777,10 @@ void attn_shared_kernel(SharedArgs a) {
 
   walk_memory<KV, D>(st, a, w, q, it.g, ids, row.limit);
   st.sum += other_half(st.sum);
+  if (row.limit == 0) {
+    st.sum = 0.f;
+    st.ref = kNoMax;
+  }
   if (!it.shared) {
     // ---- a wavefront by itself ----------------------------------------------------
     if (rr >= slot_rows || r0 + rr >= it.rows) return;

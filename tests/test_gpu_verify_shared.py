@@ -289,3 +289,20 @@ def test_binding_refuses():
                  dict(workspace=torch.zeros(100, dtype=torch.uint8, device="cuda"))):
         with pytest.raises((ValueError, TypeError, K.KapError)):
             K.verify_shared(**{**good, **over})
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("q_len", [1, 5])
+def test_padded_sequences_of_a_group(dtype, q_len):
+    # lengths of 0 among long ones, in their row block and as a block of their own,
+    # and a group of nothing else; NaN in the queries of the padded ones
+    lens = [900, 0, 0, 881, 960] + [0] * 12 + [0, 0]
+    b = Batch(dtype, [(50, [180] * 17), (9, [20, 20])], q_len=q_len, lens=lens, seed=9)
+    padded = np.array(lens) == 0
+    b.q[torch.as_tensor(padded).cuda()] = float("nan")
+    o, l = b.run()
+    want = b.want()
+    live = torch.as_tensor(~padded).cuda()
+    assert_close("O", o[live].cpu().numpy(), want[0][~padded], O_TOL)
+    assert_close("LSE", l[live].cpu().numpy(), want[1][~padded], LSE_TOL)
+    assert torch.all(o[~live] == 0) and torch.all(torch.isneginf(l[~live]))
