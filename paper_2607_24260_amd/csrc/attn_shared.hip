@@ -154,76 +154,173 @@ __device__ __forceinline__ float wave_sum(float x) {
 // most total / C, so at most `target`, workgroups plus one part per (unit, row block,
 // head): the grid. The sums are float32, their rounding well inside the slack taken of
 // C: every wavefront of the launch finds the same C, from the same operations.
-template <int WAVES>
-__device__ bool shared_map(const SharedArgs &a, int w, int wave, Item &it) {
-  const int lane = threadIdx.x & 63;
-  auto steps_of = [](const Unit &u) { return (u.pages + 1) / 2; };
-  auto blocks_of = [&](const Unit &u, bool shared) {
-    const int br = shared ? kRows : a.own_rows;
-    return div_small(u.rows + br - 1, br);
-  };
-  auto unit_of = [&](bool shared, int i) {
-    const int n = shared ? a.num_groups : a.batch;
-    if (i >= n) return Unit{0, 0, 0, 0};
-    return shared ? group_unit(a, i) : seq_unit(a, i);
-  };
-  Unit first[2];                               // of the first 64, kept for the later passes
-  first[0] = unit_of(true, lane);
-  first[1] = unit_of(false, lane);
-  // f(cost, row blocks, shared) of all units, the sum over the lanes
-  auto sum = [&](auto f) {
-    auto of = [&](const Unit &u, bool shared) {
-      return f((float)steps_of(u), (float)(u.pages > 0 ? blocks_of(u, shared) : 0), shared);
-    };
-    float x = of(first[0], true) + of(first[1], false);
-    for (int i0 = 64; i0 < a.num_groups; i0 += 64) x += of(unit_of(true, i0 + lane), true);
-    for (int i0 = 64; i0 < a.batch; i0 += 64) x += of(unit_of(false, i0 + lane), false);
-    return wave_sum(x) * (float)a.Hkv;
-  };
-  const float total = sum([](float steps, float blocks, bool) { return steps * blocks; });
+__device__ __forceinline__ int steps_of(const Unit &u) { return (u.pages + 1) / 2; }
+__device__ __forceinline__ int blocks_of(const SharedArgs &a, const Unit &u, bool shared) {
+  const int br = shared ? kRows : a.own_rows;
+  return div_small(u.rows + br - 1, br);
+}
+__device__ __forceinline__ Unit unit_of(const SharedArgs &a, bool shared, int i) {
+  if (i >= (shared ? a.num_groups : a.batch)) return Unit{0, 0, 0, 0};
+  return shared ? group_unit(a, i) : seq_unit(a, i);
+}
+__device__ __forceinline__ int parts_of(const Unit &u, int len) {
+  return div_small(steps_of(u) + len - 1, len);
+}
+
+// Steps of a part of a group's pages, and of a sequence's own. sum(f): that of
+// f(steps, row blocks, whether it is a group) of all units.
+struct Lengths {
+  int of[2];
+};
+template <int WAVES, class Sum>
+__device__ __forceinline__ Lengths part_lengths(const SharedArgs &a, Sum sum) {
+  const float total = sum([](float steps, float blocks, bool) { return steps * blocks; }) * a.Hkv;
   const float per = (float)a.target / fmaxf(total, 1.f);
   const float unfilled = sum([&](float steps, float blocks, bool shared) {
     const float full = steps * per * (shared ? 1.f : (float)WAVES);   // parts, were they all full
     return fmaxf(0.5f, 1.f - full) * blocks * (shared ? 1.f : 1.f / WAVES);
-  });
+  }) * a.Hkv;
   const float wanted = fmaxf((float)a.target - unfilled, 0.5f * a.target);
   const float most = fmaxf(total * 1.0001f / wanted, (float)a.least);
-  const int len[2] = {                         // steps of a part
-      (int)fminf(ceilf(most), 1e9f),
-      max((int)fminf(ceilf(most / WAVES), 1e9f), a.own_least)};
+  return Lengths{{(int)fminf(ceilf(most), 1e9f),
+                  max((int)fminf(ceilf(most / WAVES), 1e9f), a.own_least)}};
+}
+template <class F>
+__device__ __forceinline__ float of_unit(const SharedArgs &a, const Unit &u, bool shared, F f) {
+  return f((float)steps_of(u), (float)(u.pages > 0 ? blocks_of(a, u, shared) : 0), shared);
+}
+
+// Part `off` of the n_split * row blocks * KV heads of a unit whose first is part e.
+__device__ __forceinline__ void set_part(const SharedArgs &a, Item &it, bool shared, int unit, int e,
+                                         int off) {
+  it.shared = shared;
+  it.unit = unit;
+  it.row0 = (shared ? 0 : a.own_base) + (int64_t)e * (shared ? kRows : a.own_rows);
+  const int block = div_small(off, it.n_split);
+  it.split = off - block * it.n_split;
+  it.rb = div_small(block, a.Hkv);
+  it.g = block - it.rb * a.Hkv;
+}
+
+// The map of a large batch is made once, by a workgroup before the others start:
+// a.map holds the part lengths, the workgroups of shared parts, the parts of
+// sequences, then the first part of every group and of every sequence.
+constexpr int kPlanThreads = 1024, kMapHead = 4;
+
+template <int WAVES>
+__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs a) {
+  __shared__ float s_sum[kPlanThreads / 64];
+  __shared__ int s_run[kPlanThreads / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto sum = [&](auto f) {
+    float x = 0.f;
+    for (int i = threadIdx.x; i < a.num_groups; i += kPlanThreads)
+      x += of_unit(a, unit_of(a, true, i), true, f);
+    for (int i = threadIdx.x; i < a.batch; i += kPlanThreads)
+      x += of_unit(a, unit_of(a, false, i), false, f);
+    x = wave_sum(x);
+    __syncthreads();
+    if (lane == 0) s_sum[wave] = x;
+    __syncthreads();
+    x = 0.f;
+    for (int w = 0; w < kPlanThreads / 64; ++w) x += s_sum[w];
+    return x;
+  };
+  const Lengths len = part_lengths<WAVES>(a, sum);
+  int32_t *first = a.map + kMapHead;
+  for (int kind = 0; kind < 2; ++kind) {
+    const bool shared = kind == 0;
+    const int n = shared ? a.num_groups : a.batch;
+    int base = 0;
+    for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+      const int i = i0 + threadIdx.x;
+      const Unit u = unit_of(a, shared, i);
+      const int cnt = parts_of(u, len.of[kind]) * blocks_of(a, u, shared) * a.Hkv;
+      const int incl = wave_scan_add(cnt);
+      __syncthreads();
+      if (lane == 63) s_run[wave] = incl;
+      __syncthreads();
+      int before = base;
+      for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w < wave) before += s_run[w];
+        base += s_run[w];
+      }
+      if (i < n) first[i] = before + incl - cnt;
+    }
+    if (threadIdx.x == 0) {
+      a.map[kind] = len.of[kind];
+      a.map[2 + kind] = base;
+    }
+    first += n;
+  }
+}
+
+template <int WAVES>
+__device__ bool planned_item(const SharedArgs &a, int w, int wave, Item &it) {
+  const int lane = threadIdx.x & 63;
+  const bool shared = w < a.map[2];
+  const int32_t *first = a.map + kMapHead + (shared ? 0 : a.num_groups);
+  if (!shared) {
+    w = (w - a.map[2]) * WAVES + wave;
+    if (w >= a.map[3]) return false;
+  }
+  // the last unit whose first part is w or before
+  int lo = 0, hi = shared ? a.num_groups : a.batch;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const unsigned long long m = __ballot(i < hi && first[min(i, hi - 1)] <= w);
+    lo += (__popcll(m) - 1) * step;
+    hi = min(lo + step, hi);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  const Unit u = unit_of(a, shared, lo);
+  it.seq0 = __builtin_amdgcn_readfirstlane(u.seq0);
+  it.rows = __builtin_amdgcn_readfirstlane(u.rows);
+  it.page0 = __builtin_amdgcn_readfirstlane(u.page0);
+  it.pages = __builtin_amdgcn_readfirstlane(u.pages);
+  it.n_split = __builtin_amdgcn_readfirstlane(parts_of(u, a.map[shared ? 0 : 1]));
+  const int e = __builtin_amdgcn_readfirstlane(first[lo]);
+  if (it.n_split < 1) return false;            // (offsets that do not ascend)
+  set_part(a, it, shared, lo, e, w - e);
+  return true;
+}
+
+template <int WAVES>
+__device__ bool shared_map(const SharedArgs &a, int w, int wave, Item &it) {
+  if (a.map) return planned_item<WAVES>(a, w, wave, it);
+  const int lane = threadIdx.x & 63;
+  Unit first[2];                               // of the first 64, kept for the later passes
+  first[0] = unit_of(a, true, lane);
+  first[1] = unit_of(a, false, lane);
+  const Lengths len = part_lengths<WAVES>(a, [&](auto f) {
+    float x = of_unit(a, first[0], true, f) + of_unit(a, first[1], false, f);
+    for (int i0 = 64; i0 < a.num_groups; i0 += 64) x += of_unit(a, unit_of(a, true, i0 + lane), true, f);
+    for (int i0 = 64; i0 < a.batch; i0 += 64) x += of_unit(a, unit_of(a, false, i0 + lane), false, f);
+    return wave_sum(x);
+  });
   int base = 0;
   for (int kind = 0; kind < 2; ++kind) {
     const bool shared = kind == 0;
     const int n = shared ? a.num_groups : a.batch;
-    const int slot_rows = shared ? kRows : a.own_rows;
-    const int64_t start = shared ? 0 : a.own_base;
     if (!shared) {                             // parts are wavefronts' from here on
       w = (w - base) * WAVES + wave;
       base = 0;
     }
     for (int i0 = 0; i0 < n; i0 += 64) {
-      const Unit u = i0 == 0 ? first[kind] : unit_of(shared, i0 + lane);
-      const int rb = blocks_of(u, shared);
-      const int parts = div_small(steps_of(u) + len[kind] - 1, len[kind]);
-      const int cnt = parts * rb * a.Hkv;
+      const Unit u = i0 == 0 ? first[kind] : unit_of(a, shared, i0 + lane);
+      const int parts = parts_of(u, len.of[kind]);
+      const int cnt = parts * blocks_of(a, u, shared) * a.Hkv;
       const int incl = wave_scan_add(cnt), excl = incl - cnt;
       const unsigned long long hit = __ballot(w >= base + excl && w < base + incl);
       if (hit) {
         const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
-        it.shared = shared;
-        it.unit = i0 + l;
         it.seq0 = __builtin_amdgcn_readlane(u.seq0, l);
         it.rows = __builtin_amdgcn_readlane(u.rows, l);
         it.page0 = __builtin_amdgcn_readlane(u.page0, l);
         it.pages = __builtin_amdgcn_readlane(u.pages, l);
         it.n_split = __builtin_amdgcn_readlane(parts, l);
         const int e = base + __builtin_amdgcn_readlane(excl, l);
-        it.row0 = start + (int64_t)e * slot_rows;
-        const int off = w - e;
-        const int block = div_small(off, it.n_split);
-        it.split = off - block * it.n_split;
-        it.rb = div_small(block, a.Hkv);
-        it.g = block - it.rb * a.Hkv;
+        set_part(a, it, shared, i0 + l, e, w - e);
         return true;
       }
       base += lane63(incl);
@@ -933,6 +1030,7 @@ template <int KV, int D>
 void launch_d(const SharedArgs &a, hipStream_t s) {
   constexpr int kWaves = waves_of(KV, D);
   const dim3 grid((unsigned)a.grid), block(64 * kWaves);
+  if (a.map) hipLaunchKernelGGL(shared_plan_kernel<kWaves>, dim3(1), dim3(kPlanThreads), 0, s, a);
   hipLaunchKernelGGL((attn_shared_kernel<KV, D>), grid, block, 0, s, a);
   const int items = a.q_len * a.G * (D / 4);
   hipLaunchKernelGGL(merge_shared_kernel<D>,

@@ -846,12 +846,18 @@ kap_status kap_verify(const kap_kv_cache *kv, int32_t batch, int32_t q_len, cons
 // ---------------------------------------------------------------------------
 
 // Sizes of a call's work map and workspace: [parts of groups][parts of
-// sequences][partial o][partial lse].
+// sequences][map][partial o][partial lse].
 struct SharedPlan {
   int own_rows, target, least, own_least;
   long long grid, most_parts, own_base, part_rows;
-  size_t seq_parts, part_o, part_lse, total;
+  size_t seq_parts, map, part_o, part_lse, total;
 };
+
+// From this many sequences on the map is made once, by a launch of its own, instead
+// of by every wavefront, which looks at all of them: 64 sequences over 4096 shared
+// positions 39 us by every wavefront and 43 by a launch, 128 over 4096 62 and 66, over
+// 512 38 and 32, 256 over 1024 112 and 75, 2048 over 256 2820 and 346.
+static constexpr int kSharedPlanned = 129;
 
 // The work is spread over one workgroup per CU.
 static SharedPlan plan_shared(const kap_kv_cache *kv, int batch, int q_len, int num_groups) {
@@ -873,7 +879,8 @@ static SharedPlan plan_shared(const kap_kv_cache *kv, int batch, int q_len, int 
   p.own_base = shared * 32;
   p.part_rows = p.own_base + own * p.own_rows;
   p.seq_parts = round_up((size_t)num_groups * sizeof(kap::PartsOf), 256);
-  p.part_o = p.seq_parts + round_up((size_t)batch * sizeof(kap::PartsOf), 256);
+  p.map = p.seq_parts + round_up((size_t)batch * sizeof(kap::PartsOf), 256);
+  p.part_o = p.map + round_up(((size_t)num_groups + batch + 4) * sizeof(int32_t), 256);
   p.part_lse = p.part_o + round_up((size_t)p.part_rows * kv->head_dim * sizeof(float), 256);
   p.total = p.part_lse + round_up((size_t)p.part_rows * sizeof(float), 256);
   return p;
@@ -956,6 +963,7 @@ kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_le
   a.part_rows = p.part_rows;
   a.group_parts = reinterpret_cast<kap::PartsOf *>(base);
   a.seq_parts = reinterpret_cast<kap::PartsOf *>(base + p.seq_parts);
+  a.map = batch >= kSharedPlanned ? reinterpret_cast<int32_t *>(base + p.map) : nullptr;
   a.part_o = reinterpret_cast<float *>(base + p.part_o);
   a.part_lse = reinterpret_cast<float *>(base + p.part_lse);
   a.out = out;

@@ -212,6 +212,7 @@ struct SharedArgs {
   int least, own_least;          // least steps of a workgroup, of a wavefront by itself
   int64_t grid, most_parts;      // workgroups; most parts of a unit
   int64_t own_base, part_rows;   // rows of the partials: sequences' own from own_base on
+  int32_t *map;                  // of a large batch (see attn_shared.hip), else NULL
   PartsOf *group_parts, *seq_parts;
   float *part_o, *part_lse;      // [rows][D], [rows]: normalised, log2 domain
   float *out, *lse;

@@ -306,3 +306,19 @@ def test_padded_sequences_of_a_group(dtype, q_len):
     assert_close("O", o[live].cpu().numpy(), want[0][~padded], O_TOL)
     assert_close("LSE", l[live].cpu().numpy(), want[1][~padded], LSE_TOL)
     assert torch.all(o[~live] == 0) and torch.all(torch.isneginf(l[~live]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("batch, q_len", [(128, 1), (129, 2), (300, 1), (1100, 1)])
+def test_large_batches(dtype, batch, q_len):
+    # groups of 1 to 40 sequences, some without pages of their own, sequences in no
+    # group, and (last) more sequences and groups than a workgroup has threads
+    rng = np.random.default_rng(batch)
+    groups, left = [], batch - 7
+    while left:
+        n = min(left, int(rng.integers(1, 40 if batch < 1100 else 3)))
+        groups.append((int(rng.integers(0, 9)), [int(t) for t in rng.integers(q_len, 50, n)]))
+        left -= n
+    b = Batch(dtype, groups, Hq=4, Hkv=2, D=64, q_len=q_len, alone=7, seed=batch)
+    b.lens[rng.integers(0, batch, batch // 10)] = 0
+    b.check()
