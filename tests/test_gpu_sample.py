@@ -206,3 +206,16 @@ def test_binding_refuses():
             K.sample(**{**good, **over})
     token, prob = K.sample(x[:0], u[:0])
     assert token.shape == prob.shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [1, 40, 200, 900])
+@pytest.mark.parametrize("p", [None, 0.95])
+def test_top_k_that_ends_far_below_the_largest(dtype, k, p):
+    # the k-th token weighs less than 2^-32: what is left open of the k tokens' weight
+    # is little for few of them, and looked up for many
+    x = logits(24, 14701, dtype, 31 + k)
+    x[:, 77] = 18.0
+    t = np.linspace(0.3, 0.55, 24)
+    u = np.random.default_rng(k).uniform(0, 1, 24)
+    check(x, u, t=t, k=[k] * 24, p=None if p is None else [p] * 24)
