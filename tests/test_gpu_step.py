@@ -17,6 +17,7 @@ from test_gpu_sample import check as check_sample
 pytestmark = pytest.mark.gpu
 
 Hq, Hkv, D, VOCAB = 8, 2, 128, 997
+LEFT = ("q", "out", "lse", "token", "prob", "accepted", "carry")      # what a step leaves
 
 
 class Server:
@@ -109,9 +110,7 @@ class Server:
             int(self.lens.sum())), device="cuda"))
 
     def state(self):
-        raw = lambda t: t.clone().view(torch.uint8) if t.dtype == torch.uint8 else t.clone()
-        return [raw(t) for t in (self.kv.k_pages, self.kv.v_pages, self.q, self.out, self.lse, self.token,
-                                 self.prob, self.accepted, self.carry)]
+        return [self.kv.k_pages, self.kv.v_pages] + [getattr(self, name) for name in LEFT]
 
     def check(self, before):
         q, k, v = self.parts()
@@ -170,3 +169,46 @@ def test_a_captured_step_is_the_eager_one(dtype):
         for a, b in zip(eager.state(), graphed.state()):
             assert torch.equal(a, b)
         eager.advance(), graphed.advance()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+def test_two_steps_at_once_on_two_streams(dtype):
+    # each with its own pool and workspaces, against the same one after the other
+    pairs = [(Server(dtype, 5, seed), Server(dtype, 5, seed), torch.cuda.Stream()) for seed in (5, 6)]
+    for _ in range(3):
+        for alone, together, _ in pairs:
+            alone.feed(), together.feed()
+            alone.run()
+            torch.cuda.synchronize()
+        for _, together, stream in pairs:
+            with torch.cuda.stream(stream):
+                together.run(stream)
+        torch.cuda.synchronize()
+        for alone, together, _ in pairs:
+            for a, b in zip(alone.state(), together.state()):
+                assert torch.equal(a, b)
+            alone.advance(), together.advance()
+
+
+def test_pages_beyond_32_bit_offsets():
+    # the same step in a pool of 9.8 GB, whose last pages it uses, and in a small one
+    small = Server("fp8", 5, 41)
+    n = small.kv.k_pages.shape[0]
+    far = Server("fp8", 5, 41)
+    pages = (5 << 30) // (Hkv * D * 16) + n
+    shift = pages - n
+    k, v = (torch.empty((pages, *t.shape[1:]), dtype=torch.uint8, device="cuda")
+            for t in (small.kv.k_pages, small.kv.v_pages))
+    scales = torch.ones((pages, 2), device="cuda")
+    k[shift:], v[shift:], scales[shift:] = small.kv.k_pages, small.kv.v_pages, small.kv.kv_scales
+    far.kv = K.KVCache(k, v, Hq, torch.bfloat16, scales)
+    far.table = far.table + shift
+    for _ in range(2):
+        small.feed(), far.feed()
+        far.slots += 16 * shift
+        small.run(), far.run()
+        torch.cuda.synchronize()
+        assert torch.equal(k[shift:], small.kv.k_pages) and torch.equal(v[shift:], small.kv.v_pages)
+        for a, b in ((getattr(small, x), getattr(far, x)) for x in LEFT):
+            assert torch.equal(a, b)
+        small.advance(), far.advance()
