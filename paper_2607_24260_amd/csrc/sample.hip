@@ -20,8 +20,8 @@
 //      finds the answers among them.
 // Rows for which that is not few tokens (thousands of equal logits, a draw from
 // weights below 2^-32) are descended eight bits of the logit at a time over the
-// whole row instead, by the same last workgroup (64 rows of 151936 equal logits 0.8
-// to 1.1 ms; equal logits are added up by the wavefront, 2.3 to 3.4 ms otherwise).
+// whole row instead, by the same last workgroup (64 rows of 151936 equal logits 1.0
+// to 1.5 ms; equal logits are added up by the wavefront, 2.3 to 3.4 ms otherwise).
 //
 // The weights are summed as integers, in units of 2^-s with s = 62 - ceil(log2
 // vocab): the sums do not depend on their order, and a running weight is off by
@@ -31,10 +31,10 @@
 // Each launch reads the logits once (the later ones mostly from the caches). It is not
 // bytes that bound it: the first launch goes at 2.7 TB/s for 64 x 151936 bf16 logits
 // (7.3 us), the second computes weights (19.5 us), and the third is a chain of short
-// steps of a row (20.6 us: sums of the bins 3, search 3, collecting 5, then the last
+// steps of a row (20 us: sums of the bins 3, search 3, collecting 5, then the last
 // workgroup's sort, sums and answers), of which few rows have no others to hide it
-// behind. 46 us in all; 320 x 151937 118 us (0.8 TB/s), 16 x 128000 float32 32 us,
-// 1 x 32000 float32 19 to 24 us (by the draw).
+// behind. 45 us in all; 320 x 151937 112 us (0.9 TB/s), 16 x 128000 float32 31 us,
+// 1 x 32000 float32 17 to 23 us (by the draw).
 #include "kap_internal.h"
 
 #include <algorithm>
@@ -44,7 +44,10 @@ namespace kap {
 namespace {
 
 constexpr int kSumThreads = 512;               // of the first two launches
-constexpr int kThreads = 1024;                 // of the third
+// Of the third: half as many as a CU takes at its registers, so that one row's chain
+// falls into another's (1024: 1 row 18.6 for 17.1 us, 64 rows 45.6 for 44.8, 320 rows
+// 118 for 112; 256: 16.4, 51, 136; rows of equal logits 0.8, 1.1 and 1.8 ms).
+constexpr int kThreads = 512;
 constexpr int kSampleWaves = kThreads / 64;
 // A factor of two in weight has 32 steps, and a step a power of two of bins, two at
 // least (2048 bins then reach down to 2^-32) and kFinest at most: as many as the
@@ -405,7 +408,7 @@ __device__ __forceinline__ T wave_run(T v) {   // inclusive running sum over the
   return v;
 }
 
-// Running sums of the bins' weights and (HAS_K) counts: a thread has two bins.
+// Running sums of the bins' weights and (HAS_K) counts: a thread has a few neighbouring bins.
 constexpr int kOwnBins = kBins / kThreads;
 template <bool HAS_K>
 __device__ __forceinline__ void run_bins(const u64 *gw, const int *gc, Shared &s) {
