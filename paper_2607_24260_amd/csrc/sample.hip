@@ -155,24 +155,25 @@ struct Weights {
 // additions (splitting off whole factors of two and 32nds instead, with the fifth
 // power: fifteen 64-bit operations).
 struct FastWeights {
-  double slope, offset;                        // y = x * slope + offset
+  double top, least, slope;                    // y = z * slope, z = x - top, least at least
   double c1, c2, c3, c4;                       // of 2^(y - n)
   int beyond;                                  // bits to shift a weight below the last bin by
   __device__ static constexpr double magic() { return 6755399441055744.0; }   // 1.5 * 2^52
-  // y, and rint(y) in the lower half of t. No less than -2 kBins + 1: no unit is
-  // left of such a weight (NaN's and -inf's too).
-  __device__ double power(float x) const {
-    return fmax(fma((double)x, slope, offset), 1.0 - 2 * kBins);
-  }
+  // z: 0 for the largest logit and not above it for any other, at any slope. (Of
+  // x * slope - top * slope the rounding of a product is left, hundreds of bins at a
+  // temperature of 1e-15.) y is -2 kBins + 1 at least: no unit is left of such a weight
+  // (NaN's and -inf's too).
+  __device__ double below(float x) const { return fmax((double)x - top, least); }
+  __device__ double nearest(double z) const { return fma(z, slope, magic()); }   // low half: rint(y)
   __device__ static int bin(double t) { return -(int)(uint32_t)__double_as_longlong(t); }
-  // units of a weight with power y in bin b, of which 2^n has `unit`
-  __device__ u64 units(double y, double t, int b, double unit) const {
-    const double f = y - (t - magic());
+  // units of a weight in bin b, of which 2^n has `unit`; t: nearest(z)
+  __device__ u64 units(double z, double t, int b, double unit) const {
+    const double f = fma(z, slope, magic() - t);
     const double p = fma(f, fma(f, fma(f, fma(f, c4, c3), c2), c1), 1.0);
     const u64 v = (u64)__double_as_longlong(fma(unit, p, 4503599627370496.0)) & 0xfffffffffffffull;
     return v >> (b >= kBins ? beyond : 0);
   }
-  __device__ int bin_of(float x) const { return bin(power(x) + magic()); }
+  __device__ int bin_of(float x) const { return bin(nearest(below(x))); }
   // the units of 2^n in bin b (those below the last bin are a bin 2048 above, shifted)
   __device__ double unit_of(int b, int bits) const {
     return ldexp(exp2((b & (kBins - 1)) * (c1 * -1.4426950408889634074)), bits);
@@ -180,14 +181,15 @@ struct FastWeights {
 };
 
 __device__ __forceinline__ FastWeights fast_weights(float top, float low, float t) {
-  const double steps = kPerOctave * 1.4426950408889634074 / (double)t;
+  // (not 0 at an infinite temperature, so that -inf stays apart)
+  const double steps = fmax(kPerOctave * 1.4426950408889634074 / (double)t, 1e-300);
   const double span = ((double)top - (double)low) * steps + 1.0;
   double fine = 2.0;
   while (fine < kFinest && span * (2 * fine) < kBins) fine *= 2;
   const double slope = steps * fine, c = 0.69314718055994530942 / (kPerOctave * fine);
   // (with finer bins none of the row's tokens is below the last one)
-  return FastWeights{slope, -(double)top * slope, c, c * c / 2, c * c * c / 6, c * c * c * c / 24,
-                     fine == 2.0 ? kBins / (2 * kPerOctave) : 63};
+  return FastWeights{top, (1.0 - 2 * kBins) / slope, slope, c, c * c / 2, c * c * c / 6,
+                     c * c * c * c / 24, fine == 2.0 ? kBins / (2 * kPerOctave) : 63};
 }
 
 // What a row asks for. (An array that is not there is read as another one and the
@@ -325,13 +327,15 @@ __global__ __launch_bounds__(kSumThreads) void sample_bins_kernel(SampleArgs a) 
       u64 v[N];
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const double y = w.power(x[e0 + e]), t = y + FastWeights::magic();
+        const double z = w.below(x[e0 + e]), t = w.nearest(z);
         b[e] = FastWeights::bin(t);
-        v[e] = w.units(y, t, b[e], s_unit[b[e] & (kBins - 1)]);
+        v[e] = w.units(z, t, b[e], s_unit[b[e] & (kBins - 1)]);
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const bool in = b[e] < kBins;          // the many below stay in registers
+        // (the many below stay in registers; above the top there is nothing, unless the
+        // row is written to meanwhile)
+        const bool in = (uint32_t)b[e] < (uint32_t)kBins;
         rest += in ? 0 : v[e];
         rest_n += !in;
         if (in) atomicAdd(&s_weight[b[e]], v[e]);
@@ -339,7 +343,7 @@ __global__ __launch_bounds__(kSumThreads) void sample_bins_kernel(SampleArgs a) 
       if (counts) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          if (b[e] < kBins) atomicAdd(&s_count[b[e]], 1);
+          if ((uint32_t)b[e] < (uint32_t)kBins) atomicAdd(&s_count[b[e]], 1);
       }
     }
   });
@@ -821,9 +825,9 @@ __device__ __forceinline__ bool draw_by_bins(const SampleArgs &a, int r, int chu
   auto value_at = [&](int i) { return key_value((uint32_t)(token[i] >> 32)); };
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const float x = value_at(i);
-    const double y = fw.power(x), t = y + FastWeights::magic();
+    const double z = fw.below(x), t = fw.nearest(z);
     const int b = FastWeights::bin(t);
-    sum[i] = fw.units(y, t, b, fw.unit_of(b, a.bits));
+    sum[i] = fw.units(z, t, b, fw.unit_of(b, a.bits));
     if (i == 0 || fw.bin_of(value_at(i - 1)) != b) s.start[b] = (uint16_t)i;
     if (i == n - 1 || fw.bin_of(value_at(i + 1)) != b) s.stop[b] = (uint16_t)(i + 1);
   }

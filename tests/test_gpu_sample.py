@@ -219,3 +219,44 @@ def test_top_k_that_ends_far_below_the_largest(dtype, k, p):
     t = np.linspace(0.3, 0.55, 24)
     u = np.random.default_rng(k).uniform(0, 1, 24)
     check(x, u, t=t, k=[k] * 24, p=None if p is None else [p] * 24)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("filters", ["none", "q", "pq", "kpq"])
+def test_small_temperatures(dtype, filters):
+    """Temperatures down to 1e-29, at which logits over the temperature reach 1e30:
+    the largest logit still weighs 1, equal ones share it evenly, and no other
+    counts that the oracle does not count."""
+    temps = [1e-4, 1e-6, 1e-8, 1e-9, 1e-10, 1e-11, 1e-12, 1e-13, 1e-14, 1e-15, 1e-17, 1e-20, 1e-25, 1e-29]
+    rows, rng = 4 * len(temps), np.random.default_rng(40)
+    t = np.float32(np.tile(temps, 4))
+    x = logits(rows, 3001, dtype, 41)
+    x += torch.linspace(-20, 20, rows, device="cuda").to(x.dtype)[:, None]
+    first = x.max(dim=1).values
+    for i in range(rows):
+        x[i, rng.integers(0, 3001, 1 + i % 7)] = first[i]          # equal ones
+        if i % 3 == 0:                                             # all within a few temperatures
+            x[i] = (torch.randn(3001, device="cuda") * float(t[i])).to(x.dtype)
+    par = dict(q=rng.choice([1e-6, 0.1, 0.7, 1.0], rows), p=rng.uniform(0.1, 1, rows),
+               k=rng.integers(1, 3001, rows))
+    check(x, rng.random(rows), t=t, **{n: par[n] for n in filters if n in par})
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_of_any_magnitude(dtype):
+    # whole rows of the type's lowest and largest value, few and many of them, and rows
+    # whose logits differ by less than they are large
+    low, high = torch.finfo(DT[dtype]).min, torch.finfo(DT[dtype]).max
+    rng = np.random.default_rng(42)
+    for vocab in (700, 5003):
+        x = torch.empty((16, vocab), device="cuda", dtype=DT[dtype])
+        for i, v in enumerate([low, high, 1e15, -1e15, 1e22, -1e30, 3e7, -3e7]):
+            x[2 * i] = v
+            x[2 * i + 1] = x[2 * i] * (1 - 0.02 * torch.rand(vocab, device="cuda")).to(x.dtype)
+        x[1, 0], x[3, 5] = high, low
+        for t in (0.5, 0.7, 1.0, 1.3, 1e6):
+            # (whole weights: the uniform numbers keep off the boundaries)
+            u = (rng.integers(0, 100, 16) + 0.37) / 100.1
+            check(x, u, t=[t] * 16, least=0.9)
+            check(x, u, t=[t] * 16, q=[0.5] * 16, least=0.9)
+            check(x, u, t=[t] * 16, k=[3] * 16, p=[0.9] * 16, least=0.5)
