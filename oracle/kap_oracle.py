@@ -770,6 +770,8 @@ def sample(row: np.ndarray, u: float, temperature: float = 1.0, top_k: int = 0, 
     with np.errstate(invalid="ignore", over="ignore"):
         w = np.where(x == x[0], 1.0, np.exp((x - x[0]) / float(temperature)))
     w[x == -np.inf] = 0.0
+    if x[0] == np.inf:
+        w[x != np.inf] = 0.0
     n = len(w)
     k = top_k if 0 < top_k < n else n
     kept, near = k, []

@@ -921,7 +921,8 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleArgs a) {
     }
     return;
   }
-  const Weights wt{key_value(top), 1.4426950408889634074 / (double)want.t, a.bits};
+  // (not 0 at an infinite temperature, at which only tokens of +inf weigh where there are any)
+  const Weights wt{key_value(top), fmax(1.4426950408889634074 / (double)want.t, 1e-300), a.bits};
   const bool whole =
       by_bins(want, top) ? draw_by_bins(a, r, chunk, row, want, ends, wt, s) : chunk == 0;
   if (whole) whole_row(a, r, row, want, wt, s);

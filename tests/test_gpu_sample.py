@@ -260,3 +260,17 @@ def test_logits_of_any_magnitude(dtype):
             check(x, u, t=[t] * 16, least=0.9)
             check(x, u, t=[t] * 16, q=[0.5] * 16, least=0.9)
             check(x, u, t=[t] * 16, k=[3] * 16, p=[0.9] * 16, least=0.5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_infinite_logits_at_an_infinite_temperature(dtype):
+    x = logits(8, 3001, dtype, 43)
+    x[:6, [9, 70, 2000]] = math.inf
+    x[2:4, :5] = -math.inf
+    x[4:6, 100:200] = math.nan
+    u = [0.1, 0.2, 0.4, 0.5, 0.7, 0.9, 0.3, 0.6]
+    for par in (dict(), dict(k=[2] * 8), dict(k=[10] * 8, p=[0.9] * 8), dict(q=[0.5] * 8)):
+        # (row 3 with k = 2: u W = 0.5 * 2 is the running weight after one of the two equal
+        # tokens, exactly on the boundary, so that 7 of 8 rows are compared)
+        token, prob = check(x, u, t=[math.inf] * 8, least=7 / 8, **par)
+        assert set(token[:6]) <= {9, 70, 2000} and np.all(prob[:6] >= 1 / 3 - 1e-6)

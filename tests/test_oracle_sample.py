@@ -82,3 +82,10 @@ def test_distance_to_the_next_outcome():
     # u = 0.49 of weights 8, 4, 2, 1, 1: the boundary at 0.5 is 0.01 away
     assert abs(O.sample(ROW, 0.49)[2] - 0.01) < 1e-12
     assert abs(O.sample(ROW, 0.3, top_p=0.8)[2] - 0.05) < 1e-12      # 0.75 | 0.8: nearer than 0.8 * ...
+
+
+def test_infinite_logits_at_an_infinite_temperature():
+    inf = math.inf
+    for kw in (dict(), dict(top_k=3), dict(top_p=0.9), dict(min_p=0.5)):
+        assert O.sample([1.0, inf, 2.0, inf], 0.4, temperature=inf, **kw)[:2] == (1, 0.5)
+        assert O.sample([1.0, inf, -inf, inf], 0.6, temperature=inf, **kw)[:2] == (3, 0.5)
