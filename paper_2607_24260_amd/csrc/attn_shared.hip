@@ -594,7 +594,13 @@ __device__ __forceinline__ void add_values(State<D> &st, const Source &src, cons
     if constexpr (KV != kF32) {
       float p[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = KV == kFP8 ? w[8 * y + i] * vs[y] : w[8 * y + i];
+      for (int i = 0; i < 8; ++i) {
+        // (MASKED: of a page that is not there or that a row does not see, the scale may
+        // be anything)
+        if constexpr (KV != kFP8) p[i] = w[8 * y + i];
+        else if constexpr (MASKED) p[i] = w[8 * y + i] == 0.f ? 0.f : w[8 * y + i] * vs[y];
+        else p[i] = w[8 * y + i] * vs[y];
+      }
       split8(p, hi, lo, rest);
     }
     if constexpr (MASKED) sees = seen_words<KV>(seen, y);

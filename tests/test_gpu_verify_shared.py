@@ -322,3 +322,29 @@ def test_large_batches(dtype, batch, q_len):
     b = Batch(dtype, groups, Hq=4, Hkv=2, D=64, q_len=q_len, alone=7, seed=batch)
     b.lens[rng.integers(0, batch, batch // 10)] = 0
     b.check()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("q_len", [1, 4])
+def test_fp8_scales_that_nobody_looks_at(bad, q_len):
+    """Scales that are not finite, of page 0 (in no table row: it stands in for pages
+    that are not there), of the shared pages' last page, which one sequence ends before,
+    and of a sequence's last page, of which its earlier window rows see nothing."""
+    lens = [16 * 6 + 5 + q_len, 16 * 5 + 2, 16 * 8 + q_len - 1, 16 * 10]
+    b = Batch("fp8", [(7, [60] * 3), (3, [130])], q_len=q_len, lens=lens, seed=21)
+    unused = next(p for p in range(b.kv.k_pages.shape[0]) if p not in b.table)
+    swap = {0: unused, unused: 0}
+    b.table = np.vectorize(lambda p: swap.get(int(p), int(p)))(b.table)
+    b.table[3, 4] = -5                                       # outside the pool
+    b.table[3, 9] = 2 ** 31 - 1
+    want, scales = b.want(), b.kv.kv_scales.clone()
+    b.kv.kv_scales[0] = bad
+    for page, sees in ((int(b.table[0, 6]), [(0, 0), (2, 0)]), (int(b.table[2, 8]), [(2, 1)])):
+        b.kv.kv_scales[page] = bad
+        o, l = (t.cpu().numpy() for t in b.run())
+        blind = np.ones(l.shape, bool)
+        for seq, first in sees:
+            blind[seq, first:] = False                       # window rows that see the page
+        assert_close("O", o, want[0], O_TOL, blind)
+        assert_close("LSE", l, want[1], LSE_TOL, blind)
+        b.kv.kv_scales[page] = scales[page]
