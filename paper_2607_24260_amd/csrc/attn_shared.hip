@@ -34,13 +34,13 @@
 // of two), so that it hardly ever moves and no weight exceeds 1.
 //
 // Measured (128 dims, 8 KV heads, 32 query heads): 8 sequences over 16K shared
-// positions, bf16 (76 MB) 26.8 us: the walk itself is 9 us, as fast as the bytes come
+// positions, bf16 (76 MB) 27.1 us: the walk itself is 9 us, as fast as the bytes come
 // from the caches, and around it the launches, the work map (2), the first loads (3),
 // the workgroup's sum over its wavefronts (3) and the merge's launch (5). 64 over 32K
 // (256 rows a KV head; 35 GFLOP, of which those with V are done for each part) 97 us:
 // matrix and vector instructions of two wavefronts per SIMD. Four groups of four over
-// 32K to 128K, 5-token windows, fp8 (80 rows, 670 MB) 292 us: the same, with 96 rows
-// multiplied for 80. Two sequences over 1000 positions, float32, 64 dims 20 us: the
+// 32K to 128K, 5-token windows, fp8 (80 rows, 670 MB) 294 us: the same, with 96 rows
+// multiplied for 80. Two sequences over 1000 positions, float32, 64 dims 20.9 us: the
 // chain of launches, map, two steps a wavefront and merge.
 #include "kap_internal.h"
 
@@ -455,8 +455,9 @@ template <int D> struct State {
   float ref, sum;    // reference (powers of two), and this lane's half of the sum
 };
 
-// Moves the reference above a step's logits (c z: in powers of two, c >= 0).
-template <int D>
+// Moves the reference above a step's logits (c z: in powers of two, c >= 0). MASKED: what
+// weighs nothing against it goes, infinities and NaN too.
+template <int D, bool MASKED>
 __device__ __forceinline__ void move_reference(State<D> &st, const f32x16 &z, float c) {
   float top = max_f(z[0], z[1]);
 #pragma unroll
@@ -471,7 +472,8 @@ __device__ __forceinline__ void move_reference(State<D> &st, const f32x16 &z, fl
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) st.o[db][i] *= f;
+      for (int i = 0; i < 16; ++i)
+        st.o[db][i] = MASKED && f == 0.f ? 0.f : st.o[db][i] * f;
   }
 }
 // Weights in the place of the logits.
@@ -658,12 +660,13 @@ __device__ __forceinline__ bool in_pool(const SharedArgs &a, int id) {
 // of one register, the next 32 steps' on the way. (A load of an id right before
 // it is needed would be waited for with everything that is in flight.)
 struct PageIds {
-  int cur, next, k0, first, stride;
+  int cur, next, k0, first, stride, lane;
   __device__ int fetch(const Walk &w, int k) const {
-    const int lane = threadIdx.x & 63, e = 2 * (first + (k + (lane >> 1)) * stride) + (lane & 1);
+    const int e = 2 * (first + (k + (lane >> 1)) * stride) + (lane & 1);
     return w.table[min(e, max(w.pages - 1, 0))];
   }
-  __device__ PageIds(const Walk &w, int first_, int stride_) : k0(0), first(first_), stride(stride_) {
+  __device__ PageIds(const Walk &w, int first_, int stride_, int lane_)
+      : k0(0), first(first_), stride(stride_), lane(lane_) {
     cur = fetch(w, 0);
     next = fetch(w, 32);
   }
@@ -692,7 +695,7 @@ __device__ __forceinline__ int plain_steps(const SharedArgs &a, const Walk &w, c
   bool fine = true;
   for (int k = 0; ids.first + k * ids.stride < end; k += 32) {
     const int id = k == 0 ? ids.cur : (k == 32 ? ids.next : ids.fetch(w, k));
-    const int s = ids.first + (k + ((int)(threadIdx.x & 63) >> 1)) * ids.stride;
+    const int s = ids.first + (k + (ids.lane >> 1)) * ids.stride;
     fine &= s >= end || in_pool(a, id);
   }
   return __any(!fine) ? w.s0 : end;
@@ -703,8 +706,8 @@ __device__ __forceinline__ int plain_steps(const SharedArgs &a, const Walk &w, c
 template <int KV, bool MASKED>
 __device__ __forceinline__ float scale_logits(const SharedArgs &a, const Walk &w, f32x16 &z,
                                               uint32_t &seen, int s, const bool (&ok)[2], int limit,
-                                              const float (&ks)[2]) {
-  const int hb = (threadIdx.x & 63) >> 5;
+                                              const float (&ks)[2], int lane) {
+  const int hb = lane >> 5;
   seen = 0xffffu;
   if constexpr (KV != kFP8 && !MASKED) return a.scale_log2;
 #pragma unroll
@@ -724,11 +727,11 @@ template <int KV, int D, bool MASKED, class Source>
 __device__ __forceinline__ void take_step(State<D> &st, const SharedArgs &a, const Walk &w,
                                           const Queries<KV, D> &q, const Source &src, int s,
                                           const bool (&ok)[2], int limit, const float (&ks)[2],
-                                          const float (&vs)[2]) {
+                                          const float (&vs)[2], int lane) {
   f32x16 z = logits<KV, D>(src, q);
   uint32_t seen;
-  const float c = scale_logits<KV, MASKED>(a, w, z, seen, s, ok, limit, ks);
-  move_reference(st, z, c);
+  const float c = scale_logits<KV, MASKED>(a, w, z, seen, s, ok, limit, ks, lane);
+  move_reference<D, MASKED>(st, z, c);
   weigh(st, z, c);
   add_values<KV, D, MASKED>(st, src, z, seen, vs);
 }
@@ -745,15 +748,18 @@ __device__ __forceinline__ void scales_of(const SharedArgs &a, const int (&id)[2
   }
 }
 
+// Whether steps that every row sees in full have a loop of their own, without masks.
+template <int KV, int D> constexpr bool has_plain() { return KV != kF32 || D < 256; }
+
 // Steps first, first + stride, .. below w.s1, operands from memory.
 template <int KV, int D>
 __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, const Walk &w,
                                             const Queries<KV, D> &q, int g, PageIds ids, int limit) {
-  const int lane = threadIdx.x & 63, first = ids.first, stride = ids.stride;
+  const int lane = ids.lane, first = ids.first, stride = ids.stride;
   if (first >= w.s1) return;
   int k = 0;
   auto step = [&](int i) { return first + i * stride; };
-  if constexpr (KV != kF32 || D < 256) {
+  if constexpr (has_plain<KV, D>()) {
     // the next step's K is fetched as soon as this one's has been multiplied, and
     // so is V
     if (first < w.plain) {
@@ -777,8 +783,8 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
         r.load_k(p);
         __builtin_amdgcn_sched_barrier(0);
         uint32_t seen;
-        const float c = scale_logits<KV, false>(a, w, z, seen, step(k), fine, limit, ks);
-        move_reference(st, z, c);
+        const float c = scale_logits<KV, false>(a, w, z, seen, step(k), fine, limit, ks, lane);
+        move_reference<D, false>(st, z, c);
         weigh(st, z, c);
         add_values<KV, D, false>(st, r, z, seen, vs);
         __builtin_amdgcn_sched_barrier(0);
@@ -797,7 +803,7 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
     const Step x = ids.at(a, w, k);
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
     scales_of<KV>(a, x.id, ks, vs);
-    take_step<KV, D, true>(st, a, w, q, Pages<KV, D>(a, x.id, g, lane), step(k), x.ok, limit, ks, vs);
+    take_step<KV, D, true>(st, a, w, q, Pages<KV, D>(a, x.id, g, lane), step(k), x.ok, limit, ks, vs, lane);
   }
 }
 
@@ -841,7 +847,8 @@ void attn_shared_kernel(SharedArgs a) {
   const int steps = (it.pages + 1) / 2;
   w.s0 = (int)((long long)steps * it.split / it.n_split);
   w.s1 = (int)((long long)steps * (it.split + 1) / it.n_split);
-  const PageIds ids(w, w.s0 + (it.shared ? wave : 0), it.shared ? kWaves : 1);
+  const int first = w.s0 + (it.shared ? wave : 0), stride = it.shared ? kWaves : 1;
+  PageIds ids(w, first, stride, opaque(lane));
 
   // ---- rows ---------------------------------------------------------------------
   const int r0 = it.rb * slot_rows, rr = lane & 31;     // of the unit, of the block
@@ -871,15 +878,32 @@ void attn_shared_kernel(SharedArgs a) {
   }
   w.all = __builtin_amdgcn_readfirstlane(all);
   w.some = __builtin_amdgcn_readfirstlane(some);
-  w.plain = plain_steps(a, w, ids);
+  // A product gives 0 * inf = NaN where a weight, or one of its parts, is zero, and
+  // inf - inf where two parts differ in sign. Rather than test V on the way, a wavefront
+  // whose result is not finite walks its steps again with masks, which keep infinities
+  // and NaN of V out of the products. (Not for rows that see nothing, nor for those
+  // that a NaN logit has made NaN.) The lane is opaque, or addresses and page ids would
+  // be kept from walk to walk (15 registers more than 256-dim bf16 has). The test and
+  // what it keeps cost 0.3 us of 26.7 (8 x 16K, bf16) and 3 of 291 (fp8 windows).
   State<D> st;
+  w.plain = plain_steps(a, w, ids);
+  for (;;) {
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
-  st.ref = kNoMax;
-  st.sum = 0.f;
-
-  walk_memory<KV, D>(st, a, w, q, it.g, ids, row.limit);
-  st.sum += other_half(st.sum);
+    for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
+    st.ref = kNoMax;
+    st.sum = 0.f;
+    walk_memory<KV, D>(st, a, w, q, it.g, ids, row.limit);
+    st.sum += other_half(st.sum);
+    if (!has_plain<KV, D>() || w.plain <= first) break;
+    float top = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = max_f(top, __builtin_fabsf(st.o[db][i]));
+    if (!__any(!(top < INFINITY) && row.limit > 0 && st.sum == st.sum)) break;
+    w.plain = w.s0;
+    ids = PageIds(w, first, stride, opaque(lane));
+  }
   if (row.limit == 0) {
     st.sum = 0.f;
     st.ref = kNoMax;
@@ -922,7 +946,7 @@ void attn_shared_kernel(SharedArgs a) {
         for (int y = 0; y < 4; ++y) {
           f32x4 v;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = st.o[d][4 * y + e] * f;
+          for (int e = 0; e < 4; ++e) v[e] = f == 0.f ? 0.f : st.o[d][4 * y + e] * f;
           *reinterpret_cast<f32x4 *>(part + (wave * kRows + rr) * 36 + 8 * y + 4 * hb) = v;
         }
       }

@@ -348,3 +348,68 @@ def test_fp8_scales_that_nobody_looks_at(bad, q_len):
         assert_close("O", o, want[0], O_TOL, blind)
         assert_close("LSE", l, want[1], LSE_TOL, blind)
         b.kv.kv_scales[page] = scales[page]
+
+
+def put(kv, dtype, page, head, dim, off, value):
+    """V element as a float; fp8 pools: NaN's code (they hold no infinities)."""
+    kv.v_pages[page, head, dim, off] = 0x7F if dtype == "fp8" else value
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q_len", [1, 5])
+def test_not_finite_values_that_every_row_sees(dtype, D, q_len):
+    """Infinities and NaN of V in pages of the prefix and of a sequence that lie far
+    before its end, where no row needs a mask: +inf, -inf, NaN, or NaN of two
+    infinities, in their dims and sequences alone."""
+    b = Batch(dtype, [(40, [300, 90, 40]), (3, [700])], D=D, q_len=q_len, seed=D + q_len)
+    inf = math.inf
+    for seq, pos, dim, value in ((0, 0, 3, inf), (0, 77, 4, -inf), (0, 500, 5, math.nan),
+                                 (0, 639, 6, inf), (1, 660, 6, -inf), (0, 700, 7, inf),
+                                 (0, 901, 8, -inf), (3, 20, 9, inf), (3, 30, 9, inf), (3, 400, 10, -inf),
+                                 (3, 401, 11, 2.0 ** 120)):
+        if dtype == "fp8" and value > 2:
+            value = math.nan
+        put(b.kv, dtype, int(b.table[seq, pos // 16]), 1, dim, pos % 16, value)
+    with np.errstate(invalid="ignore"):
+        want = b.want()
+    o, l = (t.cpu().numpy() for t in b.run())
+    heads = np.arange(8) // 4 == 1
+    nan = np.isnan(want[0])
+    assert nan[:, :, heads].any() and not nan[:, :, ~heads].any()
+    assert dtype == "fp8" or (want[0] == inf).any() and (want[0] == -inf).any()
+    assert np.array_equal(np.isnan(o), nan)
+    assert_close("LSE", l, want[1], LSE_TOL)
+    large = np.abs(want[0]) > 1e30                           # 2^120 and infinities
+    assert_close("large", o[large] / 2.0 ** 110, want[0][large] / 2.0 ** 110, O_TOL)
+    assert_close("O", o, want[0], O_TOL, ~nan & ~large)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("pages", [9, 60])
+def test_weights_of_zero_meet_infinities(dtype, D, pages):
+    """Tokens thousands of powers of two below the others, alone in the first step of
+    the prefix or in a sequence's own pages, or among others: they count for nothing,
+    whatever V holds."""
+    b = Batch(dtype, [(pages, [400, 32, 90])], D=D, q_len=3, seed=pages + D)
+    b.q[..., 0] = 1.0
+    low = [(0, p) for p in (*range(32), 16 * 7 + 3)] + [(1, 16 * pages + i) for i in range(32)] + [
+        (0, 16 * pages + i) for i in (0, 5, 17, 200)] + [(2, 16 * pages + 40)]
+    for seq, pos in low:
+        page, off = int(b.table[seq, pos // 16]), pos % 16
+        if pos == int(b.lens[seq]) - 1:
+            continue
+        b.kv.k_pages[page, :, :, off] = 0
+        b.kv.k_pages[page, :, 0, off, 0] = -60000.0
+        b.kv.v_pages[page, :, :, off] = 0
+    want = b.want()
+    for i, (seq, pos) in enumerate(low):
+        page, off = int(b.table[seq, pos // 16]), pos % 16
+        if pos == int(b.lens[seq]) - 1:
+            continue
+        for dim in range(i % 3, D, 3):
+            b.kv.v_pages[page, :, dim, off] = (math.inf, -math.inf, math.nan)[i % 3]
+    o, l = (t.cpu().numpy() for t in b.run())
+    assert_close("LSE", l, want[1], LSE_TOL)
+    assert_close("O", o, want[0], O_TOL)
