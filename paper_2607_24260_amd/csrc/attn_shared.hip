@@ -639,8 +639,10 @@ __device__ __forceinline__ RowOf row_of(const SharedArgs &a, const Item &it, int
   if (r >= it.rows) return RowOf{-1, 0};
   const int per = a.q_len * a.G;
   const int b = it.seq0 + r / per, rr = r % per, i = rr / a.G;
+  // (2^27 pages hold one position more than 32 bits count: less one here)
+  const int most = (int)min((long long)a.max_pages * kPage, 0x7fffffffll);
   return RowOf{((int64_t)b * a.q_len + i) * a.Hq + it.g * a.G + (rr - i * a.G),
-               max(0, min(a.seq_lens[b], a.max_pages * kPage) - a.q_len + i + 1)};
+               max(0, min(a.seq_lens[b], most) - a.q_len + i + 1)};
 }
 
 // What a wavefront (or workgroup) walks: steps of table row `table`, whose first

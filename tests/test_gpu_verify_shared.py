@@ -413,3 +413,18 @@ def test_weights_of_zero_meet_infinities(dtype, D, pages):
     o, l = (t.cpu().numpy() for t in b.run())
     assert_close("LSE", l, want[1], LSE_TOL)
     assert_close("O", o, want[0], O_TOL)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+def test_the_longest_max_seq_len(dtype):
+    """Tables of 2^27 pages, whose positions 32 bits just do not count."""
+    b = Batch(dtype, [(5, [37])], q_len=2)
+    table = torch.zeros((1, 2 ** 27), dtype=torch.int32, device="cuda")
+    table[0, :b.table.shape[1]] = dev_i32(b.table[0])
+    want = b.want()
+    for most in (2 ** 31 - 16, 2 ** 31 - 1):
+        for sh in (5, 0):
+            o, l = K.verify_shared(b.kv, b.q, dev_i32(b.lens), table, most, dev_i32(b.offsets),
+                                   dev_i32([sh]), b.scale)
+            assert_close("O", o.cpu().numpy(), want[0], O_TOL)
+            assert_close("LSE", l.cpu().numpy(), want[1], LSE_TOL)
