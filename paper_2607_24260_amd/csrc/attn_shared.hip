@@ -642,7 +642,7 @@ __device__ __forceinline__ RowOf row_of(const SharedArgs &a, const Item &it, int
   // (2^27 pages hold one position more than 32 bits count: less one here)
   const int most = (int)min((long long)a.max_pages * kPage, 0x7fffffffll);
   return RowOf{((int64_t)b * a.q_len + i) * a.Hq + it.g * a.G + (rr - i * a.G),
-               max(0, min(a.seq_lens[b], most) - a.q_len + i + 1)};
+               max(0, clamp_to(a.seq_lens[b], 0, most) - a.q_len + i + 1)};
 }
 
 // What a wavefront (or workgroup) walks: steps of table row `table`, whose first

@@ -428,3 +428,17 @@ def test_the_longest_max_seq_len(dtype):
                                    dev_i32([sh]), b.scale)
             assert_close("O", o.cpu().numpy(), want[0], O_TOL)
             assert_close("LSE", l.cpu().numpy(), want[1], LSE_TOL)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("q_len", [1, 5])
+def test_negative_lengths(dtype, q_len):
+    # as a length of 0: nothing is seen, of the shared pages neither
+    lens = np.array([90, -1, -(2 ** 31), 2 - 2 ** 31, 81])
+    b = Batch(dtype, [(5, [20] * 5)], q_len=q_len, lens=lens)
+    o, l = (t.cpu().numpy() for t in b.run())
+    b.lens = np.maximum(lens, 0)
+    want = b.want()
+    assert_close("O", o, want[0], O_TOL)
+    assert_close("LSE", l, want[1], LSE_TOL)
+    assert np.all(o[1:4] == 0) and np.all(np.isneginf(l[1:4]))
