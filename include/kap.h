@@ -434,8 +434,9 @@ kap_status kap_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const void 
  * dims (j, j + rot_dim / 2) with KAP_ROPE_HALVES, (2 j, 2 j + 1) with
  * KAP_ROPE_PAIRS. Several axes (time, height, width) are several rows of
  * positions, and freq_axis shares the frequencies out among them; an axis
- * outside [0, num_axes) turns nothing. The angle is taken in 64 bits, the
- * rotation in 32; each output is rounded once.
+ * outside [0, num_axes) turns nothing, and neither does an angle of 0 (whatever
+ * the pair's other dim holds). The angle is taken in 64 bits, the rotation in
+ * 32; each output is rounded once.
  *   q_new, k_new, v_new: rows of Hq * D, Hkv * D, Hkv * D values (q_dtype of
  *   kv), *_stride elements apart (slices of one fused projection, say);
  *   q_new NULL: no queries. q_out [num_tokens][Hq][D] (q_dtype, 16-byte

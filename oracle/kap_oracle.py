@@ -555,8 +555,9 @@ def rotate(x: np.ndarray, positions, inv_freq, freq_axis=None, pairs: bool = Fal
         c, s = np.cos(a)[:, None], np.sin(a)[:, None]
         d0, d1 = (2 * j, 2 * j + 1) if pairs else (j, j + n)
         u, v = np.asarray(x[:, :, d0], np.float64), np.asarray(x[:, :, d1], np.float64)
-        out[:, :, d0] = u * c - v * s
-        out[:, :, d1] = v * c + u * s
+        with np.errstate(invalid="ignore"):
+            out[:, :, d0] = np.where(s == 0, u * c, u * c - v * s)
+            out[:, :, d1] = np.where(s == 0, v * c, v * c + u * s)
     return out
 
 

@@ -11,11 +11,11 @@
 // rotation, are 32-bit.
 //
 // Bound by memory: every element is read once and written once. 8192 tokens of 32
-// query and 8 KV heads of 128 dims, bf16 (201 MB): 42.5 us, 4.7 TB/s, which is what a
-// copy of that size reaches; the angles are not seen in it (42.5 us without them).
-// float32, 3711 tokens of 16 and 8 heads of 64 dims (61 MB): 15.2 us, 4.0 TB/s. A few
+// query and 8 KV heads of 128 dims, bf16 (201 MB): 41.1 us, 4.9 TB/s, which is what a
+// copy of that size reaches; the angles are not seen in it.
+// float32, 3711 tokens of 16 and 8 heads of 64 dims (61 MB): 14.9 us, 4.1 TB/s. A few
 // tokens are bound by the chain of reads from slots to scales to pages and by the
-// launch: 320 tokens with fp8 pages 8.1 us, one token 4.3 us.
+// launch: 320 tokens with fp8 pages 7.8 us, one token 4.3 us.
 //
 // A workgroup is a role (Q heads, K heads, V columns) of a tile of 16 tokens. The
 // workgroups that an XCD is given one after the other are the roles of one tile: Q's
@@ -141,6 +141,14 @@ __device__ __forceinline__ float2 turn_of(int pos, float freq) {
   return make_float2(c, s);
 }
 
+// (x, y) turned. An angle of 0 leaves both as they are, next to an infinity or NaN too
+// (which the product with a sine of 0 would make NaN).
+__device__ __forceinline__ void turn(float x, float y, float2 cs, float &p, float &q) {
+  const float xc = x * cs.x, yc = y * cs.x;
+  p = cs.y == 0.f ? xc : fmaf(-y, cs.y, xc);
+  q = cs.y == 0.f ? yc : fmaf(x, cs.y, yc);
+}
+
 // Rows of Q (chunks in neighbouring lanes: 128 and more contiguous bytes of a
 // row per token), or of K (tokens in neighbouring lanes: a page holds a chunk's
 // 16 tokens side by side). A thread has one chunk pair of one token -- eight
@@ -182,10 +190,12 @@ __device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, int bx, boo
   for (int i = threadIdx.x; i < nt * nf; i += kThreads) {
     const int t = i / nf, j = i - t * nf;
     const int axis = a.freq_axis ? a.freq_axis[j] : 0;
-    // an axis that is not there turns nothing
-    const int pos = axis >= 0 && axis < a.num_axes
-                        ? a.positions[(size_t)axis * a.num_tokens + t0 + t] : 0;
-    s_cs[i] = turn_of(pos, a.inv_freq[j]);
+    // an axis that is not there turns nothing (position and frequency are loaded for it
+    // too: 8192 tokens 41.1 us, 41.9 with branches around the loads)
+    const bool there = axis >= 0 && axis < a.num_axes;
+    const int pos = a.positions[(size_t)(there ? axis : 0) * a.num_tokens + t0 + t];
+    const float freq = a.inv_freq[j];
+    s_cs[i] = there ? turn_of(pos, freq) : make_float2(1.f, 0.f);
   }
   __syncthreads();
   if (mine && slot >= 0) {
@@ -201,17 +211,12 @@ __device__ __forceinline__ void rotate_rows(const RopeAppendArgs &a, int bx, boo
       widen8<KV>(xb[u], y);
       if (a.halves) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = x[i] * cs[i].x - y[i] * cs[i].y;
-          q[i] = y[i] * cs[i].x + x[i] * cs[i].y;
-        }
+        for (int i = 0; i < 8; ++i) turn(x[i], y[i], cs[i], p[i], q[i]);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[2 * i] = x[2 * i] * cs[i].x - x[2 * i + 1] * cs[i].y;
-          p[2 * i + 1] = x[2 * i + 1] * cs[i].x + x[2 * i] * cs[i].y;
-          q[2 * i] = y[2 * i] * cs[4 + i].x - y[2 * i + 1] * cs[4 + i].y;
-          q[2 * i + 1] = y[2 * i + 1] * cs[4 + i].x + y[2 * i] * cs[4 + i].y;
+          turn(x[2 * i], x[2 * i + 1], cs[i], p[2 * i], p[2 * i + 1]);
+          turn(y[2 * i], y[2 * i + 1], cs[4 + i], q[2 * i], q[2 * i + 1]);
         }
       }
       if (is_k) {

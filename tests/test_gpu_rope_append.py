@@ -246,3 +246,43 @@ def test_binding_refuses():
     with pytest.raises(ValueError):
         K.bind_rope_append_kv(**good, q_new=q)
     assert K.rope_append_kv(kv, k[:0], k[:0], slots[:0], pos[:0], inv) is None
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("pairs", [False, True])
+def test_an_angle_of_zero_leaves_infinities_alone(dtype, pairs):
+    # positions of 0 on one axis, frequencies of an axis that is not there
+    # (infinite ones among them): such pairs stay as they are, bit for bit
+    T, D, n = 40, 128, 48
+    kv = make_pool(dtype, 4, 4, 2, D, 30)
+    g = torch.Generator(device="cuda").manual_seed(31)
+    q, k, v = (torch.randn((T, h, D), generator=g, device="cuda").to(QDT[dtype]) for h in (4, 2, 2))
+    for x in (q, k):
+        at = torch.randint(0, x.numel(), (4 * T,), generator=g, device="cuda")
+        x.view(-1)[at] = torch.tensor([float("inf"), -float("inf"), float("nan"), -0.0],
+                                      device="cuda").to(x.dtype).repeat(T)
+    axis = torch.arange(n, dtype=torch.int32, device="cuda") % 4 - 1       # -1, 0, 1, 2: two are there
+    inv = torch.rand(n, generator=g, device="cuda")
+    inv[axis == -1] = float("inf")
+    pos = torch.stack([torch.arange(T, device="cuda") * 0, torch.arange(T, device="cuda") + 5]).int()
+    slots = torch.arange(T, device="cuda") + 3
+    got = K.rope_append_kv(kv, k, v, slots, pos, inv, q_new=q, freq_axis=axis,
+                           style=K.KAP_ROPE_PAIRS if pairs else K.KAP_ROPE_HALVES)
+    torch.cuda.synchronize()
+    still = torch.ones(D, dtype=torch.bool)
+    for j in range(n):
+        if int(axis[j]) == 1:
+            still[[2 * j, 2 * j + 1] if pairs else [j, j + n]] = False
+    assert 0 < int(still[:2 * n].sum()) < 2 * n
+    raw = lambda x: torch.where(torch.isnan(x), torch.nan, x).contiguous().view(
+        torch.int32 if x.dtype == torch.float32 else torch.int16)
+    assert torch.equal(raw(got[..., still]), raw(q[..., still]))
+    at_slots = lambda p: p.permute(0, 3, 1, 2, 4).reshape(64, 2, D)[3:3 + T]
+    if dtype == "fp8":
+        scale = kv.kv_scales[:, 0].repeat_interleave(16)[3:3 + T, None, None]
+        want = (k.float() / scale).clamp(-448, 448)[..., still]
+        assert np.all(np.isnan(numbers(at_slots(kv.k_pages)[..., still])) == want.isnan().cpu().numpy())
+        diff = np.abs(numbers(at_slots(kv.k_pages)[..., still]) - want.double().cpu().numpy())
+        assert np.nanmax(diff / half_step("fp8", np.nan_to_num(want.double().cpu().numpy()))) <= 1 + 2.0 ** -20
+    else:
+        assert torch.equal(raw(at_slots(kv.k_pages)[..., still]), raw(k[..., still]))

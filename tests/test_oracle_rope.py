@@ -65,3 +65,19 @@ def test_append_places_and_limits():
     written = ~np.isnan(kp[:, 0, 0, :, 0])
     assert written.sum() == 2 and written[1, 3] and written[2, 15]
     assert np.array_equal(~np.isnan(vp[:, 0, 0, :]), written)
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+def test_an_angle_of_zero_leaves_infinities_alone(pairs):
+    inf = np.inf
+    x = np.array([[[inf, 2.0, 3.0, -inf, 5.0, np.nan, 7.0, 8.0]]])
+    f = np.array([0.1, 0.2, inf, 0.4])
+    # position 0, and axes that do not exist
+    assert np.array_equal(O.rotate(x, [0], f[:2], None, pairs), x, equal_nan=True)
+    assert np.array_equal(O.rotate(x, [9], f, [1, -1, 7, 2], pairs), x, equal_nan=True)
+    # the other frequencies turn their pairs
+    some = O.rotate(x, [9], f, [1, 0, 7, 2], pairs)
+    turned = [2, 3] if pairs else [1, 5]
+    keep = [d for d in range(8) if d not in turned]
+    assert np.array_equal(some[0, 0, keep], x[0, 0, keep], equal_nan=True)
+    assert not np.array_equal(some[0, 0, turned], x[0, 0, turned], equal_nan=True)
