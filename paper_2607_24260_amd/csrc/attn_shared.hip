@@ -813,6 +813,12 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const SharedArgs &a, c
 // the kernel
 // ---------------------------------------------------------------------------
 
+// A launch has fewer than 2^32 threads along x: workgroups from here on go to z.
+constexpr long long kAlongX = 1ll << 21;
+__device__ __forceinline__ unsigned flat_block() {
+  return blockIdx.z * (unsigned)kAlongX + blockIdx.x;
+}
+
 template <int KV, int D>
 struct Layout {
   static constexpr int kWaves = waves_of(KV, D);
@@ -832,7 +838,7 @@ void attn_shared_kernel(SharedArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hb = lane >> 5;
   Item it;
-  if (!shared_map<kWaves>(a, blockIdx.x, wave, it)) return;   // (a shared part: all wavefronts)
+  if (!shared_map<kWaves>(a, (int)flat_block(), wave, it)) return;   // (a shared part: all wavefronts)
   const int slot_rows = it.shared ? kRows : a.own_rows;
   const int64_t part0 =
       it.row0 + ((int64_t)(it.rb * a.Hkv + it.g) * it.n_split + it.split) * slot_rows;
@@ -989,7 +995,9 @@ __global__ __launch_bounds__(kItems * kShares) void merge_shared_kernel(SharedAr
   constexpr int D4 = D / 4, kBatch = 4;
   __shared__ f32x4 s_o[kShares][kItems];
   __shared__ float s_m[kShares][kItems], s_l[kShares][kItems];
-  const int g = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
+  const unsigned unit = flat_block();
+  if (unit >= (unsigned)a.batch * (unsigned)a.Hkv) return;
+  const int g = unit % (unsigned)a.Hkv, b = unit / (unsigned)a.Hkv;
   const int grp = group_of(a, b);
   const Unit own = seq_unit(a, b);
   Unit pre{0, 0, 0, 0};
@@ -1061,12 +1069,15 @@ __global__ __launch_bounds__(kItems * kShares) void merge_shared_kernel(SharedAr
 template <int KV, int D>
 void launch_d(const SharedArgs &a, hipStream_t s) {
   constexpr int kWaves = waves_of(KV, D);
-  const dim3 grid((unsigned)a.grid), block(64 * kWaves);
+  auto along = [](long long n) { return (unsigned)std::min(n, kAlongX); };
+  auto above = [](long long n) { return (unsigned)((n + kAlongX - 1) / kAlongX); };
+  const dim3 grid(along(a.grid), 1, above(a.grid)), block(64 * kWaves);
   if (a.map) hipLaunchKernelGGL(shared_plan_kernel<kWaves>, dim3(1), dim3(kPlanThreads), 0, s, a);
   hipLaunchKernelGGL((attn_shared_kernel<KV, D>), grid, block, 0, s, a);
   const int items = a.q_len * a.G * (D / 4);
+  const long long units = (long long)a.batch * a.Hkv;
   hipLaunchKernelGGL(merge_shared_kernel<D>,
-                     dim3((unsigned)(a.batch * a.Hkv), (unsigned)((items + kItems - 1) / kItems)),
+                     dim3(along(units), (unsigned)((items + kItems - 1) / kItems), above(units)),
                      dim3(kItems * kShares), 0, s, a);
 }
 

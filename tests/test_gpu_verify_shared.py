@@ -442,3 +442,24 @@ def test_negative_lengths(dtype, q_len):
     assert_close("O", o, want[0], O_TOL)
     assert_close("LSE", l, want[1], LSE_TOL)
     assert np.all(o[1:4] == 0) and np.all(np.isneginf(l[1:4]))
+
+
+def test_more_than_2_32_threads():
+    """65535 sequences of a token, 128 heads: 2^23 workgroups of 1024 threads merge."""
+    B, H, D = 65535, 128, 64
+    k, v, _ = kv_pool(3, H, D, "bf16", 5, "cuda")
+    kv = K.KVCache(k, v, H, torch.bfloat16)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q = torch.randn((B, 1, H, D), generator=g, device="cuda", dtype=torch.bfloat16)
+    table = torch.randint(0, 3, (B, 1), generator=g, device="cuda", dtype=torch.int32)
+    lens = torch.ones(B, dtype=torch.int32, device="cuda")
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    o, l = K.verify_shared(kv, q, lens, table, 16, torch.zeros(1, dtype=torch.int32, device="cuda"),
+                           none, 0.125)
+    torch.cuda.synchronize()
+    keys, values = k[:, :, :, 0].reshape(3, H, D).double(), v[..., 0].double()
+    for b in range(0, B, 4096):                              # one key a row: its V, and its logit
+        at = table[b:b + 4096, 0].long()
+        assert torch.all((o[b:b + 4096, 0].double() - values[at]).abs() <= O_TOL)
+        z = (q[b:b + 4096, 0].double() * keys[at]).sum(-1) * 0.125
+        assert torch.all((l[b:b + 4096, 0].double() - z).abs() <= LSE_TOL)
