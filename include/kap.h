@@ -445,7 +445,7 @@ kap_status kap_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const void 
  *   inv_freq [rot_dim / 2] float32, freq_axis [rot_dim / 2] int32.
  * K and V go to slot_mapping's slots of the pool as with kap_append_kv (a
  * negative slot: padding; a slot past the pool: skipped and counted into
- * *bad_slots; the same slot twice: either token's values), float32 and bf16 as
+ * *bad_slots; the same slot twice: each value either token's), float32 and bf16 as
  * they are, fp8 as the nearest code of x / scale with the page's K or V scale
  * (+-448 beyond the range; NaN stays NaN; kv_scales are read, not changed).
  * The queries of padding tokens are turned like any other.

@@ -39,8 +39,8 @@
 // the workgroup's sum over its wavefronts (3) and the merge's launch (5). 64 over 32K
 // (256 rows a KV head; 35 GFLOP, of which those with V are done for each part) 97 us:
 // matrix and vector instructions of two wavefronts per SIMD. Four groups of four over
-// 32K to 128K, 5-token windows, fp8 (80 rows, 670 MB) 294 us: the same, with 96 rows
-// multiplied for 80. Two sequences over 1000 positions, float32, 64 dims 20.9 us: the
+// 32K to 128K, 5-token windows, fp8 (80 rows, 670 MB) 294 to 302 us: the same, with 96
+// rows multiplied for 80. Two sequences over 1000 positions, float32, 64 dims 21 us: the
 // chain of launches, map, two steps a wavefront and merge.
 #include "kap_internal.h"
 

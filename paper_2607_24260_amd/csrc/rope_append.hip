@@ -14,8 +14,9 @@
 // query and 8 KV heads of 128 dims, bf16 (201 MB): 41.1 us, 4.9 TB/s, which is what a
 // copy of that size reaches; the angles are not seen in it.
 // float32, 3711 tokens of 16 and 8 heads of 64 dims (61 MB): 14.9 us, 4.1 TB/s. A few
-// tokens are bound by the chain of reads from slots to scales to pages and by the
-// launch: 320 tokens with fp8 pages 7.8 us, one token 4.3 us.
+// tokens are bound by the launch and by chains of a few reads: 320 tokens with fp8
+// pages 7.8 us (7.0 without the angles, 0.15 less without the scales, which wait for
+// the slots), one token 4.3 us.
 //
 // A workgroup is a role (Q heads, K heads, V columns) of a tile of 16 tokens. The
 // workgroups that an XCD is given one after the other are the roles of one tile: Q's

@@ -18,22 +18,26 @@
 //   3  from the running sums of the bins, those that an answer can lie in; their
 //      tokens are collected, and the last workgroup of the row sorts them and
 //      finds the answers among them.
-// Rows for which that is not few tokens (thousands of equal logits, a draw from
-// weights below 2^-32) are descended eight bits of the logit at a time over the
-// whole row instead, by the same last workgroup (64 rows of 151936 equal logits 1.0
-// to 1.5 ms; equal logits are added up by the wavefront, 2.3 to 3.4 ms otherwise).
+// Rows for which that is not few tokens are descended eight bits of the logit at a
+// time over the whole row instead, by the same last workgroup: thousands of equal
+// logits around an answer, and bf16 logits far from zero are that (some -1e4 besides,
+// high temperatures and 256K tokens make it likelier: bins are as wide as the smallest
+// logit asks for), or a draw from weights below 2^-32. 64 rows of 151936 equal logits
+// take 1.0 to 1.5 ms (equal logits are added up by the wavefront, 2.3 to 3.4 ms
+// otherwise), of bf16 logits with mean 30 and deviation 2 1.3 to 1.9.
 //
-// The weights are summed as integers, in units of 2^-s with s = 62 - ceil(log2
-// vocab): the sums do not depend on their order, and a running weight is off by
-// less than vocab half units, where 32-bit floats would move the boundaries
+// The weights are summed as integers, in units of 2^-s with s = min(51, 62 - ceil(log2
+// vocab)): the sums do not depend on their order, and a running weight is off by less
+// than half a unit for each of its tokens (a unit for those below the last bin) and
+// 2^-44 of itself for the exponentials, where 32-bit floats would move the boundaries
 // between tokens by as much as whole tokens.
 //
 // Each launch reads the logits once (the later ones mostly from the caches). It is not
 // bytes that bound it: the first launch goes at 2.7 TB/s for 64 x 151936 bf16 logits
-// (7.3 us), the second computes weights (19.5 us), and the third is a chain of short
+// (7.1 us), the second computes weights (19.6 us), and the third is a chain of short
 // steps of a row (20 us: sums of the bins 3, search 3, collecting 5, then the last
 // workgroup's sort, sums and answers), of which few rows have no others to hide it
-// behind. 45 us in all; 320 x 151937 112 us (0.9 TB/s), 16 x 128000 float32 31 us,
+// behind. 46 us in all; 320 x 151937 112 us (0.9 TB/s), 16 x 128000 float32 30 us,
 // 1 x 32000 float32 17 to 23 us (by the draw).
 #include "kap_internal.h"
 
