@@ -274,3 +274,33 @@ def test_infinite_logits_at_an_infinite_temperature(dtype):
         # tokens, exactly on the boundary, so that 7 of 8 rows are compared)
         token, prob = check(x, u, t=[math.inf] * 8, least=7 / 8, **par)
         assert set(token[:6]) <= {9, 70, 2000} and np.all(prob[:6] >= 1 / 3 - 1e-6)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_longest_rows_and_strides(dtype):
+    """2^30 - 1 tokens, and rows more than 2^31 elements apart: a few tokens above a
+    floor of -30, whose weights are known in closed form."""
+    n = 2 ** 30 - 1
+    buf = torch.full((n + 3,), -30.0, device="cuda", dtype=DT[dtype])
+    at = [5, 0, n - 1, 2 ** 29, 777, 12345678]               # in the order of their logits
+    value = [0.0, -0.5, -0.5, -1.0, -1.5, -2.0]              # the first of the equal ones: 0
+    x = buf[3:]
+    x[torch.tensor(at, device="cuda")] = torch.tensor(value, device="cuda").to(x.dtype)
+    w = np.exp(value)
+    rest = (n - len(at)) * math.exp(-30.0)
+    for p in (None, 0.5):
+        kept = len(w) if p is None else int(np.searchsorted(np.cumsum(w), p * (w.sum() + rest))) + 1
+        total = w[:kept].sum() + (rest if p is None else 0.0)
+        for i in range(kept):
+            u = (w[:i].sum() + 0.5 * w[i]) / total
+            token, prob = K.sample(x[None], torch.tensor([u], device="cuda", dtype=torch.float32),
+                                   top_p=None if p is None else torch.tensor([p], device="cuda"))
+            assert int(token) == at[i]
+            # rounded to float32; the floor's weights, e^-30 = 2^-43, are less than half a
+            # unit of 2^-32: the sum lacks them
+            assert abs(float(prob) - w[i] / total) <= (2.0 ** -23 + rest / w.sum()) * w[i] / total
+    del buf, x
+    wide = torch.empty(2 ** 31 + 6 + 4001, device="cuda", dtype=DT[dtype])
+    far = wide.as_strided((2, 4001), (2 ** 31 + 6, 1))
+    far.copy_(logits(2, 4001, dtype, 50))
+    check(far, [0.3, 0.9], p=[0.9, 0.99])
