@@ -37,11 +37,11 @@
 // positions, bf16 (76 MB) 27.1 us: the walk itself is 9 us, as fast as the bytes come
 // from the caches, and around it the launches, the work map (2), the first loads (3),
 // the workgroup's sum over its wavefronts (3) and the merge's launch (5). 64 over 32K
-// (256 rows a KV head; 35 GFLOP, of which those with V are done for each part) 97 us:
-// matrix and vector instructions of two wavefronts per SIMD. Four groups of four over
-// 32K to 128K, 5-token windows, fp8 (80 rows, 670 MB) 294 to 302 us: the same, with 96
-// rows multiplied for 80. Two sequences over 1000 positions, float32, 64 dims 21 us: the
-// chain of launches, map, two steps a wavefront and merge.
+// (256 rows a KV head; 35 GFLOP, of which those with V are done for each part) 97 to
+// 100 us: matrix and vector instructions of two wavefronts per SIMD. Four groups of four
+// over 32K to 128K, 5-token windows, fp8 (80 rows, 670 MB) 294 to 306 us: the same, with
+// 96 rows multiplied for 80. Two sequences over 1000 positions, float32, 64 dims 21 us:
+// the chain of launches, map, two steps a wavefront and merge.
 #include "kap_internal.h"
 
 #include <algorithm>
