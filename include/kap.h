@@ -464,6 +464,58 @@ kap_status kap_rope_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const 
                               int32_t *bad_slots, void *stream);
 
 /*
+ * kap_step_tables -- block tables, slots and positions of a serving step from
+ * its requests' lengths, with the free pages kept on the device: what
+ * kap_rope_append_kv, kap_chunk_attention and kap_verify read, and the pages
+ * that rejected drafts and ended sequences leave behind.
+ *
+ * Sequence b holds the first ceil(seq_lens[b] / 16) pages of its table row. It
+ * keeps keep[b] of its tokens (NULL: all) and adds add[b] new ones; pages beyond
+ * those that keep + add need go back to the free ones (the first
+ * pinned_blocks[b] pages, shared with others, never do; NULL: none), and
+ * missing ones are taken. Free page i < count is free_pages[(head + i) mod
+ * free_size], free_state = {head, count}: pages are taken from the front, in
+ * ascending order of (sequence, block), and go back behind the last, in the same
+ * order (what was free when the call began is what can be taken).
+ *   Written: block_table [batch][table_stride] (the blocks taken; the others stay
+ * as they are, those that went back too), free_pages, free_out [2], new_lens
+ * [batch] = keep + add, q_offsets [batch + 1]: the prefix sums of add, and for
+ * new token i of sequence b, t = q_offsets[b] + i, positions[t] = keep[b] + i and
+ * slot_mapping[t] = block_table[b][position / 16] * 16 + position mod 16. Tokens
+ * from q_offsets[batch] to num_tokens are padding: slot -1, position 0.
+ *   status[b]: KAP_STEP_OK, or why sequence b adds nothing:
+ * KAP_STEP_BAD_LENGTH: not 0 <= keep <= seq_len <= 16 * table_stride, or add < 0
+ *   (the sequence stays as it was, new_lens[b] = seq_lens[b]);
+ * KAP_STEP_OVER_CAPACITY: more than table_stride pages; KAP_STEP_OVER_TOKENS: the
+ * sum of add up to b, less those that the two reasons before refused, exceeds
+ * num_tokens; KAP_STEP_OUT_OF_PAGES: the pages needed up to b, by those that no
+ * other reason refused, exceed count (the sequence keeps `keep` tokens).
+ * From the first sequence that runs out of tokens or pages on, those that need
+ * some are all refused.
+ *   new_lens may be seq_lens and free_out may be free_state; other arrays do not
+ * overlap. A head outside [0, free_size) counts as 0 and count is limited to
+ * [0, free_size]; free_size is at least the number of pages there are, or pages
+ * that come back when the ring is full are lost. batch <= 65535, num_tokens <
+ * 2^30, table_stride < 2^27.
+ */
+typedef int32_t kap_step_status;
+enum {
+  KAP_STEP_OK = 0,
+  KAP_STEP_BAD_LENGTH = 1,
+  KAP_STEP_OVER_CAPACITY = 2,
+  KAP_STEP_OVER_TOKENS = 3,
+  KAP_STEP_OUT_OF_PAGES = 4
+};
+
+kap_status kap_step_tables(int32_t batch, const int32_t *seq_lens, const int32_t *keep,
+                           const int32_t *add, const int32_t *pinned_blocks,
+                           int32_t *block_table, int32_t table_stride, int32_t *free_pages,
+                           int32_t free_size, const int32_t *free_state, int32_t num_tokens,
+                           int32_t *free_out, int32_t *new_lens, int32_t *q_offsets,
+                           int64_t *slot_mapping, int32_t *positions, int32_t *status,
+                           void *stream);
+
+/*
  * kap_compact_view -- materialise the selected-KV view as a compact physical
  * copy (Alg. 1, AssignCompactSlots and BuildBlockTable; Sec. 3.1: the
  * selected pages are compacted in access order into a reusable compact
@@ -566,6 +618,43 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
                            size_t workspace_bytes, void *stream);
 
 size_t kap_accept_top3_workspace_bytes(int32_t batch, int32_t window);
+
+/*
+ * kap_adjust_logits -- penalties for repeated tokens, biases and grammar masks:
+ * logits on their way to kap_sample (or kap_accept_top3).
+ *
+ * Row r's history is history[history_start[r] + i], i < history_len[r]; its first
+ * prompt_len[r] tokens (NULL: none) are the prompt, the others were put out. Rows
+ * may share tokens: the rows of a window over one sequence have the same start and
+ * lengths one apart. For every token v with logit x, in 32 bits, in this order:
+ *   v in the history: x / repetition[r] if x > 0, else x * repetition[r];
+ *   v put out n > 0 times: x - frequency[r] * n - presence[r];
+ *   v = bias_token[e], bias_offsets[r] <= e < bias_offsets[r + 1]: x +
+ *   bias_value[e] (listed more than once: the last e counts);
+ *   bit v mod 32 of masks[mask_row[r]][v / 32] is 0: -inf, whatever x is. A
+ *   mask_row outside [0, num_masks) masks nothing.
+ * The result is rounded once. Tokens outside [0, vocab) and places outside
+ * [0, history_size) count for nothing; bias_offsets are limited to [0, num_biases].
+ *   logits, out [rows][vocab] (logits_dtype F32 or BF16), stride and out_stride
+ *   elements between rows; out may be logits if the strides are equal (or rows =
+ *   1), else they do not overlap. history int32, history_start [rows] int64,
+ *   history_len, prompt_len [rows] int32; history NULL: none, with
+ *   repetition, frequency, presence [rows] float32 (NULL: 1, 0, 0).
+ *   bias_offsets [rows + 1], bias_token, bias_value [num_biases], NULL: none;
+ *   masks [num_masks] rows of ceil(vocab / 32) words, mask_stride words apart,
+ *   mask_row [rows]; masks NULL: none.
+ * 1 <= vocab < 2^30, rows <= 65535.
+ */
+kap_status kap_adjust_logits(int32_t rows, int32_t vocab, const void *logits, int64_t stride,
+                             kap_dtype logits_dtype, void *out, int64_t out_stride,
+                             const int32_t *history, int64_t history_size,
+                             const int64_t *history_start, const int32_t *history_len,
+                             const int32_t *prompt_len, const float *repetition,
+                             const float *frequency, const float *presence,
+                             const int32_t *bias_offsets, const int32_t *bias_token,
+                             const float *bias_value, int32_t num_biases, const uint32_t *masks,
+                             int32_t num_masks, int64_t mask_stride, const int32_t *mask_row,
+                             void *stream);
 
 /*
  * kap_sample -- one token per row of logits, drawn with given uniform numbers

@@ -794,3 +794,118 @@ def sample(row: np.ndarray, u: float, temperature: float = 1.0, top_k: int = 0, 
     if u > 0:
         near.append(np.min(np.abs(sums - goal)) / sums[-1])
     return int(order[r]), float(w[r] / sums[-1]), float(min(near, default=math.inf))
+
+
+# --------------------------------------------------------------------------
+# A step's tables, chunks of new tokens, and logits on their way to the draw
+# --------------------------------------------------------------------------
+
+STEP_OK, STEP_BAD_LENGTH, STEP_OVER_CAPACITY, STEP_OVER_TOKENS, STEP_OUT_OF_PAGES = range(5)
+
+
+def step_tables(seq_lens, add, block_table, free_pages, free_state, num_tokens: int, keep=None,
+                pinned=None):
+    """One step of requests, sequence by sequence, with a ring of free pages.
+
+    Returns a dict of block_table, free_pages (copies, updated), free_out, new_lens,
+    q_offsets, slot_mapping, positions, status. Pages come from those that are free at
+    the start, in order; those that go back follow the last free one."""
+    table, ring = np.array(block_table, np.int64), np.array(free_pages, np.int64)
+    B, stride, size = len(seq_lens), table.shape[1], len(ring)
+    head, count = (int(x) for x in free_state)
+    head = head if 0 <= head < size else 0
+    count = min(max(count, 0), size)
+    blocks = lambda n: -(-n // PAGE)                               # noqa: E731
+    asked = wanted = taken = returned = 0
+    out = dict(new_lens=[], status=[], q_offsets=[0], slot_mapping=[], positions=[])
+    for b in range(B):
+        L, n = int(seq_lens[b]), int(add[b])
+        k = L if keep is None else int(keep[b])
+        if L < 0 or k < 0 or k > L or n < 0 or blocks(L) > stride:
+            out["new_lens"].append(L)
+            out["status"].append(STEP_BAD_LENGTH)
+            out["q_offsets"].append(out["q_offsets"][-1])
+            continue
+        status = STEP_OK
+        if n > 0 and blocks(k + n) > stride:
+            status, n = STEP_OVER_CAPACITY, 0
+        asked += n
+        if n > 0 and asked > num_tokens:
+            status, n = STEP_OVER_TOKENS, 0
+        need = max(0, blocks(k + n) - blocks(L))
+        wanted += need
+        if need > 0 and wanted > count:
+            status, n, need = STEP_OUT_OF_PAGES, 0, 0
+        for j in range(need):
+            table[b, blocks(L) + j] = ring[(head + taken) % size]
+            taken += 1
+        held = max(blocks(k + n), 0 if pinned is None else max(int(pinned[b]), 0))
+        for j in range(held, blocks(L)):
+            if returned < size - count:
+                ring[(head + count + returned) % size] = table[b, j]
+            returned += 1
+        for p in range(k, k + n):
+            out["slot_mapping"].append(int(table[b, p // PAGE]) * PAGE + p % PAGE)
+            out["positions"].append(p)
+        out["new_lens"].append(k + n)
+        out["status"].append(status)
+        out["q_offsets"].append(len(out["positions"]))
+    pad = num_tokens - len(out["positions"])
+    out["slot_mapping"] += [-1] * pad
+    out["positions"] += [0] * pad
+    out = {name: np.asarray(v, np.int64) for name, v in out.items()}
+    out["free_out"] = np.array([(head + taken) % size if size else 0,
+                                count - taken + min(returned, size - count)])
+    return dict(out, block_table=table, free_pages=ring)
+
+
+def chunk_attention(pool: KVPool, q: np.ndarray, q_offsets, seq_lens, block_table, sm_scale: float,
+                    window: int = 0, sinks: int = 0):
+    """Attention of the last tokens of sequences over their pages.
+
+    q: [T][Hq][D]; rows q_offsets[b] .. q_offsets[b + 1] - 1 are the last tokens of
+    sequence b. The row at position p sees positions t <= p and, with a window, of those
+    the last ``window`` and the first ``sinks``. Returns o [T][Hq][D] and lse [T][Hq]
+    (rows of no sequence: o = 0, lse = -inf; they are not the operator's)."""
+    q = np.asarray(q, dtype=np.float64)
+    T, Hq, D = q.shape
+    Hkv = pool.k_pages.shape[1]
+    G = Hq // Hkv
+    o, lse = np.zeros((T, Hq, D)), np.full((T, Hq), -np.inf)
+    for b in range(len(seq_lens)):
+        r0, r1, L = int(q_offsets[b]), int(q_offsets[b + 1]), int(seq_lens[b])
+        for g in range(Hkv):
+            k, v, pos = full_tokens(pool, g, max(L, 0), block_table[b])
+            for r in range(r0, r1):
+                p = L - (r1 - r)
+                seen = pos <= p
+                if window > 0:
+                    seen &= (p - pos < window) | (pos < sinks)
+                rows = slice(g * G, (g + 1) * G)
+                o[r, rows], lse[r, rows] = attend(q[r, rows], k[seen], v[seen],
+                                                  [int(seen.sum())] * G, sm_scale)
+    return o, lse
+
+
+def adjust_logits(row: np.ndarray, prompt=(), told=(), repetition: float = 1.0,
+                  frequency: float = 0.0, presence: float = 0.0, biases=(), allowed=None):
+    """A row of logits after penalties, biases ((token, value) pairs, a later one for the
+    same token instead of an earlier one) and a grammar (``allowed``: bool per token).
+
+    ``prompt`` and ``told``: the tokens that the row was given, and has put out."""
+    x = np.array(row, dtype=np.float64, copy=True)
+    counts: dict = {}
+    for v in told:
+        counts[int(v)] = counts.get(int(v), 0) + 1
+    for v in set(int(v) for v in prompt) | set(counts):
+        if not 0 <= v < len(x):
+            continue
+        x[v] = x[v] / repetition if x[v] > 0 else x[v] * repetition
+        if v in counts:
+            x[v] = x[v] - frequency * counts[v] - presence
+    for v, value in dict((int(v), float(b)) for v, b in biases).items():
+        if 0 <= v < len(x):
+            x[v] += value
+    if allowed is not None:
+        x[~np.asarray(allowed, bool)] = -np.inf
+    return x

@@ -1297,6 +1297,142 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
 }
 
 // ---------------------------------------------------------------------------
+// kap_step_tables
+// ---------------------------------------------------------------------------
+
+kap_status kap_step_tables(int32_t batch, const int32_t *seq_lens, const int32_t *keep,
+                           const int32_t *add, const int32_t *pinned_blocks,
+                           int32_t *block_table, int32_t table_stride, int32_t *free_pages,
+                           int32_t free_size, const int32_t *free_state, int32_t num_tokens,
+                           int32_t *free_out, int32_t *new_lens, int32_t *q_offsets,
+                           int64_t *slot_mapping, int32_t *positions, int32_t *status,
+                           void *stream) {
+  if (batch < 0) return fail(KAP_ERR_INVALID_ARGUMENT, "batch < 0");
+  if (table_stride < 0 || free_size < 0 || num_tokens < 0)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "a size is negative");
+  if (batch == 0 && num_tokens > 0)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "%d tokens of no sequence", num_tokens);
+  if (batch == 0) return ok();
+  if (batch > 65535) return fail(KAP_ERR_UNSUPPORTED, "batch %d > 65535", batch);
+  if (num_tokens >= 1 << 30) return fail(KAP_ERR_UNSUPPORTED, "num_tokens %d >= 2^30", num_tokens);
+  if (table_stride >= 1 << 27) return fail(KAP_ERR_UNSUPPORTED, "table_stride %d >= 2^27", table_stride);
+  if (!seq_lens || !add || !free_state || !free_out || !new_lens || !q_offsets || !status ||
+      (table_stride > 0 && !block_table) || (free_size > 0 && !free_pages) ||
+      (num_tokens > 0 && (!slot_mapping || !positions)))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "a required pointer is NULL");
+  for (const void *p : {(const void *)seq_lens, (const void *)keep, (const void *)add,
+                        (const void *)pinned_blocks, (const void *)block_table,
+                        (const void *)free_pages, (const void *)free_state, (const void *)free_out,
+                        (const void *)new_lens, (const void *)q_offsets, (const void *)positions,
+                        (const void *)status})
+    if (!aligned(p, 4)) return fail(KAP_ERR_INVALID_ARGUMENT, "an array is misaligned");
+  if (!aligned(slot_mapping, 8)) return fail(KAP_ERR_INVALID_ARGUMENT, "slot_mapping is misaligned");
+  kap::StepArgs a;
+  a.batch = batch;
+  a.stride = table_stride;
+  a.ring_size = free_size;
+  a.num_tokens = num_tokens;
+  a.seq_lens = seq_lens;
+  a.keep = keep;
+  a.add = add;
+  a.pinned = pinned_blocks;
+  a.table = block_table;
+  a.ring = free_pages;
+  a.free_state = free_state;
+  a.free_out = free_out;
+  a.new_lens = new_lens;
+  a.q_offsets = q_offsets;
+  a.slots = slot_mapping;
+  a.positions = positions;
+  a.status = status;
+  (void)hipGetLastError();
+  const hipError_t e = kap::launch_step_tables(a, device_cus(), static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(KAP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+// ---------------------------------------------------------------------------
+// kap_adjust_logits
+// ---------------------------------------------------------------------------
+
+kap_status kap_adjust_logits(int32_t rows, int32_t vocab, const void *logits, int64_t stride,
+                             kap_dtype logits_dtype, void *out, int64_t out_stride,
+                             const int32_t *history, int64_t history_size,
+                             const int64_t *history_start, const int32_t *history_len,
+                             const int32_t *prompt_len, const float *repetition,
+                             const float *frequency, const float *presence,
+                             const int32_t *bias_offsets, const int32_t *bias_token,
+                             const float *bias_value, int32_t num_biases, const uint32_t *masks,
+                             int32_t num_masks, int64_t mask_stride, const int32_t *mask_row,
+                             void *stream) {
+  if (rows < 0) return fail(KAP_ERR_INVALID_ARGUMENT, "rows < 0");
+  if (vocab < 1 || vocab >= (1 << 30))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "vocab %d outside [1, 2^30)", vocab);
+  if (logits_dtype != KAP_DT_F32 && logits_dtype != KAP_DT_BF16)
+    return fail(KAP_ERR_UNSUPPORTED, "logits must be F32 or BF16");
+  if (stride < vocab || out_stride < vocab)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "a stride is less than vocab");
+  if (history_size < 0 || num_biases < 0 || num_masks < 0)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "a size is negative");
+  const int words = cdiv(vocab, 32);
+  if (masks && mask_stride < words)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "mask_stride %lld < ceil(vocab / 32) = %d",
+                (long long)mask_stride, words);
+  if (rows == 0) return ok();
+  if (rows > 65535) return fail(KAP_ERR_UNSUPPORTED, "rows %d > 65535", rows);
+  if (stride > INT64_MAX / 16 / rows || out_stride > INT64_MAX / 16 / rows ||
+      (num_masks > 0 && mask_stride > INT64_MAX / 16 / num_masks))
+    return fail(KAP_ERR_UNSUPPORTED, "a stride is too large");
+  if (!logits || !out) return fail(KAP_ERR_INVALID_ARGUMENT, "logits and out are required");
+  if (history && (!history_start || !history_len))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "history needs history_start and history_len");
+  if (bias_offsets && num_biases > 0 && (!bias_token || !bias_value))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "bias_offsets needs bias_token and bias_value");
+  if (masks && !mask_row) return fail(KAP_ERR_INVALID_ARGUMENT, "masks needs mask_row");
+  const int es = logits_dtype == KAP_DT_F32 ? 4 : 2;
+  if (!aligned(logits, es) || !aligned(out, es) || !aligned(history_start, 8))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "an array is misaligned");
+  for (const void *p : {(const void *)history, (const void *)history_len, (const void *)prompt_len,
+                        (const void *)repetition, (const void *)frequency, (const void *)presence,
+                        (const void *)bias_offsets, (const void *)bias_token,
+                        (const void *)bias_value, (const void *)masks, (const void *)mask_row})
+    if (!aligned(p, 4)) return fail(KAP_ERR_INVALID_ARGUMENT, "an array is misaligned");
+  const size_t in_bytes = (size_t)((rows - 1) * stride + vocab) * es;
+  const size_t out_bytes = (size_t)((rows - 1) * out_stride + vocab) * es;
+  const bool in_place = out == logits && (stride == out_stride || rows == 1);
+  if (!in_place && overlap(out, out_bytes, logits, in_bytes))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "out overlaps logits");
+  kap::AdjustArgs a;
+  a.rows = rows;
+  a.vocab = vocab;
+  a.f32 = logits_dtype == KAP_DT_F32;
+  a.logits = logits;
+  a.out = out;
+  a.stride = stride;
+  a.out_stride = out_stride;
+  a.history = history_size > 0 ? history : nullptr;
+  a.history_size = history_size;
+  a.history_start = history_start;
+  a.history_len = history_len;
+  a.prompt_len = prompt_len;
+  a.repetition = repetition;
+  a.frequency = frequency;
+  a.presence = presence;
+  a.bias_offsets = num_biases > 0 ? bias_offsets : nullptr;
+  a.bias_token = bias_token;
+  a.bias_value = bias_value;
+  a.num_biases = num_biases;
+  a.masks = num_masks > 0 ? masks : nullptr;
+  a.num_masks = num_masks;
+  a.mask_stride = mask_stride;
+  a.mask_row = mask_row;
+  (void)hipGetLastError();
+  const hipError_t e = kap::launch_adjust_logits(a, device_cus(), static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(KAP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+// ---------------------------------------------------------------------------
 // kap_sample
 // ---------------------------------------------------------------------------
 

@@ -218,6 +218,40 @@ struct SharedArgs {
   float *out, *lse;
 };
 
+// kap_step_tables after host validation.
+enum StepStatus { kStepOk, kStepBadLength, kStepOverCapacity, kStepOverTokens, kStepOutOfPages };
+struct StepArgs {
+  int batch, stride, ring_size, num_tokens;
+  const int32_t *seq_lens, *keep, *add, *pinned;   // keep, pinned may be NULL
+  int32_t *table, *ring;
+  const int32_t *free_state;
+  int32_t *free_out, *new_lens, *q_offsets;
+  int64_t *slots;
+  int32_t *positions, *status;
+  int tokens_here;               // set at launch: the first launch writes slots and positions
+};
+
+// kap_adjust_logits after host validation.
+struct AdjustArgs {
+  int rows, vocab, f32;
+  const void *logits;
+  void *out;
+  int64_t stride, out_stride;    // elements between rows
+  const int32_t *history;        // NULL: none
+  int64_t history_size;
+  const int64_t *history_start;  // [rows]
+  const int32_t *history_len, *prompt_len;
+  const float *repetition, *frequency, *presence;
+  const int32_t *bias_offsets, *bias_token;
+  const float *bias_value;
+  int num_biases;
+  const uint32_t *masks;         // NULL: none
+  int num_masks;
+  int64_t mask_stride;           // words between masks
+  const int32_t *mask_row;
+  int slice;                     // set at launch: tokens of a workgroup
+};
+
 // kap_sample after host validation.
 struct SampleArgs {
   int rows, vocab, f32;
@@ -249,6 +283,8 @@ hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);
 int shared_waves(int kv_type, int D);
 hipError_t launch_attn_shared(const SharedArgs &a, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
+hipError_t launch_step_tables(StepArgs a, int cus, hipStream_t s);
+hipError_t launch_adjust_logits(AdjustArgs a, int cus, hipStream_t s);
 hipError_t launch_fallback_update(const FallbackArgs &a, hipStream_t s);
 hipError_t launch_append_kv(const AppendArgs &a, hipStream_t s);
 hipError_t launch_rope_append(const RopeAppendArgs &a, hipStream_t s);

@@ -1,0 +1,224 @@
+// Block tables, slots and positions of a step from its requests' lengths: pages
+// that are no longer held go back to the ring of free pages, pages that the new
+// tokens need come from it, and every new token gets its slot and position.
+//
+// Everything is prefix sums over the sequences: of the tokens asked for (which
+// sequences get theirs), of the pages needed (which pages they get), of what is
+// granted and returned. One workgroup takes 1024 sequences at a time, with the sums
+// so far carried along; pages move one to a thread, whose sequence is found in the
+// prefix sums in LDS. There is hardly anything to move (12 bytes a token): what
+// bounds a call is its chain of loads and scans.
+//
+// Slots and positions of a small step are written by the same workgroup; of a
+// larger one by a second launch over all CUs.
+#include "kap_internal.h"
+
+#include <algorithm>
+
+namespace kap {
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kTailThreads = 256;
+constexpr int kTailOffsets = 8192;             // offsets that the second launch keeps in LDS
+
+__device__ __forceinline__ long long wave_incl(long long x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+// Inclusive prefix sums of N values over the workgroup, and their totals.
+template <int N>
+__device__ __forceinline__ void scan(const long long (&x)[N], long long (&incl)[N],
+                                     long long (&total)[N], long long (*s)[kWaves]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) incl[i] = wave_incl(x[i], lane);
+  __syncthreads();                             // (the last scan's readers)
+  if (lane == 63)
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i][wave] = incl[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    long long before = 0;
+    total[i] = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const long long v = s[i][w];
+      before += w < wave ? v : 0;
+      total[i] += v;
+    }
+    incl[i] += before;
+  }
+}
+
+// The last entry of n ascending ones that is at most k (the first is).
+template <class T>
+__device__ __forceinline__ int last_at_most(const T *first, int n, long long k) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= k) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Slot and position of token t of the step, the i-th new one of sequence b.
+__device__ __forceinline__ void write_token(const StepArgs &a, long long t, int b, int i, int add,
+                                            int new_len) {
+  const int pos = new_len - add + i;
+  const long long page = a.table[(size_t)b * a.stride + pos / kPage];
+  a.slots[t] = page * kPage + pos % kPage;
+  a.positions[t] = pos;
+}
+__device__ __forceinline__ void write_padding(const StepArgs &a, long long t) {
+  a.slots[t] = -1;
+  a.positions[t] = 0;
+}
+
+__device__ __forceinline__ long long wrapped(long long x, long long size) {
+  if (x >= size) x -= size;
+  return x >= size ? x - size : x;
+}
+
+__global__ __launch_bounds__(kThreads) void step_tables_kernel(StepArgs a) {
+  __shared__ long long s_scan[3][kWaves];
+  __shared__ long long s_back[kThreads];
+  __shared__ int s_need[kThreads], s_have[kThreads], s_held[kThreads];
+  __shared__ int s_first[kThreads + 1], s_len[kThreads];
+  const int tid = threadIdx.x;
+  const long long size = a.ring_size;
+  long long head = a.free_state[0], count = a.free_state[1];
+  if (head < 0 || head >= size) head = 0;
+  count = count < 0 ? 0 : (count > size ? size : count);
+  long long asked = 0, wanted = 0, tokens = 0, taken = 0, returned = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
+    const int b = b0 + tid;
+    const bool in = b < a.batch;
+    const int len = in ? a.seq_lens[b] : 0;
+    int keep = in && a.keep ? a.keep[b] : len;
+    int add = in ? a.add[b] : 0;
+    const int pinned = in && a.pinned ? max(a.pinned[b], 0) : 0;
+    const long long room = (long long)a.stride * kPage;
+    int status = kStepOk;
+    const bool bad = len < 0 || keep < 0 || keep > len || add < 0 || len > room;
+    if (bad) {
+      status = kStepBadLength;
+      keep = len;
+      add = 0;
+    } else if (add > 0 && (long long)keep + add > room) {
+      status = kStepOverCapacity;
+      add = 0;
+    }
+    const int have = bad ? 0 : (len + kPage - 1) / kPage;
+    {
+      const long long x[1] = {add};
+      long long incl[1], total[1];
+      scan(x, incl, total, s_scan);
+      if (add > 0 && asked + incl[0] > a.num_tokens) {
+        status = kStepOverTokens;
+        add = 0;
+      }
+      asked += total[0];
+    }
+    int need = bad ? 0 : max(0, (keep + add + kPage - 1) / kPage - have);
+    {
+      const long long x[1] = {need};
+      long long incl[1], total[1];
+      scan(x, incl, total, s_scan);
+      if (need > 0 && wanted + incl[0] > count) {
+        status = kStepOutOfPages;
+        add = need = 0;
+      }
+      wanted += total[0];
+    }
+    const int held = bad ? 0 : max((keep + add + kPage - 1) / kPage, pinned);
+    const long long x[3] = {add, need, max(0, have - held)};
+    long long incl[3], total[3];
+    scan(x, incl, total, s_scan);
+    s_need[tid] = (int)(incl[1] - x[1]);
+    s_have[tid] = have;
+    s_back[tid] = incl[2] - x[2];
+    s_held[tid] = held;
+    s_first[tid] = (int)(tokens + incl[0] - x[0]);
+    s_len[tid] = keep + add;
+    if (in) {
+      a.new_lens[b] = keep + add;
+      a.status[b] = status;
+      a.q_offsets[b + 1] = (int)(tokens + incl[0]);
+    }
+    __syncthreads();
+    // pages from the front of the ring, and back to its end: the first are among the
+    // `count` that were there, the second go beyond them, so no entry is both
+    for (long long k = tid; k < total[1]; k += kThreads) {
+      const int j = last_at_most(s_need, kThreads, k);
+      a.table[(size_t)(b0 + j) * a.stride + s_have[j] + (k - s_need[j])] =
+          a.ring[wrapped(head + taken + k, size)];
+    }
+    for (long long k = tid; k < total[2] && returned + k < size - count; k += kThreads) {
+      const int j = last_at_most(s_back, kThreads, k);
+      a.ring[wrapped(head + count + returned + k, size)] =
+          a.table[(size_t)(b0 + j) * a.stride + s_held[j] + (k - s_back[j])];
+    }
+    tokens += total[0];
+    taken += total[1];
+    returned += total[2];
+  }
+  if (tid == 0) {
+    a.q_offsets[0] = 0;
+    a.free_out[0] = (int)wrapped(head + taken, size);
+    a.free_out[1] = (int)(count - taken + (returned < size - count ? returned : size - count));
+    s_first[kThreads] = (int)tokens;
+  }
+  if (!a.tokens_here) return;
+  __syncthreads();                             // (table entries, by threads of this workgroup)
+  for (int t = tid; t < a.num_tokens; t += kThreads) {
+    if (t >= tokens) {
+      write_padding(a, t);
+      continue;
+    }
+    const int j = last_at_most(s_first, a.batch, t);
+    const int end = j + 1 < a.batch ? s_first[j + 1] : (int)tokens;
+    write_token(a, t, j, t - s_first[j], end - s_first[j], s_len[j]);
+  }
+}
+
+__global__ __launch_bounds__(kTailThreads) void step_slots_kernel(StepArgs a) {
+  __shared__ int s_first[kTailOffsets];
+  const int *first = a.q_offsets;
+  if (a.batch < kTailOffsets) {
+    for (int i = threadIdx.x; i <= a.batch; i += kTailThreads) s_first[i] = a.q_offsets[i];
+    __syncthreads();
+    first = s_first;
+  }
+  const int tokens = first[a.batch];
+  for (long long t = (long long)blockIdx.x * kTailThreads + threadIdx.x; t < a.num_tokens;
+       t += (long long)gridDim.x * kTailThreads) {
+    if (t >= tokens) {
+      write_padding(a, t);
+      continue;
+    }
+    const int b = last_at_most(first, a.batch, t);
+    write_token(a, t, b, (int)t - first[b], first[b + 1] - first[b], a.new_lens[b]);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_step_tables(StepArgs a, int cus, hipStream_t s) {
+  a.tokens_here = a.batch <= kThreads && a.num_tokens <= 4 * kThreads;
+  hipLaunchKernelGGL(step_tables_kernel, dim3(1), dim3(kThreads), 0, s, a);
+  if (!a.tokens_here && a.num_tokens > 0) {
+    const int blocks = (a.num_tokens + kTailThreads - 1) / kTailThreads;
+    hipLaunchKernelGGL(step_slots_kernel, dim3(std::min(blocks, 4 * cus)), dim3(kTailThreads), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace kap

@@ -37,6 +37,12 @@ KAP_SELECT_STOP = 1
 KAP_ROPE_HALVES = 0
 KAP_ROPE_PAIRS = 1
 
+KAP_STEP_OK = 0
+KAP_STEP_BAD_LENGTH = 1
+KAP_STEP_OVER_CAPACITY = 2
+KAP_STEP_OVER_TOKENS = 3
+KAP_STEP_OUT_OF_PAGES = 4
+
 KAP_PLAN_OK = 0
 KAP_PLAN_OVER_CAPACITY = 1
 KAP_PLAN_BAD_SCORE = 2
@@ -53,8 +59,8 @@ EXPORTS = (
     "kap_selected_decode_scheduled",
     "kap_verify", "kap_verify_workspace_bytes",
     "kap_verify_shared", "kap_verify_shared_workspace_bytes",
-    "kap_append_kv", "kap_rope_append_kv", "kap_compact_view", "kap_fallback_update", "kap_fallback_update_masked",
-    "kap_accept_top3", "kap_accept_top3_workspace_bytes", "kap_sample",
+    "kap_append_kv", "kap_rope_append_kv", "kap_step_tables", "kap_compact_view", "kap_fallback_update", "kap_fallback_update_masked",
+    "kap_accept_top3", "kap_accept_top3_workspace_bytes", "kap_adjust_logits", "kap_sample",
     "kap_sample_workspace_bytes",
     "kap_status_string", "kap_last_error", "kap_abi_version",
     "kap_stream_read",
@@ -153,6 +159,13 @@ def load_library(path: str = LIB_PATH):
     lib.kap_rope_append_kv.argtypes = [
         ctypes.POINTER(KVCacheStruct), _I32, _P, _I64, _P, _P, _I64, _P, _I64, _P, _P, _I32, _P,
         _P, _I32, _I32, _P, _P]
+    lib.kap_step_tables.restype = _I32
+    lib.kap_step_tables.argtypes = [
+        _I32, _P, _P, _P, _P, _P, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _P, _P, _P]
+    lib.kap_adjust_logits.restype = _I32
+    lib.kap_adjust_logits.argtypes = [
+        _I32, _I32, _P, _I64, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I32,
+        _P, _I32, _I64, _P, _P]
     lib.kap_compact_view.restype = _I32
     lib.kap_compact_view.argtypes = [
         ctypes.POINTER(KVCacheStruct), _I32, _P, _I32, _P, _I32, ctypes.POINTER(KVCacheStruct),
@@ -414,6 +427,75 @@ def bind_rope_append_kv(kv: KVCache, k_new, v_new, slot_mapping, positions, inv_
     return BoundCall(lib.kap_rope_append_kv, args, keep)
 
 
+def _step_call(seq_lens, add, block_table, free_pages, free_state, keep, pinned_blocks,
+               num_tokens, outputs, stream):
+    """Validate and marshal one kap_step_tables call: (args, outputs, keep)."""
+    _dev(seq_lens, "seq_lens", torch.int32, 1)
+    B = int(seq_lens.shape[0])
+    _dev(block_table, "block_table", torch.int32, 2)
+    _dev(free_pages, "free_pages", torch.int32, 1)
+    if outputs["slot_mapping"] is not None:
+        num_tokens = int(outputs["slot_mapping"].shape[0])
+    elif num_tokens is None:
+        raise ValueError("num_tokens or slot_mapping is required")
+    sizes = {"free_out": 2, "new_lens": B, "q_offsets": B + 1, "slot_mapping": num_tokens,
+             "positions": num_tokens, "status": B}
+    dt = lambda name: torch.int64 if name == "slot_mapping" else torch.int32   # noqa: E731
+    if any(t is None for t in outputs.values()):
+        with torch.cuda.stream(stream):
+            outputs = {name: torch.empty(sizes[name], dtype=dt(name), device=seq_lens.device)
+                       if t is None else t for name, t in outputs.items()}
+    checked = [("add", add, B, torch.int32), ("free_state", free_state, 2, torch.int32),
+               ("keep", keep, B, torch.int32), ("pinned_blocks", pinned_blocks, B, torch.int32)]
+    checked += [(name, t, sizes[name], dt(name)) for name, t in outputs.items()]
+    for name, t, n, d in checked:
+        if t is not None or name in ("add", "free_state"):
+            _dev(t, name, d, 1)
+            if t.shape[0] != n:
+                raise ValueError(f"{name} must have {n} entries")
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table must have {B} rows")
+    held = (seq_lens, keep, add, pinned_blocks, block_table, free_pages, free_state,
+            *outputs.values())
+    _here(*held, stream=stream)
+    o = outputs
+    args = (B, _ptr(seq_lens), _ptr(keep), _ptr(add), _ptr(pinned_blocks), _ptr(block_table),
+            block_table.shape[1], _ptr(free_pages), free_pages.shape[0], _ptr(free_state),
+            int(num_tokens), _ptr(o["free_out"]), _ptr(o["new_lens"]), _ptr(o["q_offsets"]),
+            _ptr(o["slot_mapping"]), _ptr(o["positions"]), _ptr(o["status"]), _stream(stream))
+    return args, outputs, held
+
+
+def step_tables(seq_lens, add, block_table, free_pages, free_state, *, keep=None,
+                pinned_blocks=None, num_tokens=None, free_out=None, new_lens=None, q_offsets=None,
+                slot_mapping=None, positions=None, status=None, stream=None):
+    """Block tables, slots and positions of a step of sequences that keep
+    ``keep`` (None: all) of their ``seq_lens`` tokens and add ``add`` new ones:
+    pages go to and come from the ring ``free_pages`` with ``free_state`` = (head,
+    count), ``block_table`` [B][stride] and the ring are updated in place. Returns
+    a dict of free_out, new_lens, q_offsets [B + 1], slot_mapping and positions
+    [num_tokens] (padded with -1 and 0) and status (KAP_STEP_*); see kap.h."""
+    outputs = dict(free_out=free_out, new_lens=new_lens, q_offsets=q_offsets,
+                   slot_mapping=slot_mapping, positions=positions, status=status)
+    args, outputs, _ = _step_call(seq_lens, add, block_table, free_pages, free_state, keep,
+                                  pinned_blocks, num_tokens, outputs, stream)
+    _check(load_library().kap_step_tables(*args))
+    return outputs
+
+
+def bind_step_tables(seq_lens, add, block_table, free_pages, free_state, *, free_out, new_lens,
+                     q_offsets, slot_mapping, positions, status, keep=None, pinned_blocks=None,
+                     stream=None) -> "BoundCall":
+    """step_tables marshalled once (not run here: the call moves pages)."""
+    outputs = dict(free_out=free_out, new_lens=new_lens, q_offsets=q_offsets,
+                   slot_mapping=slot_mapping, positions=positions, status=status)
+    if any(t is None for t in outputs.values()):
+        raise ValueError("a bound call needs its outputs")
+    args, _, held = _step_call(seq_lens, add, block_table, free_pages, free_state, keep,
+                               pinned_blocks, None, outputs, stream)
+    return BoundCall(load_library().kap_step_tables, args, held)
+
+
 def compact_view(src: KVCache, view_block_table, view_num_blocks, view_capacity: int,
                  dst: KVCache, out=None, stream=None) -> torch.Tensor:
     """Copy each sequence's first min(view_num_blocks[b], view_capacity) view
@@ -543,6 +625,92 @@ def accept_top3(logits, draft_tokens, top_k: int = 3, accepted=None, carry=None,
 # --------------------------------------------------------------------------
 # kap_sample
 # --------------------------------------------------------------------------
+
+def _adjust_call(logits, out, history, history_start, history_len, prompt_len, repetition,
+                 frequency, presence, bias_offsets, bias_token, bias_value, masks, mask_row,
+                 stream):
+    """Validate and marshal one kap_adjust_logits call: (args, out, keep)."""
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise ValueError("logits must be a tensor [rows][vocab]")
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("logits must be float32 or bfloat16")
+    R, V = logits.shape
+    stride = _rows(logits, "logits", logits.dtype, (R, V))
+    if out is None:
+        with torch.cuda.stream(stream):
+            out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
+    out_stride = _rows(out, "out", logits.dtype, (R, V))
+    f32, i32 = torch.float32, torch.int32
+    for name, t, dt, n in (
+            ("history", history, i32, None), ("history_start", history_start, torch.int64, R),
+            ("history_len", history_len, i32, R), ("prompt_len", prompt_len, i32, R),
+            ("repetition", repetition, f32, R), ("frequency", frequency, f32, R),
+            ("presence", presence, f32, R), ("bias_offsets", bias_offsets, i32, R + 1),
+            ("bias_token", bias_token, i32, None), ("bias_value", bias_value, f32, None),
+            ("mask_row", mask_row, i32, R)):
+        if t is not None:
+            _dev(t, name, dt, 1)
+            if n is not None and t.shape[0] != n:
+                raise ValueError(f"{name} must have {n} entries")
+    if (bias_token is None) != (bias_value is None) or (
+            bias_token is not None and bias_token.shape != bias_value.shape):
+        raise ValueError("bias_token and bias_value go together")
+    if bias_offsets is None and bias_token is not None:
+        raise ValueError("biases need bias_offsets")
+    if history is None and any(t is not None for t in (history_start, history_len, prompt_len,
+                                                       repetition, frequency, presence)):
+        raise ValueError("penalties need a history")
+    if history is not None and (history_start is None or history_len is None):
+        raise ValueError("history needs history_start and history_len")
+    if (masks is None) != (mask_row is None):
+        raise ValueError("masks and mask_row go together")
+    N, mask_stride = 0, 0
+    if masks is not None:
+        if masks.dtype not in (torch.int32, torch.uint32):
+            raise TypeError("masks must be int32 or uint32")
+        if masks.dim() != 2 or masks.shape[1] != -(-V // 32):
+            raise ValueError(f"masks must be [n][{-(-V // 32)}], got {tuple(masks.shape)}")
+        N, mask_stride = masks.shape[0], _rows(masks, "masks", masks.dtype, masks.shape)
+    held = (logits, out, history, history_start, history_len, prompt_len, repetition, frequency,
+            presence, bias_offsets, bias_token, bias_value, masks, mask_row)
+    _here(*held, stream=stream)
+    args = (R, V, _ptr(logits), stride, KAP_DT_F32 if logits.dtype == f32 else KAP_DT_BF16,
+            _ptr(out), out_stride, _ptr(history), 0 if history is None else history.shape[0],
+            _ptr(history_start), _ptr(history_len), _ptr(prompt_len), _ptr(repetition),
+            _ptr(frequency), _ptr(presence), _ptr(bias_offsets), _ptr(bias_token),
+            _ptr(bias_value), 0 if bias_token is None else bias_token.shape[0], _ptr(masks), N,
+            mask_stride, _ptr(mask_row), _stream(stream))
+    return args, out, held
+
+
+def adjust_logits(logits, out=None, *, history=None, history_start=None, history_len=None,
+                  prompt_len=None, repetition=None, frequency=None, presence=None,
+                  bias_offsets=None, bias_token=None, bias_value=None, masks=None, mask_row=None,
+                  stream=None):
+    """Penalise the tokens of each row's history, add biases (a list of tokens and
+    values per row) and mask what a grammar does not allow (bits of ``masks``
+    [n][ceil(vocab / 32)], one of them, or none, per row) in ``logits`` [rows][vocab]
+    (float32 / bfloat16; rows may lie apart). ``out`` may be ``logits``; returns it;
+    see kap.h."""
+    args, out, _ = _adjust_call(logits, out, history, history_start, history_len, prompt_len,
+                                repetition, frequency, presence, bias_offsets, bias_token,
+                                bias_value, masks, mask_row, stream)
+    _check(load_library().kap_adjust_logits(*args))
+    return out
+
+
+def bind_adjust_logits(logits, out, *, history=None, history_start=None, history_len=None,
+                       prompt_len=None, repetition=None, frequency=None, presence=None,
+                       bias_offsets=None, bias_token=None, bias_value=None, masks=None,
+                       mask_row=None, stream=None) -> "BoundCall":
+    """adjust_logits marshalled once (not run here: ``out`` may be ``logits``)."""
+    if out is None:
+        raise ValueError("a bound call needs out")
+    args, _, held = _adjust_call(logits, out, history, history_start, history_len, prompt_len,
+                                 repetition, frequency, presence, bias_offsets, bias_token,
+                                 bias_value, masks, mask_row, stream)
+    return BoundCall(load_library().kap_adjust_logits, args, held)
+
 
 def sample_workspace_bytes(rows: int, vocab: int) -> int:
     return int(load_library().kap_sample_workspace_bytes(rows, vocab))
