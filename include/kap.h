@@ -402,6 +402,41 @@ size_t kap_verify_shared_workspace_bytes(const kap_kv_cache *kv, int32_t batch, 
                                          int32_t max_seq_len, int32_t num_groups);
 
 /*
+ * kap_chunk_attention -- attention of ragged chunks of new tokens over the paged
+ * cache: a prompt's next tokens, one token of a sequence that decodes, or both in
+ * one batch (continuous batching), with a sliding window or without.
+ *
+ * Sequence b's new tokens are rows q_offsets[b] .. q_offsets[b + 1] - 1 of q, and
+ * the last ones of the seq_lens[b] in the cache (their K and V are there already):
+ * the i-th of n is at position p = seq_lens[b] - n + i. It sees the positions
+ * t <= p and, with window > 0, of those p - t < window and t < sinks only (the
+ * first `sinks` tokens stay visible). A row that sees no key (n > seq_lens[b], pages
+ * outside the pool) gets out = 0, lse = -inf. Position t is read in page
+ * block_table[b][t / 16]; an id outside the pool contributes no keys.
+ *   q, out [num_tokens][Hq][D], both q_dtype and 16-byte aligned: out is what the
+ *   output projection reads, rounded once. lse [num_tokens][Hq] float32, or NULL.
+ *   q_offsets [batch + 1] int32, ascending within [0, num_tokens] (other values:
+ *   unspecified results; rows of no sequence are left as they are). seq_lens
+ *   [batch], block_table [batch][table_stride] int32; max_seq_len (host) >= every
+ *   seq_lens[b] and <= 16 * table_stride, < 2^31 - 64. window <= 0: none; sinks
+ *   >= 0, not read without a window.
+ * Softmax weights meet V of bf16 and fp8 pages rounded to bf16 (each off by at most
+ * 2^-8 of it, as out is); logits, sums and lse are single precision throughout. batch <= 65535,
+ * num_tokens * num_q_heads < 2^30. The workspace holds scratch only (its contents do
+ * not matter).
+ */
+kap_status kap_chunk_attention(const kap_kv_cache *kv, int32_t batch, int32_t num_tokens,
+                               const void *q, const int32_t *q_offsets, const int32_t *seq_lens,
+                               const int32_t *block_table, int32_t table_stride,
+                               int32_t max_seq_len, int32_t window, int32_t sinks, float sm_scale,
+                               void *out, float *lse, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+size_t kap_chunk_attention_workspace_bytes(const kap_kv_cache *kv, int32_t batch,
+                                           int32_t num_tokens, int32_t max_seq_len,
+                                           int32_t window, int32_t sinks);
+
+/*
  * kap_append_kv -- place newly scheduled tokens' K/V into their physical KV
  * slots (the slot mapping of Sec. 3.1, "Selected-KV view materialization"):
  * how verification advances the full-context KV state KV^{full,+} of Sec. 3.2

@@ -33,8 +33,8 @@ HIPCC_FLAGS = [
 
 # Sources whose kernels must hold everything in registers: versions of the wide
 # attention kernel that spilled vector registers have returned wrong results (the
-# shared-prefix kernel is built the same way).
-NO_SPILLS = {"attn_wide.hip", "attn_shared.hip"}
+# shared-prefix and chunk kernels are built the same way).
+NO_SPILLS = {"attn_wide.hip", "attn_shared.hip", "attn_chunk.hip"}
 RESOURCE_REMARKS = "-Rpass-analysis=kernel-resource-usage"
 
 

@@ -1297,6 +1297,139 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
 }
 
 // ---------------------------------------------------------------------------
+// kap_chunk_attention
+// ---------------------------------------------------------------------------
+
+// Sizes of a call's workspace: [map][partial o][partial lse], and what the work is cut by.
+struct ChunkPlan {
+  int few_rows, target, tall_cost, few_cost, tall_least, few_least, window;
+  long long grid, part_rows;
+  size_t part_o, part_lse, total;
+};
+
+static ChunkPlan plan_chunk(const kap_kv_cache *kv, int batch, int num_tokens, int max_seq_len,
+                            int window, int sinks) {
+  ChunkPlan p;
+  const int waves = kap::chunk_waves(kv->kv_dtype, kv->head_dim), tall = 32 * waves;
+  const long long Hkv = kv->num_kv_heads;
+  const long long rows = (long long)num_tokens * (kv->num_q_heads / Hkv);
+  p.window = window > 0 && window < max_seq_len ? window : 0;
+  p.few_rows = 128;
+  p.target = device_cus();
+  p.tall_cost = 4;
+  p.few_cost = kv->kv_dtype == KAP_DT_FP8_E4M3FN ? 2 : 3;
+  p.tall_least = 8;
+  p.few_least = 2;
+  // parts: a block of rows each, and twice the target for what is split
+  const long long tall_blocks = rows / tall + std::min<long long>(batch, rows / (p.few_rows + 1));
+  const long long few_parts = (rows / 32 + batch) * Hkv + 2ll * p.target * waves;
+  p.grid = tall_blocks * Hkv + 2ll * p.target + (few_parts + waves - 1) / waves;
+  // the most steps of a block, hence the most parts of a row
+  long long steps = cdiv(max_seq_len, 32);
+  if (p.window)
+    steps = std::min<long long>(steps, cdiv(std::min(sinks, max_seq_len), 32) + 2 +
+                                           ((long long)p.window + std::min(num_tokens, tall)) / 32);
+  const long long most = (steps + p.few_least - 1) / p.few_least;
+  p.part_rows = most <= 1 ? 0
+                          : std::min<long long>(2 * rows * Hkv * most, 4ll * p.target * tall);
+  p.part_o = round_up(sizeof(int64_t) * batch + sizeof(int32_t) * (4 * (size_t)batch + 4), 256);
+  p.part_lse = p.part_o + round_up((size_t)p.part_rows * kv->head_dim * sizeof(float), 256);
+  p.total = p.part_lse + round_up((size_t)p.part_rows * sizeof(float), 256);
+  return p;
+}
+
+static bool chunk_sizes_ok(const kap_kv_cache *kv, int batch, int num_tokens, int max_seq_len) {
+  return batch > 0 && batch <= 65535 && num_tokens >= 0 && max_seq_len >= 0 &&
+         max_seq_len < 0x7fffffff - 63 && (long long)num_tokens * kv->num_q_heads < 1 << 30;
+}
+
+size_t kap_chunk_attention_workspace_bytes(const kap_kv_cache *kv, int32_t batch,
+                                           int32_t num_tokens, int32_t max_seq_len,
+                                           int32_t window, int32_t sinks) {
+  if (check_kv(kv) != KAP_OK || !chunk_sizes_ok(kv, batch, num_tokens, max_seq_len) || sinks < 0)
+    return 0;
+  return plan_chunk(kv, batch, num_tokens, max_seq_len, window, sinks).total;
+}
+
+kap_status kap_chunk_attention(const kap_kv_cache *kv, int32_t batch, int32_t num_tokens,
+                               const void *q, const int32_t *q_offsets, const int32_t *seq_lens,
+                               const int32_t *block_table, int32_t table_stride,
+                               int32_t max_seq_len, int32_t window, int32_t sinks, float sm_scale,
+                               void *out, float *lse, void *workspace, size_t workspace_bytes,
+                               void *stream) {
+  kap_status st = check_kv(kv);
+  if (st != KAP_OK) return st;
+  if (batch < 0 || num_tokens < 0 || max_seq_len < 0 || sinks < 0)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "a size is negative");
+  if (batch == 0 && num_tokens > 0)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "%d tokens of no sequence", num_tokens);
+  if (table_stride < cdiv(max_seq_len, 16))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "table_stride %d < ceil(max_seq_len/16) = %d", table_stride,
+                cdiv(max_seq_len, 16));
+  if (!(sm_scale == sm_scale) || sm_scale > 3.0e38f || sm_scale < -3.0e38f)
+    return fail(KAP_ERR_INVALID_ARGUMENT, "sm_scale must be finite");
+  if (batch == 0 || num_tokens == 0) return ok();
+  if (!chunk_sizes_ok(kv, batch, num_tokens, max_seq_len))
+    return fail(KAP_ERR_UNSUPPORTED, "batch, num_tokens or max_seq_len is too large");
+  if (kv->num_pages < 1) return fail(KAP_ERR_INVALID_ARGUMENT, "KV pool has no pages");
+  if (!q || !q_offsets || !seq_lens || !out || (max_seq_len > 0 && !block_table))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "a required pointer is NULL");
+  if (!aligned(q, 16) || !aligned(out, 16))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "q and out must be 16-byte aligned");
+  if (!aligned(q_offsets, 4) || !aligned(seq_lens, 4) || !aligned(block_table, 4) || !aligned(lse, 4))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "an array is misaligned");
+  const size_t q_bytes = (size_t)num_tokens * kv->num_q_heads * kv->head_dim *
+                         (kv->q_dtype == KAP_DT_F32 ? 4 : 2);
+  if (overlap(q, q_bytes, out, q_bytes))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "out overlaps q");
+  const ChunkPlan p = plan_chunk(kv, batch, num_tokens, max_seq_len, window, sinks);
+  if (!workspace || workspace_bytes < p.total)
+    return fail(KAP_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", p.total, workspace_bytes);
+  if (!aligned(workspace, 256))
+    return fail(KAP_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
+  char *base = static_cast<char *>(workspace);
+  kap::ChunkArgs a;
+  a.batch = batch;
+  a.num_tokens = num_tokens;
+  a.Hq = kv->num_q_heads;
+  a.Hkv = kv->num_kv_heads;
+  a.G = kv->num_q_heads / kv->num_kv_heads;
+  a.D = kv->head_dim;
+  a.kv_type = kv->kv_dtype;
+  a.k_pages = kv->k_pages;
+  a.v_pages = kv->v_pages;
+  a.kv_scales = kv->kv_scales;
+  a.num_pages = kv->num_pages;
+  a.q = q;
+  a.q_offsets = q_offsets;
+  a.seq_lens = seq_lens;
+  a.table = block_table;
+  a.stride = table_stride;
+  a.max_len = max_seq_len;
+  a.window = p.window;
+  a.sinks = p.window ? std::min(sinks, max_seq_len) : 0;
+  a.scale_log2 = (sm_scale < 0 ? -sm_scale : sm_scale) * kap::kLog2e;
+  a.q_sign = sm_scale < 0 ? (kv->q_dtype == KAP_DT_F32 ? 0x80000000u : 0x80008000u) : 0;
+  a.few_rows = p.few_rows;
+  a.target = p.target;
+  a.tall_cost = p.tall_cost;
+  a.few_cost = p.few_cost;
+  a.tall_least = p.tall_least;
+  a.few_least = p.few_least;
+  a.grid = p.grid;
+  a.part_rows = p.part_rows;
+  a.map = base;
+  a.part_o = reinterpret_cast<float *>(base + p.part_o);
+  a.part_lse = reinterpret_cast<float *>(base + p.part_lse);
+  a.out = out;
+  a.lse = lse;
+  (void)hipGetLastError();
+  const hipError_t e = kap::launch_attn_chunk(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(KAP_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+// ---------------------------------------------------------------------------
 // kap_step_tables
 // ---------------------------------------------------------------------------
 

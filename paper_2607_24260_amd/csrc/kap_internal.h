@@ -218,6 +218,36 @@ struct SharedArgs {
   float *out, *lse;
 };
 
+// kap_chunk_attention after host validation.
+struct ChunkArgs {
+  int batch, num_tokens, Hq, Hkv, G, D, kv_type;
+  const void *k_pages, *v_pages;
+  const float *kv_scales;
+  int64_t num_pages;
+  const void *q;                 // [num_tokens][Hq][D]
+  const int32_t *q_offsets;      // [batch + 1]
+  const int32_t *seq_lens, *table;
+  int stride, max_len;
+  int window, sinks;             // window 0: none
+  float scale_log2;              // |sm_scale| * log2(e)
+  uint32_t q_sign;               // flips the sign of a word of q if sm_scale < 0
+  int few_rows;                  // rows of a sequence that wavefronts take by themselves
+  int target;                    // workgroups the work is spread over
+  int tall_cost, few_cost;       // of a step of a workgroup, of a wavefront by itself
+  int tall_least, few_least;     // least steps of a part
+  int64_t grid;                  // workgroups
+  int64_t part_rows;             // rows of the partials
+  void *map;                     // see attn_chunk.hip
+  float *part_o, *part_lse;      // [rows][D], [rows]: normalised, log2 domain
+  void *out;                     // [num_tokens][Hq][D], q's type
+  float *lse;                    // [num_tokens][Hq], or NULL
+};
+// Wavefronts of a workgroup of the chunk kernel: two per SIMD, or one where
+// accumulators, queries and a step's operands leave no room for a second.
+constexpr int chunk_waves(int kv_type, int D) {
+  return D == 256 || (kv_type == kF32 && D == 128) ? 4 : 8;
+}
+
 // kap_step_tables after host validation.
 enum StepStatus { kStepOk, kStepBadLength, kStepOverCapacity, kStepOverTokens, kStepOutOfPages };
 struct StepArgs {
@@ -283,6 +313,7 @@ hipError_t launch_accept_top3(const AcceptArgs &a, hipStream_t s);
 int shared_waves(int kv_type, int D);
 hipError_t launch_attn_shared(const SharedArgs &a, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
+hipError_t launch_attn_chunk(const ChunkArgs &a, hipStream_t s);
 hipError_t launch_step_tables(StepArgs a, int cus, hipStream_t s);
 hipError_t launch_adjust_logits(AdjustArgs a, int cus, hipStream_t s);
 hipError_t launch_fallback_update(const FallbackArgs &a, hipStream_t s);

@@ -11,63 +11,16 @@
 //
 // Slots and positions of a small step are written by the same workgroup; of a
 // larger one by a second launch over all CUs.
-#include "kap_internal.h"
+#include "block_scan.h"
 
 #include <algorithm>
 
 namespace kap {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = kScanThreads, kWaves = kThreads / 64;
 constexpr int kTailThreads = 256;
 constexpr int kTailOffsets = 8192;             // offsets that the second launch keeps in LDS
-
-__device__ __forceinline__ long long wave_incl(long long x, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
-
-// Inclusive prefix sums of N values over the workgroup, and their totals.
-template <int N>
-__device__ __forceinline__ void scan(const long long (&x)[N], long long (&incl)[N],
-                                     long long (&total)[N], long long (*s)[kWaves]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int i = 0; i < N; ++i) incl[i] = wave_incl(x[i], lane);
-  __syncthreads();                             // (the last scan's readers)
-  if (lane == 63)
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i][wave] = incl[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    long long before = 0;
-    total[i] = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const long long v = s[i][w];
-      before += w < wave ? v : 0;
-      total[i] += v;
-    }
-    incl[i] += before;
-  }
-}
-
-// The last entry of n ascending ones that is at most k (the first is).
-template <class T>
-__device__ __forceinline__ int last_at_most(const T *first, int n, long long k) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= k) lo = mid;
-    else hi = mid;
-  }
-  return lo;
-}
 
 // Slot and position of token t of the step, the i-th new one of sequence b.
 __device__ __forceinline__ void write_token(const StepArgs &a, long long t, int b, int i, int add,

@@ -59,6 +59,7 @@ EXPORTS = (
     "kap_selected_decode_scheduled",
     "kap_verify", "kap_verify_workspace_bytes",
     "kap_verify_shared", "kap_verify_shared_workspace_bytes",
+    "kap_chunk_attention", "kap_chunk_attention_workspace_bytes",
     "kap_append_kv", "kap_rope_append_kv", "kap_step_tables", "kap_compact_view", "kap_fallback_update", "kap_fallback_update_masked",
     "kap_accept_top3", "kap_accept_top3_workspace_bytes", "kap_adjust_logits", "kap_sample",
     "kap_sample_workspace_bytes",
@@ -153,6 +154,13 @@ def load_library(path: str = LIB_PATH):
     lib.kap_verify_shared_workspace_bytes.restype = _SZ
     lib.kap_verify_shared_workspace_bytes.argtypes = [
         ctypes.POINTER(KVCacheStruct), _I32, _I32, _I32, _I32]
+    lib.kap_chunk_attention.restype = _I32
+    lib.kap_chunk_attention.argtypes = [
+        ctypes.POINTER(KVCacheStruct), _I32, _I32, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _F,
+        _P, _P, _P, _SZ, _P]
+    lib.kap_chunk_attention_workspace_bytes.restype = _SZ
+    lib.kap_chunk_attention_workspace_bytes.argtypes = [
+        ctypes.POINTER(KVCacheStruct), _I32, _I32, _I32, _I32, _I32]
     lib.kap_append_kv.restype = _I32
     lib.kap_append_kv.argtypes = [ctypes.POINTER(KVCacheStruct), _I32, _P, _P, _P, _P, _P]
     lib.kap_rope_append_kv.restype = _I32
@@ -1129,6 +1137,79 @@ def verify_shared(kv: KVCache, q, seq_lens, full_block_table, max_seq_len: int, 
                                        workspace, stream)
     _check(load_library().kap_verify_shared(*args))
     return res
+
+
+def chunk_attention_workspace_bytes(kv: KVCache, batch: int, num_tokens: int, max_seq_len: int, *,
+                                    window: int = 0, sinks: int = 0) -> int:
+    return int(load_library().kap_chunk_attention_workspace_bytes(
+        ctypes.byref(kv.struct), batch, num_tokens, max_seq_len, window, sinks))
+
+
+def _chunk_call(kv: KVCache, q, q_offsets, seq_lens, block_table, max_seq_len, sm_scale, out, lse,
+                workspace, window, sinks, stream):
+    """Validate and marshal one kap_chunk_attention call: (args, (out, lse), keep)."""
+    _dev(q, "q", kv.q_dtype, 3)
+    T = q.shape[0]
+    if tuple(q.shape[1:]) != (kv.num_q_heads, kv.head_dim):
+        raise ValueError("q must be [num_tokens][num_q_heads][head_dim]")
+    _dev(seq_lens, "seq_lens", torch.int32, 1)
+    B = seq_lens.shape[0]
+    _dev(q_offsets, "q_offsets", torch.int32, 1)
+    _dev(block_table, "block_table", torch.int32, 2)
+    if q_offsets.shape[0] != B + 1 or block_table.shape[0] != B:
+        raise ValueError("q_offsets must have an entry more than seq_lens, block_table as many rows")
+    need = chunk_attention_workspace_bytes(kv, B, T, max_seq_len, window=window, sinks=sinks)
+    with torch.cuda.stream(stream):
+        # (rows of no sequence are not written: zeros then)
+        out = torch.zeros_like(q) if out is None else out
+        if lse is None:
+            lse = torch.zeros((T, kv.num_q_heads), dtype=torch.float32, device=q.device)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _dev(out, "out", kv.q_dtype)
+    _dev(lse, "lse", torch.float32)
+    if out.shape != q.shape or tuple(lse.shape) != (T, kv.num_q_heads):
+        raise ValueError("out must have q's shape, lse [num_tokens][num_q_heads]")
+    have = 0
+    if workspace is not None:
+        _dev(workspace, "workspace")
+        have = workspace.numel() * workspace.element_size()
+    keep = (kv, q, q_offsets, seq_lens, block_table, out, lse, workspace)
+    _here(kv.k_pages, *keep[1:], stream=stream)
+    args = (ctypes.byref(kv.struct), B, T, _ptr(q), _ptr(q_offsets), _ptr(seq_lens),
+            _ptr(block_table), block_table.shape[1], int(max_seq_len), int(window), int(sinks),
+            float(sm_scale), _ptr(out), _ptr(lse), _ptr(workspace), have, _stream(stream))
+    return args, (out, lse), keep
+
+
+def chunk_attention(kv: KVCache, q, q_offsets, seq_lens, block_table, max_seq_len: int,
+                    sm_scale: float, *, out=None, lse=None, workspace=None, window: int = 0,
+                    sinks: int = 0, stream=None):
+    """Causal attention of each sequence's new tokens -- rows ``q_offsets[b]`` ..
+    ``q_offsets[b + 1] - 1`` of q [T][Hq][D], the last of its ``seq_lens[b]`` cached
+    ones -- over its pages; with ``window``, a row sees the last ``window`` positions
+    and the first ``sinks`` only. Returns (out [T][Hq][D] in q's dtype, lse [T][Hq]
+    float32); rows of no sequence are left as they are (zeros in a new tensor)."""
+    args, res, _ = _chunk_call(kv, q, q_offsets, seq_lens, block_table, max_seq_len, sm_scale, out,
+                               lse, workspace, window, sinks, stream)
+    _check(load_library().kap_chunk_attention(*args))
+    return res
+
+
+def bind_chunk_attention(kv: KVCache, q, q_offsets, seq_lens, block_table, max_seq_len: int,
+                         sm_scale: float, out, lse, workspace, *, window: int = 0, sinks: int = 0,
+                         stream=None) -> "BoundCall":
+    """chunk_attention marshalled once (and run once here) for tight loops and graph capture."""
+    need = chunk_attention_workspace_bytes(kv, seq_lens.shape[0], q.shape[0], max_seq_len,
+                                           window=window, sinks=sinks)
+    have = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if need > have:
+        raise ValueError(f"workspace of {need} bytes required")
+    args, _, keep = _chunk_call(kv, q, q_offsets, seq_lens, block_table, max_seq_len, sm_scale, out,
+                                lse, workspace, window, sinks, stream)
+    fn = load_library().kap_chunk_attention
+    _check(fn(*args))                                             # validates once
+    return BoundCall(fn, args, keep)
 
 
 def stream_read(buf, sink, stream=None):
