@@ -7,9 +7,11 @@
 //
 // What the history says of a slice is counted in LDS (integer atomics: the order
 // does not matter), a word a token: how often the token was put out, and, in the
-// top bit, whether the prompt has it. Biases go the same way, as the place in the list
-// of the last one for the token. The slice's logits are fetched before the history is
-// counted and meanwhile travel. Bound by the bytes: each logit is read and written once.
+// top bit, whether the prompt has it. Tokens with a bias are marked there with a bit and
+// left to the threads that walk the list; that the last of a token's entries counts
+// takes a second look only where a slice's list names a token twice. The slice's logits
+// are fetched first and travel while the history is counted. Bound by the bytes: each
+// logit is read and written once.
 #include "kap_internal.h"
 
 #include <algorithm>
@@ -32,40 +34,30 @@ template <> __device__ __forceinline__ uint16_t rounded<uint16_t>(float x) {
   return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
+constexpr int kBytes = 16;                     // of a thread's load
+constexpr int kLoads = 4;                      // of a thread, at most
+constexpr int kMost = kThreads * kLoads * kBytes / 2;   // tokens of a slice, at most
+
 // What a row asks for.
 struct Row {
   float rep, freq, pres;
-  bool told, biased;
+  bool told;
   const uint32_t *mask;      // NULL: none
 };
 
-struct Slice {
-  const uint32_t *counts;    // LDS, by token of the slice
-  const int *biases;
-  int v0;                    // first token
-};
-
-__device__ __forceinline__ float adjusted(const AdjustArgs &a, const Row &r, const Slice &s, float x,
-                                          int v, bool allowed) {
-  if (r.told) {
-    const uint32_t c = s.counts[v - s.v0];
-    if (c != 0) {
-      x = x > 0.f ? x / r.rep : x * r.rep;
-      const uint32_t n = c & ~kPrompt;
-      if (n != 0) x = x - r.freq * (float)n - r.pres;
-    }
+__device__ __forceinline__ float penalised(const Row &r, float x, uint32_t c) {
+  if (c != 0) {
+    x = x > 0.f ? x / r.rep : x * r.rep;
+    const uint32_t n = c & ~kPrompt;
+    if (n != 0) x = x - r.freq * (float)n - r.pres;
   }
-  if (r.biased) {
-    const int e = s.biases[v - s.v0];
-    if (e != 0) x += a.bias_value[e - 1];
-  }
-  return allowed ? x : -INFINITY;
+  return x;
 }
 
-// The mask's bits of tokens v .. v + 7 (those behind the last word: 0).
-__device__ __forceinline__ uint32_t mask_bits(const uint32_t *mask, int words, int v) {
+// Bits of tokens v .. v + 7 (those behind the last word: 0).
+__device__ __forceinline__ uint32_t bits_at(const uint32_t *words, int n, int v) {
   const int w = v >> 5;
-  const unsigned long long lo = mask[w], hi = w + 1 < words ? mask[w + 1] : 0u;
+  const unsigned long long lo = words[w], hi = w + 1 < n ? words[w + 1] : 0u;
   return (uint32_t)((lo | hi << 32) >> (v & 31));
 }
 
@@ -73,11 +65,28 @@ template <bool F32>
 __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
   typedef typename Elem<F32>::type T;
   constexpr int kPer = Elem<F32>::kPer;
-  extern __shared__ __align__(16) uint32_t lds[];
+  typedef T vec __attribute__((ext_vector_type(kPer)));
+  constexpr int kSlice = kMost / (F32 ? 2 : 1);
+  __shared__ __align__(16) uint32_t s_counts[kSlice + 4];
+  __shared__ uint32_t s_biased[kSlice / 32], s_claimed[kSlice / 32];
+  __shared__ int s_list[kThreads];
+  __shared__ int s_twice;
   const int row = blockIdx.y, v0 = blockIdx.x * a.slice, n = min(a.slice, a.vocab - v0);
   const int tid = threadIdx.x;
-  uint32_t *counts = lds;
-  int *biases = reinterpret_cast<int *>(lds + (a.history ? a.slice : 0));
+  const T *x = static_cast<const T *>(a.logits) + (size_t)row * a.stride + v0;
+  T *y = static_cast<T *>(a.out) + (size_t)row * a.out_stride + v0;
+  // Whole 16-byte pieces where both rows have them at the same tokens, from the `skip`-th
+  // token on; the rest one by one.
+  const int skip_x = (int)(-(reinterpret_cast<uintptr_t>(x) / sizeof(T)) & (kPer - 1));
+  const int skip_y = (int)(-(reinterpret_cast<uintptr_t>(y) / sizeof(T)) & (kPer - 1));
+  const int skip = skip_x == skip_y ? min(skip_x, n) : n;
+  const int pieces = (n - skip) / kPer;
+  vec in[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int p = tid + i * kThreads;
+    if (p < pieces) in[i] = *reinterpret_cast<const vec *>(x + skip + p * kPer);
+  }
   Row r;
   r.rep = a.repetition ? a.repetition[row] : 1.f;
   r.freq = a.frequency ? a.frequency[row] : 0.f;
@@ -89,60 +98,146 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
     e0 = min(max(a.bias_offsets[row], 0), a.num_biases);
     e1 = min(max(a.bias_offsets[row + 1], e0), a.num_biases);
   }
-  r.biased = e1 > e0;
+  const bool biased = e1 > e0;
   r.mask = nullptr;
   const int words = (a.vocab + 31) / 32;
   if (a.masks) {
     const int m = a.mask_row[row];
     if (m >= 0 && m < a.num_masks) r.mask = a.masks + (size_t)m * a.mask_stride;
   }
+  // (a piece's counts are 16-byte aligned in LDS)
+  uint32_t *counts = s_counts + (-skip & 3);
   if (r.told) {
-    for (int i = tid; i < n; i += kThreads) counts[i] = 0;
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    for (int i = 4 * tid; i < n + 4; i += 4 * kThreads)
+      *reinterpret_cast<u32x4 *>(s_counts + i) = u32x4{0, 0, 0, 0};
   }
-  if (r.biased) {
-    for (int i = tid; i < n; i += kThreads) biases[i] = 0;
+  if (biased) {
+    for (int i = tid; i < (n + 31) / 32; i += kThreads) s_biased[i] = s_claimed[i] = 0;
+    if (tid == 0) s_twice = 0;
   }
-  if (r.told || r.biased) __syncthreads();
+  if (r.told || biased) __syncthreads();
   if (r.told) {
     // (a range outside the history counts where it is inside)
     const long long start = min(max((long long)a.history_start[row], -(1ll << 31)), a.history_size);
     const int prompt = a.prompt_len ? a.prompt_len[row] : 0;
     const long long lo = start < 0 ? -start : 0;
     const long long hi = min((long long)len, a.history_size - start);
-    for (long long i = lo + tid; i < hi; i += kThreads) {
-      const uint32_t at = (uint32_t)(a.history[start + i] - v0);
-      if (at < (uint32_t)n) {
-        if (i < prompt) atomicOr(&counts[at], kPrompt);
-        else atomicAdd(&counts[at], 1u);
+    constexpr int kAtOnce = 8;
+    for (long long i0 = lo + tid; i0 < hi; i0 += kAtOnce * kThreads) {
+      int token[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const long long i = i0 + k * kThreads;
+        token[k] = i < hi ? a.history[start + i] : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const uint32_t at = (uint32_t)(token[k] - v0);
+        if (token[k] >= 0 && at < (uint32_t)n) {
+          if (i0 + k * kThreads < prompt) atomicOr(&counts[at], kPrompt);
+          else atomicAdd(&counts[at], 1u);
+        }
       }
     }
   }
-  if (r.biased)
+  if (biased)
     for (int e = e0 + tid; e < e1; e += kThreads) {
-      const uint32_t at = (uint32_t)(a.bias_token[e] - v0);
-      if (at < (uint32_t)n) atomicMax(&biases[at], e + 1);
+      const int v = a.bias_token[e];
+      const uint32_t at = (uint32_t)(v - v0), bit = 1u << (at & 31);
+      if (v >= 0 && at < (uint32_t)n && (atomicOr(&s_biased[at >> 5], bit) & bit)) s_twice = 1;
     }
-  if (r.told || r.biased) __syncthreads();
-  const Slice s{counts, biases, v0};
-  const T *x = static_cast<const T *>(a.logits) + (size_t)row * a.stride + v0;
-  T *y = static_cast<T *>(a.out) + (size_t)row * a.out_stride + v0;
-  for (int i = tid; i < n; i += kThreads) {
-    const int v = v0 + i;
-    const bool allowed = !r.mask || (mask_bits(r.mask, words, v) & 1u);
-    y[i] = rounded<T>(adjusted(a, r, s, value(x[i]), v, allowed));
+  if (r.told || biased) __syncthreads();
+
+  // a token by itself (no bias: -0, which leaves every value as it is)
+  auto write_one = [&](int at, float add) {
+    const int v = v0 + at;
+    float z = value(x[at]);
+    if (r.told) z = penalised(r, z, counts[at]);
+    z += add;
+    if (r.mask && !(bits_at(r.mask, words, v) & 1u)) z = -INFINITY;
+    y[at] = rounded<T>(z);
+  };
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int p = tid + i * kThreads;
+    if (p >= pieces) continue;
+    const int at = skip + p * kPer;
+    constexpr uint32_t kAll = (1u << kPer) - 1;
+    vec out = in[i];
+    if (r.told) {
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      u32x4 c[kPer / 4];
+      uint32_t any = 0;
+#pragma unroll
+      for (int k = 0; k < kPer / 4; ++k) {
+        c[k] = *reinterpret_cast<const u32x4 *>(counts + at + 4 * k);
+        any |= c[k][0] | c[k][1] | c[k][2] | c[k][3];
+      }
+      if (any != 0) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+          out[k] = rounded<T>(penalised(r, value((T)out[k]), c[k >> 2][k & 3]));
+      }
+    }
+    if (r.mask) {
+      const uint32_t allowed = bits_at(r.mask, words, v0 + at);
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (!(allowed >> k & 1u)) out[k] = rounded<T>(-INFINITY);
+    }
+    const uint32_t left = biased ? bits_at(s_biased, (n + 31) / 32, at) & kAll : 0;
+    if (left == 0) {
+      *reinterpret_cast<vec *>(y + at) = out;
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        if (!(left >> k & 1u)) y[at + k] = out[k];
+    }
   }
-  (void)kPer;
+  for (int i = tid; i < n - pieces * kPer; i += kThreads) {
+    const int at = i < skip ? i : i + pieces * kPer;
+    if (!biased || !(s_biased[at >> 5] >> (at & 31) & 1u)) write_one(at, -0.f);
+  }
+  if (!biased) return;
+  if (!s_twice) {
+    for (int e = e0 + tid; e < e1; e += kThreads) {
+      const int v = a.bias_token[e];
+      const uint32_t at = (uint32_t)(v - v0);
+      if (v >= 0 && at < (uint32_t)n) write_one((int)at, a.bias_value[e]);
+    }
+    return;
+  }
+  // from the end of the list, as many entries at a time as there are threads: an entry
+  // counts if none behind it has claimed its token, here or before
+  for (int last = e1; last > e0; last -= kThreads) {
+    const int e = last - 1 - tid;              // (thread 0 has the last)
+    const int v = e >= e0 ? a.bias_token[e] : -1;
+    const uint32_t at = (uint32_t)(v - v0);
+    const bool in_slice = v >= 0 && at < (uint32_t)n;
+    s_list[tid] = in_slice ? (int)at : -1;
+    __syncthreads();
+    bool counts_here = in_slice && !(s_claimed[at >> 5] >> (at & 31) & 1u);
+    for (int k = 0; k < tid && counts_here; ++k) counts_here = s_list[k] != (int)at;
+    __syncthreads();
+    if (counts_here) {
+      atomicOr(&s_claimed[at >> 5], 1u << (at & 31));
+      write_one((int)at, a.bias_value[e]);
+    }
+  }
 }
 
 }  // namespace
 
 hipError_t launch_adjust_logits(AdjustArgs a, int cus, hipStream_t s) {
-  a.slice = 8192;
-  const int slices = (a.vocab + a.slice - 1) / a.slice;
-  const size_t lds = (size_t)a.slice * 4 * ((a.history ? 1 : 0) + (a.bias_offsets ? 1 : 0));
-  const dim3 grid(slices, a.rows), block(kThreads);
-  if (a.f32) hipLaunchKernelGGL(adjust_logits_kernel<true>, grid, block, lds, s, a);
-  else hipLaunchKernelGGL(adjust_logits_kernel<false>, grid, block, lds, s, a);
+  // a workgroup's logits: 16 KB, or less where that would leave compute units idle
+  const int most = a.f32 ? kMost / 2 : kMost;
+  a.slice = most;
+  while (a.slice > most / 8 && (long long)a.rows * ((a.vocab + a.slice - 1) / a.slice) < 2ll * cus)
+    a.slice /= 2;
+  const dim3 grid((a.vocab + a.slice - 1) / a.slice, a.rows), block(kThreads);
+  if (a.f32) hipLaunchKernelGGL(adjust_logits_kernel<true>, grid, block, 0, s, a);
+  else hipLaunchKernelGGL(adjust_logits_kernel<false>, grid, block, 0, s, a);
   return hipGetLastError();
 }
 

@@ -201,6 +201,16 @@ def test_in_place_and_rows_apart(dtype, vocab):
         assert bool((big == 77.0).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tokens_named_more_than_once_in_a_list(dtype):
+    # the last entry counts, however far apart they are; lists longer than a workgroup
+    c = Call(4, 5000, dtype, 14, biased=False)
+    token = np.concatenate([np.arange(5000), [3, 3, 9], c.rng.integers(0, 5000, 3000), [4999] * 300, [7]])
+    c.set(bias_token=token, bias_value=np.asarray(c.rng.uniform(-9, 5, len(token)), np.float32),
+          bias_offsets=np.array([0, 5000, 5003, len(token) - 1, len(token)]))
+    c.check()
+
+
 def test_results_do_not_depend_on_the_run():
     c = Call(8, 30000, "bf16", 12, longest=5000)
     first = K.adjust_logits(c.x, **c.kw)
