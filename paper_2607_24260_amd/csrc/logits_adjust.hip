@@ -19,7 +19,7 @@
 namespace kap {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr uint32_t kPrompt = 0x80000000u;
 
 template <bool F32> struct Elem { typedef float type; static constexpr int kPer = 4; };
@@ -35,7 +35,7 @@ template <> __device__ __forceinline__ uint16_t rounded<uint16_t>(float x) {
 }
 
 constexpr int kBytes = 16;                     // of a thread's load
-constexpr int kLoads = 4;                      // of a thread, at most
+constexpr int kLoads = 2;                      // of a thread, at most
 constexpr int kMost = kThreads * kLoads * kBytes / 2;   // tokens of a slice, at most
 
 // What a row asks for.
@@ -123,22 +123,38 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
     const int prompt = a.prompt_len ? a.prompt_len[row] : 0;
     const long long lo = start < 0 ? -start : 0;
     const long long hi = min((long long)len, a.history_size - start);
-    constexpr int kAtOnce = 8;
-    for (long long i0 = lo + tid; i0 < hi; i0 += kAtOnce * kThreads) {
-      int token[kAtOnce];
+    // 16 bytes of it at a time, from the 16-byte boundary at or before its first token on
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const int32_t *first = a.history + start;
+    const int before = (int)(reinterpret_cast<uintptr_t>(first + lo) / 4 & 3);
+    constexpr int kAtOnce = 4;
+    for (long long i0 = lo - before + 4 * tid; i0 < hi; i0 += 4 * kAtOnce * kThreads) {
+      i32x4 token[kAtOnce];
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
-        const long long i = i0 + k * kThreads;
-        token[k] = i < hi ? a.history[start + i] : -1;
-      }
+        const long long i = i0 + 4 * k * kThreads;
+        token[k] = i32x4{-1, -1, -1, -1};
+        // (not across the ends of the array, though within a 16-byte line)
+        if (start + i >= 0 && start + i + 4 <= a.history_size && i < hi) {
+          token[k] = *reinterpret_cast<const i32x4 *>(first + i);
+        } else {
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const uint32_t at = (uint32_t)(token[k] - v0);
-        if (token[k] >= 0 && at < (uint32_t)n) {
-          if (i0 + k * kThreads < prompt) atomicOr(&counts[at], kPrompt);
-          else atomicAdd(&counts[at], 1u);
+          for (int c = 0; c < 4; ++c)
+            if (i + c >= lo && i + c < hi) token[k][c] = first[i + c];
         }
       }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const long long i = i0 + 4 * k * kThreads + c;
+          const int v = token[k][c];
+          const uint32_t at = (uint32_t)(v - v0);
+          if (i >= lo && i < hi && v >= 0 && at < (uint32_t)n) {
+            if (i < prompt) atomicOr(&counts[at], kPrompt);
+            else atomicAdd(&counts[at], 1u);
+          }
+        }
     }
   }
   if (biased)
