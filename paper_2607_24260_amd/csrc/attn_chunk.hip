@@ -169,6 +169,9 @@ struct Item {
   int b, g, r0, r1;
   Range r;
   int j0, j1;
+  int own0, own1;    // of which these rows see something in [own0, own1) (tall: of the block's)
+  bool tall;
+  int last_rows;     // where the block's last wavefront with rows starts
   int64_t part;
 };
 
@@ -206,14 +209,20 @@ __device__ bool item_of(const ChunkArgs &a, int w, int wave, int lane, Item &it)
   const int slot = min(it.s.block, it.s.rows), skip = tall ? wave * kRows : 0;
   it.part = splits > 1 ? m.row0[it.b] + ((int64_t)(block * a.Hkv + it.g) * splits + split) * slot + skip
                        : -1;
-  it.r0 = block * it.s.block + skip;
+  it.tall = tall;
+  {
+    const int first = block * it.s.block, rows = min(it.s.block, it.s.rows - first);
+    it.last_rows = first + (rows - 1) / kRows * kRows;
+  }
+  it.r0 = min(block * it.s.block + skip, it.s.rows);
   it.r1 = min(it.r0 + kRows, it.s.rows);
-  if (it.r0 >= it.s.rows) return false;
-  if (tall) {                                  // what these rows see of the block's steps
+  it.own0 = it.j0;
+  it.own1 = it.j1;
+  if (tall && it.r0 < it.r1) {                 // what these rows see of the block's steps
     const Range own = range_of(a, it.s, it.r0, it.r1);
-    it.j1 = min(it.j1, it.r.sinks + own.steps - own.sinks + own.from - it.r.from);
-    if (a.sinks == 0) it.j0 = max(it.j0, own.from - it.r.from);
-    it.j1 = max(it.j1, it.j0);
+    it.own1 = min(it.j1, it.r.sinks + own.steps - own.sinks + own.from - it.r.from);
+    if (a.sinks == 0) it.own0 = max(it.j0, own.from - it.r.from);
+    it.own1 = max(it.own1, it.own0);
   }
   return true;
 }
@@ -328,14 +337,10 @@ struct Sight {
   int lo, hi, all_lo, all_hi, some_lo, some_hi;
 };
 
-// Moves the reference above a step's logits (c z: in powers of two, c >= 0). MASKED: what
+// Moves the reference above the lane's largest logit (in powers of two). MASKED: what
 // weighs nothing against it goes, infinities and NaN too.
 template <int D, bool MASKED>
-__device__ __forceinline__ void move_reference(State<D> &st, const f32x16 &z, float c) {
-  float top = max_f(z[0], z[1]);
-#pragma unroll
-  for (int i = 2; i < 16; ++i) top = max_f(top, z[i]);
-  top *= c;
+__device__ __forceinline__ void raise_reference(State<D> &st, float top) {
   if (__any(top > st.ref)) {
     top = max_f(top, other_half(top));
     const float ref = top > st.ref ? top + kDefer : st.ref;
@@ -348,6 +353,14 @@ __device__ __forceinline__ void move_reference(State<D> &st, const f32x16 &z, fl
       for (int i = 0; i < 16; ++i)
         st.o[db][i] = MASKED && f == 0.f ? 0.f : st.o[db][i] * f;
   }
+}
+// The same for a step's logits (c z: in powers of two, c >= 0).
+template <int D, bool MASKED>
+__device__ __forceinline__ void move_reference(State<D> &st, const f32x16 &z, float c) {
+  float top = max_f(z[0], z[1]);
+#pragma unroll
+  for (int i = 2; i < 16; ++i) top = max_f(top, z[i]);
+  raise_reference<D, MASKED>(st, top * c);
 }
 // Weights in the place of the logits.
 template <int D>
@@ -550,52 +563,54 @@ __device__ __forceinline__ void scales_of(const ChunkArgs &a, const int (&id)[2]
 // Whether steps that every row sees in full have a loop of their own, without masks.
 template <int KV, int D> constexpr bool has_plain() { return KV != kF32 || D < 256; }
 
-// All steps of a walk, operands from memory; those of [ja, jb) are seen by every row in
-// full and their pages are there; they come first: the next step's K is fetched as soon
-// as this one's has been multiplied, and so is V.
+// Steps [ja, jb) of a walk, which every row sees in full and whose pages are there,
+// operands from memory: the next step's K is fetched as soon as this one's has been
+// multiplied, and so is V.
 template <int KV, int D>
-__device__ __forceinline__ void walk_memory(State<D> &st, const ChunkArgs &a, const Walk &w,
-                                            const Queries<KV, D> &q, int g, PageIds ids,
-                                            const Sight &see, int ja, int jb) {
+__device__ __forceinline__ void walk_plain(State<D> &st, const ChunkArgs &a, const Walk &w,
+                                           const Queries<KV, D> &q, int g, PageIds ids,
+                                           const Sight &see, int ja, int jb) {
   const int lane = ids.lane;
-  if constexpr (has_plain<KV, D>()) {
-    if (ja < jb) {
-      const bool fine[2] = {true, true};
-      float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f}, ks1[2] = {1.f, 1.f}, vs1[2] = {1.f, 1.f};
-      Held<KV, D> r;
-      {
-        const Step x = ids.at(a, w, ja);
-        const Pages<KV, D> p(a, x.id, g, lane);
-        r.load_k(p);
-        r.load_v(p);
-        scales_of<KV>(a, x.id, ks, vs);
-      }
-      for (int j = ja;; ++j) {
-        const bool more = j + 1 < jb;
-        const Step x = ids.at(a, w, j + 1);
-        const Pages<KV, D> p(a, x.id, g, lane, more);
-        scales_of<KV>(a, x.id, ks1, vs1);
-        f32x16 z = logits<KV, D>(r, q);
-        __builtin_amdgcn_sched_barrier(0);
-        r.load_k(p);
-        __builtin_amdgcn_sched_barrier(0);
-        uint32_t seen;
-        const float c = scale_logits<KV, false>(a, z, seen, 0, fine, see, ks, lane);
-        move_reference<D, false>(st, z, c);
-        weigh(st, z, c);
-        add_values<KV, D, false>(st, r, z, seen, vs);
-        __builtin_amdgcn_sched_barrier(0);
-        r.load_v(p);
-        if (!more) break;
+  const bool fine[2] = {true, true};
+  float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f}, ks1[2] = {1.f, 1.f}, vs1[2] = {1.f, 1.f};
+  Held<KV, D> r;
+  {
+    const Step x = ids.at(a, w, ja);
+    const Pages<KV, D> p(a, x.id, g, lane);
+    r.load_k(p);
+    r.load_v(p);
+    scales_of<KV>(a, x.id, ks, vs);
+  }
+  for (int j = ja;; ++j) {
+    const bool more = j + 1 < jb;
+    const Step x = ids.at(a, w, j + 1);
+    const Pages<KV, D> p(a, x.id, g, lane, more);
+    scales_of<KV>(a, x.id, ks1, vs1);
+    f32x16 z = logits<KV, D>(r, q);
+    __builtin_amdgcn_sched_barrier(0);
+    r.load_k(p);
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t seen;
+    const float c = scale_logits<KV, false>(a, z, seen, 0, fine, see, ks, lane);
+    move_reference<D, false>(st, z, c);
+    weigh(st, z, c);
+    add_values<KV, D, false>(st, r, z, seen, vs);
+    __builtin_amdgcn_sched_barrier(0);
+    r.load_v(p);
+    if (!more) break;
 #pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-          ks[pg] = ks1[pg];
-          vs[pg] = vs1[pg];
-        }
-      }
+    for (int pg = 0; pg < 2; ++pg) {
+      ks[pg] = ks1[pg];
+      vs[pg] = vs1[pg];
     }
   }
-  // the others: those before, and those behind
+}
+
+// The other steps: those before ja, and those from jb on.
+template <int KV, int D>
+__device__ __forceinline__ void walk_masked(State<D> &st, const ChunkArgs &a, const Walk &w,
+                                            const Queries<KV, D> &q, int g, int lane,
+                                            const Sight &see, int ja, int jb) {
   Step x = step_at(a, w, w.j0 < ja ? w.j0 : jb);
   for (int j = w.j0 < ja ? w.j0 : jb; j < w.j1;) {
     const int next = j + 1 == ja ? jb : j + 1;
@@ -605,6 +620,286 @@ __device__ __forceinline__ void walk_memory(State<D> &st, const ChunkArgs &a, co
     take_step<KV, D, true>(st, a, q, Pages<KV, D>(a, x.id, g, lane), w.step(j), x.ok, see, ks, vs, lane);
     x = x1;
     j = next;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// a workgroup's share: its wavefronts' rows over the same steps
+// ---------------------------------------------------------------------------
+
+// The pages of two steps (a stage) are brought into LDS as operands, 1 KB each (16 bytes a
+// lane, as the lane reads them back; fp8 widened on the way). A wavefront's logits are a
+// stage ahead of its weights: while the vector unit weighs one stage's keys, the matrix
+// unit multiplies the next one's. So K is staged one ahead of V; there are two buffers of
+// either.
+// Steps of a stage (256 dims: two would not fit the registers).
+template <int D> constexpr int stage_steps() { return D == 256 ? 1 : 2; }
+template <int KV, int D> constexpr bool has_lds() { return !q_in_lds<KV, D>(); }
+// 16-byte words of a stage's K, and as many of its V.
+template <int KV, int D> constexpr int half_words() { return stage_steps<D>() * operands<KV, D>() * 64; }
+
+// A step's K or V operands in LDS, from the lane's first on.
+template <int KV, int D>
+struct StagedKeys {
+  const u32x4 *at;
+  __device__ u32x4 key(int c) const { return at[c * 64]; }
+};
+template <int KV, int D>
+struct StagedValues {
+  const u32x4 *at;
+  __device__ u32x4 value(int y, int db) const { return at[(y * (D / 32) + db) * 64]; }
+};
+
+// Operands that a wavefront brings in, on their way: every WAVES-th of a stage's K, and of
+// another's V.
+template <int KV, int D, int WAVES>
+struct Fetch {
+  static constexpr int kStage = stage_steps<D>(), kOps = operands<KV, D>(), kEach = kStage * kOps / WAVES;
+  static_assert(kOps == v_parts<KV>() * (D / 32) && kStage * kOps % WAVES == 0 &&
+                (kOps % WAVES == 0 || WAVES == kStage * kOps), "");
+  static constexpr size_t kTile = (size_t)kPage * D * elem_bytes(KV);
+  Operand<KV> k[kEach], v[kEach];
+  // the step of the wavefront's e-th operand
+  __device__ __forceinline__ static Step step_of(const Step (&st)[kStage], int e, int wave) {
+    if constexpr (WAVES <= kOps) return st[e * WAVES / kOps];
+    else return wave < kOps ? st[0] : st[kStage - 1];
+  }
+  __device__ __forceinline__ void issue_k(const ChunkArgs &a, const Step (&st)[kStage], int g, int wave,
+                                          int lane) {
+    const int i = lane & 31, hb = lane >> 5, tok = key_of_row<KV>(i) & 15;
+    const int at = tok * 8 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 128 * elem_bytes(KV));
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int op = e * WAVES + wave, o = op % kOps;
+      const Step p = step_of(st, e, wave);
+      const char *const base =
+          static_cast<const char *>(a.k_pages) + o * (KV == kF32 ? 512 : 256 * elem_bytes(KV));
+      const char *const p0 = base + ((size_t)p.id[0] * a.Hkv + g) * kTile;
+      const char *const p1 = base + ((size_t)p.id[1] * a.Hkv + g) * kTile;
+      k[e] = *reinterpret_cast<const Operand<KV> *>((i < 16 ? p0 : p1) + at);
+    }
+  }
+  __device__ __forceinline__ void issue_v(const ChunkArgs &a, const Step (&st)[kStage], int g, int wave,
+                                          int lane) {
+    const int i = lane & 31, hb = lane >> 5;
+    const int at = i * 16 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 8 * elem_bytes(KV));
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int op = e * WAVES + wave, o = op % kOps, y = o / (D / 32), db = o % (D / 32);
+      const Step p = step_of(st, e, wave);
+      const int page = __builtin_amdgcn_readfirstlane((KV == kF32 ? y >> 1 : y) ? p.id[1] : p.id[0]);
+      const char *const base = static_cast<const char *>(a.v_pages) +
+                               ((size_t)page * a.Hkv + g) * kTile + db * 512 * elem_bytes(KV) +
+                               (KV == kF32 ? (y & 1) * 32 : 0);
+      v[e] = *reinterpret_cast<const Operand<KV> *>(base + at);
+    }
+  }
+  __device__ __forceinline__ void write_k(u32x4 *to, int wave, int lane) const {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) to[(e * WAVES + wave) * 64 + lane] = wide(k[e]);
+  }
+  __device__ __forceinline__ void write_v(u32x4 *to, int wave, int lane) const {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) to[(e * WAVES + wave) * 64 + lane] = wide(v[e]);
+  }
+};
+
+// A stage's logits as the products gave them.
+template <int D> struct Stage {
+  f32x16 z[stage_steps<D>()];
+  float top[stage_steps<D>()][2];              // the lane's largest of a page's keys
+};
+template <int D>
+__device__ __forceinline__ void find_tops(Stage<D> &p) {
+#pragma unroll
+  for (int s = 0; s < stage_steps<D>(); ++s)
+#pragma unroll
+    for (int pg = 0; pg < 2; ++pg) {
+      float t = p.z[s][8 * pg];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) t = max_f(t, p.z[s][8 * pg + i]);
+      p.top[s][pg] = t;
+    }
+}
+template <int KV, int D>
+__device__ __forceinline__ void multiply_keys(Stage<D> &p, const u32x4 *k, const Queries<KV, D> &q) {
+#pragma unroll
+  for (int s = 0; s < stage_steps<D>(); ++s)
+    p.z[s] = logits<KV, D>(StagedKeys<KV, D>{k + s * operands<KV, D>() * 64}, q);
+  find_tops(p);
+}
+
+// The stage whose logits are in p, and whose V is at v; K of the next one is at k.
+template <int KV, int D>
+__device__ __forceinline__ void take_stage(State<D> &st, const ChunkArgs &a, Stage<D> &p, Stage<D> &next,
+                                           const Queries<KV, D> &q, const u32x4 *k, const u32x4 *v,
+                                           const float (&ks)[stage_steps<D>()][2],
+                                           const float (&vs)[stage_steps<D>()][2]) {
+  constexpr int kStage = stage_steps<D>();
+  float c[kStage][2];                          // factors to powers of two, >= 0
+#pragma unroll
+  for (int s = 0; s < kStage; ++s)
+#pragma unroll
+    for (int pg = 0; pg < 2; ++pg) {
+      c[s][pg] = KV == kFP8 ? a.scale_log2 * ks[s][pg] : a.scale_log2;
+      if constexpr (KV == kFP8) {
+        if (c[s][pg] < 0.f) {                  // (a negative scale of a page)
+          c[s][pg] = -c[s][pg];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p.z[s][8 * pg + i] = -p.z[s][8 * pg + i];
+          float t = p.z[s][8 * pg];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) t = max_f(t, p.z[s][8 * pg + i]);
+          p.top[s][pg] = t;
+        }
+      }
+    }
+  float top = -INFINITY;
+#pragma unroll
+  for (int s = 0; s < kStage; ++s) {
+    if constexpr (KV == kFP8) top = max_f(top, max_f(p.top[s][0] * c[s][0], p.top[s][1] * c[s][1]));
+    else top = max_f(top, max_f(p.top[s][0], p.top[s][1]));
+  }
+  raise_reference<D, false>(st, KV == kFP8 ? top : top * a.scale_log2);
+  // One block of instructions: the products of the next stage's keys, this one's weights and
+  // its products with V, operands read from LDS a group ahead of their use. The order is
+  // laid out at the end.
+  constexpr int kOps = operands<KV, D>(), kDims = D / 32;
+#pragma unroll
+  for (int s = 0; s < kStage; ++s) {
+    next.z[s] = zero16();
+#pragma unroll
+    for (int o = 0; o < kOps; ++o) {
+      const u32x4 x = k[(s * kOps + o) * 64], y = q.at(o);
+      if constexpr (KV == kF32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) next.z[s] = mfma(__uint_as_float(x[e]), __uint_as_float(y[e]), next.z[s]);
+      } else {
+        next.z[s] = mfma(x, y, next.z[s]);
+      }
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < kStage; ++s) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p.z[s][i] = exp2_fast(fmaf(p.z[s][i], c[s][i >> 3], -st.ref));
+      st.sum += p.z[s][i];
+    }
+#pragma unroll
+    for (int y = 0; y < v_parts<KV>(); ++y) {
+      u32x4 w;
+      if constexpr (KV != kF32)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float lo = p.z[s][8 * y + 2 * i], hi = p.z[s][8 * y + 2 * i + 1];
+          if constexpr (KV == kFP8) {
+            lo *= vs[s][y];
+            hi *= vs[s][y];
+          }
+          w[i] = round_bf16x2(lo, hi);
+        }
+#pragma unroll
+      for (int db = 0; db < kDims; ++db) {
+        const u32x4 x = v[((s * v_parts<KV>() + y) * kDims + db) * 64];
+        if constexpr (KV == kF32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            st.o[db] = mfma(__uint_as_float(x[e]), p.z[s][4 * y + e], st.o[db]);
+        } else {
+          st.o[db] = mfma(x, w, st.o[db]);
+        }
+      }
+    }
+  }
+  find_tops(next);
+  {
+    constexpr int kGroup = 4, kGroups = 2 * kStage * kOps / kGroup, kPer = KV == kF32 ? 4 : 1;
+    constexpr int kVector = KV == kF32 ? 1 : (KV == kFP8 ? 10 : 8) * kStage * 8 / (kGroups * kGroup);
+    __builtin_amdgcn_sched_group_barrier(0x100, kGroup, 0);
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x) {
+      if (x + 1 < kGroups) __builtin_amdgcn_sched_group_barrier(0x100, kGroup, 0);
+#pragma unroll
+      for (int y = 0; y < kGroup * kPer; ++y) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, kVector, 0);
+      }
+    }
+  }
+}
+
+// The stages of a workgroup's block from step w.j0 on that start below `end`, whose pages
+// are all in the pool. A wavefront takes those that its rows see in full: [ja, jb), whole
+// stages from w.j0 on.
+template <int KV, int D, int WAVES>
+__device__ __forceinline__ void walk_staged(State<D> &st, const ChunkArgs &a, const Walk &w,
+                                            const Queries<KV, D> &q, int g, PageIds ids, int end,
+                                            int ja, int jb, u32x4 *lds, int wave) {
+  constexpr int kHalf = half_words<KV, D>(), kStage = stage_steps<D>();
+  if (end <= w.j0) return;
+  const int lane = ids.lane;
+  u32x4 *const keys = lds, *const values = lds + 2 * kHalf;
+  Fetch<KV, D, WAVES> f;
+  // the pages of a stage and of the next, and the scales of the first
+  Step cur[kStage], next[kStage];
+  float ks[kStage][2], vs[kStage][2];
+  auto pages = [&](Step (&x)[kStage], int j) {
+#pragma unroll
+    for (int s = 0; s < kStage; ++s) x[s] = ids.at(a, w, j + s);
+  };
+  float ks1[kStage][2], vs1[kStage][2];
+  auto scales = [&] {
+#pragma unroll
+    for (int s = 0; s < kStage; ++s) {
+      ks1[s][0] = ks1[s][1] = vs1[s][0] = vs1[s][1] = 1.f;
+      scales_of<KV>(a, cur[s].id, ks1[s], vs1[s]);
+    }
+  };
+  auto turn_scales = [&] {
+#pragma unroll
+    for (int s = 0; s < kStage; ++s)
+#pragma unroll
+      for (int pg = 0; pg < 2; ++pg) {
+        ks[s][pg] = ks1[s][pg];
+        vs[s][pg] = vs1[s][pg];
+      }
+  };
+  pages(cur, w.j0);
+  pages(next, w.j0 + kStage);
+  f.issue_k(a, cur, g, wave, lane);
+  f.issue_v(a, cur, g, wave, lane);
+  f.write_k(keys, wave, lane);
+  f.issue_k(a, next, g, wave, lane);
+  f.write_v(values, wave, lane);
+  f.write_k(keys + kHalf, wave, lane);
+  scales();
+  turn_scales();
+  __syncthreads();
+  Stage<D> p0, p1;
+  if (ja == w.j0 && ja < jb) multiply_keys<KV, D>(p0, keys + lane, q);
+  __syncthreads();
+  // In LDS: this stage's V, the next one's K; on their way: the next one's V, and K of the
+  // one after it (behind the last: some page's, not used).
+  auto one = [&](int j, int slot, Stage<D> &p, Stage<D> &after) {
+    f.issue_v(a, next, g, wave, lane);
+#pragma unroll
+    for (int s = 0; s < kStage; ++s) cur[s] = next[s];
+    scales();
+    pages(next, j + 2 * kStage);
+    f.issue_k(a, next, g, wave, lane);
+    const u32x4 *const k = keys + (slot ^ 1) * kHalf + lane;
+    if (j >= ja && j < jb) take_stage<KV, D>(st, a, p, after, q, k, values + slot * kHalf + lane, ks, vs);
+    else if (j + kStage == ja && ja < jb) multiply_keys<KV, D>(after, k, q);
+    turn_scales();
+    f.write_k(keys + slot * kHalf, wave, lane);
+    f.write_v(values + (slot ^ 1) * kHalf, wave, lane);
+    __syncthreads();
+  };
+  for (int j = w.j0; j < end; j += 2 * kStage) {
+    one(j, 0, p0, p1);
+    if (j + kStage >= end) break;
+    one(j + kStage, 1, p1, p0);
   }
 }
 
@@ -638,11 +933,12 @@ __global__ __launch_bounds__(64 * waves_of(KV, D))
 __attribute__((amdgpu_waves_per_eu(waves_of(KV, D) / 4)))
 void attn_chunk_kernel(ChunkArgs a) {
   constexpr int kWaves = waves_of(KV, D);
-  __shared__ __align__(16) u32x4 s_q[q_in_lds<KV, D>() ? kWaves * operands<KV, D>() * 64 : 1];
+  __shared__ __align__(16) u32x4 s_mem[q_in_lds<KV, D>() ? kWaves * operands<KV, D>() * 64
+                                                         : 4 * half_words<KV, D>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hb = lane >> 5;
   Item it;
-  if (!item_of<kWaves>(a, (int)flat_block(), wave, lane, it)) return;
+  if (!item_of<kWaves>(a, (int)flat_block(), wave, lane, it)) return;   // (tall: all wavefronts)
 
   Walk w;
   w.table = a.table + (size_t)it.b * a.stride;
@@ -656,7 +952,7 @@ void attn_chunk_kernel(ChunkArgs a) {
   const int r = it.r0 + (lane & 31);
   const bool live = r < it.r1;
   int token;
-  const int64_t row = row_at(a, it.s, it.g, live ? r : it.r0, token);
+  const int64_t row = row_at(a, it.s, it.g, live ? r : min(it.r0, it.s.rows - 1), token);
   Sight see;
   see.hi = live ? max(0, it.s.len - it.s.n + token + 1) : 0;
   see.lo = a.window > 0 ? max(0, see.hi - a.window) : 0;
@@ -664,7 +960,7 @@ void attn_chunk_kernel(ChunkArgs a) {
   {
     constexpr int kBytes = KV == kF32 ? 4 : 2;
     const char *p = static_cast<const char *>(a.q) + row * D * kBytes + hb * 16;
-    u32x4 *lds = s_q + (q_in_lds<KV, D>() ? wave * operands<KV, D>() * 64 + lane : 0);
+    u32x4 *lds = s_mem + (q_in_lds<KV, D>() ? wave * operands<KV, D>() * 64 + lane : 0);
     q.lds = lds;
 #pragma unroll
     for (int c = 0; c < operands<KV, D>(); ++c) {
@@ -696,31 +992,55 @@ void attn_chunk_kernel(ChunkArgs a) {
   see.some_lo = __builtin_amdgcn_readfirstlane(see.some_lo);
 
   State<D> st;
+  auto clear = [&] {
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
-  st.ref = kNoMax;
-  st.sum = 0.f;
-  if (see.some_hi > 0 && w.j0 < w.j1) {
+    for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
+    st.ref = kNoMax;
+    st.sum = 0.f;
+  };
+  clear();
+  if (w.j0 < w.j1) {
     PageIds ids(w, lane);
-    // steps that every row sees in full, if all their pages are in the pool
-    int ja = max(w.j0, (see.all_lo + kKeys - 1) / kKeys - w.shift);
-    int jb = max(ja, min(w.j1, see.all_hi / kKeys - w.shift));
+    // whether all pages are in the pool
+    bool fine = true;
+    for (int k = 0; w.j0 + k < w.j1; k += 32) {
+      const int id = k == 0 ? ids.cur : (k == 32 ? ids.next : PageIds::fetch(w, k, lane));
+      const int j = w.j0 + k + (lane >> 1);
+      fine &= j >= w.j1 || 2 * w.step(j) + (lane & 1) >= w.pages || in_pool(a, id);
+    }
+    fine = !__any(!fine);
+    // steps that every row sees in full
+    int ja = max(it.own0, (see.all_lo + kKeys - 1) / kKeys - w.shift);
+    int jb = max(ja, min(it.own1, see.all_hi / kKeys - w.shift));
     if (ja < w.sinks) ja = min(jb, w.sinks);
-    {
-      bool fine = true;
-      for (int k = 0; w.j0 + k < jb; k += 32) {
-        const int id = k == 0 ? ids.cur : (k == 32 ? ids.next : PageIds::fetch(w, k, lane));
-        const int j = w.j0 + k + (lane >> 1);
-        fine &= j < ja || j >= jb || in_pool(a, id);
+    if (see.some_hi == 0) it.own1 = it.own0;   // (no row sees anything)
+    if (!fine || !has_plain<KV, D>() || it.own0 >= it.own1) ja = jb = it.own0;
+    bool staged = false;
+    if constexpr (has_lds<KV, D>()) {
+      if (it.tall && fine) {
+        // whole stages; those that start beyond what the block's last 32 rows all see are
+        // nobody's
+        constexpr int kStage = stage_steps<D>();
+        ja = w.j0 + (ja - w.j0 + kStage - 1) / kStage * kStage;
+        jb = max(ja, w.j0 + (jb - w.j0) / kStage * kStage);
+        const int last = div_small(it.last_rows, a.G);
+        const int end = min(w.j1, max(0, it.s.len - it.s.n + last + 1) / kKeys - w.shift);
+        walk_staged<KV, D, kWaves>(st, a, w, q, it.g, ids, end, ja, jb, s_mem, wave);
+        staged = true;
+        if (ja >= jb) ja = jb = it.own0;
       }
-      if (!has_plain<KV, D>() || __any(!fine)) ja = jb = w.j0;
     }
     // A product gives 0 * inf = NaN where a weight is zero. Rather than test V on the way, a
     // wavefront whose result is not finite walks its steps again with masks, which keep
     // infinities and NaN of V out of the products. (Not for rows that see nothing, nor for
     // those that a NaN logit has made NaN.)
+    w.j0 = it.own0;
+    w.j1 = it.own1;
     for (;;) {
-      walk_memory<KV, D>(st, a, w, q, it.g, ids, see, ja, jb);
+      if (has_plain<KV, D>() && !staged && ja < jb)
+        walk_plain<KV, D>(st, a, w, q, it.g, PageIds(w, opaque(lane)), see, ja, jb);
+      if (w.j0 < w.j1) walk_masked<KV, D>(st, a, w, q, it.g, opaque(lane), see, ja, jb);
+      staged = false;
       st.sum += other_half(st.sum);
       if (ja >= jb) break;
       float top = 0.f;
@@ -730,11 +1050,7 @@ void attn_chunk_kernel(ChunkArgs a) {
         for (int i = 0; i < 16; ++i) top = max_f(top, __builtin_fabsf(st.o[db][i]));
       if (!__any(!(top < INFINITY) && see.hi > 0 && st.sum == st.sum)) break;
       ja = jb = w.j0;
-      ids = PageIds(w, opaque(lane));
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
-      st.ref = kNoMax;
-      st.sum = 0.f;
+      clear();
     }
   }
   if (see.hi == 0) st.sum = 0.f;
