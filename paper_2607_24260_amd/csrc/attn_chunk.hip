@@ -660,37 +660,39 @@ struct Fetch {
   static constexpr size_t kTile = (size_t)kPage * D * elem_bytes(KV);
   Operand<KV> k[kEach], v[kEach];
   // the step of the wavefront's e-th operand
-  __device__ __forceinline__ static Step step_of(const Step (&st)[kStage], int e, int wave) {
-    if constexpr (WAVES <= kOps) return st[e * WAVES / kOps];
-    else return wave < kOps ? st[0] : st[kStage - 1];
+  __device__ __forceinline__ static int step_of(int e, int wave) {
+    if constexpr (WAVES <= kOps) return e * WAVES / kOps;
+    else return wave < kOps ? 0 : kStage - 1;
   }
-  __device__ __forceinline__ void issue_k(const ChunkArgs &a, const Step (&st)[kStage], int g, int wave,
-                                          int lane) {
+  // ids: the page of step s of the stage, first or second, in lane 4 s + 2 pg
+  __device__ __forceinline__ static const char *tile(const ChunkArgs &a, const void *pages, int ids, int s,
+                                                     int pg, int g) {
+    const int id = __builtin_amdgcn_readlane(ids, 4 * s + 2 * pg);
+    return static_cast<const char *>(pages) + ((size_t)id * a.Hkv + g) * kTile;
+  }
+  __device__ __forceinline__ void issue_k(const ChunkArgs &a, int ids, int g, int wave, int lane) {
     const int i = lane & 31, hb = lane >> 5, tok = key_of_row<KV>(i) & 15;
     const int at = tok * 8 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 128 * elem_bytes(KV));
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const int op = e * WAVES + wave, o = op % kOps;
-      const Step p = step_of(st, e, wave);
-      const char *const base =
-          static_cast<const char *>(a.k_pages) + o * (KV == kF32 ? 512 : 256 * elem_bytes(KV));
-      const char *const p0 = base + ((size_t)p.id[0] * a.Hkv + g) * kTile;
-      const char *const p1 = base + ((size_t)p.id[1] * a.Hkv + g) * kTile;
-      k[e] = *reinterpret_cast<const Operand<KV> *>((i < 16 ? p0 : p1) + at);
+      const int s = step_of(e, wave), o = (e * WAVES + wave) % kOps;
+      uint64_t p0 = reinterpret_cast<uint64_t>(tile(a, a.k_pages, ids, s, 0, g));
+      uint64_t p1 = reinterpret_cast<uint64_t>(tile(a, a.k_pages, ids, s, 1, g));
+      asm("" : "+s"(p0), "+s"(p1));            // (or the products are the vector unit's, lane by lane)
+      // (an address of global memory: a generic one would be waited for with LDS)
+      typedef const __attribute__((address_space(1))) decltype(k[e].x) *from;
+      k[e].x = *reinterpret_cast<from>((i < 16 ? p0 : p1) + at +
+                                       o * (KV == kF32 ? 512 : 256 * elem_bytes(KV)));
     }
   }
-  __device__ __forceinline__ void issue_v(const ChunkArgs &a, const Step (&st)[kStage], int g, int wave,
-                                          int lane) {
+  __device__ __forceinline__ void issue_v(const ChunkArgs &a, int ids, int g, int wave, int lane) {
     const int i = lane & 31, hb = lane >> 5;
     const int at = i * 16 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 8 * elem_bytes(KV));
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const int op = e * WAVES + wave, o = op % kOps, y = o / (D / 32), db = o % (D / 32);
-      const Step p = step_of(st, e, wave);
-      const int page = __builtin_amdgcn_readfirstlane((KV == kF32 ? y >> 1 : y) ? p.id[1] : p.id[0]);
-      const char *const base = static_cast<const char *>(a.v_pages) +
-                               ((size_t)page * a.Hkv + g) * kTile + db * 512 * elem_bytes(KV) +
-                               (KV == kF32 ? (y & 1) * 32 : 0);
+      const int o = (e * WAVES + wave) % kOps, y = o / (D / 32), db = o % (D / 32);
+      const char *const base = tile(a, a.v_pages, ids, step_of(e, wave), KV == kF32 ? y >> 1 : y, g) +
+                               db * 512 * elem_bytes(KV) + (KV == kF32 ? (y & 1) * 32 : 0);
       v[e] = *reinterpret_cast<const Operand<KV> *>(base + at);
     }
   }
@@ -832,68 +834,61 @@ __device__ __forceinline__ void take_stage(State<D> &st, const ChunkArgs &a, Sta
 // The stages of a workgroup's block from step w.j0 on that start below `end`, whose pages
 // are all in the pool. A wavefront takes those that its rows see in full: [ja, jb), whole
 // stages from w.j0 on.
+//   Page ids and fp8 scales come through vector loads, a stage before they are needed and
+// with the data that is waited for anyway: scalar loads would return in any order, among
+// the reads of LDS, and a load under a condition would have every stage wait for all.
 template <int KV, int D, int WAVES>
 __device__ __forceinline__ void walk_staged(State<D> &st, const ChunkArgs &a, const Walk &w,
-                                            const Queries<KV, D> &q, int g, PageIds ids, int end,
-                                            int ja, int jb, u32x4 *lds, int wave) {
+                                            const Queries<KV, D> &q, int g, int lane, int end, int ja,
+                                            int jb, u32x4 *lds, int wave) {
   constexpr int kHalf = half_words<KV, D>(), kStage = stage_steps<D>();
   if (end <= w.j0) return;
-  const int lane = ids.lane;
   u32x4 *const keys = lds, *const values = lds + 2 * kHalf;
   Fetch<KV, D, WAVES> f;
-  // the pages of a stage and of the next, and the scales of the first
-  Step cur[kStage], next[kStage];
-  float ks[kStage][2], vs[kStage][2];
-  auto pages = [&](Step (&x)[kStage], int j) {
-#pragma unroll
-    for (int s = 0; s < kStage; ++s) x[s] = ids.at(a, w, j + s);
+  // (behind the last step and page: the last's)
+  auto pages = [&](int j) {
+    const int e = 2 * w.step(min(j + (lane >> 2 & (kStage - 1)), w.j1 - 1)) + (lane >> 1 & 1);
+    return w.table[min(e, w.pages - 1)];
   };
-  float ks1[kStage][2], vs1[kStage][2];
-  auto scales = [&] {
-#pragma unroll
-    for (int s = 0; s < kStage; ++s) {
-      ks1[s][0] = ks1[s][1] = vs1[s][0] = vs1[s][1] = 1.f;
-      scales_of<KV>(a, cur[s].id, ks1[s], vs1[s]);
-    }
-  };
-  auto turn_scales = [&] {
-#pragma unroll
-    for (int s = 0; s < kStage; ++s)
-#pragma unroll
-      for (int pg = 0; pg < 2; ++pg) {
-        ks[s][pg] = ks1[s][pg];
-        vs[s][pg] = vs1[s][pg];
-      }
-  };
-  pages(cur, w.j0);
-  pages(next, w.j0 + kStage);
-  f.issue_k(a, cur, g, wave, lane);
-  f.issue_v(a, cur, g, wave, lane);
+  auto scales = [&](int ids) { return KV == kFP8 ? a.kv_scales[2 * (size_t)ids + (lane & 1)] : 1.f; };
+  int ids = pages(w.j0), ids1 = pages(w.j0 + kStage), ids2 = pages(w.j0 + 2 * kStage);
+  float sc = scales(ids), sc1 = 1.f;           // this stage's, the next one's
+  f.issue_k(a, ids, g, wave, lane);
+  f.issue_v(a, ids, g, wave, lane);
   f.write_k(keys, wave, lane);
-  f.issue_k(a, next, g, wave, lane);
+  f.issue_k(a, ids1, g, wave, lane);
   f.write_v(values, wave, lane);
   f.write_k(keys + kHalf, wave, lane);
-  scales();
-  turn_scales();
   __syncthreads();
   Stage<D> p0, p1;
   if (ja == w.j0 && ja < jb) multiply_keys<KV, D>(p0, keys + lane, q);
   __syncthreads();
   // In LDS: this stage's V, the next one's K; on their way: the next one's V, and K of the
-  // one after it (behind the last: some page's, not used).
+  // one after it.
   auto one = [&](int j, int slot, Stage<D> &p, Stage<D> &after) {
-    f.issue_v(a, next, g, wave, lane);
-#pragma unroll
-    for (int s = 0; s < kStage; ++s) cur[s] = next[s];
-    scales();
-    pages(next, j + 2 * kStage);
-    f.issue_k(a, next, g, wave, lane);
+    sc1 = scales(ids1);
+    const int ids3 = pages(j + 3 * kStage);
+    f.issue_v(a, ids1, g, wave, lane);
+    f.issue_k(a, ids2, g, wave, lane);
     const u32x4 *const k = keys + (slot ^ 1) * kHalf + lane;
-    if (j >= ja && j < jb) take_stage<KV, D>(st, a, p, after, q, k, values + slot * kHalf + lane, ks, vs);
-    else if (j + kStage == ja && ja < jb) multiply_keys<KV, D>(after, k, q);
-    turn_scales();
+    if (j >= ja && j < jb) {
+      float ks[kStage][2], vs[kStage][2];
+#pragma unroll
+      for (int s = 0; s < kStage; ++s)
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+          ks[s][pg] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc), 4 * s + 2 * pg));
+          vs[s][pg] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc), 4 * s + 2 * pg + 1));
+        }
+      take_stage<KV, D>(st, a, p, after, q, k, values + slot * kHalf + lane, ks, vs);
+    } else if (j + kStage == ja && ja < jb) {
+      multiply_keys<KV, D>(after, k, q);
+    }
     f.write_k(keys + slot * kHalf, wave, lane);
     f.write_v(values + (slot ^ 1) * kHalf, wave, lane);
+    ids1 = ids2;
+    ids2 = ids3;
+    sc = sc1;
     __syncthreads();
   };
   for (int j = w.j0; j < end; j += 2 * kStage) {
@@ -1025,7 +1020,7 @@ void attn_chunk_kernel(ChunkArgs a) {
         jb = max(ja, w.j0 + (jb - w.j0) / kStage * kStage);
         const int last = div_small(it.last_rows, a.G);
         const int end = min(w.j1, max(0, it.s.len - it.s.n + last + 1) / kKeys - w.shift);
-        walk_staged<KV, D, kWaves>(st, a, w, q, it.g, ids, end, ja, jb, s_mem, wave);
+        walk_staged<KV, D, kWaves>(st, a, w, q, it.g, opaque(lane), end, ja, jb, s_mem, wave);
         staged = true;
         if (ja >= jb) ja = jb = it.own0;
       }
