@@ -422,8 +422,11 @@ size_t kap_verify_shared_workspace_bytes(const kap_kv_cache *kv, int32_t batch, 
  *   >= 0, not read without a window.
  * Softmax weights meet V of bf16 and fp8 pages rounded to bf16 (each off by at most
  * 2^-8 of it, as out is); logits, sums and lse are single precision throughout. batch <= 65535,
- * num_tokens * num_q_heads < 2^30. The workspace holds scratch only (its contents do
- * not matter).
+ * num_tokens * num_q_heads < 2^30.
+ *   The workspace keeps arrival counters in its first 64 bytes times the device's
+ * compute units: zero when a call starts, and left zero by it; the rest is scratch. So
+ * zero-fill it once when allocating it; it then serves any sequence of calls of this
+ * kind that fit it, one after the other (other entry points have theirs).
  */
 kap_status kap_chunk_attention(const kap_kv_cache *kv, int32_t batch, int32_t num_tokens,
                                const void *q, const int32_t *q_offsets, const int32_t *seq_lens,

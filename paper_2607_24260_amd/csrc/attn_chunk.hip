@@ -21,24 +21,35 @@ constexpr int waves_of(int kv, int D) { return chunk_waves(kv, D); }
 // work map
 // ---------------------------------------------------------------------------
 
+// How the rows of a sequence are taken:
+//   tall: in blocks of 32 rows a wavefront, a workgroup's wavefronts over the same steps;
+//   team: in blocks of 32, a workgroup's wavefronts sharing the steps;
+//   solo: in blocks of 32, a wavefront by itself.
+// The steps of tall and team blocks may be split over several workgroups (parts), the last
+// of which merges what they leave.
+enum Kind { kTall, kTeam, kSolo };
+
 // A sequence's part in a call.
 struct Seq {
   int q0, n, len;    // first row of q, new tokens, length
   int rows;          // n * G
-  bool tall;         // more rows than a few wavefronts': workgroups take them
-  int block, blocks; // rows of a block, blocks
 };
-
-__device__ __forceinline__ Seq seq_of(const ChunkArgs &a, int b, int tall_rows) {
+__device__ __forceinline__ Seq seq_of(const ChunkArgs &a, int b) {
   Seq s;
   s.q0 = clamp_to(a.q_offsets[b], 0, a.num_tokens);
   s.n = clamp_to(a.q_offsets[b + 1], s.q0, a.num_tokens) - s.q0;
   s.len = clamp_to(a.seq_lens[b], 0, a.max_len);
   s.rows = s.n * a.G;
-  s.tall = s.rows > a.few_rows;
-  s.block = s.tall ? tall_rows : kRows;
-  s.blocks = div_small(s.rows + s.block - 1, s.block);
   return s;
+}
+
+// r / G for 0 <= r < 2^31, given 1 / G to double precision: within one, then mended.
+__device__ __forceinline__ int token_of(const ChunkArgs &a, int r) {
+  int q = (int)((double)r * a.rcp_g);
+  const int rest = r - q * a.G;
+  q += rest >= a.G ? 1 : 0;
+  q -= rest < 0 ? 1 : 0;
+  return q;
 }
 
 // Steps that rows [r0, r1) of a sequence walk: the first `sinks` of them, then those
@@ -47,7 +58,7 @@ struct Range {
   int sinks, from, steps;
 };
 __device__ __forceinline__ Range range_of(const ChunkArgs &a, const Seq &s, int r0, int r1) {
-  const int p0 = s.len - s.n + div_small(r0, a.G), p1 = s.len - s.n + div_small(r1 - 1, a.G);
+  const int p0 = s.len - s.n + token_of(a, r0), p1 = s.len - s.n + token_of(a, r1 - 1);
   Range r;
   const int hi = max(0, p1 + 1);
   const int lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
@@ -56,98 +67,189 @@ __device__ __forceinline__ Range range_of(const ChunkArgs &a, const Seq &s, int 
   r.steps = r.sinks + (hi + kKeys - 1) / kKeys - r.from;
   return r;
 }
-__device__ __forceinline__ Range block_range(const ChunkArgs &a, const Seq &s, int block) {
-  return range_of(a, s, block * s.block, min((block + 1) * s.block, s.rows));
+__device__ __forceinline__ Range block_range(const ChunkArgs &a, const Seq &s, int size, int block) {
+  return range_of(a, s, block * size, min((block + 1) * size, s.rows));
 }
 
-// The map: what a part of a tall sequence's block, and of another's, walks at most;
-// their number; blocks to merge. Then, per sequence, sums before it: of tall parts, of
-// others, of blocks to merge; its splits and the first row of its partials.
-enum MapHead { kMapTall, kMapFew, kMapMerge, kMapHead = 4 };
+// What the cut goes by: a sequence's blocks, and the steps of one, on average and at most,
+// in blocks of 32 rows and in tall ones.
+struct Steps {
+  int blocks;
+  float mean, most;
+};
+struct Info {
+  int n, rows;
+  Steps by32, tall;
+};
+__device__ __forceinline__ Steps steps_of(const ChunkArgs &a, const Seq &s, int size) {
+  Steps f{(s.rows + size - 1) / size, 0.f, 0.f};
+  if (f.blocks > 0) {
+    const float x = (float)block_range(a, s, size, 0).steps;
+    const float y = (float)block_range(a, s, size, f.blocks - 1).steps;
+    f.mean = 0.5f * (x + y);
+    f.most = fmaxf(x, y);
+  }
+  return f;
+}
+template <int WAVES>
+__device__ __forceinline__ Info info_of(const ChunkArgs &a, const Seq &s) {
+  return Info{s.n, s.rows, steps_of(a, s, kRows), steps_of(a, s, kRows * WAVES)};
+}
+
+template <class T> __device__ __forceinline__ T pick(bool c, T x, T y) { return c ? x : y; }
+
+// The cut: whether every sequence goes to teams, or short ones to wavefronts by themselves,
+// and the steps of a tall part and of a team's.
+struct Cut {
+  bool small, solo;
+  float tall_len, team_len;
+  __device__ __forceinline__ Kind kind(const ChunkArgs &a, const Info &f) const {
+    if (!small && f.rows > a.few_rows) return kTall;
+    return solo && f.by32.most <= 8.f ? kSolo : kTeam;
+  }
+  __device__ __forceinline__ int splits(Kind k, const Info &f) const {
+    if (k == kSolo) return 1;
+    const float most = pick(k == kTall, f.tall.most, f.by32.most);
+    const float l = pick(k == kTall, tall_len, team_len);
+    return l >= most ? 1 : (int)ceilf(most / l);
+  }
+};
+
+// Workgroups are as long as each other, as near as the costs of steps say: as many as fit
+// the device at once (target), or, where there are more blocks than that, as the next
+// multiple of it. sum(f): that of f(Info) of all sequences, in single precision: every
+// wavefront that computes it finds the same. Small calls go to teams throughout: a tall
+// block's rows would leave most of the device idle.
+template <int WAVES, class Sum>
+__device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum) {
+  const float Hkv = (float)a.Hkv, target = (float)a.target;
+  Cut c;
+  const double tokens = sum([](const Info &f) { return (double)f.n; });
+  const float blocks = sum([](const Info &f) { return (float)f.by32.blocks; }) * Hkv;
+  const float steps = sum([](const Info &f) { return (float)f.by32.blocks * f.by32.mean; }) * Hkv;
+  const float few =
+      sum([&](const Info &f) { return f.rows <= a.few_rows ? (float)f.by32.blocks : 0.f; }) * Hkv;
+  c.small = blocks <= 2.f * target && steps <= 8.f * target * WAVES;
+  c.solo = few > 2.f * target;
+  const float tall_cost = (float)a.tall_cost, team_cost = (float)a.team_cost;
+  const float total = sum([&](const Info &f) {
+    const bool tall = c.kind(a, f) == kTall;
+    return tall ? (float)f.tall.blocks * f.tall.mean * tall_cost
+                : (float)f.by32.blocks * f.by32.mean * team_cost;
+  }) * Hkv;
+  auto groups = [&](const Info &f) {
+    const Kind k = c.kind(a, f);
+    return (float)pick(k == kTall, f.tall.blocks, f.by32.blocks) * (float)c.splits(k, f) *
+           (k == kSolo ? 1.f / WAVES : 1.f);
+  };
+  c.tall_len = c.team_len = 1e9f;
+  const float least = sum(groups) * Hkv;       // workgroups, with nothing split
+  const float most = ceilf(fmaxf(least / target, 1.f)) * target;
+  float per = fmaxf(total / most, 1.f);
+  bool fits = false;
+  for (int i = 0; i < 5 && !fits; ++i) {
+    c.tall_len = fmaxf(ceilf(per / tall_cost), (float)a.tall_least);
+    c.team_len = fmaxf(ceilf(per / team_cost), (float)a.team_least);
+    const float got = sum(groups) * Hkv;
+    fits = got <= most;
+    per *= fmaxf(got / most, 1.05f);
+  }
+  // (more tokens than there are: offsets that do not ascend)
+  if (!fits || tokens > (double)a.num_tokens) c.tall_len = c.team_len = 1e9f;
+  return c;
+}
+
+// What a workgroup does, or with solo blocks a wavefront.
+struct Part {
+  int b;
+  Kind kind;
+  int splits, off;             // off: of the parts of a sequence
+  int64_t row0;                // rows of the partials of a sequence, from here on
+  int ticket;                  // arrival counters of a sequence, from here on
+};
+// Parts of a sequence, blocks that are merged, rows of partials.
+struct Parts {
+  int splits, parts, merges;
+  long long rows;
+};
+template <int WAVES>
+__device__ __forceinline__ Parts parts_of(const ChunkArgs &a, const Cut &c, const Info &f) {
+  const Kind k = c.kind(a, f);
+  Parts p;
+  p.splits = c.splits(k, f);
+  const int blocks = pick(k == kTall, f.tall.blocks, f.by32.blocks) * a.Hkv;
+  p.parts = blocks * p.splits;
+  p.merges = p.splits > 1 ? blocks : 0;
+  p.rows = p.splits > 1 ? (long long)p.parts * min(k == kTall ? kRows * WAVES : kRows, f.rows) : 0;
+  return p;
+}
+
+// Of more sequences than lanes the map is made once, by a workgroup before the others start:
+// parts of each kind, then per sequence: parts of its kind before it, its kind and splits,
+// first counter, first row.
+constexpr int kMapHead = 4;
 struct MapOf {
-  int32_t *head, *tall, *few, *merge, *splits;
   int64_t *row0;
+  int32_t *head, *first[3], *kind, *splits, *ticket;
 };
 __device__ __forceinline__ MapOf map_of(const ChunkArgs &a) {
   MapOf m;
   m.row0 = reinterpret_cast<int64_t *>(a.map);
   m.head = reinterpret_cast<int32_t *>(m.row0 + a.batch);
-  m.tall = m.head + kMapHead;
-  m.few = m.tall + a.batch;
-  m.merge = m.few + a.batch;
-  m.splits = m.merge + a.batch;
+  m.first[0] = m.head + kMapHead;
+  m.first[1] = m.first[0] + a.batch;
+  m.first[2] = m.first[1] + a.batch;
+  m.kind = m.first[2] + a.batch;
+  m.splits = m.kind + a.batch;
+  m.ticket = m.splits + a.batch;
   return m;
 }
 
 template <int WAVES>
 __global__ __launch_bounds__(kScanThreads) void chunk_plan_kernel(ChunkArgs a) {
-  __shared__ long long s_scan[4][kScanWaves];
+  __shared__ long long s_scan[5][kScanWaves];
+  __shared__ double s_sum[kScanWaves];
   const MapOf m = map_of(a);
-  constexpr int kTall = kRows * WAVES;
-  // the steps there are, in those of a workgroup with a tall block
-  long long sum = 0;
-  for (int b = threadIdx.x; b < a.batch; b += kScanThreads) {
-    const Seq s = seq_of(a, b, kTall);
-    if (s.blocks == 0) continue;
-    const long long steps =
-        (block_range(a, s, 0).steps + block_range(a, s, s.blocks - 1).steps + 1) / 2;
-    sum += steps * s.blocks * (s.tall ? a.tall_cost : a.few_cost);
-  }
-  {
-    const long long x[1] = {sum};
-    long long incl[1], total[1];
-    scan(x, incl, total, s_scan);
-    sum = total[0] * a.Hkv;
-  }
-  // of a part, were all alike
-  const long long per = max(1ll, (sum + a.target - 1) / a.target);
-  const int tall_len = (int)min(max((per + a.tall_cost - 1) / a.tall_cost, (long long)a.tall_least), 1ll << 30);
-  const int few_len =
-      (int)min(max((per + WAVES * a.few_cost - 1) / (WAVES * a.few_cost), (long long)a.few_least), 1ll << 30);
-  long long tall = 0, few = 0, merge = 0, rows = 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Cut c = cut_of<WAVES>(a, [&](auto f) {
+    decltype(f(Info{})) x = 0;
+    for (int b = threadIdx.x; b < a.batch; b += kScanThreads) x += f(info_of<WAVES>(a, seq_of(a, b)));
+    x = wave_sum(x);
+    __syncthreads();
+    if (lane == 0) s_sum[wave] = x;
+    __syncthreads();
+    x = 0;
+    for (int w = 0; w < kScanWaves; ++w) x += (decltype(x))s_sum[w];
+    return x;
+  });
+  long long before[5] = {0, 0, 0, 0, 0};       // parts of each kind, merges, rows
   for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
     const int b = b0 + threadIdx.x;
     const bool in = b < a.batch;
-    Seq s{};
-    int splits = 0;
-    long long slots = 0;
+    Kind k = kTeam;
+    Parts p{0, 0, 0, 0};
     if (in) {
-      s = seq_of(a, b, kTall);
-      if (s.blocks > 0) {
-        const int most = max(block_range(a, s, 0).steps, block_range(a, s, s.blocks - 1).steps);
-        const int len = s.tall ? tall_len : few_len;
-        splits = max(1, div_small(most + len - 1, len));
-        if (splits > 1) slots = (long long)splits * s.blocks * a.Hkv * min(s.block, s.rows);
-      }
+      const Info f = info_of<WAVES>(a, seq_of(a, b));
+      k = c.kind(a, f);
+      p = parts_of<WAVES>(a, c, f);
     }
-    {
-      const long long x[1] = {slots};
-      long long incl[1], total[1];
-      scan(x, incl, total, s_scan);
-      if (slots > 0 && rows + incl[0] > a.part_rows) splits = 1;   // no room for its partials
-      if (in) m.row0[b] = rows + incl[0] - slots;
-      rows += total[0];
-    }
-    const long long parts = (long long)s.blocks * splits * a.Hkv;
-    const long long x[3] = {s.tall ? parts : 0, s.tall ? 0 : parts,
-                            splits > 1 ? (long long)s.blocks * a.Hkv : 0};
-    long long incl[3], total[3];
+    const long long x[5] = {k == kTall ? p.parts : 0, k == kTeam ? p.parts : 0, k == kSolo ? p.parts : 0,
+                            p.merges, p.rows};
+    long long incl[5], total[5];
     scan(x, incl, total, s_scan);
     if (in) {
-      m.tall[b] = (int)(tall + incl[0] - x[0]);
-      m.few[b] = (int)(few + incl[1] - x[1]);
-      m.merge[b] = (int)(merge + incl[2] - x[2]);
-      m.splits[b] = splits;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) m.first[i][b] = (int)(before[i] + incl[i] - x[i]);
+      m.kind[b] = k;
+      m.splits[b] = p.splits;
+      m.ticket[b] = (int)(before[3] + incl[3] - x[3]);
+      m.row0[b] = before[4] + incl[4] - x[4];
     }
-    tall += total[0];
-    few += total[1];
-    merge += total[2];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) before[i] += total[i];
   }
-  if (threadIdx.x == 0) {
-    m.head[kMapTall] = (int)tall;
-    m.head[kMapFew] = (int)few;
-    m.head[kMapMerge] = (int)merge;
-  }
+  if (threadIdx.x == 0)
+    for (int i = 0; i < 3; ++i) m.head[i] = (int)before[i];
 }
 
 // The last of the sequences whose sum is at most w (by a whole wavefront).
@@ -162,63 +264,132 @@ __device__ __forceinline__ int find(const int32_t *first, int n, int w, int lane
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// What a wavefront does: rows [r0, r1) of a sequence's KV head g over steps [j0, j1) of
-// a range, and where the result goes (part < 0: out).
+// Workgroups are numbered tall parts first, then teams', then solo blocks.
+template <int WAVES>
+__device__ __forceinline__ bool part_of(const ChunkArgs &a, int w, int wave, int lane, Part &p) {
+  if (a.map) {
+    const MapOf m = map_of(a);
+    int k = 0;
+    if (w >= m.head[0]) {
+      w -= m.head[0];
+      k = 1;
+      if (w >= m.head[1]) {
+        w = (w - m.head[1]) * WAVES + wave;
+        k = 2;
+        if (w >= m.head[2]) return false;
+      }
+    }
+    const int32_t *first = m.first[0] + (size_t)k * a.batch;
+    p.b = find(first, a.batch, w, lane);
+    p.kind = (Kind)m.kind[p.b];
+    p.splits = m.splits[p.b];
+    p.off = w - first[p.b];
+    p.row0 = m.row0[p.b];
+    p.ticket = m.ticket[p.b];
+    return p.kind == k;
+  }
+  Info f{};
+  if (lane < a.batch) f = info_of<WAVES>(a, seq_of(a, lane));
+  const Cut c = cut_of<WAVES>(a, [&](auto g) { return wave_sum(g(f)); });
+  const Kind kind = c.kind(a, f);
+  const Parts x = parts_of<WAVES>(a, c, f);
+  const int merged = wave_scan_add(x.merges) - x.merges;
+  long long rows = 0;
+  {
+    // (rows by 64-bit sums only where something is split)
+    if (__any(x.rows > 0)) rows = wave_incl(x.rows, lane) - x.rows;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int mine = kind == k ? x.parts : 0, incl = wave_scan_add(mine);
+    const unsigned long long hit = __ballot(w >= incl - mine && w < incl);
+    if (hit) {
+      const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
+      p.b = l;
+      p.kind = (Kind)k;
+      p.splits = __builtin_amdgcn_readlane(x.splits, l);
+      p.off = w - __builtin_amdgcn_readlane(incl - mine, l);
+      p.row0 = (int64_t)__builtin_amdgcn_readlane((int)(rows >> 32), l) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)rows, l);
+      p.ticket = __builtin_amdgcn_readlane(merged, l);
+      return true;
+    }
+    w -= lane63(incl);
+    if (k == 1) w = w * WAVES + wave;
+  }
+  return false;
+}
+
+// What a wavefront does: rows [r0, r1) of a sequence's KV head g over steps of its block's
+// range.
 struct Item {
   Seq s;
   int b, g, r0, r1;
+  Kind kind;
   Range r;
-  int j0, j1;
-  int own0, own1;    // of which these rows see something in [own0, own1) (tall: of the block's)
-  bool tall;
-  int last_rows;     // where the block's last wavefront with rows starts
-  int64_t part;
+  int j0, j1;        // the workgroup's (tall) or wavefront's steps
+  int own0, own1;    // of which these rows see something in [own0, own1)
+  int last_rows;     // tall: where the block's last wavefront with rows starts
+};
+// Where its results go.
+struct Goal {
+  int64_t first_part, part;   // the block's partials, this part's
+  int splits, ticket;
+  Kind kind;
+  int q0, rows, g;   // of the sequence; KV head
+  int base, height;  // the block's first row, its rows
 };
 
 template <int WAVES>
-__device__ bool item_of(const ChunkArgs &a, int w, int wave, int lane, Item &it) {
-  const MapOf m = map_of(a);
-  constexpr int kTall = kRows * WAVES;
-  const bool tall = w < m.head[kMapTall];
-  if (!tall) {
-    w = (w - m.head[kMapTall]) * WAVES + wave;
-    if (w >= m.head[kMapFew]) return false;
-  }
-  const int32_t *first = tall ? m.tall : m.few;
-  it.b = find(first, a.batch, w, lane);
-  it.s = seq_of(a, it.b, kTall);
-  const int splits = m.splits[it.b], off = w - first[it.b];
-  if (off < 0 || splits < 1) return false;     // (offsets that do not ascend)
-  int block, split;
-  if (tall) {                                  // the longest first; KV heads share out the XCDs
-    const int at = div_small(off, a.Hkv);
-    it.g = off - at * a.Hkv;
-    block = div_small(at, splits);
-    split = at - block * splits;
-    block = it.s.blocks - 1 - block;
+__device__ __forceinline__ bool item_of(const ChunkArgs &a, int w, int wave, int lane, Item &it,
+                                        Goal &goal) {
+  Part p;
+  if (!part_of<WAVES>(a, w, wave, lane, p)) return false;
+  it.b = p.b;
+  it.kind = p.kind;
+  it.s = seq_of(a, p.b);
+  const int size = p.kind == kTall ? kRows * WAVES : kRows, blocks = (it.s.rows + size - 1) / size;
+  int block, split = 0;
+  if (p.kind == kTall) {                       // the longest first; KV heads share out the XCDs
+    const int at = div_small(p.off, a.Hkv);
+    it.g = p.off - at * a.Hkv;
+    block = div_small(at, p.splits);
+    split = at - block * p.splits;
+    block = blocks - 1 - block;
   } else {
-    const int at = div_small(off, splits);
-    split = off - at * splits;
+    const int at = div_small(p.off, p.splits);
+    split = p.off - at * p.splits;
     block = div_small(at, a.Hkv);
     it.g = at - block * a.Hkv;
   }
-  if (block < 0 || block >= it.s.blocks) return false;
-  it.r = block_range(a, it.s, block);
-  it.j0 = (int)((long long)it.r.steps * split / splits);
-  it.j1 = (int)((long long)it.r.steps * (split + 1) / splits);
-  const int slot = min(it.s.block, it.s.rows), skip = tall ? wave * kRows : 0;
-  it.part = splits > 1 ? m.row0[it.b] + ((int64_t)(block * a.Hkv + it.g) * splits + split) * slot + skip
-                       : -1;
-  it.tall = tall;
-  {
-    const int first = block * it.s.block, rows = min(it.s.block, it.s.rows - first);
-    it.last_rows = first + (rows - 1) / kRows * kRows;
+  if (block < 0 || block >= blocks) return false;   // (offsets that do not ascend)
+  const int base = block * size, height = min(size, it.s.rows - base);
+  it.r = range_of(a, it.s, base, base + height);
+  it.j0 = (int)((long long)it.r.steps * split / p.splits);
+  it.j1 = (int)((long long)it.r.steps * (split + 1) / p.splits);
+  const int slot = min(size, it.s.rows), at = block * a.Hkv + it.g;
+  goal.first_part = p.row0 + (int64_t)at * p.splits * slot;
+  goal.part = goal.first_part + (int64_t)split * slot;
+  goal.splits = p.splits;
+  goal.ticket = p.ticket + at;
+  goal.kind = p.kind;
+  goal.q0 = it.s.q0;
+  goal.rows = it.s.rows;
+  goal.g = it.g;
+  goal.base = base;
+  goal.height = height;
+  const int skip = p.kind == kTall ? wave * kRows : 0;
+  it.r0 = min(base + skip, it.s.rows);
+  it.r1 = min(it.r0 + kRows, base + height);
+  it.last_rows = base + (height - 1) / kRows * kRows;
+  if (p.kind == kTeam) {
+    const int n = it.j1 - it.j0;
+    it.j1 = it.j0 + (int)((long long)n * (wave + 1) / WAVES);
+    it.j0 += (int)((long long)n * wave / WAVES);
   }
-  it.r0 = min(block * it.s.block + skip, it.s.rows);
-  it.r1 = min(it.r0 + kRows, it.s.rows);
   it.own0 = it.j0;
   it.own1 = it.j1;
-  if (tall && it.r0 < it.r1) {                 // what these rows see of the block's steps
+  if (p.kind == kTall && it.r0 < it.r1) {      // what these rows see of the block's steps
     const Range own = range_of(a, it.s, it.r0, it.r1);
     it.own1 = min(it.j1, it.r.sinks + own.steps - own.sinks + own.from - it.r.from);
     if (a.sinks == 0) it.own0 = max(it.j0, own.from - it.r.from);
@@ -249,22 +420,26 @@ struct Step {
   bool ok[2];
 };
 
+// The tiles of a KV head: page id's begin id * stride bytes from these.
+struct Tiles {
+  const char *k, *v;
+  uint32_t stride;
+  __device__ const char *key(int id) const { return k + (uint64_t)(uint32_t)id * stride; }
+  __device__ const char *value(int id) const { return v + (uint64_t)(uint32_t)id * stride; }
+};
+
 // Operands of a step in memory, for the lane that multiplies them.
 template <int KV, int D>
 struct Pages {
-  static constexpr size_t kTile = (size_t)kPage * D * elem_bytes(KV);
   const char *k, *v[2];
   // not live: the loads are issued all the same, all lanes' from one place
-  __device__ Pages(const ChunkArgs &a, const int (&id)[2], int g, int lane, bool live = true) {
+  __device__ Pages(const Tiles &head, const int (&id)[2], int lane, bool live = true) {
     const int i = lane & 31, hb = lane >> 5, tok = key_of_row<KV>(i) & 15;
     const int k_at = tok * 8 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 128 * elem_bytes(KV));
     const int v_at = i * 16 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 8 * elem_bytes(KV));
-    k = static_cast<const char *>(a.k_pages) +
-        ((size_t)(i < 16 && live ? id[0] : id[1]) * a.Hkv + g) * kTile + (live ? k_at : 0);
+    k = head.key(i < 16 && live ? id[0] : id[1]) + (live ? k_at : 0);
 #pragma unroll
-    for (int pg = 0; pg < 2; ++pg)
-      v[pg] = static_cast<const char *>(a.v_pages) + ((size_t)id[pg] * a.Hkv + g) * kTile +
-              (live ? v_at : 0);
+    for (int pg = 0; pg < 2; ++pg) v[pg] = head.value(id[pg]) + (live ? v_at : 0);
   }
   __device__ Operand<KV> raw_key(int c) const {
     return *reinterpret_cast<const Operand<KV> *>(k + c * (KV == kF32 ? 512 : 256 * elem_bytes(KV)));
@@ -477,37 +652,6 @@ __device__ __forceinline__ Step step_at(const ChunkArgs &a, const Walk &w, int j
   }
   return x;
 }
-// Page ids of steps j0, j0 + 1, ..: 32 steps' in the lanes of one register, the next 32
-// steps' on the way.
-struct PageIds {
-  int cur, next, k0, lane;
-  __device__ static int fetch(const Walk &w, int k, int lane) {
-    const int e = 2 * w.step(w.j0 + k + (lane >> 1)) + (lane & 1);
-    return w.table[min(e, max(w.pages - 1, 0))];
-  }
-  __device__ PageIds(const Walk &w, int lane_) : k0(0), lane(lane_) {
-    cur = fetch(w, 0, lane);
-    next = fetch(w, 32, lane);
-  }
-  // of step j; j never goes back
-  __device__ Step at(const ChunkArgs &a, const Walk &w, int j) {
-    const int k = j - w.j0;
-    if (k - k0 >= 32) {
-      k0 += 32;
-      cur = next;
-      next = fetch(w, k0 + 32, lane);
-    }
-    const int s = w.step(j);
-    Step x;
-#pragma unroll
-    for (int pg = 0; pg < 2; ++pg) {
-      const int id = __builtin_amdgcn_readlane(cur, 2 * (k - k0) + pg);
-      x.ok[pg] = j < w.j1 && 2 * s + pg < w.pages && in_pool(a, id);
-      x.id[pg] = x.ok[pg] ? id : 0;
-    }
-    return x;
-  }
-};
 
 // Raw logits to powers of two, up to the factor that is returned (not negative:
 // the sign of sm_scale is in Q). MASKED: keys that a row does not see to -inf.
@@ -565,27 +709,38 @@ template <int KV, int D> constexpr bool has_plain() { return KV != kF32 || D < 2
 
 // Steps [ja, jb) of a walk, which every row sees in full and whose pages are there,
 // operands from memory: the next step's K is fetched as soon as this one's has been
-// multiplied, and so is V.
+// multiplied, and so is V. Page ids and scales come through vector loads a step before they
+// are needed: in order with the others, so that none is waited for by itself.
 template <int KV, int D>
 __device__ __forceinline__ void walk_plain(State<D> &st, const ChunkArgs &a, const Walk &w,
-                                           const Queries<KV, D> &q, int g, PageIds ids,
+                                           const Queries<KV, D> &q, const Tiles &head, int lane,
                                            const Sight &see, int ja, int jb) {
-  const int lane = ids.lane;
+  // lanes 4 i + 2 pg (+ 1): of page pg
+  auto pages = [&](int j) { return w.table[2 * w.step(min(j, jb - 1)) + (lane >> 1 & 1)]; };
+  auto scales = [&](int ids) { return KV == kFP8 ? a.kv_scales[2 * (size_t)ids + (lane & 1)] : 1.f; };
   const bool fine[2] = {true, true};
-  float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f}, ks1[2] = {1.f, 1.f}, vs1[2] = {1.f, 1.f};
+  int ids = pages(ja), ids1 = pages(ja + 1);
+  float sc = scales(ids);
   Held<KV, D> r;
   {
-    const Step x = ids.at(a, w, ja);
-    const Pages<KV, D> p(a, x.id, g, lane);
+    const int id[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 2)};
+    const Pages<KV, D> p(head, id, lane);
     r.load_k(p);
     r.load_v(p);
-    scales_of<KV>(a, x.id, ks, vs);
   }
   for (int j = ja;; ++j) {
     const bool more = j + 1 < jb;
-    const Step x = ids.at(a, w, j + 1);
-    const Pages<KV, D> p(a, x.id, g, lane, more);
-    scales_of<KV>(a, x.id, ks1, vs1);
+    const int id[2] = {__builtin_amdgcn_readlane(ids1, 0), __builtin_amdgcn_readlane(ids1, 2)};
+    const Pages<KV, D> p(head, id, lane, more);
+    const float sc1 = scales(ids1);
+    ids1 = pages(j + 2);
+    float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
+    if constexpr (KV == kFP8)
+#pragma unroll
+      for (int pg = 0; pg < 2; ++pg) {
+        ks[pg] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc), 2 * pg));
+        vs[pg] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc), 2 * pg + 1));
+      }
     f32x16 z = logits<KV, D>(r, q);
     __builtin_amdgcn_sched_barrier(0);
     r.load_k(p);
@@ -598,18 +753,14 @@ __device__ __forceinline__ void walk_plain(State<D> &st, const ChunkArgs &a, con
     __builtin_amdgcn_sched_barrier(0);
     r.load_v(p);
     if (!more) break;
-#pragma unroll
-    for (int pg = 0; pg < 2; ++pg) {
-      ks[pg] = ks1[pg];
-      vs[pg] = vs1[pg];
-    }
+    sc = sc1;
   }
 }
 
 // The other steps: those before ja, and those from jb on.
 template <int KV, int D>
 __device__ __forceinline__ void walk_masked(State<D> &st, const ChunkArgs &a, const Walk &w,
-                                            const Queries<KV, D> &q, int g, int lane,
+                                            const Queries<KV, D> &q, const Tiles &head, int lane,
                                             const Sight &see, int ja, int jb) {
   Step x = step_at(a, w, w.j0 < ja ? w.j0 : jb);
   for (int j = w.j0 < ja ? w.j0 : jb; j < w.j1;) {
@@ -617,7 +768,7 @@ __device__ __forceinline__ void walk_masked(State<D> &st, const ChunkArgs &a, co
     const Step x1 = step_at(a, w, next);
     float ks[2] = {1.f, 1.f}, vs[2] = {1.f, 1.f};
     scales_of<KV>(a, x.id, ks, vs);
-    take_step<KV, D, true>(st, a, q, Pages<KV, D>(a, x.id, g, lane), w.step(j), x.ok, see, ks, vs, lane);
+    take_step<KV, D, true>(st, a, q, Pages<KV, D>(head, x.id, lane), w.step(j), x.ok, see, ks, vs, lane);
     x = x1;
     j = next;
   }
@@ -657,7 +808,6 @@ struct Fetch {
   static constexpr int kStage = stage_steps<D>(), kOps = operands<KV, D>(), kEach = kStage * kOps / WAVES;
   static_assert(kOps == v_parts<KV>() * (D / 32) && kStage * kOps % WAVES == 0 &&
                 (kOps % WAVES == 0 || WAVES == kStage * kOps), "");
-  static constexpr size_t kTile = (size_t)kPage * D * elem_bytes(KV);
   Operand<KV> k[kEach], v[kEach];
   // the step of the wavefront's e-th operand
   __device__ __forceinline__ static int step_of(int e, int wave) {
@@ -665,19 +815,17 @@ struct Fetch {
     else return wave < kOps ? 0 : kStage - 1;
   }
   // ids: the page of step s of the stage, first or second, in lane 4 s + 2 pg
-  __device__ __forceinline__ static const char *tile(const ChunkArgs &a, const void *pages, int ids, int s,
-                                                     int pg, int g) {
-    const int id = __builtin_amdgcn_readlane(ids, 4 * s + 2 * pg);
-    return static_cast<const char *>(pages) + ((size_t)id * a.Hkv + g) * kTile;
+  __device__ __forceinline__ static int page(int ids, int s, int pg) {
+    return __builtin_amdgcn_readlane(ids, 4 * s + 2 * pg);
   }
-  __device__ __forceinline__ void issue_k(const ChunkArgs &a, int ids, int g, int wave, int lane) {
+  __device__ __forceinline__ void issue_k(const Tiles &head, int ids, int wave, int lane) {
     const int i = lane & 31, hb = lane >> 5, tok = key_of_row<KV>(i) & 15;
     const int at = tok * 8 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 128 * elem_bytes(KV));
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int s = step_of(e, wave), o = (e * WAVES + wave) % kOps;
-      uint64_t p0 = reinterpret_cast<uint64_t>(tile(a, a.k_pages, ids, s, 0, g));
-      uint64_t p1 = reinterpret_cast<uint64_t>(tile(a, a.k_pages, ids, s, 1, g));
+      uint64_t p0 = reinterpret_cast<uint64_t>(head.key(page(ids, s, 0)));
+      uint64_t p1 = reinterpret_cast<uint64_t>(head.key(page(ids, s, 1)));
       asm("" : "+s"(p0), "+s"(p1));            // (or the products are the vector unit's, lane by lane)
       // (an address of global memory: a generic one would be waited for with LDS)
       typedef const __attribute__((address_space(1))) decltype(k[e].x) *from;
@@ -685,13 +833,13 @@ struct Fetch {
                                        o * (KV == kF32 ? 512 : 256 * elem_bytes(KV)));
     }
   }
-  __device__ __forceinline__ void issue_v(const ChunkArgs &a, int ids, int g, int wave, int lane) {
+  __device__ __forceinline__ void issue_v(const Tiles &head, int ids, int wave, int lane) {
     const int i = lane & 31, hb = lane >> 5;
     const int at = i * 16 * elem_bytes(KV) + hb * (KV == kF32 ? 16 : 8 * elem_bytes(KV));
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int o = (e * WAVES + wave) % kOps, y = o / (D / 32), db = o % (D / 32);
-      const char *const base = tile(a, a.v_pages, ids, step_of(e, wave), KV == kF32 ? y >> 1 : y, g) +
+      const char *const base = head.value(page(ids, step_of(e, wave), KV == kF32 ? y >> 1 : y)) +
                                db * 512 * elem_bytes(KV) + (KV == kF32 ? (y & 1) * 32 : 0);
       v[e] = *reinterpret_cast<const Operand<KV> *>(base + at);
     }
@@ -839,7 +987,7 @@ __device__ __forceinline__ void take_stage(State<D> &st, const ChunkArgs &a, Sta
 // the reads of LDS, and a load under a condition would have every stage wait for all.
 template <int KV, int D, int WAVES>
 __device__ __forceinline__ void walk_staged(State<D> &st, const ChunkArgs &a, const Walk &w,
-                                            const Queries<KV, D> &q, int g, int lane, int end, int ja,
+                                            const Queries<KV, D> &q, const Tiles &head, int lane, int end, int ja,
                                             int jb, u32x4 *lds, int wave) {
   constexpr int kHalf = half_words<KV, D>(), kStage = stage_steps<D>();
   if (end <= w.j0) return;
@@ -853,10 +1001,10 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const ChunkArgs &a, co
   auto scales = [&](int ids) { return KV == kFP8 ? a.kv_scales[2 * (size_t)ids + (lane & 1)] : 1.f; };
   int ids = pages(w.j0), ids1 = pages(w.j0 + kStage), ids2 = pages(w.j0 + 2 * kStage);
   float sc = scales(ids), sc1 = 1.f;           // this stage's, the next one's
-  f.issue_k(a, ids, g, wave, lane);
-  f.issue_v(a, ids, g, wave, lane);
+  f.issue_k(head, ids, wave, lane);
+  f.issue_v(head, ids, wave, lane);
   f.write_k(keys, wave, lane);
-  f.issue_k(a, ids1, g, wave, lane);
+  f.issue_k(head, ids1, wave, lane);
   f.write_v(values, wave, lane);
   f.write_k(keys + kHalf, wave, lane);
   __syncthreads();
@@ -868,8 +1016,8 @@ __device__ __forceinline__ void walk_staged(State<D> &st, const ChunkArgs &a, co
   auto one = [&](int j, int slot, Stage<D> &p, Stage<D> &after) {
     sc1 = scales(ids1);
     const int ids3 = pages(j + 3 * kStage);
-    f.issue_v(a, ids1, g, wave, lane);
-    f.issue_k(a, ids2, g, wave, lane);
+    f.issue_v(head, ids1, wave, lane);
+    f.issue_k(head, ids2, wave, lane);
     const u32x4 *const k = keys + (slot ^ 1) * kHalf + lane;
     if (j >= ja && j < jb) {
       float ks[kStage][2], vs[kStage][2];
@@ -909,9 +1057,9 @@ __device__ __forceinline__ unsigned flat_block() {
 }
 
 // Row r of a sequence's KV head g in q and out.
-__device__ __forceinline__ int64_t row_at(const ChunkArgs &a, const Seq &s, int g, int r, int &token) {
-  token = div_small(r, a.G);
-  return (int64_t)(s.q0 + token) * a.Hq + g * a.G + (r - token * a.G);
+__device__ __forceinline__ int64_t row_at(const ChunkArgs &a, int q0, int g, int r, int &token) {
+  token = token_of(a, r);
+  return (int64_t)(q0 + token) * a.Hq + g * a.G + (r - token * a.G);
 }
 
 template <int KV>
@@ -923,17 +1071,102 @@ __device__ __forceinline__ void store4(const ChunkArgs &a, int64_t at, f32x4 v) 
         u32x2{round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3])};
 }
 
+// Partials travel between workgroups by agent-scope stores and loads, eight bytes each.
+__device__ __forceinline__ void leave(float *at, float x, float y) {
+  __hip_atomic_store(reinterpret_cast<uint64_t *>(at),
+                     (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void pick_up(const float *at, float &x, float &y) {
+  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(at), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+  x = __uint_as_float((uint32_t)v);
+  y = __uint_as_float((uint32_t)(v >> 32));
+}
+
+// Four dims of a result, from a part's sums, normalised: out, or partials if the block is
+// split; lse in powers of two.
+template <int KV, int D>
+__device__ __forceinline__ void put4(const ChunkArgs &a, const Goal &goal, int rl, int d, f32x4 v,
+                                     float lse) {
+  if (goal.splits > 1) {
+    const int64_t at = goal.part + rl;
+    leave(a.part_o + at * D + d, v[0], v[1]);
+    leave(a.part_o + at * D + d + 2, v[2], v[3]);
+    if (d == 0) __hip_atomic_store(a.part_lse + at, lse, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  } else {
+    int token;
+    const int64_t row = row_at(a, goal.q0, goal.g, goal.base + rl, token);
+    store4<KV>(a, row * D + d, v);
+    if (d == 0 && a.lse) a.lse[row] = lse * kLn2;
+  }
+}
+
+// The rows of a block over its parts, by the workgroup that left the last one.
+template <int KV, int D>
+__device__ __forceinline__ void merge_parts(const ChunkArgs &a, const Goal &goal) {
+  constexpr int kBatch = 4;
+  const int slot = goal.kind == kTall ? min(kRows * waves_of(KV, D), goal.rows) : min(kRows, goal.rows);
+  for (int i = threadIdx.x; i < goal.height * (D / 4); i += blockDim.x) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4;
+    float m = kNoMax, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int t0 = 0; t0 < goal.splits; t0 += kBatch) {
+      float lse[kBatch];
+      float v[kBatch][4];
+#pragma unroll
+      for (int t = 0; t < kBatch; ++t) {
+        const int64_t at = goal.first_part + (int64_t)min(t0 + t, goal.splits - 1) * slot + r;
+        lse[t] = __hip_atomic_load(a.part_lse + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        pick_up(a.part_o + at * D + d, v[t][0], v[t][1]);
+        pick_up(a.part_o + at * D + d + 2, v[t][2], v[t][3]);
+      }
+#pragma unroll
+      for (int t = 0; t < kBatch; ++t) {
+        if (t0 + t >= goal.splits || lse[t] == -INFINITY) continue;   // (no key seen)
+        const float mm = max_f(m, lse[t]), f = exp2_fast(m - mm), x = exp2_fast(lse[t] - mm);
+        m = mm;
+        l = l * f + x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (f == 0.f ? 0.f : o[e] * f) + (x == 0.f ? 0.f : v[t][e] * x);
+      }
+    }
+    int token;
+    const int64_t row = row_at(a, goal.q0, goal.g, goal.base + r, token);
+    f32x4 res;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) res[e] = l == 0.f ? 0.f : o[e] / l;
+    store4<KV>(a, row * D + d, res);
+    if (d == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  }
+}
+
+// 16-byte words of LDS: queries (float32, 256 dims) or staged operands, and a team's
+// results, a row of D + 4 floats each (the 4: rows begin in different banks).
+template <int KV, int D> constexpr int team_words() { return waves_of(KV, D) * kRows * (D + 4) / 4; }
+template <int KV, int D> constexpr int lds_words() {
+  const int work = q_in_lds<KV, D>() ? waves_of(KV, D) * operands<KV, D>() * 64 : 4 * half_words<KV, D>();
+  return work > team_words<KV, D>() ? work : team_words<KV, D>();
+}
+
 template <int KV, int D>
 __global__ __launch_bounds__(64 * waves_of(KV, D))
 __attribute__((amdgpu_waves_per_eu(waves_of(KV, D) / 4)))
 void attn_chunk_kernel(ChunkArgs a) {
   constexpr int kWaves = waves_of(KV, D);
-  __shared__ __align__(16) u32x4 s_mem[q_in_lds<KV, D>() ? kWaves * operands<KV, D>() * 64
-                                                         : 4 * half_words<KV, D>()];
+  __shared__ __align__(16) u32x4 s_mem[lds_words<KV, D>()];
+  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+  __shared__ Goal s_goal[kWaves];
+  __shared__ int s_last;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hb = lane >> 5;
   Item it;
-  if (!item_of<kWaves>(a, (int)flat_block(), wave, lane, it)) return;   // (tall: all wavefronts)
+  {
+    // (all wavefronts, or with solo blocks one by one, which meet at no barrier)
+    Goal goal;
+    if (!item_of<kWaves>(a, (int)flat_block(), wave, lane, it, goal)) return;
+    s_goal[wave] = goal;                       // (scalar registers are short until the end)
+  }
 
   Walk w;
   w.table = a.table + (size_t)it.b * a.stride;
@@ -947,7 +1180,7 @@ void attn_chunk_kernel(ChunkArgs a) {
   const int r = it.r0 + (lane & 31);
   const bool live = r < it.r1;
   int token;
-  const int64_t row = row_at(a, it.s, it.g, live ? r : min(it.r0, it.s.rows - 1), token);
+  const int64_t row = row_at(a, it.s.q0, it.g, live ? r : min(it.r0, it.s.rows - 1), token);
   Sight see;
   see.hi = live ? max(0, it.s.len - it.s.n + token + 1) : 0;
   see.lo = a.window > 0 ? max(0, see.hi - a.window) : 0;
@@ -986,6 +1219,14 @@ void attn_chunk_kernel(ChunkArgs a) {
   see.some_hi = __builtin_amdgcn_readfirstlane(see.some_hi);
   see.some_lo = __builtin_amdgcn_readfirstlane(see.some_lo);
 
+  Tiles head;
+  {
+    constexpr uint32_t kTile = kPage * D * elem_bytes(KV);
+    head.stride = a.Hkv * kTile;
+    head.k = static_cast<const char *>(a.k_pages) + (size_t)it.g * kTile;
+    head.v = static_cast<const char *>(a.v_pages) + (size_t)it.g * kTile;
+  }
+
   State<D> st;
   auto clear = [&] {
 #pragma unroll
@@ -995,13 +1236,11 @@ void attn_chunk_kernel(ChunkArgs a) {
   };
   clear();
   if (w.j0 < w.j1) {
-    PageIds ids(w, lane);
     // whether all pages are in the pool
     bool fine = true;
-    for (int k = 0; w.j0 + k < w.j1; k += 32) {
-      const int id = k == 0 ? ids.cur : (k == 32 ? ids.next : PageIds::fetch(w, k, lane));
-      const int j = w.j0 + k + (lane >> 1);
-      fine &= j >= w.j1 || 2 * w.step(j) + (lane & 1) >= w.pages || in_pool(a, id);
+    for (int j = w.j0 + (lane >> 1); j < w.j1; j += 32) {
+      const int e = 2 * w.step(j) + (lane & 1);
+      fine &= e >= w.pages || in_pool(a, w.table[e]);
     }
     fine = !__any(!fine);
     // steps that every row sees in full
@@ -1012,15 +1251,15 @@ void attn_chunk_kernel(ChunkArgs a) {
     if (!fine || !has_plain<KV, D>() || it.own0 >= it.own1) ja = jb = it.own0;
     bool staged = false;
     if constexpr (has_lds<KV, D>()) {
-      if (it.tall && fine) {
+      if (it.kind == kTall && fine) {
         // whole stages; those that start beyond what the block's last 32 rows all see are
         // nobody's
         constexpr int kStage = stage_steps<D>();
         ja = w.j0 + (ja - w.j0 + kStage - 1) / kStage * kStage;
         jb = max(ja, w.j0 + (jb - w.j0) / kStage * kStage);
-        const int last = div_small(it.last_rows, a.G);
+        const int last = token_of(a, it.last_rows);
         const int end = min(w.j1, max(0, it.s.len - it.s.n + last + 1) / kKeys - w.shift);
-        walk_staged<KV, D, kWaves>(st, a, w, q, it.g, opaque(lane), end, ja, jb, s_mem, wave);
+        walk_staged<KV, D, kWaves>(st, a, w, q, head, opaque(lane), end, ja, jb, s_mem, wave);
         staged = true;
         if (ja >= jb) ja = jb = it.own0;
       }
@@ -1033,8 +1272,8 @@ void attn_chunk_kernel(ChunkArgs a) {
     w.j1 = it.own1;
     for (;;) {
       if (has_plain<KV, D>() && !staged && ja < jb)
-        walk_plain<KV, D>(st, a, w, q, it.g, PageIds(w, opaque(lane)), see, ja, jb);
-      if (w.j0 < w.j1) walk_masked<KV, D>(st, a, w, q, it.g, opaque(lane), see, ja, jb);
+        walk_plain<KV, D>(st, a, w, q, head, opaque(lane), see, ja, jb);
+      if (w.j0 < w.j1) walk_masked<KV, D>(st, a, w, q, head, opaque(lane), see, ja, jb);
       staged = false;
       st.sum += other_half(st.sum);
       if (ja >= jb) break;
@@ -1048,81 +1287,83 @@ void attn_chunk_kernel(ChunkArgs a) {
       clear();
     }
   }
-  if (see.hi == 0) st.sum = 0.f;
-  if (!live) return;
-  const float inv = st.sum == 0.f ? 0.f : 1.f / st.sum;
-  const float lse = st.sum == 0.f ? -INFINITY : st.ref + log2f(st.sum);
-  const int64_t part = it.part + (lane & 31);
+  if (see.hi == 0) {
+    st.sum = 0.f;
+    st.ref = kNoMax;
+  }
+
+  Goal goal = s_goal[wave];
+  goal.splits = __builtin_amdgcn_readfirstlane(goal.splits);
+  goal.kind = (Kind)__builtin_amdgcn_readfirstlane(goal.kind);
+
+  // ---- a wavefront's rows ---------------------------------------------------------
+  if (goal.kind != kTeam) {
+    if (live) {
+      const float inv = st.sum == 0.f ? 0.f : 1.f / st.sum;
+      const float lse = st.sum == 0.f ? -INFINITY : st.ref + log2f(st.sum);
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
+      for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
+        for (int y = 0; y < 4; ++y) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = st.sum == 0.f ? 0.f : st.o[db][4 * y + e] * inv;
+          put4<KV, D>(a, goal, r - goal.base, 32 * db + 8 * y + 4 * hb, v, lse);
+        }
+    }
+  } else {
+    // ---- a team's: sums of its wavefronts, in LDS -----------------------------------
+    constexpr int kLine = D + 4;
+    float *part = reinterpret_cast<float *>(s_mem);
+    const int rr = lane & 31;
+    if (q_in_lds<KV, D>()) __syncthreads();    // (the queries have been read)
+    if (live) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = st.o[db][4 * y + e];
+          *reinterpret_cast<f32x4 *>(part + (wave * goal.height + rr) * kLine + 32 * db + 8 * y + 4 * hb) = v;
+        }
+      s_m[wave][rr] = st.ref;                  // (both lanes of a row: the same)
+      s_l[wave][rr] = st.sum;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < goal.height * (D / 4); i += 64 * kWaves) {
+      const int rl = i / (D / 4), d = i % (D / 4) * 4;
+      float m = s_m[0][rl];
+#pragma unroll
+      for (int t = 1; t < kWaves; ++t) m = max_f(m, s_m[t][rl]);
+      float l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < kWaves; ++t) {
+        const float f = exp2_fast(s_m[t][rl] - m);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (t * goal.height + rl) * kLine + d);
+        l += s_l[t][rl] * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += f == 0.f ? 0.f : x[e] * f;
+      }
       f32x4 v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = st.sum == 0.f ? 0.f : st.o[db][4 * y + e] * inv;
-      const int d = 32 * db + 8 * y + 4 * hb;
-      if (it.part >= 0) *reinterpret_cast<f32x4 *>(a.part_o + part * D + d) = v;
-      else store4<KV>(a, row * D + d, v);
-    }
-  if (hb == 0) {
-    if (it.part >= 0) a.part_lse[part] = lse;
-    else if (a.lse) a.lse[row] = lse * kLn2;
-  }
-}
-
-// ---------------------------------------------------------------------------
-// merge: the rows of a block over its splits
-// ---------------------------------------------------------------------------
-
-constexpr int kMergeThreads = 256;
-
-template <int KV, int D>
-__global__ __launch_bounds__(kMergeThreads) void merge_chunk_kernel(ChunkArgs a) {
-  const MapOf m = map_of(a);
-  const int lane = threadIdx.x & 63, total = m.head[kMapMerge];
-  for (int w = blockIdx.x; w < total; w += gridDim.x) {
-    const int b = find(m.merge, a.batch, w, lane);
-    const Seq s = seq_of(a, b, kRows * waves_of(KV, D));
-    const int off = w - m.merge[b], block = div_small(off, a.Hkv), g = off - block * a.Hkv;
-    const int splits = m.splits[b], slot = min(s.block, s.rows);
-    if (off < 0 || block >= s.blocks || splits < 2) continue;   // (offsets that do not ascend)
-    const int64_t row0 = m.row0[b] + (int64_t)off * splits * slot;
-    const int r0 = block * s.block, rows = min(s.rows - r0, s.block);
-    for (int i = threadIdx.x; i < rows * (D / 4); i += kMergeThreads) {
-      const int rl = i / (D / 4), d = i % (D / 4) * 4;
-      float mx = -INFINITY, l = 0.f;
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int t = 0; t < splits; ++t) {
-        const int64_t at = row0 + (int64_t)t * slot + rl;
-        const float lse = a.part_lse[at];
-        if (lse == -INFINITY) continue;          // no key seen
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + d);
-        const float mm = max_f(mx, lse);
-        const float f = exp2_fast(mx - mm), x = exp2_fast(lse - mm);
-        mx = mm;
-        l = l * f + x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (f == 0.f ? 0.f : o[e] * f) + (x == 0.f ? 0.f : v[e] * x);
-      }
-      int token;
-      const int64_t row = row_at(a, s, g, r0 + rl, token);
-      f32x4 res;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) res[e] = l == 0.f ? 0.f : o[e] / l;
-      store4<KV>(a, row * D + d, res);
-      if (d == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (mx + log2f(l)) * kLn2;
+      for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : o[e] / l;
+      put4<KV, D>(a, goal, rl, d, v, l == 0.f ? -INFINITY : m + log2f(l));
     }
   }
+  if (goal.splits == 1) return;
+  if (last_arrival_of(a.tickets + (size_t)goal.ticket * kTicketStride, goal.splits, &s_last))
+    merge_parts<KV, D>(a, goal);
 }
 
 template <int KV, int D>
 void launch_d(const ChunkArgs &a, hipStream_t s) {
   constexpr int kWaves = waves_of(KV, D);
-  const dim3 grid((unsigned)std::min<long long>(a.grid, kAlongX), 1, (unsigned)((a.grid + kAlongX - 1) / kAlongX));
-  hipLaunchKernelGGL(chunk_plan_kernel<kWaves>, dim3(1), dim3(kScanThreads), 0, s, a);
+  const dim3 grid((unsigned)std::min<long long>(a.grid, kAlongX), 1,
+                  (unsigned)((a.grid + kAlongX - 1) / kAlongX));
+  if (a.map) hipLaunchKernelGGL(chunk_plan_kernel<kWaves>, dim3(1), dim3(kScanThreads), 0, s, a);
   hipLaunchKernelGGL((attn_chunk_kernel<KV, D>), grid, dim3(64 * kWaves), 0, s, a);
-  if (a.part_rows > 0)
-    hipLaunchKernelGGL((merge_chunk_kernel<KV, D>), dim3(4 * a.target), dim3(kMergeThreads), 0, s, a);
 }
 
 template <int KV>

@@ -97,12 +97,6 @@ __device__ __forceinline__ Unit seq_unit(const SharedArgs &a, int b) {
   return Unit{b, a.q_len * a.G, sh, max(0, np - sh)};
 }
 
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
-}
-
 // Work item of a wavefront. C steps are what a workgroup gets; shared pages are
 // split into parts of up to C steps, a workgroup each, a sequence's own into parts of
 // up to C over the wavefronts of a workgroup, a wavefront each. The last part of a

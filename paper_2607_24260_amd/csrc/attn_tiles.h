@@ -33,6 +33,13 @@ __device__ __forceinline__ float other_half(float x) {
   return __int_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
+template <class T>
+__device__ __forceinline__ T wave_sum(T x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+
 // Key (0..31, of two pages) in row i of K's operand, and the in-page key of
 // accumulator register r (page r / 8) in half hb of the wavefront.
 template <int KV>

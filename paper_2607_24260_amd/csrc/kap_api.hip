@@ -116,6 +116,8 @@ constexpr int kVerifyUnevenFactor = 4;
 constexpr int kMinChunkDecode = 16;
 constexpr int kMinChunkVerify = 8;
 
+int elem_bytes(kap_dtype t) { return t == KAP_DT_F32 ? 4 : (t == KAP_DT_BF16 ? 2 : 1); }
+
 int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // Resident workgroups per CU of a tuned kernel (cached per device).
@@ -978,10 +980,6 @@ kap_status kap_verify_shared(const kap_kv_cache *kv, int32_t batch, int32_t q_le
 // kap_append_kv / kap_compact_view
 // ---------------------------------------------------------------------------
 
-static int elem_bytes(kap_dtype t) {
-  return t == KAP_DT_F32 ? 4 : (t == KAP_DT_BF16 ? 2 : 1);
-}
-
 kap_status kap_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const void *k_new,
                          const void *v_new, const int64_t *slot_mapping, int32_t *bad_slots,
                          void *stream) {
@@ -1300,41 +1298,60 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
 // kap_chunk_attention
 // ---------------------------------------------------------------------------
 
-// Sizes of a call's workspace: [map][partial o][partial lse], and what the work is cut by.
+// Sizes of a call's workspace: [arrival counters][map][partial o][partial lse], and what the
+// work is cut by.
 struct ChunkPlan {
-  int few_rows, target, tall_cost, few_cost, tall_least, few_least, window;
-  long long grid, part_rows;
-  size_t part_o, part_lse, total;
+  int few_rows, target, tall_cost, team_cost, tall_least, team_least, window;
+  long long grid;
+  size_t map, part_o, part_lse, total;
 };
+
+// Up to as many sequences as a wavefront has lanes each finds its part by itself.
+static constexpr int kChunkPlanned = 65;
 
 static ChunkPlan plan_chunk(const kap_kv_cache *kv, int batch, int num_tokens, int max_seq_len,
                             int window, int sinks) {
   ChunkPlan p;
-  const int waves = kap::chunk_waves(kv->kv_dtype, kv->head_dim), tall = 32 * waves;
+  const int D = kv->head_dim;
+  const bool f32 = kv->kv_dtype == KAP_DT_F32;
+  const int waves = kap::chunk_waves(kv->kv_dtype, D), tall = 32 * waves;
   const long long Hkv = kv->num_kv_heads;
   const long long rows = (long long)num_tokens * (kv->num_q_heads / Hkv);
   p.window = window > 0 && window < max_seq_len ? window : 0;
-  p.few_rows = 128;
+  // (256-dim float32 heads have no staged walk)
+  p.few_rows = f32 && D == 256 ? 0x7fffffff : 128;
   p.target = device_cus();
-  p.tall_cost = 4;
-  p.few_cost = kv->kv_dtype == KAP_DT_FP8_E4M3FN ? 2 : 3;
+  // in eighths of a microsecond: 32 keys with all rows of a tall block, and as their
+  // bytes come from memory
+  p.tall_cost = std::max(1, f32 ? D * 28 / 128 : D / 16);
+  p.team_cost = std::max(1, 64 * D * elem_bytes(kv->kv_dtype) * 5 / 16384);
   p.tall_least = 8;
-  p.few_least = 2;
-  // parts: a block of rows each, and twice the target for what is split
-  const long long tall_blocks = rows / tall + std::min<long long>(batch, rows / (p.few_rows + 1));
-  const long long few_parts = (rows / 32 + batch) * Hkv + 2ll * p.target * waves;
-  p.grid = tall_blocks * Hkv + 2ll * p.target + (few_parts + waves - 1) / waves;
-  // the most steps of a block, hence the most parts of a row
+  p.team_least = 16;
+  // workgroups: a block each, and what filling the device to a multiple of its size adds
+  const long long tall_blocks =
+      rows <= p.few_rows ? 0 : rows / tall + std::min<long long>(batch, rows / (p.few_rows + 1ll));
+  const long long few_blocks = rows / 32 + batch;
+  const long long teams = p.few_rows > 128 ? few_blocks * Hkv
+                                           : std::min(few_blocks * Hkv, std::max<long long>(
+                                                 4ll * batch * Hkv, 2ll * p.target));
+  p.grid = tall_blocks * Hkv + teams + p.target;
+  // What is split: fewer workgroups than the grid, each with the rows of a tall block or, of
+  // teams, at most 32; only where a block has more steps than a part's least.
   long long steps = cdiv(max_seq_len, 32);
   if (p.window)
     steps = std::min<long long>(steps, cdiv(std::min(sinks, max_seq_len), 32) + 2 +
                                            ((long long)p.window + std::min(num_tokens, tall)) / 32);
-  const long long most = (steps + p.few_least - 1) / p.few_least;
-  p.part_rows = most <= 1 ? 0
-                          : std::min<long long>(2 * rows * Hkv * most, 4ll * p.target * tall);
-  p.part_o = round_up(sizeof(int64_t) * batch + sizeof(int32_t) * (4 * (size_t)batch + 4), 256);
-  p.part_lse = p.part_o + round_up((size_t)p.part_rows * kv->head_dim * sizeof(float), 256);
-  p.total = p.part_lse + round_up((size_t)p.part_rows * sizeof(float), 256);
+  const bool splits = steps > std::min(p.tall_least, p.team_least);
+  const long long parts = splits ? 2ll * p.target : 0;
+  const long long part_rows =
+      std::min(parts * (tall_blocks > 0 ? tall : 32), 2 * rows * Hkv * steps);
+  // (as many counters for every call: one's scratch is never another's counters)
+  p.map = round_up((size_t)p.target * kap::kTicketStride * sizeof(int32_t), 256);
+  p.part_o = p.map + (batch < kChunkPlanned
+                          ? 0
+                          : round_up(sizeof(int64_t) * batch + sizeof(int32_t) * (6 * (size_t)batch + 4), 256));
+  p.part_lse = p.part_o + round_up((size_t)part_rows * D * sizeof(float), 256);
+  p.total = p.part_lse + round_up((size_t)part_rows * sizeof(float), 256);
   return p;
 }
 
@@ -1410,15 +1427,16 @@ kap_status kap_chunk_attention(const kap_kv_cache *kv, int32_t batch, int32_t nu
   a.sinks = p.window ? std::min(sinks, max_seq_len) : 0;
   a.scale_log2 = (sm_scale < 0 ? -sm_scale : sm_scale) * kap::kLog2e;
   a.q_sign = sm_scale < 0 ? (kv->q_dtype == KAP_DT_F32 ? 0x80000000u : 0x80008000u) : 0;
+  a.rcp_g = 1.0 / a.G;
   a.few_rows = p.few_rows;
   a.target = p.target;
   a.tall_cost = p.tall_cost;
-  a.few_cost = p.few_cost;
+  a.team_cost = p.team_cost;
   a.tall_least = p.tall_least;
-  a.few_least = p.few_least;
+  a.team_least = p.team_least;
   a.grid = p.grid;
-  a.part_rows = p.part_rows;
-  a.map = base;
+  a.tickets = reinterpret_cast<int32_t *>(base);
+  a.map = batch < kChunkPlanned ? nullptr : base + p.map;
   a.part_o = reinterpret_cast<float *>(base + p.part_o);
   a.part_lse = reinterpret_cast<float *>(base + p.part_lse);
   a.out = out;

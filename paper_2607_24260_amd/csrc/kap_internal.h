@@ -231,13 +231,14 @@ struct ChunkArgs {
   int window, sinks;             // window 0: none
   float scale_log2;              // |sm_scale| * log2(e)
   uint32_t q_sign;               // flips the sign of a word of q if sm_scale < 0
-  int few_rows;                  // rows of a sequence that wavefronts take by themselves
-  int target;                    // workgroups the work is spread over
-  int tall_cost, few_cost;       // of a step of a workgroup, of a wavefront by itself
-  int tall_least, few_least;     // least steps of a part
+  double rcp_g;                  // 1 / G
+  int few_rows;                  // sequences of more rows: tall blocks (attn_chunk.hip)
+  int target;                    // workgroups that run at once
+  int tall_cost, team_cost;      // of a workgroup's step
+  int tall_least, team_least;    // least steps of a part
   int64_t grid;                  // workgroups
-  int64_t part_rows;             // rows of the partials
-  void *map;                     // see attn_chunk.hip
+  int32_t *tickets;              // arrival counters kTicketStride apart, zero between calls
+  void *map;                     // of a large batch, else NULL
   float *part_o, *part_lse;      // [rows][D], [rows]: normalised, log2 domain
   void *out;                     // [num_tokens][Hq][D], q's type
   float *lse;                    // [num_tokens][Hq], or NULL

@@ -1164,16 +1164,11 @@ def _chunk_call(kv: KVCache, q, q_offsets, seq_lens, block_table, max_seq_len, s
         out = torch.zeros_like(q) if out is None else out
         if lse is None:
             lse = torch.zeros((T, kv.num_q_heads), dtype=torch.float32, device=q.device)
-        if workspace is None and need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace, have = _workspace(need, q.device, workspace)
     _dev(out, "out", kv.q_dtype)
     _dev(lse, "lse", torch.float32)
     if out.shape != q.shape or tuple(lse.shape) != (T, kv.num_q_heads):
         raise ValueError("out must have q's shape, lse [num_tokens][num_q_heads]")
-    have = 0
-    if workspace is not None:
-        _dev(workspace, "workspace")
-        have = workspace.numel() * workspace.element_size()
     keep = (kv, q, q_offsets, seq_lens, block_table, out, lse, workspace)
     _here(kv.k_pages, *keep[1:], stream=stream)
     args = (ctypes.byref(kv.struct), B, T, _ptr(q), _ptr(q_offsets), _ptr(seq_lens),

@@ -330,22 +330,30 @@ def test_climbing_logits(dtype):
 
 
 @DTYPES
-def test_the_workspace_holds_scratch_only(dtype):
-    c = Chunks(dtype, [(1, 8000), (260, 3000), (2, 500)], seed=13)
-    want = c.run()
-    need = K.chunk_attention_workspace_bytes(c.kv, 3, c.T, c.most)
+def test_the_workspace_holds_zero_counters_and_scratch(dtype):
+    # one workspace for calls of several sizes, one after the other; the counters come back
+    # zero, what is behind them does not matter
+    calls = [Chunks(dtype, [(1, 8000), (260, 3000), (2, 500)], seed=13),
+             Chunks(dtype, [(1, 900 + 40 * i) for i in range(70)], seed=14),
+             Chunks(dtype, [(1, 20000)], Hq=2, Hkv=1, seed=15)]
+    want = [c.run() for c in calls]
+    need = max(K.chunk_attention_workspace_bytes(c.kv, len(c.lens), c.T, c.most) for c in calls)
+    counters = 64 * torch.cuda.get_device_properties(0).multi_processor_count
     for seed in range(3):
         ws = torch.randint(0, 256, (need,), dtype=torch.uint8, device="cuda",
                            generator=torch.Generator(device="cuda").manual_seed(seed))
-        for x, y in zip(c.run(workspace=ws), want):
-            assert torch.equal(x, y)
+        ws[:counters] = 0
+        for c, w in zip(calls, want):
+            for x, y in zip(c.run(workspace=ws), w):
+                assert torch.equal(x, y)
+            assert not bool(ws[:counters].any())
 
 
 def test_without_lse():
     c = Chunks("bf16", [(1, 3000), (100, 200)], seed=14)
     want = c.run()[0]
     out = torch.full_like(c.q, FILL)
-    ws = torch.empty(K.chunk_attention_workspace_bytes(c.kv, 2, c.T, c.most), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(K.chunk_attention_workspace_bytes(c.kv, 2, c.T, c.most), dtype=torch.uint8, device="cuda")
     off, lens, table = dev_i32(c.offsets), dev_i32(c.lens), dev_i32(c.table)
     import ctypes
     assert K.load_library().kap_chunk_attention(
@@ -370,7 +378,7 @@ def test_captured_with_other_lengths(dtype):
     d = dict(off=dev_i32(c.offsets), lens=dev_i32(c.lens), table=dev_i32(c.table))
     out, lse = torch.full_like(c.q, FILL), torch.full(c.q.shape[:2], FILL, device="cuda")
     most = c.most + 64
-    ws = torch.empty(K.chunk_attention_workspace_bytes(c.kv, 4, c.T, most), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(K.chunk_attention_workspace_bytes(c.kv, 4, c.T, most), dtype=torch.uint8, device="cuda")
     stream = torch.cuda.Stream()
     torch.cuda.synchronize()
     call = K.bind_chunk_attention(c.kv, c.q, d["off"], d["lens"], d["table"], most, c.scale, out, lse, ws,
