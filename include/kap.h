@@ -423,7 +423,7 @@ size_t kap_verify_shared_workspace_bytes(const kap_kv_cache *kv, int32_t batch, 
  * Softmax weights meet V of bf16 and fp8 pages rounded to bf16 (each off by at most
  * 2^-8 of it, as out is); logits, sums and lse are single precision throughout. batch <= 65535,
  * num_tokens * num_q_heads < 2^30.
- *   The workspace keeps arrival counters in its first 64 bytes times the device's
+ *   The workspace keeps arrival counters in its first 128 bytes times the device's
  * compute units: zero when a call starts, and left zero by it; the rest is scratch. So
  * zero-fill it once when allocating it; it then serves any sequence of calls of this
  * kind that fit it, one after the other (other entry points have theirs).

@@ -9,6 +9,7 @@
 #include "block_scan.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace kap {
 namespace {
@@ -20,6 +21,25 @@ constexpr int waves_of(int kv, int D) { return chunk_waves(kv, D); }
 // ---------------------------------------------------------------------------
 // work map
 // ---------------------------------------------------------------------------
+
+// Sum over a wavefront, the same in every lane: a float by row shifts (no LDS), a whole
+// number exactly.
+__device__ __forceinline__ float wave_total(float x) {
+  auto from = [](float v, auto shift, auto rows) {
+    return __int_as_float(dpp_or_zero<decltype(shift)::value, decltype(rows)::value>(__float_as_int(v)));
+  };
+  using std::integral_constant;
+  x += from(x, integral_constant<int, 0x111>(), integral_constant<int, 0xF>());
+  x += from(x, integral_constant<int, 0x112>(), integral_constant<int, 0xF>());
+  x += from(x, integral_constant<int, 0x114>(), integral_constant<int, 0xF>());
+  x += from(x, integral_constant<int, 0x118>(), integral_constant<int, 0xF>());
+  x += from(x, integral_constant<int, 0x142>(), integral_constant<int, 0xA>());
+  x += from(x, integral_constant<int, 0x143>(), integral_constant<int, 0xC>());
+  return __int_as_float(lane63(__float_as_int(x)));
+}
+__device__ __forceinline__ long long wave_total(int x) {   // x >= 0
+  return ((long long)lane63(wave_scan_add(x >> 16)) << 16) + lane63(wave_scan_add(x & 0xffff));
+}
 
 // How the rows of a sequence are taken:
 //   tall: in blocks of 32 rows a wavefront, a workgroup's wavefronts over the same steps;
@@ -115,22 +135,35 @@ struct Cut {
   }
 };
 
-// Workgroups are as long as each other, as near as the costs of steps say: as many as fit
-// the device at once (target), or, where there are more blocks than that, as the next
-// multiple of it. sum(f): that of f(Info) of all sequences, in single precision: every
-// wavefront that computes it finds the same. Small calls go to teams throughout: a tall
-// block's rows would leave most of the device idle.
-template <int WAVES, class Sum>
-__device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum) {
+// Steps of a sequence's longest part.
+__device__ __forceinline__ float part_steps(const Cut &c, Kind k, const Info &f) {
+  return pick(k == kTall, f.tall.most, f.by32.most) / (float)c.splits(k, f);
+}
+
+// Small calls go to teams throughout: a tall block's rows would leave most of the device
+// idle. Blocks are split so that all parts run at once, as long as each other as near as the
+// costs of steps say, or fill as many rounds as the blocks need, or to a half, a third, ..
+// of the longest, if that is expected to end earlier. Parts about as long as each other end in
+// rounds; others with the work over the workgroups that run at once, and half a part more,
+// for which some of them idle. (Costs in eighths of a microsecond; a part 15 us around its
+// steps, twice that if it is split.)
+//   sum(f), most(f): that of f(Info) of all sequences, in single precision: every wavefront
+// that computes it finds the same.
+constexpr float kPartCost = 120.f;
+
+//   ROUNDS: there may be more blocks than workgroups that run at once.
+template <int WAVES, bool ROUNDS, class Sum, class Most>
+__device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum, Most greatest) {
   const float Hkv = (float)a.Hkv, target = (float)a.target;
   Cut c;
-  const double tokens = sum([](const Info &f) { return (double)f.n; });
+  const long long tokens = sum([](const Info &f) { return f.n; });
   const float blocks = sum([](const Info &f) { return (float)f.by32.blocks; }) * Hkv;
   const float steps = sum([](const Info &f) { return (float)f.by32.blocks * f.by32.mean; }) * Hkv;
-  const float few =
-      sum([&](const Info &f) { return f.rows <= a.few_rows ? (float)f.by32.blocks : 0.f; }) * Hkv;
   c.small = blocks <= 2.f * target && steps <= 8.f * target * WAVES;
-  c.solo = few > 2.f * target;
+  c.solo = false;
+  if constexpr (ROUNDS)
+    c.solo = sum([&](const Info &f) { return f.rows <= a.few_rows ? (float)f.by32.blocks : 0.f; }) * Hkv >
+             2.f * target;
   const float tall_cost = (float)a.tall_cost, team_cost = (float)a.team_cost;
   const float total = sum([&](const Info &f) {
     const bool tall = c.kind(a, f) == kTall;
@@ -142,25 +175,57 @@ __device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum) {
     return (float)pick(k == kTall, f.tall.blocks, f.by32.blocks) * (float)c.splits(k, f) *
            (k == kSolo ? 1.f / WAVES : 1.f);
   };
-  c.tall_len = c.team_len = 1e9f;
-  const float least = sum(groups) * Hkv;       // workgroups, with nothing split
-  const float most = ceilf(fmaxf(least / target, 1.f)) * target;
-  float per = fmaxf(total / most, 1.f);
-  bool fits = false;
-  for (int i = 0; i < 5 && !fits; ++i) {
+  auto cut_to = [&](float per) {               // workgroups, with parts of that cost
     c.tall_len = fmaxf(ceilf(per / tall_cost), (float)a.tall_least);
     c.team_len = fmaxf(ceilf(per / team_cost), (float)a.team_least);
-    const float got = sum(groups) * Hkv;
-    fits = got <= most;
-    per *= fmaxf(got / most, 1.05f);
+    return sum(groups) * Hkv;
+  };
+  const float whole = 1e9f, least = cut_to(whole);
+  float best = whole;
+  // (more tokens than there are, offsets that do not ascend: nothing is split)
+  if (tokens <= a.num_tokens && total > 0.f) {
+    // the most rounds that are full with what fits them
+    const float most = ceilf(fmaxf(least / target, 1.f)) * target;
+    float per = fmaxf(total / most, 1.f), n = cut_to(per);
+    for (int i = 0; i < 4 && n > most; ++i) {
+      per *= fmaxf(n / most, 1.05f);
+      n = cut_to(per);
+    }
+    if constexpr (!ROUNDS) {
+      if (n <= most) return c;
+    } else {
+      const float bound = least + 2.f * target;
+      float time = 1e30f, longest = 0.f;
+      // cut to parts of `per`: if it is expected to end earlier
+      auto try_out = [&](float per) {
+        const float n = cut_to(per), mean = total / n;
+        const float part = greatest([&](const Info &f) {
+          const Kind k = c.kind(a, f);
+          return part_steps(c, k, f) * pick(k == kTall, tall_cost, team_cost);
+        });
+        if (per == whole) longest = part;
+        float t;
+        if (n <= target) t = part + kPartCost + (n > least ? kPartCost : 0.f);
+        else
+          t = (kPartCost * n + kPartCost * (n - least)) / target +
+              (part <= 1.25f * mean ? ceilf(n / target) * part : total / target + 0.5f * mean);
+        if (n <= bound && t < time) {
+          time = t;
+          best = per;
+        }
+      };
+      try_out(whole);
+      if (n <= most) try_out(per);
+      for (int i = 2; i <= 4; ++i) try_out(longest / (float)i);
+    }
   }
-  // (more tokens than there are: offsets that do not ascend)
-  if (!fits || tokens > (double)a.num_tokens) c.tall_len = c.team_len = 1e9f;
+  cut_to(best);
   return c;
 }
 
 // What a workgroup does, or with solo blocks a wavefront.
 struct Part {
+  Seq s;
   int b;
   Kind kind;
   int splits, off;             // off: of the parts of a sequence
@@ -183,53 +248,186 @@ __device__ __forceinline__ Parts parts_of(const ChunkArgs &a, const Cut &c, cons
   p.rows = p.splits > 1 ? (long long)p.parts * min(k == kTall ? kRows * WAVES : kRows, f.rows) : 0;
   return p;
 }
+// Parts are handed out the longest first (one that starts late would end alone): sequences
+// in classes of a quarter of an octave of their parts' steps.
+constexpr int kClasses = 8;
+__device__ __forceinline__ int class_of(float longest, float steps) {
+  return (int)fminf(fmaxf(4.f * __builtin_amdgcn_logf(longest / fmaxf(steps, 1e-3f)), 0.f),
+                    (float)(kClasses - 1));
+}
 
-// Of more sequences than lanes the map is made once, by a workgroup before the others start:
-// parts of each kind, then per sequence: parts of its kind before it, its kind and splits,
-// first counter, first row.
-constexpr int kMapHead = 4;
+// Workgroups take tall parts and teams' alternately, in proportion, eight at a time (one of
+// each XCD): the ones keep the matrix units busy, the others the memory. Solo blocks come
+// last. Workgroup w's kind, and in w its place among the parts of that kind.
+__device__ __forceinline__ int place(int tall, int team, int waves, int wave, int &w) {
+  const int nt = (tall + 7) / 8, nm = (team + 7) / 8, group = w >> 3;
+  if (group >= nt + nm) {
+    w = (w - 8 * (nt + nm)) * waves + wave;
+    return kSolo;
+  }
+  const int before = nt == 0 ? 0 : (nm == 0 ? group : (int)((long long)group * nt / (nt + nm)));
+  const bool is_tall = nm == 0 || (nt > 0 && (int)((long long)(group + 1) * nt / (nt + nm)) > before);
+  w = (is_tall ? before : group - before) * 8 + (w & 7);
+  return is_tall ? kTall : kTeam;
+}
+
+// The map of a call with more blocks than run at once, or more sequences than lanes, is made
+// once, by a launch before: the parts of each kind; sequences in the order of their classes;
+// for each of them, in that order, the parts of each kind before it, and what is its own.
+struct MapSeq {
+  int b, splits, ticket, q0;
+  int64_t row0;
+  int n, len;
+};
 struct MapOf {
-  int64_t *row0;
-  int32_t *head, *first[3], *kind, *splits, *ticket;
+  MapSeq *seq;
+  int32_t *head, *first, *order;   // first: [3][batch]
 };
 __device__ __forceinline__ MapOf map_of(const ChunkArgs &a) {
   MapOf m;
-  m.row0 = reinterpret_cast<int64_t *>(a.map);
-  m.head = reinterpret_cast<int32_t *>(m.row0 + a.batch);
-  m.first[0] = m.head + kMapHead;
-  m.first[1] = m.first[0] + a.batch;
-  m.first[2] = m.first[1] + a.batch;
-  m.kind = m.first[2] + a.batch;
-  m.splits = m.kind + a.batch;
-  m.ticket = m.splits + a.batch;
+  m.seq = reinterpret_cast<MapSeq *>(a.map);
+  m.head = reinterpret_cast<int32_t *>(m.seq + a.batch);
+  m.first = m.head + 4;
+  m.order = m.first + 3 * (size_t)a.batch;
   return m;
 }
 
+// Of up to 64 sequences, by one wavefront.
+template <int WAVES>
+__global__ __launch_bounds__(64) void chunk_plan_small_kernel(ChunkArgs a) {
+  const MapOf m = map_of(a);
+  const int lane = threadIdx.x;
+  Seq s{};
+  Info f{};
+  if (lane < a.batch) {
+    s = seq_of(a, lane);
+    f = info_of<WAVES>(a, s);
+  }
+  auto sum = [&](auto g) { return wave_total(g(f)); };
+  auto most = [&](float x) { return __int_as_float(lane63(wave_scan_max(__float_as_int(x)))); };
+  const Cut c = cut_of<WAVES, true>(a, sum, [&](auto g) { return most(g(f)); });
+  const Kind kind = c.kind(a, f);
+  const Parts x = parts_of<WAVES>(a, c, f);
+  const float steps = part_steps(c, kind, f);
+  const int cls = class_of(most(steps), steps);
+  const int merged = wave_scan_add(x.merges) - x.merges;
+  const long long rows = wave_incl(x.rows, lane) - x.rows;
+  int at = 0, before[3] = {0, 0, 0}, first[3] = {0, 0, 0}, place = 0;
+#pragma unroll 1
+  for (int i = 0; i < kClasses; ++i) {
+    const bool in = lane < a.batch && cls == i;
+    const unsigned long long here = __ballot(in);
+    if (!here) continue;
+    if (in) place = at + __popcll(here & ((1ull << lane) - 1));
+    at += __popcll(here);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const int n = in && kind == k ? x.parts : 0, incl = wave_scan_add(n);
+      if (in) first[k] = before[k] + incl - n;
+      before[k] += lane63(incl);
+    }
+  }
+  if (lane < a.batch) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) m.first[k * a.batch + place] = first[k];
+    m.seq[place] = MapSeq{lane, x.splits, merged, s.q0, rows, s.n, s.len};
+  }
+  if (lane == 0)
+    for (int k = 0; k < 3; ++k) m.head[k] = before[k];
+}
+
+// Of more, by a workgroup.
 template <int WAVES>
 __global__ __launch_bounds__(kScanThreads) void chunk_plan_kernel(ChunkArgs a) {
   __shared__ long long s_scan[5][kScanWaves];
   __shared__ double s_sum[kScanWaves];
+  __shared__ int s_count[kClasses][kScanWaves];
   const MapOf m = map_of(a);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Cut c = cut_of<WAVES>(a, [&](auto f) {
-    decltype(f(Info{})) x = 0;
-    for (int b = threadIdx.x; b < a.batch; b += kScanThreads) x += f(info_of<WAVES>(a, seq_of(a, b)));
-    x = wave_sum(x);
+  // f of all sequences, folded by `in_wave` over each wavefront and by `fold` over those
+  auto over_all = [&](auto f, auto in_wave, auto fold) {
+    typedef decltype(in_wave(f(Info{}))) T;
+    T x = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
+      const int b = b0 + threadIdx.x;
+      Info info{};
+      if (b < a.batch) info = info_of<WAVES>(a, seq_of(a, b));
+      x = fold(x, in_wave(f(info)));
+    }
     __syncthreads();
-    if (lane == 0) s_sum[wave] = x;
+    if (lane == 0) s_sum[wave] = (double)x;
     __syncthreads();
     x = 0;
-    for (int w = 0; w < kScanWaves; ++w) x += (decltype(x))s_sum[w];
+#pragma unroll 1
+    for (int w = 0; w < kScanWaves; ++w) x = fold(x, (T)s_sum[w]);
     return x;
-  });
+  };
+  auto sum = [&](auto f) {
+    return over_all(f, [](auto x) { return wave_total(x); }, [](auto x, auto y) { return x + y; });
+  };
+  auto greatest = [&](auto f) {
+    return over_all(
+        f, [](float x) { return __int_as_float(lane63(wave_scan_max(__float_as_int(x)))); },
+        [](float x, float y) { return fmaxf(x, y); });
+  };
+  const Cut c = cut_of<WAVES, true>(a, sum, greatest);
+  const float longest = greatest([&](const Info &f) { return part_steps(c, c.kind(a, f), f); });
+  // their order: how many there are of each class, then the place of each
+  int count[kClasses];
+#pragma unroll
+  for (int i = 0; i < kClasses; ++i) count[i] = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
+      const int b = b0 + threadIdx.x;
+      int cls = -1;
+      if (b < a.batch) {
+        const Info f = info_of<WAVES>(a, seq_of(a, b));
+        cls = class_of(longest, part_steps(c, c.kind(a, f), f));
+      }
+      int rank = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kClasses; ++i) {
+        const unsigned long long here = __ballot(cls == i);
+        if (cls == i) rank = __popcll(here & ((1ull << lane) - 1));
+        if (lane == 0) s_count[i][wave] = __popcll(here);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kClasses; ++i) {
+        int before = 0, all = 0;
+#pragma unroll 1
+        for (int w = 0; w < kScanWaves; ++w) {
+          before += w < wave ? s_count[i][w] : 0;
+          all += s_count[i][w];
+        }
+        if (pass == 1 && cls == i) m.order[count[i] + before + rank] = b;
+        count[i] += all;
+      }
+    }
+    if (pass == 0) {                           // of the classes before
+      int run = 0;
+#pragma unroll
+      for (int i = 0; i < kClasses; ++i) {
+        const int n = count[i];
+        count[i] = run;
+        run += n;
+      }
+    }
+  }
+  __syncthreads();
   long long before[5] = {0, 0, 0, 0, 0};       // parts of each kind, merges, rows
-  for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
-    const int b = b0 + threadIdx.x;
-    const bool in = b < a.batch;
+  for (int i0 = 0; i0 < a.batch; i0 += kScanThreads) {
+    const int i = i0 + threadIdx.x;
+    const bool in = i < a.batch;
     Kind k = kTeam;
     Parts p{0, 0, 0, 0};
+    Seq s{};
+    int b = 0;
     if (in) {
-      const Info f = info_of<WAVES>(a, seq_of(a, b));
+      b = m.order[i];
+      s = seq_of(a, b);
+      const Info f = info_of<WAVES>(a, s);
       k = c.kind(a, f);
       p = parts_of<WAVES>(a, c, f);
     }
@@ -239,21 +437,22 @@ __global__ __launch_bounds__(kScanThreads) void chunk_plan_kernel(ChunkArgs a) {
     scan(x, incl, total, s_scan);
     if (in) {
 #pragma unroll
-      for (int i = 0; i < 3; ++i) m.first[i][b] = (int)(before[i] + incl[i] - x[i]);
-      m.kind[b] = k;
-      m.splits[b] = p.splits;
-      m.ticket[b] = (int)(before[3] + incl[3] - x[3]);
-      m.row0[b] = before[4] + incl[4] - x[4];
+      for (int k = 0; k < 3; ++k) m.first[k * (size_t)a.batch + i] = (int)(before[k] + incl[k] - x[k]);
+      m.seq[i] = MapSeq{b,   p.splits, (int)(before[3] + incl[3] - x[3]), s.q0, before[4] + incl[4] - x[4],
+                        s.n, s.len};
     }
 #pragma unroll
-    for (int i = 0; i < 5; ++i) before[i] += total[i];
+    for (int k = 0; k < 5; ++k) before[k] += total[k];
   }
   if (threadIdx.x == 0)
-    for (int i = 0; i < 3; ++i) m.head[i] = (int)before[i];
+    for (int k = 0; k < 3; ++k) m.head[k] = (int)before[k];
 }
 
-// The last of the sequences whose sum is at most w (by a whole wavefront).
-__device__ __forceinline__ int find(const int32_t *first, int n, int w, int lane) {
+// The last of n ascending sums that is at most w (by a whole wavefront); value: the lane's
+// of the first 64.
+__device__ __forceinline__ int find(const int32_t *first, int value, int n, int w, int lane) {
+  if (n <= 64)
+    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < n && value <= w)) - 1);
   int lo = 0, hi = n;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) / 64, i = lo + lane * step;
@@ -264,60 +463,59 @@ __device__ __forceinline__ int find(const int32_t *first, int n, int w, int lane
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// Workgroups are numbered tall parts first, then teams', then solo blocks.
 template <int WAVES>
 __device__ __forceinline__ bool part_of(const ChunkArgs &a, int w, int wave, int lane, Part &p) {
   if (a.map) {
     const MapOf m = map_of(a);
-    int k = 0;
-    if (w >= m.head[0]) {
-      w -= m.head[0];
-      k = 1;
-      if (w >= m.head[1]) {
-        w = (w - m.head[1]) * WAVES + wave;
-        k = 2;
-        if (w >= m.head[2]) return false;
-      }
-    }
-    const int32_t *first = m.first[0] + (size_t)k * a.batch;
-    p.b = find(first, a.batch, w, lane);
-    p.kind = (Kind)m.kind[p.b];
-    p.splits = m.splits[p.b];
-    p.off = w - first[p.b];
-    p.row0 = m.row0[p.b];
-    p.ticket = m.ticket[p.b];
-    return p.kind == k;
+    const int head[3] = {m.head[0], m.head[1], m.head[2]};
+    int value[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) value[k] = m.first[k * (size_t)a.batch + min(lane, a.batch - 1)];
+    const int k = place(head[0], head[1], WAVES, wave, w);
+    if (w >= pick(k == 0, head[0], pick(k == 1, head[1], head[2]))) return false;
+    const int32_t *first = m.first + k * (size_t)a.batch;
+    const int i = find(first, pick(k == 0, value[0], pick(k == 1, value[1], value[2])), a.batch, w, lane);
+    if (i < 0) return false;
+    const MapSeq x = m.seq[i];
+    p.s = Seq{x.q0, x.n, x.len, x.n * a.G};
+    p.b = x.b;
+    p.kind = (Kind)k;
+    p.splits = x.splits;
+    p.off = w - first[i];
+    p.row0 = x.row0;
+    p.ticket = x.ticket;
+    return p.splits > 0;
   }
+  Seq s{};
   Info f{};
-  if (lane < a.batch) f = info_of<WAVES>(a, seq_of(a, lane));
-  const Cut c = cut_of<WAVES>(a, [&](auto g) { return wave_sum(g(f)); });
+  if (lane < a.batch) {
+    s = seq_of(a, lane);
+    f = info_of<WAVES>(a, s);
+  }
+  const Cut c = cut_of<WAVES, false>(a, [&](auto g) { return wave_total(g(f)); }, 0);
   const Kind kind = c.kind(a, f);
   const Parts x = parts_of<WAVES>(a, c, f);
-  const int merged = wave_scan_add(x.merges) - x.merges;
-  long long rows = 0;
-  {
-    // (rows by 64-bit sums only where something is split)
-    if (__any(x.rows > 0)) rows = wave_incl(x.rows, lane) - x.rows;
+  const int k = place(lane63(wave_scan_add(kind == kTall ? x.parts : 0)),
+                      lane63(wave_scan_add(kind == kTeam ? x.parts : 0)), WAVES, wave, w);
+  const int n = kind == k ? x.parts : 0, incl = wave_scan_add(n);
+  const unsigned long long hit = __ballot(w >= incl - n && w < incl);
+  if (!hit) return false;
+  const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
+  auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+  p.s = Seq{of(s.q0), of(s.n), of(s.len), of(s.rows)};
+  p.b = l;
+  p.kind = (Kind)k;
+  p.splits = of(x.splits);
+  p.off = w - of(incl - n);
+  p.row0 = 0;
+  p.ticket = 0;
+  if (p.splits > 1) {
+    const int merged = wave_scan_add(x.merges) - x.merges;
+    const long long rows = wave_incl(x.rows, lane) - x.rows;
+    p.ticket = of(merged);
+    p.row0 = (int64_t)of((int)(rows >> 32)) << 32 | (uint32_t)of((int)rows);
   }
-#pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    const int mine = kind == k ? x.parts : 0, incl = wave_scan_add(mine);
-    const unsigned long long hit = __ballot(w >= incl - mine && w < incl);
-    if (hit) {
-      const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)hit) - 1);
-      p.b = l;
-      p.kind = (Kind)k;
-      p.splits = __builtin_amdgcn_readlane(x.splits, l);
-      p.off = w - __builtin_amdgcn_readlane(incl - mine, l);
-      p.row0 = (int64_t)__builtin_amdgcn_readlane((int)(rows >> 32), l) << 32 |
-               (uint32_t)__builtin_amdgcn_readlane((int)rows, l);
-      p.ticket = __builtin_amdgcn_readlane(merged, l);
-      return true;
-    }
-    w -= lane63(incl);
-    if (k == 1) w = w * WAVES + wave;
-  }
-  return false;
+  return true;
 }
 
 // What a wavefront does: rows [r0, r1) of a sequence's KV head g over steps of its block's
@@ -347,7 +545,7 @@ __device__ __forceinline__ bool item_of(const ChunkArgs &a, int w, int wave, int
   if (!part_of<WAVES>(a, w, wave, lane, p)) return false;
   it.b = p.b;
   it.kind = p.kind;
-  it.s = seq_of(a, p.b);
+  it.s = p.s;
   const int size = p.kind == kTall ? kRows * WAVES : kRows, blocks = (it.s.rows + size - 1) / size;
   int block, split = 0;
   if (p.kind == kTall) {                       // the longest first; KV heads share out the XCDs
@@ -1362,7 +1560,10 @@ void launch_d(const ChunkArgs &a, hipStream_t s) {
   constexpr int kWaves = waves_of(KV, D);
   const dim3 grid((unsigned)std::min<long long>(a.grid, kAlongX), 1,
                   (unsigned)((a.grid + kAlongX - 1) / kAlongX));
-  if (a.map) hipLaunchKernelGGL(chunk_plan_kernel<kWaves>, dim3(1), dim3(kScanThreads), 0, s, a);
+  if (a.map && a.batch <= 64)
+    hipLaunchKernelGGL(chunk_plan_small_kernel<kWaves>, dim3(1), dim3(64), 0, s, a);
+  else if (a.map)
+    hipLaunchKernelGGL(chunk_plan_kernel<kWaves>, dim3(1), dim3(kScanThreads), 0, s, a);
   hipLaunchKernelGGL((attn_chunk_kernel<KV, D>), grid, dim3(64 * kWaves), 0, s, a);
 }
 

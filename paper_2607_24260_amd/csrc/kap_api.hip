@@ -1302,12 +1302,10 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
 // work is cut by.
 struct ChunkPlan {
   int few_rows, target, tall_cost, team_cost, tall_least, team_least, window;
+  bool planned;                  // the work map is made by a launch of its own
   long long grid;
   size_t map, part_o, part_lse, total;
 };
-
-// Up to as many sequences as a wavefront has lanes each finds its part by itself.
-static constexpr int kChunkPlanned = 65;
 
 static ChunkPlan plan_chunk(const kap_kv_cache *kv, int batch, int num_tokens, int max_seq_len,
                             int window, int sinks) {
@@ -1327,29 +1325,31 @@ static ChunkPlan plan_chunk(const kap_kv_cache *kv, int batch, int num_tokens, i
   p.team_cost = std::max(1, 64 * D * elem_bytes(kv->kv_dtype) * 5 / 16384);
   p.tall_least = 8;
   p.team_least = 16;
-  // workgroups: a block each, and what filling the device to a multiple of its size adds
+  // workgroups: a block each, and what splitting may add
   const long long tall_blocks =
       rows <= p.few_rows ? 0 : rows / tall + std::min<long long>(batch, rows / (p.few_rows + 1ll));
   const long long few_blocks = rows / 32 + batch;
   const long long teams = p.few_rows > 128 ? few_blocks * Hkv
                                            : std::min(few_blocks * Hkv, std::max<long long>(
                                                  4ll * batch * Hkv, 2ll * p.target));
-  p.grid = tall_blocks * Hkv + teams + p.target;
-  // What is split: fewer workgroups than the grid, each with the rows of a tall block or, of
-  // teams, at most 32; only where a block has more steps than a part's least.
+  // Workgroups find their part by themselves if a wavefront has a lane for every sequence and
+  // they all run at once; else a launch before them writes a map.
+  p.planned = batch > 64 || tall_blocks * Hkv + teams > p.target;
+  p.grid = tall_blocks * Hkv + teams + 2ll * p.target + 16;   // (16: places by eights)
+  // What is split is at most 2 target blocks and 4 target parts, each with the rows of a
+  // tall block or, of teams, at most 32; and only where a block has more steps than a
+  // part's least.
   long long steps = cdiv(max_seq_len, 32);
   if (p.window)
     steps = std::min<long long>(steps, cdiv(std::min(sinks, max_seq_len), 32) + 2 +
                                            ((long long)p.window + std::min(num_tokens, tall)) / 32);
   const bool splits = steps > std::min(p.tall_least, p.team_least);
-  const long long parts = splits ? 2ll * p.target : 0;
+  const long long parts = splits ? 4ll * p.target : 0;
   const long long part_rows =
       std::min(parts * (tall_blocks > 0 ? tall : 32), 2 * rows * Hkv * steps);
   // (as many counters for every call: one's scratch is never another's counters)
-  p.map = round_up((size_t)p.target * kap::kTicketStride * sizeof(int32_t), 256);
-  p.part_o = p.map + (batch < kChunkPlanned
-                          ? 0
-                          : round_up(sizeof(int64_t) * batch + sizeof(int32_t) * (6 * (size_t)batch + 4), 256));
+  p.map = round_up((size_t)2 * p.target * kap::kTicketStride * sizeof(int32_t), 256);
+  p.part_o = p.map + (p.planned ? round_up(48 * (size_t)batch + 16, 256) : 0);
   p.part_lse = p.part_o + round_up((size_t)part_rows * D * sizeof(float), 256);
   p.total = p.part_lse + round_up((size_t)part_rows * sizeof(float), 256);
   return p;
@@ -1436,7 +1436,7 @@ kap_status kap_chunk_attention(const kap_kv_cache *kv, int32_t batch, int32_t nu
   a.team_least = p.team_least;
   a.grid = p.grid;
   a.tickets = reinterpret_cast<int32_t *>(base);
-  a.map = batch < kChunkPlanned ? nullptr : base + p.map;
+  a.map = p.planned ? base + p.map : nullptr;
   a.part_o = reinterpret_cast<float *>(base + p.part_o);
   a.part_lse = reinterpret_cast<float *>(base + p.part_lse);
   a.out = out;

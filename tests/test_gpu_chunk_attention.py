@@ -338,7 +338,7 @@ def test_the_workspace_holds_zero_counters_and_scratch(dtype):
              Chunks(dtype, [(1, 20000)], Hq=2, Hkv=1, seed=15)]
     want = [c.run() for c in calls]
     need = max(K.chunk_attention_workspace_bytes(c.kv, len(c.lens), c.T, c.most) for c in calls)
-    counters = 64 * torch.cuda.get_device_properties(0).multi_processor_count
+    counters = 128 * torch.cuda.get_device_properties(0).multi_processor_count
     for seed in range(3):
         ws = torch.randint(0, 256, (need,), dtype=torch.uint8, device="cuda",
                            generator=torch.Generator(device="cuda").manual_seed(seed))
