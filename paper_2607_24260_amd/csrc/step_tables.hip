@@ -18,7 +18,9 @@
 namespace kap {
 namespace {
 
-constexpr int kThreads = kScanThreads, kWaves = kThreads / 64;
+constexpr int kSmall = 256;                    // sequences that a small workgroup takes
+constexpr int kOwn = 4;                        // pages that a thread moves for its sequence
+constexpr int kRuns = 8;                       // runs of 64 that a wavefront moves at once
 constexpr int kTailThreads = 256;
 constexpr int kTailOffsets = 8192;             // offsets that the second launch keeps in LDS
 
@@ -40,10 +42,59 @@ __device__ __forceinline__ long long wrapped(long long x, long long size) {
   return x >= size ? x - size : x;
 }
 
+// Moves n pages of each lane between its table entries and the ring's, from entry r0 on: up
+// to kOwn by the lane itself, more by the wavefront, in runs of 64, several at once, of one
+// lane or of several.
+template <bool TAKE>
+__device__ __forceinline__ void move_pages(const StepArgs &a, int n, int32_t *table, int r0) {
+  const int lane = threadIdx.x & 63;
+  auto ring_at = [&](int first, int i) {
+    const unsigned at = (unsigned)first + (unsigned)i, size = a.ring_size;
+    return a.ring + (at >= size ? at - size : at);
+  };
+  {
+    int32_t page[kOwn];
+    const bool own = n <= kOwn;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (own && i < n) page[i] = TAKE ? *ring_at(r0, i) : table[i];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (own && i < n) *(TAKE ? table + i : ring_at(r0, i)) = page[i];
+  }
+  unsigned long long left = __ballot(n > kOwn);
+  const uint64_t mine = reinterpret_cast<uint64_t>(table);
+  int at = 0;
+  while (left) {
+    int32_t page[kRuns], *to[kRuns];
+    bool in[kRuns];
+#pragma unroll
+    for (int u = 0; u < kRuns; ++u) {
+      const int l = left ? __builtin_amdgcn_readfirstlane(__ffsll((long long)left) - 1) : 0;
+      const int count = left ? __builtin_amdgcn_readlane(n, l) : 0, i = at + lane;
+      int32_t *const entry = reinterpret_cast<int32_t *>(
+                                 (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), l) << 32 |
+                                 (uint32_t)__builtin_amdgcn_readlane((int)mine, l)) + i;
+      in[u] = i < count;
+      int32_t *const slot = ring_at(__builtin_amdgcn_readlane(r0, l), in[u] ? i : 0);
+      to[u] = TAKE ? entry : slot;
+      if (in[u]) page[u] = *(TAKE ? slot : entry);
+      at += 64;
+      if (at >= count) {
+        left &= left - 1;
+        at = 0;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kRuns; ++u)
+      if (in[u]) *to[u] = page[u];
+  }
+}
+
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepArgs a) {
+  constexpr int kWaves = kThreads / 64;
   __shared__ long long s_scan[3][kWaves];
-  __shared__ long long s_back[kThreads];
-  __shared__ int s_need[kThreads], s_have[kThreads], s_held[kThreads];
   __shared__ int s_first[kThreads + 1], s_len[kThreads];
   const int tid = threadIdx.x;
   const long long size = a.ring_size;
@@ -71,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepArgs a) {
     }
     const int have = bad ? 0 : (len + kPage - 1) / kPage;
     {
-      const long long x[1] = {add};
+      const int x[1] = {add};
       long long incl[1], total[1];
       scan(x, incl, total, s_scan);
       if (add > 0 && asked + incl[0] > a.num_tokens) {
@@ -82,7 +133,7 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepArgs a) {
     }
     int need = bad ? 0 : max(0, (keep + add + kPage - 1) / kPage - have);
     {
-      const long long x[1] = {need};
+      const int x[1] = {need};
       long long incl[1], total[1];
       scan(x, incl, total, s_scan);
       if (need > 0 && wanted + incl[0] > count) {
@@ -92,13 +143,9 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepArgs a) {
       wanted += total[0];
     }
     const int held = bad ? 0 : max((keep + add + kPage - 1) / kPage, pinned);
-    const long long x[3] = {add, need, max(0, have - held)};
+    const int x[3] = {add, need, max(0, have - held)};
     long long incl[3], total[3];
     scan(x, incl, total, s_scan);
-    s_need[tid] = (int)(incl[1] - x[1]);
-    s_have[tid] = have;
-    s_back[tid] = incl[2] - x[2];
-    s_held[tid] = held;
     s_first[tid] = (int)(tokens + incl[0] - x[0]);
     s_len[tid] = keep + add;
     if (in) {
@@ -109,16 +156,11 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(StepArgs a) {
     __syncthreads();
     // pages from the front of the ring, and back to its end: the first are among the
     // `count` that were there, the second go beyond them, so no entry is both
-    for (long long k = tid; k < total[1]; k += kThreads) {
-      const int j = last_at_most(s_need, kThreads, k);
-      a.table[(size_t)(b0 + j) * a.stride + s_have[j] + (k - s_need[j])] =
-          a.ring[wrapped(head + taken + k, size)];
-    }
-    for (long long k = tid; k < total[2] && returned + k < size - count; k += kThreads) {
-      const int j = last_at_most(s_back, kThreads, k);
-      a.ring[wrapped(head + count + returned + k, size)] =
-          a.table[(size_t)(b0 + j) * a.stride + s_held[j] + (k - s_back[j])];
-    }
+    int32_t *const row = a.table + (size_t)b * a.stride;
+    move_pages<true>(a, need, row + have, (int)wrapped(head + taken + incl[1] - need, size));
+    const long long before = returned + incl[2] - x[2];
+    move_pages<false>(a, (int)min((long long)x[2], max(size - count - before, 0ll)), row + held,
+                      (int)wrapped(head + count + min(before, size), size));
     tokens += total[0];
     taken += total[1];
     returned += total[2];
@@ -165,8 +207,14 @@ __global__ __launch_bounds__(kTailThreads) void step_slots_kernel(StepArgs a) {
 }  // namespace
 
 hipError_t launch_step_tables(StepArgs a, int cus, hipStream_t s) {
-  a.tokens_here = a.batch <= kThreads && a.num_tokens <= 4 * kThreads;
-  hipLaunchKernelGGL(step_tables_kernel, dim3(1), dim3(kThreads), 0, s, a);
+  // Slots of a step of up to 4096 tokens are written by the first launch, if its threads hold
+  // all sequences' offsets.
+  const bool small = a.batch <= kSmall;
+  a.tokens_here = a.batch <= kScanThreads && a.num_tokens <= 4 * (small ? kSmall : kScanThreads);
+  if (small)
+    hipLaunchKernelGGL(step_tables_kernel<kSmall>, dim3(1), dim3(kSmall), 0, s, a);
+  else
+    hipLaunchKernelGGL(step_tables_kernel<kScanThreads>, dim3(1), dim3(kScanThreads), 0, s, a);
   if (!a.tokens_here && a.num_tokens > 0) {
     const int blocks = (a.num_tokens + kTailThreads - 1) / kTailThreads;
     hipLaunchKernelGGL(step_slots_kernel, dim3(std::min(blocks, 4 * cus)), dim3(kTailThreads), 0, s, a);
