@@ -105,6 +105,57 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
     const int m = a.mask_row[row];
     if (m >= 0 && m < a.num_masks) r.mask = a.masks + (size_t)m * a.mask_stride;
   }
+  uint32_t allowed[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int p = tid + i * kThreads;
+    allowed[i] = r.mask && p < pieces ? bits_at(r.mask, words, v0 + skip + p * kPer) : ~0u;
+  }
+  // The history 16 bytes at a time, from the 16-byte boundary at or before its first token
+  // on: tokens [before, end) from there, of which those below `prompt` are the prompt's.
+  // (A range outside the history counts where it is inside.)
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  constexpr int kAtOnce = 4;
+  const int32_t *told = a.history;
+  uint32_t before = 0, end = 0, prompt = 0;
+  long long there = 0;                         // tokens from `told` on to the end of the array
+  bool low = false;                            // and whether those before the first are in it
+  if (r.told) {
+    const long long start = min(max((long long)a.history_start[row], -(1ll << 31)), a.history_size);
+    const long long lo = start < 0 ? -start : 0, hi = min((long long)len, a.history_size - start);
+    const int32_t *first = a.history + start + lo;
+    before = (uint32_t)(reinterpret_cast<uintptr_t>(first) / 4 & 3);
+    told = first - before;
+    end = hi > lo ? before + (uint32_t)(hi - lo) : 0;
+    there = a.history_size - (start + lo) + before;
+    low = start + lo >= before;
+    const long long own = (long long)(a.prompt_len ? a.prompt_len[row] : 0) - lo + before;
+    prompt = (uint32_t)min(max(own, 0ll), 0xffffffffll);
+  }
+  auto fetch = [&](i32x4 (&token)[kAtOnce], uint32_t j0) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint32_t j = j0 + 4 * k * kThreads;
+      token[k] = i32x4{-1, -1, -1, -1};
+      if (j >= end) continue;
+      // (not across the ends of the array, though within a 16-byte line)
+      if ((j >= before || low) && j + 4ll <= there) {
+        token[k] = *reinterpret_cast<const i32x4 *>(told + j);
+        if (j < before || j + 4 > end) {
+#pragma unroll
+          for (uint32_t c = 0; c < 4; ++c)
+            if (j + c < before || j + c >= end) token[k][c] = -1;
+        }
+      } else {
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c)
+          if (j + c >= before && j + c < end) token[k][c] = told[j + c];
+      }
+    }
+  };
+  i32x4 token[kAtOnce];
+  fetch(token, 4 * tid);
+  const int e_own = e0 + tid, v_own = e_own < e1 ? a.bias_token[e_own] : -1;
   // (a piece's counts are 16-byte aligned in LDS)
   uint32_t *counts = s_counts + (-skip & 3);
   if (r.told) {
@@ -117,51 +168,25 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
     if (tid == 0) s_twice = 0;
   }
   if (r.told || biased) __syncthreads();
-  if (r.told) {
-    // (a range outside the history counts where it is inside)
-    const long long start = min(max((long long)a.history_start[row], -(1ll << 31)), a.history_size);
-    const int prompt = a.prompt_len ? a.prompt_len[row] : 0;
-    const long long lo = start < 0 ? -start : 0;
-    const long long hi = min((long long)len, a.history_size - start);
-    // 16 bytes of it at a time, from the 16-byte boundary at or before its first token on
-    typedef int i32x4 __attribute__((ext_vector_type(4)));
-    const int32_t *first = a.history + start;
-    const int before = (int)(reinterpret_cast<uintptr_t>(first + lo) / 4 & 3);
-    constexpr int kAtOnce = 4;
-    for (long long i0 = lo - before + 4 * tid; i0 < hi; i0 += 4 * kAtOnce * kThreads) {
-      i32x4 token[kAtOnce];
+  for (uint32_t j0 = 4 * tid; j0 < end; j0 += 4 * kAtOnce * kThreads) {
+    if (j0 != 4u * tid) fetch(token, j0);
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const long long i = i0 + 4 * k * kThreads;
-        token[k] = i32x4{-1, -1, -1, -1};
-        // (not across the ends of the array, though within a 16-byte line)
-        if (start + i >= 0 && start + i + 4 <= a.history_size && i < hi) {
-          token[k] = *reinterpret_cast<const i32x4 *>(first + i);
-        } else {
+    for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (i + c >= lo && i + c < hi) token[k][c] = first[i + c];
+      for (int c = 0; c < 4; ++c) {
+        // (n is at most 2^13 and v0 below 2^30: a negative token is far from both)
+        const uint32_t at = (uint32_t)(token[k][c] - v0);
+        if (at < (uint32_t)n) {
+          if (j0 + 4 * k * kThreads + c < prompt) atomicOr(&counts[at], kPrompt);
+          else atomicAdd(&counts[at], 1u);
         }
       }
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const long long i = i0 + 4 * k * kThreads + c;
-          const int v = token[k][c];
-          const uint32_t at = (uint32_t)(v - v0);
-          if (i >= lo && i < hi && v >= 0 && at < (uint32_t)n) {
-            if (i < prompt) atomicOr(&counts[at], kPrompt);
-            else atomicAdd(&counts[at], 1u);
-          }
-        }
-    }
   }
   if (biased)
-    for (int e = e0 + tid; e < e1; e += kThreads) {
-      const int v = a.bias_token[e];
+    for (int e = e_own; e < e1; e += kThreads) {
+      const int v = e == e_own ? v_own : a.bias_token[e];
       const uint32_t at = (uint32_t)(v - v0), bit = 1u << (at & 31);
-      if (v >= 0 && at < (uint32_t)n && (atomicOr(&s_biased[at >> 5], bit) & bit)) s_twice = 1;
+      if (at < (uint32_t)n && (atomicOr(&s_biased[at >> 5], bit) & bit)) s_twice = 1;
     }
   if (r.told || biased) __syncthreads();
 
@@ -197,10 +222,9 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
       }
     }
     if (r.mask) {
-      const uint32_t allowed = bits_at(r.mask, words, v0 + at);
 #pragma unroll
       for (int k = 0; k < kPer; ++k)
-        if (!(allowed >> k & 1u)) out[k] = rounded<T>(-INFINITY);
+        if (!(allowed[i] >> k & 1u)) out[k] = rounded<T>(-INFINITY);
     }
     const uint32_t left = biased ? bits_at(s_biased, (n + 31) / 32, at) & kAll : 0;
     if (left == 0) {
@@ -217,10 +241,9 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
   }
   if (!biased) return;
   if (!s_twice) {
-    for (int e = e0 + tid; e < e1; e += kThreads) {
-      const int v = a.bias_token[e];
-      const uint32_t at = (uint32_t)(v - v0);
-      if (v >= 0 && at < (uint32_t)n) write_one((int)at, a.bias_value[e]);
+    for (int e = e_own; e < e1; e += kThreads) {
+      const uint32_t at = (uint32_t)((e == e_own ? v_own : a.bias_token[e]) - v0);
+      if (at < (uint32_t)n) write_one((int)at, a.bias_value[e]);
     }
     return;
   }
@@ -230,7 +253,7 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
     const int e = last - 1 - tid;              // (thread 0 has the last)
     const int v = e >= e0 ? a.bias_token[e] : -1;
     const uint32_t at = (uint32_t)(v - v0);
-    const bool in_slice = v >= 0 && at < (uint32_t)n;
+    const bool in_slice = at < (uint32_t)n;
     s_list[tid] = in_slice ? (int)at : -1;
     __syncthreads();
     bool counts_here = in_slice && !(s_claimed[at >> 5] >> (at & 31) & 1u);
