@@ -37,6 +37,9 @@ __device__ __forceinline__ float wave_total(float x) {
   x += from(x, integral_constant<int, 0x143>(), integral_constant<int, 0xC>());
   return __int_as_float(lane63(__float_as_int(x)));
 }
+__device__ __forceinline__ long long wave_total(long long x) {
+  return __shfl(wave_incl(x, threadIdx.x & 63), 63, 64);
+}
 __device__ __forceinline__ long long wave_total(int x) {   // x >= 0
   return ((long long)lane63(wave_scan_add(x >> 16)) << 16) + lane63(wave_scan_add(x & 0xffff));
 }
@@ -118,14 +121,15 @@ __device__ __forceinline__ Info info_of(const ChunkArgs &a, const Seq &s) {
 
 template <class T> __device__ __forceinline__ T pick(bool c, T x, T y) { return c ? x : y; }
 
-// The cut: whether every sequence goes to teams, or short ones to wavefronts by themselves,
-// and the steps of a tall part and of a team's.
+// The cut: whether every sequence goes to teams, which ones to wavefronts by themselves, and
+// the steps of a tall part and of a team's.
 struct Cut {
-  bool small, solo;
+  bool small;
+  float solo;                  // blocks of up to so many steps go to wavefronts by themselves
   float tall_len, team_len;
   __device__ __forceinline__ Kind kind(const ChunkArgs &a, const Info &f) const {
     if (!small && f.rows > a.few_rows) return kTall;
-    return solo && f.by32.most <= 8.f ? kSolo : kTeam;
+    return f.by32.most <= solo ? kSolo : kTeam;
   }
   __device__ __forceinline__ int splits(Kind k, const Info &f) const {
     if (k == kSolo) return 1;
@@ -160,10 +164,14 @@ __device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum, Most greatest
   const float blocks = sum([](const Info &f) { return (float)f.by32.blocks; }) * Hkv;
   const float steps = sum([](const Info &f) { return (float)f.by32.blocks * f.by32.mean; }) * Hkv;
   c.small = blocks <= 2.f * target && steps <= 8.f * target * WAVES;
-  c.solo = false;
-  if constexpr (ROUNDS)
-    c.solo = sum([&](const Info &f) { return f.rows <= a.few_rows ? (float)f.by32.blocks : 0.f; }) * Hkv >
-             2.f * target;
+  // (many blocks: those no longer than about a wavefront's share of them all)
+  c.solo = -1.f;
+  if constexpr (ROUNDS) {
+    auto few = [&](const Info &f) { return f.rows <= a.few_rows ? (float)f.by32.blocks : 0.f; };
+    if (sum(few) * Hkv > 2.f * target)
+      c.solo = fmaxf(8.f, 1.25f * sum([&](const Info &f) { return few(f) * f.by32.mean; }) * Hkv /
+                              (target * WAVES));
+  }
   const float tall_cost = (float)a.tall_cost, team_cost = (float)a.team_cost;
   const float total = sum([&](const Info &f) {
     const bool tall = c.kind(a, f) == kTall;
@@ -344,23 +352,19 @@ __global__ __launch_bounds__(kScanThreads) void chunk_plan_kernel(ChunkArgs a) {
   __shared__ int s_count[kClasses][kScanWaves];
   const MapOf m = map_of(a);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // (the first sequence of each thread, kept: often there are no others)
+  auto info_at = [&](int b) { return b < a.batch ? info_of<WAVES>(a, seq_of(a, b)) : Info{}; };
+  const Info kept = info_at(threadIdx.x);
   // f of all sequences, folded by `in_wave` over each wavefront and by `fold` over those
   auto over_all = [&](auto f, auto in_wave, auto fold) {
     typedef decltype(in_wave(f(Info{}))) T;
-    T x = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += kScanThreads) {
-      const int b = b0 + threadIdx.x;
-      Info info{};
-      if (b < a.batch) info = info_of<WAVES>(a, seq_of(a, b));
-      x = fold(x, in_wave(f(info)));
-    }
+    T x = in_wave(f(kept));
+    for (int b0 = kScanThreads; b0 < a.batch; b0 += kScanThreads)
+      x = fold(x, in_wave(f(info_at(b0 + threadIdx.x))));
     __syncthreads();
     if (lane == 0) s_sum[wave] = (double)x;
     __syncthreads();
-    x = 0;
-#pragma unroll 1
-    for (int w = 0; w < kScanWaves; ++w) x = fold(x, (T)s_sum[w]);
-    return x;
+    return in_wave(lane < kScanWaves ? (T)s_sum[lane] : (T)0);
   };
   auto sum = [&](auto f) {
     return over_all(f, [](auto x) { return wave_total(x); }, [](auto x, auto y) { return x + y; });
@@ -381,7 +385,7 @@ __global__ __launch_bounds__(kScanThreads) void chunk_plan_kernel(ChunkArgs a) {
       const int b = b0 + threadIdx.x;
       int cls = -1;
       if (b < a.batch) {
-        const Info f = info_of<WAVES>(a, seq_of(a, b));
+        const Info f = b0 == 0 ? kept : info_at(b);
         cls = class_of(longest, part_steps(c, c.kind(a, f), f));
       }
       int rank = 0;
@@ -395,12 +399,10 @@ __global__ __launch_bounds__(kScanThreads) void chunk_plan_kernel(ChunkArgs a) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kClasses; ++i) {
-        int before = 0, all = 0;
-#pragma unroll 1
-        for (int w = 0; w < kScanWaves; ++w) {
-          before += w < wave ? s_count[i][w] : 0;
-          all += s_count[i][w];
-        }
+        const int mine = lane < kScanWaves ? s_count[i][lane] : 0, incl = wave_scan_add(mine);
+        const int all = lane63(incl);
+        const int before =
+            __builtin_amdgcn_readlane(incl - mine, __builtin_amdgcn_readfirstlane(wave));
         if (pass == 1 && cls == i) m.order[count[i] + before + rank] = b;
         count[i] += all;
       }
