@@ -190,8 +190,9 @@ __device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum, Most greatest
   };
   const float whole = 1e9f, least = cut_to(whole);
   float best = whole;
-  // (more tokens than there are, offsets that do not ascend: nothing is split)
-  if (tokens <= a.num_tokens && total > 0.f) {
+  // (nothing is split: with more tokens than there are, as offsets say that do not ascend;
+  // or where the float counts below would not be exact, and the counters' number relies on them)
+  if (tokens <= a.num_tokens && total > 0.f && least <= 1048576.f) {
     // the most rounds that are full with what fits them
     const float most = ceilf(fmaxf(least / target, 1.f)) * target;
     float per = fmaxf(total / most, 1.f), n = cut_to(per);
@@ -486,7 +487,7 @@ __device__ __forceinline__ bool part_of(const ChunkArgs &a, int w, int wave, int
     p.off = w - first[i];
     p.row0 = x.row0;
     p.ticket = x.ticket;
-    return p.splits > 0;
+    return p.splits > 0 && p.off >= 0;         // (offsets that do not ascend)
   }
   Seq s{};
   Info f{};
@@ -989,16 +990,11 @@ template <int KV, int D> constexpr bool has_lds() { return !q_in_lds<KV, D>(); }
 // 16-byte words of a stage's K, and as many of its V.
 template <int KV, int D> constexpr int half_words() { return stage_steps<D>() * operands<KV, D>() * 64; }
 
-// A step's K or V operands in LDS, from the lane's first on.
+// A step's K operands in LDS, from the lane's first on.
 template <int KV, int D>
 struct StagedKeys {
   const u32x4 *at;
   __device__ u32x4 key(int c) const { return at[c * 64]; }
-};
-template <int KV, int D>
-struct StagedValues {
-  const u32x4 *at;
-  __device__ u32x4 value(int y, int db) const { return at[(y * (D / 32) + db) * 64]; }
 };
 
 // Operands that a wavefront brings in, on their way: every WAVES-th of a stage's K, and of
