@@ -453,6 +453,9 @@ def _step_call(seq_lens, add, block_table, free_pages, free_state, keep, pinned_
         with torch.cuda.stream(stream):
             outputs = {name: torch.empty(sizes[name], dtype=dt(name), device=seq_lens.device)
                        if t is None else t for name, t in outputs.items()}
+            if B == 0:                             # (nothing is run: what such a step leaves)
+                outputs["free_out"].copy_(free_state)
+                outputs["q_offsets"].zero_()
     checked = [("add", add, B, torch.int32), ("free_state", free_state, 2, torch.int32),
                ("keep", keep, B, torch.int32), ("pinned_blocks", pinned_blocks, B, torch.int32)]
     checked += [(name, t, sizes[name], dt(name)) for name, t in outputs.items()]
@@ -1139,10 +1142,15 @@ def verify_shared(kv: KVCache, q, seq_lens, full_block_table, max_seq_len: int, 
     return res
 
 
+def _int32(x) -> int:
+    """A window or number of sinks, of which there may be more than any length."""
+    return max(min(int(x), 2 ** 31 - 1), -1)
+
+
 def chunk_attention_workspace_bytes(kv: KVCache, batch: int, num_tokens: int, max_seq_len: int, *,
                                     window: int = 0, sinks: int = 0) -> int:
     return int(load_library().kap_chunk_attention_workspace_bytes(
-        ctypes.byref(kv.struct), batch, num_tokens, max_seq_len, window, sinks))
+        ctypes.byref(kv.struct), batch, num_tokens, max_seq_len, _int32(window), _int32(sinks)))
 
 
 def _chunk_call(kv: KVCache, q, q_offsets, seq_lens, block_table, max_seq_len, sm_scale, out, lse,
@@ -1172,7 +1180,7 @@ def _chunk_call(kv: KVCache, q, q_offsets, seq_lens, block_table, max_seq_len, s
     keep = (kv, q, q_offsets, seq_lens, block_table, out, lse, workspace)
     _here(kv.k_pages, *keep[1:], stream=stream)
     args = (ctypes.byref(kv.struct), B, T, _ptr(q), _ptr(q_offsets), _ptr(seq_lens),
-            _ptr(block_table), block_table.shape[1], int(max_seq_len), int(window), int(sinks),
+            _ptr(block_table), block_table.shape[1], int(max_seq_len), _int32(window), _int32(sinks),
             float(sm_scale), _ptr(out), _ptr(lse), _ptr(workspace), have, _stream(stream))
     return args, (out, lse), keep
 

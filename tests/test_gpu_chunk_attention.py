@@ -364,6 +364,15 @@ def test_without_lse():
     assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("window", [2 ** 31, 2 ** 32 + 5, -2 ** 32 + 5])
+def test_windows_beyond_32_bits_are_none(window):
+    c = Chunks("bf16", [(3, 90), (70, 400)])
+    plain = c.run()
+    c.window = window
+    for got, want in zip(c.run(), plain):
+        assert torch.equal(got, want)
+
+
 def test_nothing_to_do():
     for seqs in ([(0, 5), (0, 0)], [(1, 0)], [(3, 1)]):
         Chunks("bf16", seqs, seed=15).check()

@@ -101,6 +101,12 @@ def test_no_pages_no_tokens():
     both([40, 0], [0, 0], [[1, 2, 3], [0, 0, 0]], [6, 7], (1, 2), 3, keep=[0, 0])
 
 
+def test_a_step_of_no_sequence():
+    got = call([], [], np.zeros((0, 4)), [5, 6, 7], (1, 2), 0)
+    assert got["free_out"].tolist() == [1, 2] and got["q_offsets"].tolist() == [0]
+    assert got["free_pages"].tolist() == [5, 6, 7]
+
+
 def test_long_prompts():
     # pages by the thousand for one sequence; slots of a second launch
     rng = np.random.default_rng(5)
