@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t *words, int n, int v)
 }
 
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
+__global__ __launch_bounds__(kThreads, 8) void adjust_logits_kernel(AdjustArgs a) {
   typedef typename Elem<F32>::type T;
   constexpr int kPer = Elem<F32>::kPer;
   typedef T vec __attribute__((ext_vector_type(kPer)));
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(AdjustArgs a) {
   // on: tokens [before, end) from there, of which those below `prompt` are the prompt's.
   // (A range outside the history counts where it is inside.)
   typedef int i32x4 __attribute__((ext_vector_type(4)));
-  constexpr int kAtOnce = 4;
+  constexpr int kAtOnce = 2;
   const int32_t *told = a.history;
   uint32_t before = 0, end = 0, prompt = 0;
   long long there = 0;                         // tokens from `told` on to the end of the array
