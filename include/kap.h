@@ -21,8 +21,10 @@
  * kap_selected_decode_scheduled then reads instead of computing it in every
  * proposal step (the view is fixed across the k steps of a cycle);
  * kap_selected_decode_masked takes token-granular views; kap_append_kv,
- * kap_rope_append_kv and kap_compact_view maintain the pool; kap_fallback_update switches sequences
- * to full-context access (Sec. 3.2, "Runtime stability and fallback");
+ * kap_rope_append_kv and kap_compact_view maintain the pool; kap_step_tables gives a step's
+ * tokens their pages and slots; kap_chunk_attention takes prompts' chunks and single tokens
+ * in one batch; kap_fallback_update switches sequences to full-context access (Sec. 3.2,
+ * "Runtime stability and fallback"); kap_adjust_logits applies penalties, biases and masks;
  * kap_sample draws tokens; kap_accept_top3 scores draft windows.
  *
  * Conventions shared by every call
@@ -43,7 +45,8 @@
  *   num_kv_heads); the rest of the workspace is scratch whose contents do not
  *   matter, so one workspace may serve any sequence of decode and verify calls
  *   that fit it. Calls that can run concurrently must not share a workspace.
- *   kap_compile_plan's workspace has no such block.
+ *   kap_compile_plan's workspace has no such block; kap_chunk_attention has one of its
+ *   own size (see there), so its workspace serves its own calls only.
  * - Alignment: k_pages and v_pages, and the q and out arrays of decode and
  *   verify, must be 16-byte aligned (KAP_ERR_INVALID_ARGUMENT otherwise).
  * - Grid sizes depend only on host integers, never on device data, so the
@@ -73,7 +76,8 @@
  * num_q_heads a multiple of num_kv_heads; kv_dtype F32 with q_dtype F32, or
  * kv_dtype BF16 / FP8_E4M3FN with q_dtype BF16.
  *
- * Outputs of attention are float32: out = softmax(z) V and lse = natural
+ * Outputs of attention are float32 (kap_chunk_attention's out: q_dtype): out = softmax(z) V
+ * and lse = natural
  * log-sum-exp of z, with z = sm_scale * <q, k>. A row that sees no key gets
  * out = 0 and lse = -inf.
  */

@@ -3,8 +3,25 @@
 //
 // The rows of a (sequence, KV head) are its new tokens times the query heads of the
 // KV head, token by token. A wavefront holds 32 rows and walks 32 keys (two pages) a
-// step (attn_tiles.h). Rows see positions lo <= t < hi and t < sinks; a block of rows
-// walks the steps that hold its sinks, then those from its lowest lo to its highest hi.
+// step (attn_tiles.h): S^T = K Q^T, o <- o e^(m - m') + V^T e^(S^T - m'), with a running
+// reference m that moves only when a logit exceeds it. Rows see positions lo <= t < hi and
+// t < sinks; a block of rows walks the steps that hold its sinks, then those from its
+// lowest lo to its highest hi, those that every row sees in full without masks.
+//
+// A step reads 2 * 32 * D elements and multiplies 4 * 32 * 32 * D for 32 rows: with few
+// rows memory bounds it, with many the matrix units. So single tokens and short chunks are
+// taken 32 rows at a time, a workgroup's wavefronts sharing the keys ("team"); chunks of
+// more than 128 rows by up to 256 rows over the same keys, staged through LDS once for all
+// ("tall": a wavefront reads 1/8 of what it multiplies); and short sequences by the
+// hundred by a wavefront each, which meets no other ("solo": 1000 of 300 tokens 283 us,
+// by teams 465). One launch does all kinds at once. On one device, bf16, 32 heads over 8
+// KV heads of 128 dims:
+//   one token at 2048: 14 us; 64 tokens that see 4096 of 32768: 195 us, 5.5 TB/s;
+//   8192-token prompt: 560 us, 0.98 PFLOP/s (fp8: two chunks of 2048 at 32768: 1000 us,
+//   0.90); 4096 tokens at 16384: 1.1 PFLOP/s. The same loop without the fetches runs at 1.2,
+//   also without exponentials and sums at 1.25, also without LDS reads at 1.4: what
+//   remains beside the products are the operand reads of eight wavefronts from one LDS,
+//   the fetches and the barriers.
 #include "attn_tiles.h"
 #include "block_scan.h"
 
@@ -150,7 +167,8 @@ __device__ __forceinline__ float part_steps(const Cut &c, Kind k, const Info &f)
 // of the longest, if that is expected to end earlier. Parts about as long as each other end in
 // rounds; others with the work over the workgroups that run at once, and half a part more,
 // for which some of them idle. (Costs in eighths of a microsecond; a part 15 us around its
-// steps, twice that if it is split.)
+// steps, twice that if it is split. 48 single tokens and four chunks of 512 at 8192: 311 us
+// unsplit, 365 with all split to fill the rounds, 290 as expected here and longest first.)
 //   sum(f), most(f): that of f(Info) of all sequences, in single precision: every wavefront
 // that computes it finds the same.
 constexpr float kPartCost = 120.f;
@@ -266,7 +284,8 @@ __device__ __forceinline__ int class_of(float longest, float steps) {
 }
 
 // Workgroups take tall parts and teams' alternately, in proportion, eight at a time (one of
-// each XCD): the ones keep the matrix units busy, the others the memory. Solo blocks come
+// each XCD): the ones keep the matrix units busy, the others the memory (48 tokens and four
+// chunks: 299 us, 360 one kind after the other). Solo blocks come
 // last. Workgroup w's kind, and in w its place among the parts of that kind.
 __device__ __forceinline__ int place(int tall, int team, int waves, int wave, int &w) {
   const int nt = (tall + 7) / 8, nm = (team + 7) / 8, group = w >> 3;
@@ -281,7 +300,8 @@ __device__ __forceinline__ int place(int tall, int team, int waves, int wave, in
 }
 
 // The map of a call with more blocks than run at once, or more sequences than lanes, is made
-// once, by a launch before: the parts of each kind; sequences in the order of their classes;
+// once, by a launch before (6 to 8 us, 26 of more than 64 sequences; a workgroup that makes
+// it for itself: 2 to 3): the parts of each kind; sequences in the order of their classes;
 // for each of them, in that order, the parts of each kind before it, and what is its own.
 struct MapSeq {
   int b, splits, ticket, q0;
@@ -983,7 +1003,9 @@ __device__ __forceinline__ void walk_masked(State<D> &st, const ChunkArgs &a, co
 // lane, as the lane reads them back; fp8 widened on the way). A wavefront's logits are a
 // stage ahead of its weights: while the vector unit weighs one stage's keys, the matrix
 // unit multiplies the next one's. So K is staged one ahead of V; there are two buffers of
-// either.
+// either. (8192-token prompt: 590 us, 639 with every wavefront reading the pages by itself;
+// 549 with page ids and scales a stage ahead. Loads straight into LDS, with no registers on
+// the way, were no faster: 0.985 against 1.0 PFLOP/s at 4096 tokens on 16384.)
 // Steps of a stage (256 dims: two would not fit the registers).
 template <int D> constexpr int stage_steps() { return D == 256 ? 1 : 2; }
 template <int KV, int D> constexpr bool has_lds() { return !q_in_lds<KV, D>(); }

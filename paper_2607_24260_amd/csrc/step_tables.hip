@@ -5,12 +5,15 @@
 // Everything is prefix sums over the sequences: of the tokens asked for (which
 // sequences get theirs), of the pages needed (which pages they get), of what is
 // granted and returned. One workgroup takes 1024 sequences at a time, with the sums
-// so far carried along; pages move one to a thread, whose sequence is found in the
-// prefix sums in LDS. There is hardly anything to move (12 bytes a token): what
-// bounds a call is its chain of loads and scans.
+// so far carried along (256 where that is enough: fewer wavefronts to wait for); a
+// sequence's few pages are moved by its thread, many by the wavefront. There is hardly
+// anything to move (12 bytes a token): what bounds a call is its chain of loads and scans,
+// 4.2 us for one sequence, 5 for 64 and their 320 tokens.
 //
 // Slots and positions of a small step are written by the same workgroup; of a
-// larger one by a second launch over all CUs.
+// larger one by a second launch over all CUs. (1000 sequences of which 60 end, and eight
+// prompts' 32768 tokens: 17 us, and 4.5 for the second. The pages' sequences searched for
+// in the prefix sums, page by page, took 32 in all.)
 #include "block_scan.h"
 
 #include <algorithm>
