@@ -19,9 +19,10 @@
 //   one token at 2048: 14 us; 64 tokens that see 4096 of 32768: 195 us, 5.5 TB/s;
 //   8192-token prompt: 560 us, 0.98 PFLOP/s (fp8: two chunks of 2048 at 32768: 1000 us,
 //   0.90); 4096 tokens at 16384: 1.1 PFLOP/s. The same loop without the fetches runs at 1.2,
-//   also without exponentials and sums at 1.25, also without LDS reads at 1.4: what
-//   remains beside the products are the operand reads of eight wavefronts from one LDS,
-//   the fetches and the barriers.
+//   also without exponentials and sums at 1.25, also without LDS reads at 1.4: eight
+//   wavefronts' operands, 1 KB for every product of 32 cycles, take all that LDS gives
+//   (128 bytes a cycle), so the products of the four matrix units and the reads of the one
+//   LDS each last as long as the other; the matrix units are busy half of the time.
 #include "attn_tiles.h"
 #include "block_scan.h"
 
