@@ -167,12 +167,13 @@ __device__ __forceinline__ float part_steps(const Cut &c, Kind k, const Info &f)
 // costs of steps say, or fill as many rounds as the blocks need, or to a half, a third, ..
 // of the longest, if that is expected to end earlier. Parts about as long as each other end in
 // rounds; others with the work over the workgroups that run at once, and half a part more,
-// for which some of them idle. (Costs in eighths of a microsecond; a part 15 us around its
-// steps, twice that if it is split. 48 single tokens and four chunks of 512 at 8192: 311 us
+// for which some of them idle. (Costs in eighths of a microsecond: a part 15 us around its
+// steps; as much again if it is split, 45 where parts of tall blocks leave 256 rows: a
+// 1024-token prompt 47 us whole, 67 in halves, 700 tokens 39 and 73. 48 single tokens and four chunks of 512 at 8192: 311 us
 // unsplit, 365 with all split to fill the rounds, 290 as expected here and longest first.)
 //   sum(f), most(f): that of f(Info) of all sequences, in single precision: every wavefront
 // that computes it finds the same.
-constexpr float kPartCost = 120.f;
+constexpr float kPartCost = 120.f, kTallSplitCost = 360.f;
 
 //   ROUNDS: there may be more blocks than workgroups that run at once.
 template <int WAVES, bool ROUNDS, class Sum, class Most>
@@ -197,6 +198,11 @@ __device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum, Most greatest
     return tall ? (float)f.tall.blocks * f.tall.mean * tall_cost
                 : (float)f.by32.blocks * f.by32.mean * team_cost;
   }) * Hkv;
+  float split_cost = kPartCost;
+  if constexpr (ROUNDS) {
+    if (sum([&](const Info &f) { return c.kind(a, f) == kTall ? 1.f : 0.f; }) > 0.f)
+      split_cost = kTallSplitCost;
+  }
   auto groups = [&](const Info &f) {
     const Kind k = c.kind(a, f);
     return (float)pick(k == kTall, f.tall.blocks, f.by32.blocks) * (float)c.splits(k, f) *
@@ -233,9 +239,9 @@ __device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum, Most greatest
         });
         if (per == whole) longest = part;
         float t;
-        if (n <= target) t = part + kPartCost + (n > least ? kPartCost : 0.f);
+        if (n <= target) t = part + kPartCost + (n > least ? split_cost : 0.f);
         else
-          t = (kPartCost * n + kPartCost * (n - least)) / target +
+          t = (kPartCost * n + split_cost * (n - least)) / target +
               (part <= 1.25f * mean ? ceilf(n / target) * part : total / target + 0.5f * mean);
         if (n <= bound && t < time) {
           time = t;
