@@ -25,6 +25,7 @@
 //   LDS each last as long as the other; the matrix units are busy half of the time.
 #include "attn_tiles.h"
 #include "block_scan.h"
+#include "chunk_cut.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -32,8 +33,6 @@
 namespace kap {
 namespace {
 
-constexpr int kRows = 32;                      // of a wavefront
-constexpr int kKeys = 32;                      // of a step
 constexpr int waves_of(int kv, int D) { return chunk_waves(kv, D); }
 
 // ---------------------------------------------------------------------------
@@ -62,201 +61,6 @@ __device__ __forceinline__ long long wave_total(int x) {   // x >= 0
   return ((long long)lane63(wave_scan_add(x >> 16)) << 16) + lane63(wave_scan_add(x & 0xffff));
 }
 
-// How the rows of a sequence are taken:
-//   tall: in blocks of 32 rows a wavefront, a workgroup's wavefronts over the same steps;
-//   team: in blocks of 32, a workgroup's wavefronts sharing the steps;
-//   solo: in blocks of 32, a wavefront by itself.
-// The steps of tall and team blocks may be split over several workgroups (parts), the last
-// of which merges what they leave.
-enum Kind { kTall, kTeam, kSolo };
-
-// A sequence's part in a call.
-struct Seq {
-  int q0, n, len;    // first row of q, new tokens, length
-  int rows;          // n * G
-};
-__device__ __forceinline__ Seq seq_of(const ChunkArgs &a, int b) {
-  Seq s;
-  s.q0 = clamp_to(a.q_offsets[b], 0, a.num_tokens);
-  s.n = clamp_to(a.q_offsets[b + 1], s.q0, a.num_tokens) - s.q0;
-  s.len = clamp_to(a.seq_lens[b], 0, a.max_len);
-  s.rows = s.n * a.G;
-  return s;
-}
-
-// r / G for 0 <= r < 2^31, given 1 / G to double precision: within one, then mended.
-__device__ __forceinline__ int token_of(const ChunkArgs &a, int r) {
-  int q = (int)((double)r * a.rcp_g);
-  const int rest = r - q * a.G;
-  q += rest >= a.G ? 1 : 0;
-  q -= rest < 0 ? 1 : 0;
-  return q;
-}
-
-// Steps that rows [r0, r1) of a sequence walk: the first `sinks` of them, then those
-// from `from` on.
-struct Range {
-  int sinks, from, steps;
-};
-__device__ __forceinline__ Range range_of(const ChunkArgs &a, const Seq &s, int r0, int r1) {
-  const int p0 = s.len - s.n + token_of(a, r0), p1 = s.len - s.n + token_of(a, r1 - 1);
-  Range r;
-  const int hi = max(0, p1 + 1);
-  const int lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
-  r.from = min(lo, hi) / kKeys;
-  r.sinks = min((min(a.sinks, hi) + kKeys - 1) / kKeys, r.from);
-  r.steps = r.sinks + (hi + kKeys - 1) / kKeys - r.from;
-  return r;
-}
-__device__ __forceinline__ Range block_range(const ChunkArgs &a, const Seq &s, int size, int block) {
-  return range_of(a, s, block * size, min((block + 1) * size, s.rows));
-}
-
-// What the cut goes by: a sequence's blocks, and the steps of one, on average and at most,
-// in blocks of 32 rows and in tall ones.
-struct Steps {
-  int blocks;
-  float mean, most;
-};
-struct Info {
-  int n, rows;
-  Steps by32, tall;
-};
-__device__ __forceinline__ Steps steps_of(const ChunkArgs &a, const Seq &s, int size) {
-  Steps f{(s.rows + size - 1) / size, 0.f, 0.f};
-  if (f.blocks > 0) {
-    const float x = (float)block_range(a, s, size, 0).steps;
-    const float y = (float)block_range(a, s, size, f.blocks - 1).steps;
-    f.mean = 0.5f * (x + y);
-    f.most = fmaxf(x, y);
-  }
-  return f;
-}
-template <int WAVES>
-__device__ __forceinline__ Info info_of(const ChunkArgs &a, const Seq &s) {
-  return Info{s.n, s.rows, steps_of(a, s, kRows), steps_of(a, s, kRows * WAVES)};
-}
-
-template <class T> __device__ __forceinline__ T pick(bool c, T x, T y) { return c ? x : y; }
-
-// The cut: whether every sequence goes to teams, which ones to wavefronts by themselves, and
-// the steps of a tall part and of a team's.
-struct Cut {
-  bool small;
-  float solo;                  // blocks of up to so many steps go to wavefronts by themselves
-  float tall_len, team_len;
-  __device__ __forceinline__ Kind kind(const ChunkArgs &a, const Info &f) const {
-    if (!small && f.rows > a.few_rows) return kTall;
-    return f.by32.most <= solo ? kSolo : kTeam;
-  }
-  __device__ __forceinline__ int splits(Kind k, const Info &f) const {
-    if (k == kSolo) return 1;
-    const float most = pick(k == kTall, f.tall.most, f.by32.most);
-    const float l = pick(k == kTall, tall_len, team_len);
-    return l >= most ? 1 : (int)ceilf(most / l);
-  }
-};
-
-// Steps of a sequence's longest part.
-__device__ __forceinline__ float part_steps(const Cut &c, Kind k, const Info &f) {
-  return pick(k == kTall, f.tall.most, f.by32.most) / (float)c.splits(k, f);
-}
-
-// Small calls go to teams throughout: a tall block's rows would leave most of the device
-// idle. Blocks are split so that all parts run at once, as long as each other as near as the
-// costs of steps say, or fill as many rounds as the blocks need, or to a half, a third, ..
-// of the longest, if that is expected to end earlier. Parts about as long as each other end in
-// rounds; others with the work over the workgroups that run at once, and half a part more,
-// for which some of them idle. (Costs in eighths of a microsecond: a part 15 us around its
-// steps; as much again if it is split, 45 where parts of tall blocks leave 256 rows: a
-// 1024-token prompt 47 us whole, 67 in halves, 700 tokens 39 and 73. 48 single tokens and four chunks of 512 at 8192: 311 us
-// unsplit, 365 with all split to fill the rounds, 290 as expected here and longest first.)
-//   sum(f), most(f): that of f(Info) of all sequences, in single precision: every wavefront
-// that computes it finds the same.
-constexpr float kPartCost = 120.f, kTallSplitCost = 360.f;
-
-//   ROUNDS: there may be more blocks than workgroups that run at once.
-template <int WAVES, bool ROUNDS, class Sum, class Most>
-__device__ __forceinline__ Cut cut_of(const ChunkArgs &a, Sum sum, Most greatest) {
-  const float Hkv = (float)a.Hkv, target = (float)a.target;
-  Cut c;
-  const long long tokens = sum([](const Info &f) { return f.n; });
-  const float blocks = sum([](const Info &f) { return (float)f.by32.blocks; }) * Hkv;
-  const float steps = sum([](const Info &f) { return (float)f.by32.blocks * f.by32.mean; }) * Hkv;
-  c.small = blocks <= 2.f * target && steps <= 8.f * target * WAVES;
-  // (many blocks: those no longer than about a wavefront's share of them all)
-  c.solo = -1.f;
-  if constexpr (ROUNDS) {
-    auto few = [&](const Info &f) { return f.rows <= a.few_rows ? (float)f.by32.blocks : 0.f; };
-    if (sum(few) * Hkv > 2.f * target)
-      c.solo = fmaxf(8.f, 1.25f * sum([&](const Info &f) { return few(f) * f.by32.mean; }) * Hkv /
-                              (target * WAVES));
-  }
-  const float tall_cost = (float)a.tall_cost, team_cost = (float)a.team_cost;
-  const float total = sum([&](const Info &f) {
-    const bool tall = c.kind(a, f) == kTall;
-    return tall ? (float)f.tall.blocks * f.tall.mean * tall_cost
-                : (float)f.by32.blocks * f.by32.mean * team_cost;
-  }) * Hkv;
-  float split_cost = kPartCost;
-  if constexpr (ROUNDS) {
-    if (sum([&](const Info &f) { return c.kind(a, f) == kTall ? 1.f : 0.f; }) > 0.f)
-      split_cost = kTallSplitCost;
-  }
-  auto groups = [&](const Info &f) {
-    const Kind k = c.kind(a, f);
-    return (float)pick(k == kTall, f.tall.blocks, f.by32.blocks) * (float)c.splits(k, f) *
-           (k == kSolo ? 1.f / WAVES : 1.f);
-  };
-  auto cut_to = [&](float per) {               // workgroups, with parts of that cost
-    c.tall_len = fmaxf(ceilf(per / tall_cost), (float)a.tall_least);
-    c.team_len = fmaxf(ceilf(per / team_cost), (float)a.team_least);
-    return sum(groups) * Hkv;
-  };
-  const float whole = 1e9f, least = cut_to(whole);
-  float best = whole;
-  // (nothing is split: with more tokens than there are, as offsets say that do not ascend;
-  // or where the float counts below would not be exact, and the counters' number relies on them)
-  if (tokens <= a.num_tokens && total > 0.f && least <= 1048576.f) {
-    // the most rounds that are full with what fits them
-    const float most = ceilf(fmaxf(least / target, 1.f)) * target;
-    float per = fmaxf(total / most, 1.f), n = cut_to(per);
-    for (int i = 0; i < 4 && n > most; ++i) {
-      per *= fmaxf(n / most, 1.05f);
-      n = cut_to(per);
-    }
-    if constexpr (!ROUNDS) {
-      if (n <= most) return c;
-    } else {
-      const float bound = least + 2.f * target;
-      float time = 1e30f, longest = 0.f;
-      // cut to parts of `per`: if it is expected to end earlier
-      auto try_out = [&](float per) {
-        const float n = cut_to(per), mean = total / n;
-        const float part = greatest([&](const Info &f) {
-          const Kind k = c.kind(a, f);
-          return part_steps(c, k, f) * pick(k == kTall, tall_cost, team_cost);
-        });
-        if (per == whole) longest = part;
-        float t;
-        if (n <= target) t = part + kPartCost + (n > least ? split_cost : 0.f);
-        else
-          t = (kPartCost * n + split_cost * (n - least)) / target +
-              (part <= 1.25f * mean ? ceilf(n / target) * part : total / target + 0.5f * mean);
-        if (n <= bound && t < time) {
-          time = t;
-          best = per;
-        }
-      };
-      try_out(whole);
-      if (n <= most) try_out(per);
-      for (int i = 2; i <= 4; ++i) try_out(longest / (float)i);
-    }
-  }
-  cut_to(best);
-  return c;
-}
-
 // What a workgroup does, or with solo blocks a wavefront.
 struct Part {
   Seq s;
@@ -266,44 +70,12 @@ struct Part {
   int64_t row0;                // rows of the partials of a sequence, from here on
   int ticket;                  // arrival counters of a sequence, from here on
 };
-// Parts of a sequence, blocks that are merged, rows of partials.
-struct Parts {
-  int splits, parts, merges;
-  long long rows;
-};
-template <int WAVES>
-__device__ __forceinline__ Parts parts_of(const ChunkArgs &a, const Cut &c, const Info &f) {
-  const Kind k = c.kind(a, f);
-  Parts p;
-  p.splits = c.splits(k, f);
-  const int blocks = pick(k == kTall, f.tall.blocks, f.by32.blocks) * a.Hkv;
-  p.parts = blocks * p.splits;
-  p.merges = p.splits > 1 ? blocks : 0;
-  p.rows = p.splits > 1 ? (long long)p.parts * min(k == kTall ? kRows * WAVES : kRows, f.rows) : 0;
-  return p;
-}
 // Parts are handed out the longest first (one that starts late would end alone): sequences
 // in classes of a quarter of an octave of their parts' steps.
 constexpr int kClasses = 8;
 __device__ __forceinline__ int class_of(float longest, float steps) {
   return (int)fminf(fmaxf(4.f * __builtin_amdgcn_logf(longest / fmaxf(steps, 1e-3f)), 0.f),
                     (float)(kClasses - 1));
-}
-
-// Workgroups take tall parts and teams' alternately, in proportion, eight at a time (one of
-// each XCD): the ones keep the matrix units busy, the others the memory (48 tokens and four
-// chunks: 299 us, 360 one kind after the other). Solo blocks come
-// last. Workgroup w's kind, and in w its place among the parts of that kind.
-__device__ __forceinline__ int place(int tall, int team, int waves, int wave, int &w) {
-  const int nt = (tall + 7) / 8, nm = (team + 7) / 8, group = w >> 3;
-  if (group >= nt + nm) {
-    w = (w - 8 * (nt + nm)) * waves + wave;
-    return kSolo;
-  }
-  const int before = nt == 0 ? 0 : (nm == 0 ? group : (int)((long long)group * nt / (nt + nm)));
-  const bool is_tall = nm == 0 || (nt > 0 && (int)((long long)(group + 1) * nt / (nt + nm)) > before);
-  w = (is_tall ? before : group - before) * 8 + (w & 7);
-  return is_tall ? kTall : kTeam;
 }
 
 // The map of a call with more blocks than run at once, or more sequences than lanes, is made

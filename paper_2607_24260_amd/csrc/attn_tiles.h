@@ -53,7 +53,7 @@ __device__ __forceinline__ int key_of_reg(int r, int hb) {
 
 constexpr int elem_bytes(int kv) { return kv == kF32 ? 4 : (kv == kBF16 ? 2 : 1); }
 
-__device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return min(max(x, lo), hi); }
+__host__ __device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
 // ---------------------------------------------------------------------------
 // operands

@@ -10,6 +10,7 @@
 #include <mutex>
 #include <string>
 
+#include "chunk_cut.h"
 #include "kap_internal.h"
 
 namespace {
@@ -1298,64 +1299,10 @@ kap_status kap_accept_top3(int32_t batch, int32_t window, int32_t vocab, const v
 // kap_chunk_attention
 // ---------------------------------------------------------------------------
 
-// Sizes of a call's workspace: [arrival counters][map][partial o][partial lse], and what the
-// work is cut by.
-struct ChunkPlan {
-  int few_rows, target, tall_cost, team_cost, tall_least, team_least, window;
-  bool planned;                  // the work map is made by a launch of its own
-  long long grid;
-  size_t map, part_o, part_lse, total;
-};
-
-static ChunkPlan plan_chunk(const kap_kv_cache *kv, int batch, int num_tokens, int max_seq_len,
-                            int window, int sinks) {
-  ChunkPlan p;
-  const int D = kv->head_dim;
-  const bool f32 = kv->kv_dtype == KAP_DT_F32;
-  const int waves = kap::chunk_waves(kv->kv_dtype, D), tall = 32 * waves;
-  const long long Hkv = kv->num_kv_heads;
-  const long long rows = (long long)num_tokens * (kv->num_q_heads / Hkv);
-  p.window = window > 0 && window < max_seq_len ? window : 0;
-  // (256-dim float32 heads have no staged walk)
-  p.few_rows = f32 && D == 256 ? 0x7fffffff : 128;
-  p.target = device_cus();
-  // in eighths of a microsecond: 32 keys with all rows of a tall block, and as their
-  // bytes come from memory
-  p.tall_cost = std::max(1, f32 ? D * 28 / 128 : D / 16);
-  p.team_cost = std::max(1, 64 * D * elem_bytes(kv->kv_dtype) * 5 / 16384);
-  p.tall_least = 8;
-  // (16-bit and fp8: 8 to 64 steps differ by less than the exchange costs; products of float32
-  // take eight times as long: one token at 2048, 128 dims 19.6 us with 4, 29.5 with 16, 256
-  // dims 32 and 76)
-  p.team_least = f32 ? 4 : 16;
-  // workgroups: a block each, and what splitting may add
-  const long long tall_blocks =
-      rows <= p.few_rows ? 0 : rows / tall + std::min<long long>(batch, rows / (p.few_rows + 1ll));
-  const long long few_blocks = rows / 32 + batch;
-  const long long teams = p.few_rows > 128 ? few_blocks * Hkv
-                                           : std::min(few_blocks * Hkv, std::max<long long>(
-                                                 4ll * batch * Hkv, 2ll * p.target));
-  // Workgroups find their part by themselves if a wavefront has a lane for every sequence and
-  // they all run at once; else a launch before them writes a map.
-  p.planned = batch > 64 || tall_blocks * Hkv + teams > p.target;
-  p.grid = tall_blocks * Hkv + teams + 2ll * p.target + 16;   // (16: places by eights)
-  // What is split is at most 2 target blocks and 4 target parts, each with the rows of a
-  // tall block or, of teams, at most 32; and only where a block has more steps than a
-  // part's least.
-  long long steps = cdiv(max_seq_len, 32);
-  if (p.window)
-    steps = std::min<long long>(steps, cdiv(std::min(sinks, max_seq_len), 32) + 2 +
-                                           ((long long)p.window + std::min(num_tokens, tall)) / 32);
-  const bool splits = steps > std::min(p.tall_least, p.team_least);
-  const long long parts = splits ? 4ll * p.target : 0;
-  const long long part_rows =
-      std::min(parts * (tall_blocks > 0 ? tall : 32), 2 * rows * Hkv * steps);
-  // (as many counters for every call: one's scratch is never another's counters)
-  p.map = round_up((size_t)2 * p.target * kap::kTicketStride * sizeof(int32_t), 256);
-  p.part_o = p.map + (p.planned ? round_up(48 * (size_t)batch + 16, 256) : 0);
-  p.part_lse = p.part_o + round_up((size_t)part_rows * D * sizeof(float), 256);
-  p.total = p.part_lse + round_up((size_t)part_rows * sizeof(float), 256);
-  return p;
+static kap::ChunkPlan plan_chunk(const kap_kv_cache *kv, int batch, int num_tokens, int max_seq_len,
+                                 int window, int sinks) {
+  return kap::plan_chunk(kv->kv_dtype, kv->head_dim, kv->num_q_heads, kv->num_kv_heads, batch,
+                         num_tokens, max_seq_len, window, sinks, device_cus());
 }
 
 static bool chunk_sizes_ok(const kap_kv_cache *kv, int batch, int num_tokens, int max_seq_len) {
@@ -1402,7 +1349,7 @@ kap_status kap_chunk_attention(const kap_kv_cache *kv, int32_t batch, int32_t nu
                          (kv->q_dtype == KAP_DT_F32 ? 4 : 2);
   if (overlap(q, q_bytes, out, q_bytes))
     return fail(KAP_ERR_INVALID_ARGUMENT, "out overlaps q");
-  const ChunkPlan p = plan_chunk(kv, batch, num_tokens, max_seq_len, window, sinks);
+  const kap::ChunkPlan p = plan_chunk(kv, batch, num_tokens, max_seq_len, window, sinks);
   if (!workspace || workspace_bytes < p.total)
     return fail(KAP_ERR_WORKSPACE_TOO_SMALL, "workspace needs %zu bytes, got %zu", p.total, workspace_bytes);
   if (!aligned(workspace, 256))
