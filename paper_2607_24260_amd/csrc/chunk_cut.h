@@ -52,7 +52,8 @@ __host__ __device__ __forceinline__ Range range_of(const ChunkArgs &a, const Seq
   const int p0 = s.len - s.n + token_of(a, r0), p1 = s.len - s.n + token_of(a, r1 - 1);
   Range r;
   const int hi = max(0, p1 + 1);
-  const int lo = a.window > 0 ? max(0, p0 - a.window + 1) : 0;
+  // (rows before position 0 see nothing; less a window of nearly 2^31 they would wrap)
+  const int lo = a.window > 0 ? max(0, max(p0, 0) - a.window + 1) : 0;
   r.from = min(lo, hi) / kKeys;
   r.sinks = min((min(a.sinks, hi) + kKeys - 1) / kKeys, r.from);
   r.steps = r.sinks + (hi + kKeys - 1) / kKeys - r.from;

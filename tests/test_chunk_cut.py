@@ -116,3 +116,15 @@ def test_the_cut_of_any_batch_fits(lib, kv, D):
     # every kind was there: planned calls, tall parts, teams', solo ones, merges
     few = kv == F32 and D == 256
     assert met[0] and met[2] and met[3] and met[4] and (met[1] or few), met
+
+
+@pytest.mark.parametrize("n, length, G, r0, r1", [
+    (700, 500, 1, 0, 256),            # 200 rows that see nothing, 56 that see 1 to 56 keys
+    (200, 120, 1, 0, 128), (2 ** 30 - 1, 5, 1, 0, 256), (2 ** 30 - 1, 5, 1, 2 ** 30 - 33, 2 ** 30 - 1)])
+@pytest.mark.parametrize("window", [1, 100, 2 ** 30, 2 ** 31 - 300, 2 ** 31 - 66])
+def test_ranges_of_long_windows_and_more_rows_than_tokens(lib, n, length, G, r0, r1, window):
+    most = 2 ** 31 - 65               # the longest there is; windows below it are not "none"
+    want = seen_steps(n, length, G, window, 0, r0, r1)
+    assert walked(lib, n, length, G, most, window, 0, r0, r1) == want
+    want = seen_steps(n, length, G, window, 40, r0, r1)
+    assert walked(lib, n, length, G, most, window, 40, r0, r1) == want

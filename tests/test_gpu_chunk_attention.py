@@ -373,6 +373,19 @@ def test_windows_beyond_32_bits_are_none(window):
         assert torch.equal(got, want)
 
 
+def test_more_rows_than_tokens_under_the_longest_window():
+    # tall blocks whose first rows are before position 0, a window just below the longest
+    # length there is
+    c = Chunks("bf16", [(700, 500)], Hq=32, Hkv=32, seed=20)
+    plain = c.check()
+    c.most = 2 ** 31 - 65
+    table = np.full((1, -(-c.most // 16)), -5, np.int32)
+    table[:, :c.table.shape[1]] = c.table
+    c.table, c.window = table, c.most - 1
+    for got, want in zip(c.run(), plain):
+        assert torch.equal(got, want)
+
+
 def test_nothing_to_do():
     for seqs in ([(0, 5), (0, 0)], [(1, 0)], [(3, 1)]):
         Chunks("bf16", seqs, seed=15).check()
