@@ -538,7 +538,8 @@ kap_status kap_rope_append_kv(const kap_kv_cache *kv, int32_t num_tokens, const 
  * overlap. A head outside [0, free_size) counts as 0 and count is limited to
  * [0, free_size]; free_size is at least the number of pages there are, or pages
  * that come back when the ring is full are lost. batch <= 65535, num_tokens <
- * 2^30, table_stride < 2^27.
+ * 2^30, table_stride < 2^27. With batch 0 nothing is enqueued and nothing written: the
+ * free pages stay those of free_state, also where free_out is another array.
  */
 typedef int32_t kap_step_status;
 enum {

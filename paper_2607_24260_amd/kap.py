@@ -453,9 +453,6 @@ def _step_call(seq_lens, add, block_table, free_pages, free_state, keep, pinned_
         with torch.cuda.stream(stream):
             outputs = {name: torch.empty(sizes[name], dtype=dt(name), device=seq_lens.device)
                        if t is None else t for name, t in outputs.items()}
-            if B == 0:                             # (nothing is run: what such a step leaves)
-                outputs["free_out"].copy_(free_state)
-                outputs["q_offsets"].zero_()
     checked = [("add", add, B, torch.int32), ("free_state", free_state, 2, torch.int32),
                ("keep", keep, B, torch.int32), ("pinned_blocks", pinned_blocks, B, torch.int32)]
     checked += [(name, t, sizes[name], dt(name)) for name, t in outputs.items()]
@@ -477,6 +474,25 @@ def _step_call(seq_lens, add, block_table, free_pages, free_state, keep, pinned_
     return args, outputs, held
 
 
+def _step_fn(seq_lens, free_pages, free_state, outputs, stream):
+    """kap_step_tables, which enqueues nothing for a step of no sequence; what such a step
+    leaves -- the free pages as they are, no tokens -- is written here."""
+    fn = load_library().kap_step_tables
+    if seq_lens.shape[0] > 0:
+        return fn
+
+    def none(*args):
+        status = fn(*args)
+        if status == KAP_OK:
+            size = free_pages.shape[0]
+            with torch.cuda.stream(stream):
+                head, count = free_state.clamp(min=0).unbind()
+                outputs["free_out"].copy_(torch.stack((head * (head < size), count.clamp(max=size))))
+                outputs["q_offsets"].zero_()
+        return status
+    return none
+
+
 def step_tables(seq_lens, add, block_table, free_pages, free_state, *, keep=None,
                 pinned_blocks=None, num_tokens=None, free_out=None, new_lens=None, q_offsets=None,
                 slot_mapping=None, positions=None, status=None, stream=None):
@@ -490,7 +506,7 @@ def step_tables(seq_lens, add, block_table, free_pages, free_state, *, keep=None
                    slot_mapping=slot_mapping, positions=positions, status=status)
     args, outputs, _ = _step_call(seq_lens, add, block_table, free_pages, free_state, keep,
                                   pinned_blocks, num_tokens, outputs, stream)
-    _check(load_library().kap_step_tables(*args))
+    _check(_step_fn(seq_lens, free_pages, free_state, outputs, stream)(*args))
     return outputs
 
 
@@ -504,7 +520,7 @@ def bind_step_tables(seq_lens, add, block_table, free_pages, free_state, *, free
         raise ValueError("a bound call needs its outputs")
     args, _, held = _step_call(seq_lens, add, block_table, free_pages, free_state, keep,
                                pinned_blocks, None, outputs, stream)
-    return BoundCall(load_library().kap_step_tables, args, held)
+    return BoundCall(_step_fn(seq_lens, free_pages, free_state, outputs, stream), args, held)
 
 
 def compact_view(src: KVCache, view_block_table, view_num_blocks, view_capacity: int,

@@ -107,6 +107,28 @@ def test_a_step_of_no_sequence():
     assert got["free_pages"].tolist() == [5, 6, 7]
 
 
+@pytest.mark.parametrize("bound", [False, True])
+@pytest.mark.parametrize("state", [(1, 2), (0, 3), (-1, 9), (3, -4), (2 ** 31 - 1, -2 ** 31)])
+def test_a_step_of_no_sequence_in_arrays_that_are_there(bound, state):
+    i32 = lambda *x: dev_i32(np.array(x, int))                     # noqa: E731
+    out = dict(free_out=i32(77, 77), new_lens=i32(), q_offsets=i32(77), positions=i32(), status=i32(),
+               slot_mapping=torch.zeros(0, dtype=torch.int64, device="cuda"))
+    want = O.step_tables([], [], np.zeros((0, 4)), [5, 6, 7], state, 0)
+    stream = torch.cuda.Stream()
+    free = i32(*state)
+    for other in (None, stream):
+        for o in (out, dict(out, free_out=free)):                  # and in place
+            o["free_out"].copy_(i32(77, 77)), o["q_offsets"].fill_(77), free.copy_(i32(*state))
+            args = (i32(), i32(), torch.zeros((0, 4), dtype=torch.int32, device="cuda"), i32(5, 6, 7), free)
+            torch.cuda.synchronize()
+            if bound:
+                K.bind_step_tables(*args, stream=other, **o)()
+            else:
+                K.step_tables(*args, stream=other, **o)
+            torch.cuda.synchronize()
+            assert o["free_out"].tolist() == list(want["free_out"]) and o["q_offsets"].tolist() == [0]
+
+
 def test_long_prompts():
     # pages by the thousand for one sequence; slots of a second launch
     rng = np.random.default_rng(5)
