@@ -211,6 +211,51 @@ def test_tokens_named_more_than_once_in_a_list(dtype):
     c.check()
 
 
+def slice_of(rows, vocab, dtype):
+    """Tokens of a workgroup: 16 KB of logits, halved while that leaves compute units idle."""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    most = 8192 if dtype == "bf16" else 4096
+    size = most
+    while size > most // 8 and rows * -(-vocab // size) < 2 * cus:
+        size //= 2
+    return size
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("part", [1, 2, 4, 8])
+@pytest.mark.parametrize("slices, odd", [(8, 1), (1, -3)])
+def test_slices_of_every_size(dtype, part, slices, odd):
+    # as many rows as make the slice a whole, a half, .. of the largest
+    most = 8192 if dtype == "bf16" else 4096
+    size, vocab = most // part, slices * most + most // 2 + odd
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    rows = -(-2 * cus // -(-vocab // size)) if part < 8 else 3
+    assert slice_of(rows, vocab, dtype) == size
+    c = Call(rows, vocab, dtype, 20 + part, longest=900)
+    n = len(c.host["history"])
+    # tokens all over the vocabulary, some of them often; lists that name some twice
+    c.set(history=np.where(c.rng.random(n) < 0.3, c.rng.integers(0, 9, n) * (vocab // 9), c.rng.integers(-2, vocab + 2, n)))
+    lists = c.rng.choice([0, 3, 700], rows)
+    offs = np.concatenate([[0], np.cumsum(lists)])
+    pool = c.rng.integers(-2, vocab + 2, 3000)
+    c.set(bias_offsets=offs, bias_token=c.rng.choice(pool, offs[-1]) if part % 4 else c.rng.permutation(offs[-1]) % vocab,
+          bias_value=np.asarray(c.rng.uniform(-9, 5, offs[-1]), np.float32))
+    plain = c.check()
+    for pad, shift in ((0, 0), (5, 3)):
+        big = torch.full((rows * (vocab + pad) + 9,), 77.0, dtype=DT[dtype], device="cuda")
+        view = big[shift:shift + rows * (vocab + pad)].view(rows, -1)[:, :vocab]
+        view.copy_(c.x)
+        K.adjust_logits(view, view, **c.kw)                         # in place
+        assert torch.equal(view, plain)
+        view.fill_(77.0)
+        assert bool((big == 77.0).all())
+        out = torch.full((rows * (vocab + pad + 1) + 9,), 55.0, dtype=DT[dtype], device="cuda")
+        o = out[shift:shift + rows * (vocab + pad + 1)].view(rows, -1)[:, :vocab]
+        assert torch.equal(K.adjust_logits(c.x, o, **c.kw), plain)
+        o.fill_(55.0)
+        assert bool((out == 55.0).all())
+
+
 def test_results_do_not_depend_on_the_run():
     c = Call(8, 30000, "bf16", 12, longest=5000)
     first = K.adjust_logits(c.x, **c.kw)
