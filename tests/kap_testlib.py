@@ -106,3 +106,23 @@ def assert_close(name, got, want, tol, mask=None):
     assert not np.isnan(diff).any(), f"{name}: NaN"
     assert worst <= tol, f"{name}: max abs err {worst:.3e} > {tol:.1e}"
     return worst
+
+
+def server_batch(kind: str):
+    """Batches of more than 64 sequences, (new tokens, length) each: ``decode``: single tokens,
+    some of long contexts, beside prompts' chunks; ``short``: hundreds of short sequences with
+    a few new tokens each; ``all``: those with chunks and long single tokens among them."""
+    rng = np.random.default_rng(len(kind))
+    chunks = [(200, 900), (433, 433), (700, 5000)]
+    if kind == "decode":
+        seqs = [(1, int(L)) for L in rng.integers(1, 1500, 97)]
+        seqs[5:50:9] = [(1, int(L)) for L in rng.integers(9000, 25000, 5)]
+    else:
+        seqs = [(int(n), int(n + c)) for n, c in zip(rng.integers(0, 31, 640), rng.integers(0, 500, 640))]
+        if kind == "short":
+            return seqs
+        for i in range(9):
+            seqs.insert(60 * i, (1 + i % 3, 7000 + 1500 * i))
+    for i, c in zip((3, 40, len(seqs)), chunks):
+        seqs.insert(i, c)
+    return seqs

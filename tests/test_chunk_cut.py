@@ -10,6 +10,8 @@ import pytest
 
 from paper_2607_24260_amd import build as B
 
+from kap_testlib import server_batch
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 I32, I64 = ctypes.c_int32, ctypes.c_int64
 F32, BF16, FP8 = 0, 1, 2
@@ -128,3 +130,22 @@ def test_ranges_of_long_windows_and_more_rows_than_tokens(lib, n, length, G, r0,
     assert walked(lib, n, length, G, most, window, 0, r0, r1) == want
     want = seen_steps(n, length, G, window, 40, r0, r1)
     assert walked(lib, n, length, G, most, window, 40, r0, r1) == want
+
+
+@pytest.mark.parametrize("kv, D", KINDS)
+@pytest.mark.parametrize("Hkv", [2, 8])
+@pytest.mark.parametrize("window, sinks", [(0, 0), (100, 20)])
+def test_the_kinds_of_the_batches_that_are_compared(lib, kv, D, Hkv, window, sinks):
+    # what the batches of test_gpu_chunk_attention.test_servers are there for
+    few = kv == F32 and D == 256                                   # (no tall blocks)
+    got = {k: check(lib, kv, D, 4 * Hkv, Hkv, server_batch(k), window, sinks, 256) for k in ("decode", "short", "all")}
+    assert all(planned for planned, *_ in got.values())
+    _, tall, team, solo, merged = got["decode"]
+    assert (tall > 0) != few and (team > 0 or window > 0)
+    if not window and Hkv == 2 and (D == 64 or few):
+        assert merged > 0
+    _, tall, team, solo, merged = got["short"]
+    assert tall == 0 and solo > 0 and (team > 0) == (D == 64 and not window and Hkv == 2 or
+                                                     (kv, D, Hkv, window) in ((BF16, 128, 2, 0), (FP8, 128, 2, 0)))
+    _, tall, team, solo, merged = got["all"]
+    assert (tall > 0) != few and solo > 0 and (team > 0) != (window > 0)

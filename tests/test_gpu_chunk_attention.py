@@ -19,7 +19,7 @@ from oracle import kap_oracle as O
 from paper_2607_24260_amd import kap as K
 from paper_2607_24260_amd.workloads import kv_pool
 
-from kap_testlib import dev_i32
+from kap_testlib import dev_i32, server_batch
 
 pytestmark = pytest.mark.gpu
 
@@ -196,6 +196,16 @@ def test_many_sequences(dtype, B):
     rng = np.random.default_rng(B)
     seqs = [(int(n), int(n + c)) for n, c in zip(rng.choice([0, 1, 1, 1, 2, 6], B), rng.integers(0, 90, B))]
     Chunks(dtype, seqs, Hq=4, Hkv=1, D=64, seed=B).check()
+
+
+@DTYPES
+@pytest.mark.parametrize("kind", ["decode", "short", "all"])
+@pytest.mark.parametrize("D, Hkv", [(64, 2), (128, 2), (128, 8), (256, 2)])
+@pytest.mark.parametrize("window, sinks", [(0, 0), (100, 20)])
+def test_servers(dtype, kind, D, Hkv, window, sinks):
+    # more than 64 sequences: blocks of all rows, of teams and of wavefronts by themselves in one
+    # launch, split and whole
+    Chunks(dtype, server_batch(kind), Hq=4 * Hkv, Hkv=Hkv, D=D, window=window, sinks=sinks, seed=D + Hkv).check()
 
 
 @DTYPES
