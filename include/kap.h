@@ -424,9 +424,10 @@ size_t kap_verify_shared_workspace_bytes(const kap_kv_cache *kv, int32_t batch, 
  *   [batch], block_table [batch][table_stride] int32; max_seq_len (host) >= every
  *   seq_lens[b] and <= 16 * table_stride, < 2^31 - 64. window <= 0: none; sinks
  *   >= 0, not read without a window.
- * Softmax weights meet V of bf16 and fp8 pages rounded to bf16 (each off by at most
- * 2^-8 of it, as out is); logits, sums and lse are single precision throughout. batch <= 65535,
- * num_tokens * num_q_heads < 2^30.
+ * Softmax weights meet V of bf16 and fp8 pages in two parts of bf16 (2^-16 of a weight is
+ * left); those of sequences with more than 128 rows (new tokens times num_q_heads /
+ * num_kv_heads) may be rounded to bf16 once (off by at most 2^-8 of it, as out is). Logits,
+ * sums and lse are single precision throughout. batch <= 65535, num_tokens * num_q_heads < 2^30.
  *   The workspace keeps arrival counters in its first 128 bytes times the device's
  * compute units: zero when a call starts, and left zero by it; the rest is scratch. So
  * zero-fill it once when allocating it; it then serves any sequence of calls of this

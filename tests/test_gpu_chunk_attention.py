@@ -208,6 +208,23 @@ def test_servers(dtype, kind, D, Hkv, window, sinks):
     Chunks(dtype, server_batch(kind), Hq=4 * Hkv, Hkv=Hkv, D=D, window=window, sinks=sinks, seed=D + Hkv).check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+@pytest.mark.parametrize("seqs", [[(1, 17), (5, 40), (1, 900), (9, 1000), (30, 31)], [(1, 20000)],
+                                  server_batch("short")])
+@pytest.mark.parametrize("D, window", [(64, 0), (128, 0), (256, 0), (128, 70)])
+def test_weights_of_few_rows_keep_16_bits(dtype, seqs, D, window):
+    # up to 128 rows a sequence: each weight is off by 2^-8 of 2^-8 (two parts of bf16), and
+    # the output is rounded once
+    c = Chunks(dtype, seqs, Hkv=2, D=D, window=window, seed=21)
+    out, _ = c.run()
+    o, _, mean, far, most = c.want()
+    z = (D + 4) * 2.0 ** -24 * abs(c.scale) * far
+    near = mean * (2 * z + most * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -16) + most * 8 * 2.0 ** -118
+    tol = near + 2.0 ** -8 * (o.abs() + near)
+    live = int(c.offsets[-1])
+    assert bool(((out.double() - o).abs() <= tol)[:live].all())
+
+
 @DTYPES
 def test_random_batches(dtype):
     rng = np.random.default_rng(12)
