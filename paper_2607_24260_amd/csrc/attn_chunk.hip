@@ -586,9 +586,11 @@ __device__ __forceinline__ void add_classes(State<D> &st, const Source &src, con
 // of the others are kept out of the products, where a weight of zero would spread
 // them, and added by class where the weight is not zero.
 //   Weights meet 16-bit V as two parts of bf16, what the first rounds off in the second (2^-16
-// of a weight is left): memory bounds the walks that come here, and the second products cost
-// them 1 to 2% (one token at 2048 14.1 to 14.5 us, 64 of a window of 4096 200 to 202), for an
-// error against 64 bits of 0.0017 instead of 0.0023, which is what rounding the result costs.
+// of a weight is left), for an error against 64 bits of 0.0017 instead of 0.0023, which is what
+// rounding the result costs. Memory bounds most walks that come here, which hardly notice the
+// second products (one token at 2048 14.2 to 14.5 us, 64 with a window of 4096 199 to 200; 64
+// chunks of 12 tokens at 4000 224 to 227); blocks that share their keys in the caches do (fp8:
+// 64 of 24 tokens at 4000 225 to 248 us).
 template <int KV, int D, bool MASKED, class Source>
 __device__ __forceinline__ void add_values(State<D> &st, const Source &src, const f32x16 &w,
                                            uint32_t seen, const float (&vs)[2]) {
@@ -609,10 +611,10 @@ __device__ __forceinline__ void add_values(State<D> &st, const Source &src, cons
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p[i] = round_bf16x2(x[2 * i], x[2 * i + 1]);
-        // (an fp8 page's scale may be infinite: nothing is left of such a weight)
-        auto less = [](float x, float part) { return KV == kFP8 && x == part ? 0.f : x - part; };
-        rest[i] = round_bf16x2(less(x[2 * i], __uint_as_float(p[i] << 16)),
-                               less(x[2 * i + 1], __uint_as_float(p[i] & 0xffff0000u)));
+        rest[i] = round_bf16x2(x[2 * i] - __uint_as_float(p[i] << 16),
+                               x[2 * i + 1] - __uint_as_float(p[i] & 0xffff0000u));
+        // (infinite weights, of pages of such a scale, leave nothing)
+        if constexpr (KV == kFP8) rest[i] &= __builtin_fabsf(vs[y]) < INFINITY ? ~0u : 0u;
       }
     }
     if constexpr (MASKED) sees = seen_words<KV>(seen, y);

@@ -327,6 +327,19 @@ def test_what_some_rows_see_reaches_those_alone(dtype, value):
         assert np.abs(lse.cpu().numpy()[:live] - l[:live]).max() < 1e-3
 
 
+@pytest.mark.parametrize("scale", [math.inf, -math.inf, math.nan])
+def test_infinite_and_nan_scales_of_seen_pages(scale):
+    # values of ones under the scale: every row that sees the page gets it
+    c = Chunks("fp8", [(1, 60), (5, 300), (200, 260), (4, 90)], seed=22)
+    for b in range(3):
+        c.kv.v_pages[int(c.table[b, 1])] = 0x38
+        c.kv.kv_scales[int(c.table[b, 1]), 1] = scale
+    want = Chunks("fp8", [(1, 60), (5, 300), (200, 260), (4, 90)], seed=22).run()
+    out, lse = c.run()
+    assert torch.equal(lse, want[1]) and torch.equal(out[206:], want[0][206:])
+    assert bool((torch.isnan(out[:206]) if math.isnan(scale) else out[:206] == scale).all())
+
+
 @DTYPES
 def test_nan_in_a_query_and_in_a_seen_key(dtype):
     c = Chunks(dtype, [(5, 100), (40, 90), (1, 50)], seed=10)
