@@ -13,10 +13,10 @@
 // taken 32 rows at a time, a workgroup's wavefronts sharing the keys ("team"); chunks of
 // more than 128 rows by up to 256 rows over the same keys, staged through LDS once for all
 // ("tall": a wavefront reads 1/8 of what it multiplies); and short sequences by the
-// hundred by a wavefront each, which meets no other ("solo": 1000 of 300 tokens 283 us,
+// hundred by a wavefront each, which meets no other ("solo": 1000 of 300 tokens 270 us,
 // by teams 465). One launch does all kinds at once. On one device, bf16, 32 heads over 8
 // KV heads of 128 dims:
-//   one token at 2048: 14 us; 64 tokens that see 4096 of 32768: 195 us, 5.5 TB/s;
+//   one token at 2048: 14.5 us; 64 tokens that see 4096 of 32768: 200 us, 5.4 TB/s;
 //   8192-token prompt: 560 us, 0.98 PFLOP/s (fp8: two chunks of 2048 at 32768: 1000 us,
 //   0.90); 4096 tokens at 16384: 1.1 PFLOP/s. The same loop without the fetches runs at 1.2,
 //   also without exponentials and sums at 1.25, also without LDS reads at 1.4: eight

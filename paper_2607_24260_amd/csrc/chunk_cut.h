@@ -119,8 +119,10 @@ __host__ __device__ __forceinline__ float part_steps(const Cut &c, Kind k, const
 // of the longest, if that is expected to end earlier. Parts about as long as each other end in
 // rounds; others with the work over the workgroups that run at once, and half a part more,
 // for which some of them idle. (Costs in eighths of a microsecond: a part 15 us around its
-// steps; as much again if it is split, 45 where parts of tall blocks leave 256 rows: a
-// 1024-token prompt 47 us whole, 67 in halves, 700 tokens 39 and 73. 48 single tokens and four chunks of 512 at 8192: 311 us
+// steps; each part that splitting adds 15 more, or 45 in a call with tall blocks, whose parts
+// leave 256 rows: a 1024-token prompt 47 us whole, 67 in halves, 700 tokens 39 and 73. Teams'
+// parts of such a call, of 32 rows, are charged the 45 too: single tokens beside a prompt are
+// split less than by themselves. 48 single tokens and four chunks of 512 at 8192: 311 us
 // unsplit, 365 with all split to fill the rounds, 290 as expected here and longest first.)
 //   sum(f), most(f): that of f(Info) of all sequences, in single precision: every wavefront
 // that computes it finds the same.
@@ -259,7 +261,10 @@ inline ChunkPlan plan_chunk(int kv_type, int D, int Hq, int num_kv_heads, int ba
   const long long Hkv = num_kv_heads;
   const long long rows = (long long)num_tokens * (Hq / Hkv);
   p.window = window > 0 && window < max_seq_len ? window : 0;
-  // (256-dim float32 heads have no staged walk)
+  // More rows go to tall blocks: 64 sequences of 160 rows at 1000 tokens, bf16, 128 dims, 97 us
+  // so and 223 in teams, of 96 rows 80 and 127, of 124 rows 87 and 175: of many sequences those
+  // of 65 to 128 rows would be faster in tall blocks too. (256-dim float32 heads have no staged
+  // walk: a prompt of 1500 tokens, 16 heads over 8, 388 us, of 128 dims 161.)
   p.few_rows = f32 && D == 256 ? 0x7fffffff : 128;
   p.target = cus;
   // in eighths of a microsecond: 32 keys with all rows of a tall block, and as their

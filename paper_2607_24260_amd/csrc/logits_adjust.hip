@@ -14,7 +14,7 @@
 // logit is read and written once -- and by the history, which every slice of a row reads:
 // 320 rows of 151937 bf16 logits with 4096 tokens 56 us, 3.5 TB/s (a large copy: 4.7; on the
 // same tensors again and again, which the caches hold in part, 48.5 us, the others below too); 64
-// of 151936 with 8192 tokens 17 us; one of 32000 in float32 4.5 us, the launch.
+// of 151936 with 8192 tokens 18 us; one of 32000 in float32 4.5 us, the launch.
 //   512 threads, two pieces of 16 bytes each, in 41 registers: four workgroups a compute
 // unit (256 threads 52 us, 1024 65; four history loads in flight instead of two, for which
 // only three workgroups fit, 54; 16 equal slices a row in one round of larger
